@@ -337,6 +337,118 @@ stamp_status_t stamp_debug_layout(const stamp_plan_desc_t* desc, int32_t relaid,
  * Runs on the default stream, allocates 4 bytes, blocks for a few tens of milliseconds. */
 stamp_status_t stamp_debug_mfma_rate(int32_t engine, double* tera_ops_per_s_host);
 
+/* ==== 8-bit floating point layers with block scales, dense and by expert, and the router in front of them ====
+ *
+ * For the calls of a model in which there is no token sequence to transform: single tokens while an answer is generated (the
+ * transform of one token is the identity), and tokens that a router has dealt to experts (an expert's rows are no contiguous
+ * sequence).  All conventions of the top of this file hold (device pointers, streams, workspaces, errors before any launch), but
+ * for one: non-finite activations are defined here, see Q8.
+ *
+ * Q8, the quantizer of activations: the 128 consecutive channels of a block (the last block of a row may be shorter) share a scale.
+ *     a = max(max |x|, 1.75 * 2^-118)                      (so that a block of zeros has a normal scale, too)
+ *     STAMP_SCALE_F32   scale = fl(a / 448), inv = fl(448 / a)
+ *     STAMP_SCALE_POW2  scale = the smallest power of two with a <= 448 scale, inv = 1 / scale
+ *     code = E4M3(fl(x * inv)), round to nearest even      (OCP E4M3: 448 is its largest number, no infinity)
+ *   A block that holds an infinity or NaN has a NaN as its scale, and so every output of its row is NaN.
+ * Weights hold E4M3 codes with one scale for every block of 128 output columns x 128 input channels (last blocks shorter).
+ *
+ *     Y[m, n] = sum over blocks b of  sa[m, b] sw[n / 128, b] sum over c in b of  qa[m, c] qw[n, c]   + bias[n]
+ *
+ * The products of a block are summed in fp32 on the matrix cores, the blocks in fp32; Y is rounded once.
+ * STAMP_SCALE_POW2 plans apply both scales as the matrix instructions' own operand scales. */
+
+typedef struct stamp_fp8_plan stamp_fp8_plan_t; /* opaque, library-owned: the weights of one layer, or of all experts of one layer */
+
+enum { STAMP_E4M3 = 2 }; /* w_dtype of stamp_fp8_desc_t, besides STAMP_F32 and STAMP_BF16: codes, with scales */
+typedef enum { STAMP_SCALE_F32 = 0, STAMP_SCALE_POW2 = 1 } stamp_scale_format_t;
+
+typedef struct {
+  int32_t d_in, d_out;    /* 1 .. 65536 and 1 .. 2^20 */
+  int32_t experts;        /* 0: one layer (stamp_fp8_linear_forward); 1 .. 1024: that many, by stamp_fp8_grouped_forward */
+  int32_t gated;          /* 1: every expert has two matrices, gate and up, for stamp_experts_forward alone; d_out is the width of one */
+  int32_t x_dtype, y_dtype; /* STAMP_F32, STAMP_BF16 */
+  int32_t w_dtype;        /* STAMP_F32, STAMP_BF16 (quantized here: scale as in Q8 over a block), STAMP_E4M3 (codes, taken as they are) */
+  int32_t w_is_out_by_in; /* 1: W [experts][2 if gated][d_out, d_in] (E4M3 codes are given so), 0: [..][d_in, d_out] */
+  int32_t scale_format;   /* stamp_scale_format_t, of activations and weights */
+} stamp_fp8_desc_t;
+
+/* Validates desc and lays the weights out for the kernels.  W_dev and w_scales_dev_or_null (fp32 [experts][2 if gated]
+ * [ceil(d_out / 128)][ceil(d_in / 128)], for STAMP_E4M3 only) and bias_dev_or_null (fp32 [experts][d_out]; none for a gated plan)
+ * are read on hip_stream.  STAMP_SCALE_POW2 with STAMP_E4M3: every scale has to be a normal power of two; that is looked up on
+ * the device, for which the call waits for hip_stream, and STAMP_ERR_UNSUPPORTED is returned where one is not. */
+stamp_status_t stamp_fp8_plan_create(const stamp_fp8_desc_t* desc, const void* W_dev, const float* w_scales_dev_or_null,
+                                     const float* bias_dev_or_null, void* hip_stream, stamp_fp8_plan_t** out);
+stamp_status_t stamp_fp8_plan_destroy(stamp_fp8_plan_t* plan);
+
+/* Bytes of workspace (256-byte aligned pointer) of the calls below with up to `rows` rows; 0 for a NULL plan or rows < 0. */
+size_t stamp_fp8_workspace_bytes(const stamp_fp8_plan_t* plan, int32_t rows);
+
+/* Q8 alone, for one quantized activation that feeds several layers: X [rows, d_in] (row m at X + m * ld_x, in elements) ->
+ * codes [rows][Kp] bytes, Kp = d_in rounded up to 128, zeros behind the last channel, and scales [Kp / 128][ld_scales] fp32, that of row m
+ * and block b at b * ld_scales + m; ld_scales >= rows and a multiple of 4, both pointers 16-byte aligned. */
+stamp_status_t stamp_fp8_quantize_act(const stamp_fp8_plan_t* plan, int32_t rows, const void* X_dev, int64_t ld_x, uint8_t* codes_dev,
+                                      float* scales_dev, int64_t ld_scales, void* hip_stream);
+
+/* The layer: Q8 and the product.  rows >= 0; row m of X at X + m * ld_x, of Y at Y + m * ld_y, in elements (ld >= the row's length;
+ * any alignment that the element type has). */
+stamp_status_t stamp_fp8_linear_forward(const stamp_fp8_plan_t* plan, int32_t rows, const void* X_dev, int64_t ld_x, void* Y_dev,
+                                        int64_t ld_y, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+/* The product alone, from what stamp_fp8_quantize_act wrote (for a plan of the same d_in and scale_format). */
+stamp_status_t stamp_fp8_linear_forward_q(const stamp_fp8_plan_t* plan, int32_t rows, const uint8_t* codes_dev, const float* scales_dev,
+                                          int64_t ld_scales, void* Y_dev, int64_t ld_y, void* workspace_dev, size_t workspace_bytes,
+                                          void* hip_stream);
+
+/* The product by expert: rows offsets[e] .. offsets[e + 1] - 1 of X and Y belong to expert e (offsets_dev: int32 [experts + 1] in
+ * device memory, not falling, from 0 on, the last at most rows; an expert may have none).  Rows behind the last offset are neither read
+ * for any other row's result nor written.  Offsets that break these rules are cut to 0 .. rows: the results are then unspecified,
+ * no access is out of bounds. */
+stamp_status_t stamp_fp8_grouped_forward(const stamp_fp8_plan_t* plan, int32_t rows, const int32_t* offsets_dev, const void* X_dev,
+                                         int64_t ld_x, void* Y_dev, int64_t ld_y, void* workspace_dev, size_t workspace_bytes,
+                                         void* hip_stream);
+
+/* The router.  logits [tokens, experts] (row t at + t * ld, in elements).  Of every token the top_k experts with the largest logits, in
+ * falling order, the lower index first where two are equal; a logit that is -infinity or NaN is masked and never chosen.
+ * Weights: softmax of the logits over the chosen ones (renormalize = 1) or over all that are not masked (0); where the largest is
+ * +infinity, those that are share the whole.  Slot (t, j) that found no expert (all others masked, or top_k > experts): id -1, weight 0,
+ * row -1.  The other slots, sorted by expert and then by (t, j), are the rows of the experts' products.
+ *   ids, weights, row_of_slot  [tokens, top_k]     offsets  [experts + 1]: rows of expert e are offsets[e] .. offsets[e + 1] - 1
+ *   token_of_row  [tokens * top_k]: the row's token, -1 behind the last row
+ * experts 1 .. 1024, top_k 1 .. 32, tokens 0 .. 2^22, tokens * top_k < 2^31. */
+typedef struct {
+  int32_t tokens, experts, top_k;
+  int32_t* ids_dev;
+  float* weights_dev;
+  int32_t* offsets_dev;
+  int32_t* token_of_row_dev;
+  int32_t* row_of_slot_dev;
+} stamp_routing_t;
+size_t stamp_route_workspace_bytes(int32_t tokens, int32_t experts, int32_t top_k);
+stamp_status_t stamp_route_topk(const stamp_routing_t* routing, const void* logits_dev, int32_t logits_dtype, int64_t ld,
+                                int32_t renormalize, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+
+/* The experts' gated MLP on the rows of a routing (as stamp_route_topk wrote it; entries out of range are cut to the range):
+ *     h = silu(Xq Wgate) * (Xq Wup)  in fp32, per row,   r = Q8(h) Wdown (+ bias),   Y[t] = sum over slots j of  weights[t, j] r[row(t, j)]
+ * up: a gated plan [d -> ff], down: a plan [ff -> d] with as many experts and the same scale_format; X [tokens, d] in up's x_dtype,
+ * Y [tokens, d] in down's y_dtype.  A token without any row gets zeros.  Between the down product and the sum the rows are held in
+ * down's y_dtype: for a bf16 Y that rounds every term once more, by what Y itself is rounded. */
+size_t stamp_experts_workspace_bytes(const stamp_fp8_plan_t* up, const stamp_fp8_plan_t* down, int32_t tokens, int32_t top_k);
+stamp_status_t stamp_experts_forward(const stamp_fp8_plan_t* up, const stamp_fp8_plan_t* down, const stamp_routing_t* routing,
+                                     const void* X_dev, int64_t ld_x, void* Y_dev, int64_t ld_y, void* workspace_dev,
+                                     size_t workspace_bytes, void* hip_stream);
+
+/* For tests: a plan's codes [experts][2 if gated][d_out][d_in] and scales in the layout of w_scales_dev, copied to host.
+ * Synchronizes the device. */
+stamp_status_t stamp_fp8_debug_weight_codes(const stamp_fp8_plan_t* plan, uint8_t* codes_host, float* scales_host);
+
+/* Which kernel a call with that many rows runs: 0 for a NULL plan, else one of these. */
+typedef enum {
+  STAMP_FP8_ROUTE_ROWS = 1,      /* few rows (on average per expert): weights streamed past them */
+  STAMP_FP8_ROUTE_TILES_64 = 2,  /* tiles of 64 rows x 256 columns */
+  STAMP_FP8_ROUTE_TILES_128 = 3,
+  STAMP_FP8_ROUTE_TILES_256 = 4
+} stamp_fp8_route_t;
+int32_t stamp_fp8_debug_route(const stamp_fp8_plan_t* plan, int32_t rows);
+
 const char* stamp_status_string(stamp_status_t status);
 
 #ifdef __cplusplus

@@ -19,4 +19,15 @@ from .binding import (  # noqa: F401
     STAMP_L_WHT,
     STAMP_L_DCT,
 )
+from .fp8 import (  # noqa: F401
+    Fp8Desc,
+    Fp8Plan,
+    Routing,
+    route_topk,
+    experts_forward,
+    experts_workspace,
+    STAMP_E4M3,
+    STAMP_SCALE_F32,
+    STAMP_SCALE_POW2,
+)
 from .marshal import plan_desc_for, to_device_x, XFORM_CODE  # noqa: F401

@@ -1,0 +1,178 @@
+// 8-bit floating point layers with block scales: plan, layouts and launchers (gfx950).
+//
+// Places: a plan's output columns are dealt to groups of 64, so that after the matrix instructions a lane holds neighbouring columns of
+// one row.  The weights are the first operand of v_mfma_f32_16x16x128_f8f6f4, a block of 128 input channels in one instruction: lane
+// 16 f + i gives row i of it, and element r of lane 16 f + m of the result is row 4 f + r of column m.  With the tokens as columns a lane
+// has one token, whose scale it then needs once, and rows 4 f .. 4 f + 3 of every instruction b = 0 .. 3 of a group:
+//   plain  column 64 g + 16 f + 4 b + r: 16 neighbours
+//   gated  column 32 g + 8 f + 4 (b / 2) + r of the gate (b even) or the up matrix (b odd): 8 neighbours of both; four groups are a block
+//          of 128 of the next layer's input
+//
+// Operand image of the weights, [matrix set e][group][block of 128 channels][b][h][lane][16 bytes]: lane 16 f + i's parts h = 0, 1 are
+// channels 32 f + 16 h .. + 15 of row i (any dealing of the channels is right that is the same for both operands).  A wave reads 1 KB of
+// consecutive addresses, from memory or LDS.  Activations stay in rows: [row][Kp] bytes.
+#ifndef STAMP_FP8_H_
+#define STAMP_FP8_H_
+
+#include "stamp_internal.h"
+
+constexpr int kF8Block = 128;
+constexpr int kF8Group = 64;                        // places of a group
+constexpr int kF8GroupBytes = kF8Group * kF8Block;  // of a group and block of channels
+constexpr int kF8MaxExperts = 1024;
+
+struct stamp_fp8_plan {
+  stamp_fp8_desc_t desc;
+  int32_t sets;        // experts, or 1
+  int32_t Kb, Kp;      // blocks of the input channels, bytes of a row of codes
+  int32_t groups;      // of a set
+  int32_t nblk;        // blocks of 128 output columns of one matrix
+  uint8_t* w_dev;      // operand image
+  float* sw_dev;       // [sets][2 if gated][nblk][Kb]
+  float* bias_dev;     // [sets][d_out] or nullptr
+};
+
+// column of place (b, row i of the instruction) in group g; gated: of the gate matrix for even b
+STAMP_HD int f8_column(int gated, int g, int b, int i) {
+  return gated ? 32 * g + 8 * (i >> 2) + 4 * (b >> 1) + (i & 3) : 64 * g + 16 * (i >> 2) + 4 * b + (i & 3);
+}
+STAMP_HD size_t f8_w_offset(int groups, int Kb, int set, int g, int kb, int b, int h, int lane) {
+  return ((((size_t)set * groups + g) * Kb + kb) * 8 + b * 2 + h) * 1024 + (size_t)lane * 16;
+}
+
+// The product's arguments.
+struct StampF8Gemm {
+  const uint8_t* A;        // codes [a_rows][Kp]
+  const float* SA;         // scales [Kb][ld_sa], by row of the product
+  int64_t ld_sa;
+  const int32_t* index;    // row of A of every row of the product, or nullptr: the same
+  int32_t a_rows;
+  int32_t rows;
+  const int32_t* offsets;  // [sets + 1] or nullptr (one set)
+  const uint8_t* W;
+  const float* SW;
+  const float* bias;
+  int32_t sets, groups, Kb, nblk, N, pow2, gated, y_bf16;
+  void* Y;                 // rows of N values; gated: codes [rows][ld_y] and scales [ld_y / 128][ld_sh]
+  int64_t ld_y;
+  float* SH;
+  int64_t ld_sh;
+};
+
+int stamp_f8_route(int sets, int groups, int Kb, int rows);
+hipError_t stamp_launch_f8_weights(stamp_fp8_plan* p, const void* W, const float* w_scales, hipStream_t st, uint32_t* flag);
+// row_of_slot != nullptr: row t's scales go to the places of its top_k slots (rows of the product, below nrows)
+hipError_t stamp_launch_f8_quant(const void* X, int x_bf16, int64_t ld_x, int rows, int d, int pow2, uint8_t* codes, float* scales, int64_t ld_s,
+                                 const int32_t* row_of_slot, int top_k, int nrows, hipStream_t st);
+hipError_t stamp_launch_f8_rows(const StampF8Gemm& a, hipStream_t st);
+hipError_t stamp_launch_f8_tiles(const StampF8Gemm& a, int bm, hipStream_t st);
+hipError_t stamp_launch_route(const stamp_routing_t& r, const void* logits, int bf16, int64_t ld, int renorm, void* ws, hipStream_t st);
+size_t stamp_route_ws(int tokens, int experts, int top_k);
+hipError_t stamp_launch_combine(const stamp_routing_t& r, const void* rows, int y_bf16, int64_t ld_rows, int nrows, void* Y, int64_t ld_y, int d,
+                                hipStream_t st);
+
+// ---- device helpers ----
+#ifdef __HIPCC__
+namespace f8 {
+
+typedef int v4i __attribute__((ext_vector_type(4)));
+typedef int v8i __attribute__((ext_vector_type(8)));
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+
+constexpr uint32_t kSmallest = (127u - 118u) << 23 | 0x600000u;  // 1.75 * 2^-118
+constexpr uint32_t kInfBits = 0x7f800000u;
+
+// Scale and multiplier of a block from the bits of its largest magnitude: as bits, magnitudes compare as integers, and infinities and NaN
+// are above all numbers.
+__device__ __forceinline__ void scale_of(uint32_t amax, int pow2, float* scale, float* inv) {
+  const uint32_t a = amax > kSmallest ? amax : kSmallest;
+  if (a >= kInfBits) {
+    *scale = *inv = __uint_as_float(0x7fc00000u);
+  } else if (pow2) {
+    const uint32_t e = (a >> 23) - 8 + ((a & 0x7fffffu) > 0x600000u ? 1 : 0);  // 448 = 1.75 * 2^8
+    *scale = __uint_as_float(e << 23);
+    *inv = __uint_as_float((254 - e) << 23);
+  } else {
+    *scale = __fdiv_rn(__uint_as_float(a), 448.0f);
+    *inv = __fdiv_rn(448.0f, __uint_as_float(a));
+  }
+}
+__device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
+  int v = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, v, true);
+}
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_max(uint32_t v) {
+  const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, 0xf, 0xf, false);
+  return v > o ? v : o;
+}
+// largest of 8 neighbouring lanes, in all of them: pairs, quads, the mirrored half row
+__device__ __forceinline__ uint32_t max8(uint32_t v) { return dpp_max<0x141>(dpp_max<0x4e>(dpp_max<0xb1>(v))); }
+
+__device__ __forceinline__ uint32_t abs_bits(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+__device__ __forceinline__ float bf16_lo(uint32_t v) { return __uint_as_float(v << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t v) { return __uint_as_float(v & 0xffff0000u); }
+__device__ __forceinline__ uint16_t to_bf16(float x) {
+  const __bf16 b = (__bf16)x;
+  return __builtin_bit_cast(uint16_t, b);
+}
+__device__ __forceinline__ uint32_t to_bf16x2(float x, float y) {
+  typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+  const b2 v = {(__bf16)x, (__bf16)y};
+  return __builtin_bit_cast(uint32_t, v);
+}
+
+// Rows of set e, cut to 0 .. rows.
+__device__ __forceinline__ void rows_of(const StampF8Gemm& a, int e, int* lo, int* hi) {
+  if (a.offsets == nullptr) {
+    *lo = 0;
+    *hi = a.rows;
+    return;
+  }
+  const int l = min(max(a.offsets[e], 0), a.rows);
+  *lo = l;
+  *hi = min(max(a.offsets[e + 1], l), a.rows);
+}
+
+// The tile-th tile of BM rows, counted over the sets: its set and rows; false where there is none.  Every wave finds it by itself.
+__device__ __forceinline__ bool find_tile(const StampF8Gemm& a, int BM, int tile, int* set, int* row0, int* nrows) {
+  if (a.offsets == nullptr) {
+    *set = 0;
+    *row0 = tile * BM;
+    *nrows = min(BM, a.rows - *row0);
+    return *nrows > 0;
+  }
+  const int lane = threadIdx.x & 63;
+  int base = 0;
+  for (int e0 = 0; e0 < a.sets; e0 += 64) {
+    int lo = 0, hi = 0;
+    if (e0 + lane < a.sets) rows_of(a, e0 + lane, &lo, &hi);
+    int incl = (hi - lo + BM - 1) / BM;
+    const int own = incl;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int o = __shfl_up(incl, d);
+      if (lane >= d) incl += o;
+    }
+    const uint64_t past = __ballot(base + incl > tile);
+    if (past != 0) {
+      const int src = __builtin_ctzll(past);
+      const int first = base + __shfl(incl - own, src);
+      const int l = __shfl(lo, src), h = __shfl(hi, src);
+      *set = __builtin_amdgcn_readfirstlane(e0 + src);
+      *row0 = __builtin_amdgcn_readfirstlane(l + (tile - first) * BM);
+      *nrows = __builtin_amdgcn_readfirstlane(min(BM, h - *row0));
+      return true;
+    }
+    base += __shfl(incl, 63);
+  }
+  return false;
+}
+
+__device__ __forceinline__ float silu(float g) { return g / (1.0f + __expf(-g)); }
+
+}  // namespace f8
+#endif
+#endif  // STAMP_FP8_H_

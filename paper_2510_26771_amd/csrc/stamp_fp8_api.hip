@@ -1,0 +1,360 @@
+// C entry points of the 8-bit floating point layers, the router and the experts.
+#include <stdlib.h>
+#include <string.h>
+
+#include <new>
+
+#include "stamp_fp8.h"
+
+namespace {
+
+constexpr int32_t kMaxRows = 1 << 24;
+
+size_t align256(size_t n) { return (n + 255) / 256 * 256; }
+int64_t scales_ld(int32_t rows) { return ((int64_t)rows + 3) / 4 * 4; }
+int type_size(int32_t dtype) { return dtype == STAMP_BF16 ? 2 : 4; }
+bool is_float_type(int32_t t) { return t == STAMP_F32 || t == STAMP_BF16; }
+
+stamp_status_t validate(const stamp_fp8_desc_t* d) {
+  if (d->d_in < 1 || d->d_out < 1 || d->experts < 0) return STAMP_ERR_SHAPE;
+  if (d->gated < 0 || d->gated > 1 || d->w_is_out_by_in < 0 || d->w_is_out_by_in > 1) return STAMP_ERR_SHAPE;
+  if (!is_float_type(d->x_dtype) || !is_float_type(d->y_dtype)) return STAMP_ERR_SHAPE;
+  if (!is_float_type(d->w_dtype) && d->w_dtype != STAMP_E4M3) return STAMP_ERR_SHAPE;
+  if (d->scale_format != STAMP_SCALE_F32 && d->scale_format != STAMP_SCALE_POW2) return STAMP_ERR_SHAPE;
+  if (d->gated && d->experts == 0) return STAMP_ERR_SHAPE;
+  if (d->d_in > 65536 || d->d_out > (1 << 20) || d->experts > kF8MaxExperts) return STAMP_ERR_UNSUPPORTED;
+  if (d->w_dtype == STAMP_E4M3 && !d->w_is_out_by_in) return STAMP_ERR_UNSUPPORTED;
+  return STAMP_OK;
+}
+
+StampF8Gemm gemm_args(const stamp_fp8_plan* p) {
+  StampF8Gemm a;
+  memset(&a, 0, sizeof(a));
+  a.W = p->w_dev;
+  a.SW = p->sw_dev;
+  a.bias = p->bias_dev;
+  a.sets = p->sets;
+  a.groups = p->groups;
+  a.Kb = p->Kb;
+  a.nblk = p->nblk;
+  a.N = p->desc.d_out;
+  a.pow2 = p->desc.scale_format == STAMP_SCALE_POW2;
+  a.gated = p->desc.gated;
+  a.y_bf16 = p->desc.y_dtype == STAMP_BF16;
+  return a;
+}
+
+hipError_t product(const StampF8Gemm& a, hipStream_t st) {
+  switch (stamp_f8_route(a.sets, a.groups, a.Kb, a.rows)) {
+    case STAMP_FP8_ROUTE_ROWS: return stamp_launch_f8_rows(a, st);
+    case STAMP_FP8_ROUTE_TILES_64: return stamp_launch_f8_tiles(a, 64, st);
+    case STAMP_FP8_ROUTE_TILES_128: return stamp_launch_f8_tiles(a, 128, st);
+    default: return stamp_launch_f8_tiles(a, 256, st);
+  }
+}
+
+struct LinearWs {
+  size_t codes, scales, total;
+};
+LinearWs linear_ws(const stamp_fp8_plan* p, int32_t rows) {
+  LinearWs w;
+  w.codes = 0;
+  w.scales = align256((size_t)rows * p->Kp);
+  w.total = w.scales + align256((size_t)p->Kb * scales_ld(rows) * sizeof(float));
+  return w;
+}
+
+struct ExpertsWs {
+  size_t codes, scales, h, sh, rows, total;
+  int64_t ld_rows;
+};
+ExpertsWs experts_ws(const stamp_fp8_plan* up, const stamp_fp8_plan* down, int32_t tokens, int32_t top_k) {
+  ExpertsWs w;
+  const int64_t slots = (int64_t)tokens * top_k, ld = scales_ld((int32_t)slots);
+  w.codes = 0;
+  w.scales = align256((size_t)tokens * up->Kp);
+  w.h = w.scales + align256((size_t)up->Kb * ld * sizeof(float));
+  w.sh = w.h + align256((size_t)slots * down->Kp);
+  w.rows = w.sh + align256((size_t)down->Kb * ld * sizeof(float));
+  w.ld_rows = (down->desc.d_out + 7) / 8 * 8;
+  w.total = w.rows + align256((size_t)slots * w.ld_rows * type_size(down->desc.y_dtype));
+  return w;
+}
+
+stamp_status_t check_ws(const void* ws, size_t bytes, size_t need) {
+  if (need == 0) return STAMP_OK;
+  return ws == nullptr || reinterpret_cast<uintptr_t>(ws) % 256 != 0 || bytes < need ? STAMP_ERR_WORKSPACE : STAMP_OK;
+}
+
+// a matrix of `rows` rows of n elements, ld apart: element-aligned
+stamp_status_t check_matrix(const void* p, int32_t dtype, int64_t ld, int64_t n) {
+  if (p == nullptr) return STAMP_ERR_NULL;
+  return ld < n || reinterpret_cast<uintptr_t>(p) % type_size(dtype) != 0 ? STAMP_ERR_SHAPE : STAMP_OK;
+}
+
+stamp_status_t check_routing(const stamp_routing_t* r) {
+  if (r->tokens < 0 || r->experts < 1 || r->top_k < 1) return STAMP_ERR_SHAPE;
+  if (r->experts > kF8MaxExperts || r->top_k > 32 || r->tokens > (1 << 22)) return STAMP_ERR_UNSUPPORTED;
+  if (r->offsets_dev == nullptr) return STAMP_ERR_NULL;
+  if (r->tokens > 0 && (r->ids_dev == nullptr || r->weights_dev == nullptr || r->token_of_row_dev == nullptr || r->row_of_slot_dev == nullptr))
+    return STAMP_ERR_NULL;
+  return STAMP_OK;
+}
+
+stamp_status_t done(hipError_t e) { return e == hipSuccess ? STAMP_OK : STAMP_ERR_DEVICE; }
+
+// linear_forward, grouped_forward
+stamp_status_t forward(const stamp_fp8_plan* p, int32_t rows, const int32_t* offsets, bool grouped, const void* X, int64_t ld_x, void* Y, int64_t ld_y,
+                       void* ws, size_t ws_bytes, hipStream_t st) {
+  if (p == nullptr) return STAMP_ERR_NULL;
+  if (p->desc.gated || (p->desc.experts > 0) != grouped) return STAMP_ERR_UNSUPPORTED;
+  if (rows < 0 || rows > kMaxRows) return STAMP_ERR_SHAPE;
+  if (grouped && offsets == nullptr) return STAMP_ERR_NULL;
+  if (rows == 0) return STAMP_OK;
+  stamp_status_t s = check_matrix(X, p->desc.x_dtype, ld_x, p->desc.d_in);
+  if (s == STAMP_OK) s = check_matrix(Y, p->desc.y_dtype, ld_y, p->desc.d_out);
+  const LinearWs w = linear_ws(p, rows);
+  if (s == STAMP_OK) s = check_ws(ws, ws_bytes, w.total);
+  if (s != STAMP_OK) return s;
+  uint8_t* codes = static_cast<uint8_t*>(ws) + w.codes;
+  float* scales = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + w.scales);
+  StampF8Gemm a = gemm_args(p);
+  hipError_t e = stamp_launch_f8_quant(X, p->desc.x_dtype == STAMP_BF16, ld_x, rows, p->desc.d_in, a.pow2, codes, scales, scales_ld(rows), nullptr, 0, 0, st);
+  if (e != hipSuccess) return STAMP_ERR_DEVICE;
+  a.A = codes;
+  a.SA = scales;
+  a.ld_sa = scales_ld(rows);
+  a.a_rows = a.rows = rows;
+  a.offsets = offsets;
+  a.Y = Y;
+  a.ld_y = ld_y;
+  return done(product(a, st));
+}
+
+}  // namespace
+
+// Kernel for a product of `rows` rows over `sets` weights.
+int stamp_f8_route(int sets, int groups, int Kb, int rows) {
+  const int avg = (int)(((int64_t)rows + sets - 1) / sets);
+  if (avg <= 32) return STAMP_FP8_ROUTE_ROWS;
+  if (avg <= 64) return STAMP_FP8_ROUTE_TILES_64;
+  if (avg <= 512) return STAMP_FP8_ROUTE_TILES_128;
+  return STAMP_FP8_ROUTE_TILES_256;
+}
+
+extern "C" {
+
+stamp_status_t stamp_fp8_plan_create(const stamp_fp8_desc_t* desc, const void* W_dev, const float* w_scales_dev, const float* bias_dev, void* hip_stream,
+                                     stamp_fp8_plan_t** out) {
+  if (desc == nullptr || out == nullptr) return STAMP_ERR_NULL;
+  *out = nullptr;
+  const stamp_status_t vs = validate(desc);
+  if (vs != STAMP_OK) return vs;
+  if (W_dev == nullptr || (desc->w_dtype == STAMP_E4M3) != (w_scales_dev != nullptr)) return STAMP_ERR_NULL;
+  if (desc->gated && bias_dev != nullptr) return STAMP_ERR_UNSUPPORTED;
+  stamp_fp8_plan* p = new (std::nothrow) stamp_fp8_plan;
+  if (p == nullptr) return STAMP_ERR_ALLOC;
+  p->desc = *desc;
+  p->sets = desc->experts > 0 ? desc->experts : 1;
+  p->Kb = (desc->d_in + kF8Block - 1) / kF8Block;
+  p->Kp = p->Kb * kF8Block;
+  const int per_group = desc->gated ? kF8Group / 2 : kF8Group;
+  p->groups = (desc->d_out + per_group - 1) / per_group;
+  p->nblk = (desc->d_out + kF8Block - 1) / kF8Block;
+  p->w_dev = nullptr;
+  p->sw_dev = p->bias_dev = nullptr;
+  hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+  const size_t image = (size_t)p->sets * p->groups * p->Kb * kF8GroupBytes;
+  const size_t nscales = (size_t)p->sets * (desc->gated ? 2 : 1) * p->nblk * p->Kb, nbias = (size_t)p->sets * desc->d_out;
+  const bool look = desc->w_dtype == STAMP_E4M3 && desc->scale_format == STAMP_SCALE_POW2;
+  uint32_t* flag = nullptr;
+  bool ok = hipMalloc(reinterpret_cast<void**>(&p->w_dev), image) == hipSuccess &&
+            hipMalloc(reinterpret_cast<void**>(&p->sw_dev), nscales * sizeof(float)) == hipSuccess;
+  if (ok && bias_dev != nullptr) ok = hipMalloc(reinterpret_cast<void**>(&p->bias_dev), nbias * sizeof(float)) == hipSuccess;
+  if (ok && look) ok = hipMalloc(reinterpret_cast<void**>(&flag), sizeof(uint32_t)) == hipSuccess;
+  if (!ok) {
+    (void)hipGetLastError();
+    (void)stamp_fp8_plan_destroy(p);
+    return STAMP_ERR_ALLOC;
+  }
+  uint32_t found = 0;
+  if (look) ok = hipMemcpyAsync(flag, &found, sizeof(found), hipMemcpyHostToDevice, st) == hipSuccess;
+  if (ok) ok = stamp_launch_f8_weights(p, W_dev, w_scales_dev, st, flag) == hipSuccess;
+  if (ok && bias_dev != nullptr) ok = hipMemcpyAsync(p->bias_dev, bias_dev, nbias * sizeof(float), hipMemcpyDeviceToDevice, st) == hipSuccess;
+  if (ok && look) ok = hipMemcpyAsync(&found, flag, sizeof(found), hipMemcpyDeviceToHost, st) == hipSuccess && hipStreamSynchronize(st) == hipSuccess;
+  if (flag != nullptr) (void)hipFree(flag);
+  if (!ok || found != 0) {
+    (void)hipStreamSynchronize(st);
+    (void)hipGetLastError();
+    (void)stamp_fp8_plan_destroy(p);
+    return ok ? STAMP_ERR_UNSUPPORTED : STAMP_ERR_DEVICE;
+  }
+  *out = p;
+  return STAMP_OK;
+}
+
+stamp_status_t stamp_fp8_plan_destroy(stamp_fp8_plan_t* p) {
+  if (p == nullptr) return STAMP_ERR_NULL;
+  if (p->w_dev) (void)hipFree(p->w_dev);
+  if (p->sw_dev) (void)hipFree(p->sw_dev);
+  if (p->bias_dev) (void)hipFree(p->bias_dev);
+  delete p;
+  return STAMP_OK;
+}
+
+size_t stamp_fp8_workspace_bytes(const stamp_fp8_plan_t* p, int32_t rows) {
+  if (p == nullptr || rows < 0 || rows > kMaxRows) return 0;
+  return linear_ws(p, rows).total;
+}
+
+stamp_status_t stamp_fp8_quantize_act(const stamp_fp8_plan_t* p, int32_t rows, const void* X_dev, int64_t ld_x, uint8_t* codes_dev, float* scales_dev,
+                                      int64_t ld_scales, void* hip_stream) {
+  if (p == nullptr) return STAMP_ERR_NULL;
+  if (rows < 0 || rows > kMaxRows) return STAMP_ERR_SHAPE;
+  if (rows == 0) return STAMP_OK;
+  const stamp_status_t s = check_matrix(X_dev, p->desc.x_dtype, ld_x, p->desc.d_in);
+  if (s != STAMP_OK) return s;
+  if (codes_dev == nullptr || scales_dev == nullptr) return STAMP_ERR_NULL;
+  if (ld_scales < rows || ld_scales % 4 != 0 || (reinterpret_cast<uintptr_t>(codes_dev) | reinterpret_cast<uintptr_t>(scales_dev)) % 16 != 0) return STAMP_ERR_SHAPE;
+  return done(stamp_launch_f8_quant(X_dev, p->desc.x_dtype == STAMP_BF16, ld_x, rows, p->desc.d_in, p->desc.scale_format == STAMP_SCALE_POW2, codes_dev,
+                                    scales_dev, ld_scales, nullptr, 0, 0, reinterpret_cast<hipStream_t>(hip_stream)));
+}
+
+stamp_status_t stamp_fp8_linear_forward(const stamp_fp8_plan_t* p, int32_t rows, const void* X_dev, int64_t ld_x, void* Y_dev, int64_t ld_y,
+                                        void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+  return forward(p, rows, nullptr, false, X_dev, ld_x, Y_dev, ld_y, workspace_dev, workspace_bytes, reinterpret_cast<hipStream_t>(hip_stream));
+}
+
+stamp_status_t stamp_fp8_linear_forward_q(const stamp_fp8_plan_t* p, int32_t rows, const uint8_t* codes_dev, const float* scales_dev, int64_t ld_scales,
+                                          void* Y_dev, int64_t ld_y, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+  if (p == nullptr) return STAMP_ERR_NULL;
+  if (p->desc.experts > 0) return STAMP_ERR_UNSUPPORTED;
+  if (rows < 0 || rows > kMaxRows) return STAMP_ERR_SHAPE;
+  if (rows == 0) return STAMP_OK;
+  if (codes_dev == nullptr || scales_dev == nullptr) return STAMP_ERR_NULL;
+  if (ld_scales < rows || ld_scales % 4 != 0 || (reinterpret_cast<uintptr_t>(codes_dev) | reinterpret_cast<uintptr_t>(scales_dev)) % 16 != 0) return STAMP_ERR_SHAPE;
+  stamp_status_t s = check_matrix(Y_dev, p->desc.y_dtype, ld_y, p->desc.d_out);
+  if (s == STAMP_OK) s = check_ws(workspace_dev, workspace_bytes, linear_ws(p, rows).total);
+  if (s != STAMP_OK) return s;
+  StampF8Gemm a = gemm_args(p);
+  a.A = codes_dev;
+  a.SA = scales_dev;
+  a.ld_sa = ld_scales;
+  a.a_rows = a.rows = rows;
+  a.Y = Y_dev;
+  a.ld_y = ld_y;
+  return done(product(a, reinterpret_cast<hipStream_t>(hip_stream)));
+}
+
+stamp_status_t stamp_fp8_grouped_forward(const stamp_fp8_plan_t* p, int32_t rows, const int32_t* offsets_dev, const void* X_dev, int64_t ld_x, void* Y_dev,
+                                         int64_t ld_y, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+  return forward(p, rows, offsets_dev, true, X_dev, ld_x, Y_dev, ld_y, workspace_dev, workspace_bytes, reinterpret_cast<hipStream_t>(hip_stream));
+}
+
+size_t stamp_route_workspace_bytes(int32_t tokens, int32_t experts, int32_t top_k) {
+  if (tokens < 0 || tokens > (1 << 22) || experts < 1 || experts > kF8MaxExperts || top_k < 1 || top_k > 32) return 0;
+  return stamp_route_ws(tokens, experts, top_k);
+}
+
+stamp_status_t stamp_route_topk(const stamp_routing_t* r, const void* logits_dev, int32_t logits_dtype, int64_t ld, int32_t renormalize, void* workspace_dev,
+                                size_t workspace_bytes, void* hip_stream) {
+  if (r == nullptr) return STAMP_ERR_NULL;
+  stamp_status_t s = check_routing(r);
+  if (s != STAMP_OK) return s;
+  if (!is_float_type(logits_dtype) || renormalize < 0 || renormalize > 1) return STAMP_ERR_SHAPE;
+  if (r->tokens > 0) s = check_matrix(logits_dev, logits_dtype, ld, r->experts);
+  if (s == STAMP_OK) s = check_ws(workspace_dev, workspace_bytes, stamp_route_ws(r->tokens, r->experts, r->top_k));
+  if (s != STAMP_OK) return s;
+  return done(stamp_launch_route(*r, logits_dev, logits_dtype == STAMP_BF16, ld, renormalize, workspace_dev, reinterpret_cast<hipStream_t>(hip_stream)));
+}
+
+size_t stamp_experts_workspace_bytes(const stamp_fp8_plan_t* up, const stamp_fp8_plan_t* down, int32_t tokens, int32_t top_k) {
+  if (up == nullptr || down == nullptr || tokens < 0 || top_k < 1 || (int64_t)tokens * top_k > kMaxRows) return 0;
+  return experts_ws(up, down, tokens, top_k).total;
+}
+
+stamp_status_t stamp_experts_forward(const stamp_fp8_plan_t* up, const stamp_fp8_plan_t* down, const stamp_routing_t* r, const void* X_dev, int64_t ld_x,
+                                     void* Y_dev, int64_t ld_y, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+  if (up == nullptr || down == nullptr || r == nullptr) return STAMP_ERR_NULL;
+  if (!up->desc.gated || down->desc.gated || down->desc.experts == 0) return STAMP_ERR_UNSUPPORTED;
+  if (up->desc.experts != down->desc.experts || up->desc.d_out != down->desc.d_in || up->desc.d_in != down->desc.d_out ||
+      up->desc.scale_format != down->desc.scale_format || r->experts != up->desc.experts)
+    return STAMP_ERR_SHAPE;
+  stamp_status_t s = check_routing(r);
+  if (s != STAMP_OK) return s;
+  if ((int64_t)r->tokens * r->top_k > kMaxRows) return STAMP_ERR_UNSUPPORTED;
+  if (r->tokens == 0) return STAMP_OK;
+  s = check_matrix(X_dev, up->desc.x_dtype, ld_x, up->desc.d_in);
+  if (s == STAMP_OK) s = check_matrix(Y_dev, down->desc.y_dtype, ld_y, down->desc.d_out);
+  const ExpertsWs w = experts_ws(up, down, r->tokens, r->top_k);
+  if (s == STAMP_OK) s = check_ws(workspace_dev, workspace_bytes, w.total);
+  if (s != STAMP_OK) return s;
+  hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+  uint8_t* ws = static_cast<uint8_t*>(workspace_dev);
+  const int32_t slots = r->tokens * r->top_k;
+  const int64_t ld = scales_ld(slots);
+
+  StampF8Gemm a = gemm_args(up);
+  float* scales = reinterpret_cast<float*>(ws + w.scales);
+  if (stamp_launch_f8_quant(X_dev, up->desc.x_dtype == STAMP_BF16, ld_x, r->tokens, up->desc.d_in, a.pow2, ws + w.codes, scales, ld, r->row_of_slot_dev,
+                            r->top_k, slots, st) != hipSuccess)
+    return STAMP_ERR_DEVICE;
+  a.A = ws + w.codes;
+  a.SA = scales;
+  a.ld_sa = ld;
+  a.index = r->token_of_row_dev;
+  a.a_rows = r->tokens;
+  a.rows = slots;
+  a.offsets = r->offsets_dev;
+  a.Y = ws + w.h;
+  a.ld_y = down->Kp;
+  a.SH = reinterpret_cast<float*>(ws + w.sh);
+  a.ld_sh = ld;
+  if (product(a, st) != hipSuccess) return STAMP_ERR_DEVICE;
+
+  StampF8Gemm b = gemm_args(down);
+  b.A = ws + w.h;
+  b.SA = a.SH;
+  b.ld_sa = ld;
+  b.a_rows = b.rows = slots;
+  b.offsets = r->offsets_dev;
+  b.Y = ws + w.rows;
+  b.ld_y = w.ld_rows;
+  if (product(b, st) != hipSuccess) return STAMP_ERR_DEVICE;
+  return done(stamp_launch_combine(*r, b.Y, b.y_bf16, w.ld_rows, slots, Y_dev, ld_y, down->desc.d_out, st));
+}
+
+stamp_status_t stamp_fp8_debug_weight_codes(const stamp_fp8_plan_t* p, uint8_t* codes_host, float* scales_host) {
+  if (p == nullptr || codes_host == nullptr || scales_host == nullptr) return STAMP_ERR_NULL;
+  const stamp_fp8_desc_t& d = p->desc;
+  const size_t image = (size_t)p->sets * p->groups * p->Kb * kF8GroupBytes;
+  uint8_t* h = static_cast<uint8_t*>(malloc(image));
+  if (h == nullptr) return STAMP_ERR_ALLOC;
+  if (hipDeviceSynchronize() != hipSuccess || hipMemcpy(h, p->w_dev, image, hipMemcpyDeviceToHost) != hipSuccess ||
+      hipMemcpy(scales_host, p->sw_dev, (size_t)p->sets * (d.gated ? 2 : 1) * p->nblk * p->Kb * sizeof(float), hipMemcpyDeviceToHost) != hipSuccess) {
+    free(h);
+    return STAMP_ERR_DEVICE;
+  }
+  for (int set = 0; set < p->sets; ++set)
+    for (int g = 0; g < p->groups; ++g)
+      for (int b = 0; b < 4; ++b)
+        for (int i = 0; i < 16; ++i) {
+          const int n = f8_column(d.gated, g, b, i);
+          if (n >= d.d_out) continue;
+          const size_t mat = d.gated ? 2 * (size_t)set + (b & 1) : (size_t)set;
+          uint8_t* row = codes_host + (mat * d.d_out + n) * d.d_in;
+          for (int c = 0; c < d.d_in; c += 16) {
+            const uint8_t* s = h + f8_w_offset(p->groups, p->Kb, set, g, c >> 7, b, (c >> 4) & 1, 16 * ((c >> 5) & 3) + i);
+            memcpy(row + c, s, d.d_in - c < 16 ? d.d_in - c : 16);
+          }
+        }
+  free(h);
+  return STAMP_OK;
+}
+
+int32_t stamp_fp8_debug_route(const stamp_fp8_plan_t* p, int32_t rows) {
+  if (p == nullptr || rows < 0) return 0;
+  return stamp_f8_route(p->sets, p->groups, p->Kb, rows);
+}
+
+}  // extern "C"

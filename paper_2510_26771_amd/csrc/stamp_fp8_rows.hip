@@ -1,0 +1,157 @@
+// Product of the 8-bit floating point layers for few rows (on average per expert).
+//
+// Bound by the weights' bytes: every byte is read once and feeds one matrix instruction per 16 rows.  So nothing is staged: a wave takes
+// some 16-place blocks of a group and a part of the depth, and reads its operand straight into registers in runs of 1 KB; the parts of
+// the depth are summed in LDS in a fixed order.
+#include "stamp_fp8.h"
+
+namespace {
+using namespace f8;
+
+constexpr int kWaves = 8;
+
+// MT: tiles of 16 rows held at once.  NB: blocks of 16 places per wave.  S: parts of the depth; kWaves / S waves lie side by side.
+template <int MT, int NB, int S, bool POW2, bool GATED>
+__global__ __launch_bounds__(kWaves * 64) void k_f8_rows(StampF8Gemm a) {
+  constexpr int kSide = kWaves / S;           // waves side by side
+  constexpr int kPlaces = kSide * NB * 16;    // places of the workgroup
+  constexpr int kLd = kPlaces + 4;            // floats of a row of partial sums
+  constexpr int kRows = 16 * MT;
+  __shared__ float red[S][kRows][kLd];
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int side = wave % kSide, part = wave / kSide;
+  const int set = blockIdx.y;
+  int lo, hi;
+  rows_of(a, set, &lo, &hi);
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  hi = __builtin_amdgcn_readfirstlane(hi);
+  const int blk0 = (blockIdx.x * kSide + side) * NB;  // first of the wave's blocks, counted over the groups
+  const int g = blk0 >> 2, b0 = blk0 & 3;
+  const bool in = g < a.groups;
+  const int kb0 = (int)((int64_t)a.Kb * part / S), kb1 = (int)((int64_t)a.Kb * (part + 1) / S);
+  const uint8_t* w0 = a.W + (((size_t)set * a.groups + (in ? g : 0)) * a.Kb) * kF8GroupBytes + b0 * 2048 + lane * 16;
+  const float* sw0 = a.SW + (size_t)set * (GATED ? 2 : 1) * a.nblk * a.Kb + (size_t)(GATED ? (in ? g : 0) >> 2 : (in ? g : 0) >> 1) * a.Kb;
+  const int Kp = a.Kb * 128;
+
+  for (int r0 = lo; r0 < hi; r0 += kRows) {
+    f4 acc[MT][NB];
+#pragma unroll
+    for (int mi = 0; mi < MT; ++mi)
+#pragma unroll
+      for (int b = 0; b < NB; ++b) acc[mi][b] = f4{0, 0, 0, 0};
+    const uint8_t* arow[MT];
+    int srow[MT];
+#pragma unroll
+    for (int mi = 0; mi < MT; ++mi) {
+      const int r = min(r0 + 16 * mi + (lane & 15), hi - 1);
+      int ar = r;
+      if (a.index != nullptr) ar = min(max(a.index[r], 0), a.a_rows - 1);
+      arow[mi] = a.A + (size_t)ar * Kp + 32 * (lane >> 4);
+      srow[mi] = r;
+    }
+    if (in) {
+      for (int kb = kb0; kb < kb1; ++kb) {
+        const uint8_t* w = w0 + (size_t)kb * kF8GroupBytes;
+        v8i B[NB], X[MT];
+        float sx[MT];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          const v4i l = *reinterpret_cast<const v4i*>(w + b * 2048), h = *reinterpret_cast<const v4i*>(w + b * 2048 + 1024);
+          B[b] = __builtin_shufflevector(l, h, 0, 1, 2, 3, 4, 5, 6, 7);
+        }
+#pragma unroll
+        for (int mi = 0; mi < MT; ++mi) {
+          const v4i* s = reinterpret_cast<const v4i*>(arow[mi] + (size_t)kb * 128);
+          X[mi] = __builtin_shufflevector(s[0], s[1], 0, 1, 2, 3, 4, 5, 6, 7);
+          sx[mi] = a.SA[(int64_t)kb * a.ld_sa + srow[mi]];
+        }
+        const float sw = sw0[kb], su = GATED ? sw0[(size_t)a.nblk * a.Kb + kb] : 0.0f;
+#pragma unroll
+        for (int mi = 0; mi < MT; ++mi) {
+#pragma unroll
+          for (int b = 0; b < NB; ++b) {
+            const float s = GATED && ((b0 + b) & 1) ? su : sw;
+            if constexpr (POW2) {
+              acc[mi][b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(B[b], X[mi], acc[mi][b], 0, 0, 0, (int)(__float_as_uint(s) >> 23), 0,
+                                                                           (int)(__float_as_uint(sx[mi]) >> 23));
+            } else {
+              const f4 z = {0, 0, 0, 0};
+              const f4 p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(B[b], X[mi], z, 0, 0, 0, 0, 0, 0);
+              const float f = sx[mi] * s;
+#pragma unroll
+              for (int r = 0; r < 4; ++r) acc[mi][b][r] = __builtin_fmaf(p[r], f, acc[mi][b][r]);
+            }
+          }
+        }
+      }
+    }
+    // partial sums: element r of block b is row 4 f + r of the instruction, token lane % 16
+    __syncthreads();
+#pragma unroll
+    for (int mi = 0; mi < MT; ++mi)
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+        *reinterpret_cast<f4*>(&red[part][16 * mi + (lane & 15)][(side * NB + b) * 16 + 4 * (lane >> 4)]) = acc[mi][b];
+    __syncthreads();
+    const int nr = min(kRows, hi - r0);
+    if constexpr (!GATED) {
+      for (int u = t; u < kRows * kPlaces; u += kWaves * 64) {
+        const int m = u / kPlaces, pl = u % kPlaces;
+        const int blk = blockIdx.x * (kSide * NB) + (pl >> 4);
+        const int n = f8_column(0, blk >> 2, blk & 3, pl & 15);
+        if (m >= nr || n >= a.N) continue;
+        float v = red[0][m][pl];
+#pragma unroll
+        for (int s = 1; s < S; ++s) v += red[s][m][pl];
+        if (a.bias != nullptr) v += a.bias[(size_t)set * a.N + n];
+        const int64_t o = (int64_t)(r0 + m) * a.ld_y + n;
+        if (a.y_bf16) static_cast<uint16_t*>(a.Y)[o] = to_bf16(v);
+        else static_cast<float*>(a.Y)[o] = v;
+      }
+    } else {
+      // 256 places are a block of 128 columns: 8 lanes of 16 columns each take a row
+      static_assert(kPlaces == 256, "a block of the next layer's input in one workgroup");
+      for (int u = t; u < kRows * 8; u += kWaves * 64) {
+        const int m = u >> 3, c0 = (u & 7) * 16;
+        float hv[16];
+        uint32_t amax = 0;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          const int c = c0 + j, ch = blockIdx.x * 128 + c;  // of group c / 32: f = c / 8 % 4, pair c / 4 % 2
+          const int pl = (c >> 5) * 64 + ((c >> 2) & 1) * 32 + ((c >> 3) & 3) * 4 + (c & 3);
+          float gt = red[0][m][pl], up = red[0][m][pl + 16];
+#pragma unroll
+          for (int s = 1; s < S; ++s) gt += red[s][m][pl], up += red[s][m][pl + 16];
+          hv[j] = ch < a.N ? silu(gt) * up : 0.0f;
+          amax = max(amax, abs_bits(hv[j]));
+        }
+        amax = max8(amax);
+        float scale, inv;
+        scale_of(amax, POW2, &scale, &inv);
+        u4 o;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[j] = pack4(hv[4 * j] * inv, hv[4 * j + 1] * inv, hv[4 * j + 2] * inv, hv[4 * j + 3] * inv);
+        if (m < nr) {
+          *reinterpret_cast<u4*>(static_cast<uint8_t*>(a.Y) + (int64_t)(r0 + m) * a.ld_y + blockIdx.x * 128 + c0) = o;
+          if ((u & 7) == 0) a.SH[(int64_t)blockIdx.x * a.ld_sh + r0 + m] = scale;
+        }
+      }
+    }
+  }
+}
+
+template <int MT, int NB, int S, bool GATED>
+hipError_t go(const StampF8Gemm& a, hipStream_t st) {
+  const int places = kWaves / S * NB * 16;
+  const dim3 grid((a.groups * 64 + places - 1) / places, a.sets);
+  if (a.pow2) k_f8_rows<MT, NB, S, true, GATED><<<grid, kWaves * 64, 0, st>>>(a);
+  else k_f8_rows<MT, NB, S, false, GATED><<<grid, kWaves * 64, 0, st>>>(a);
+  return hipGetLastError();
+}
+}  // namespace
+
+hipError_t stamp_launch_f8_rows(const StampF8Gemm& a, hipStream_t st) {
+  const int avg = (a.rows + a.sets - 1) / a.sets;
+  if (a.gated) return avg <= 16 ? go<1, 4, 2, true>(a, st) : go<2, 4, 2, true>(a, st);
+  return avg <= 16 ? go<1, 1, 8, false>(a, st) : go<2, 1, 8, false>(a, st);
+}
