@@ -53,19 +53,27 @@ struct StampF8Gemm {
   const float* SW;
   const float* bias;
   int32_t sets, groups, Kb, nblk, N, pow2, gated, y_bf16;
+  int32_t wide_sums;       // products on the bf16 matrix instructions (f8_wide_sums)
   void* Y;                 // rows of N values; gated: codes [rows][ld_y] and scales [ld_y / 128][ld_sh]
   int64_t ld_y;
   float* SH;
   int64_t ld_sh;
 };
 
-int stamp_f8_route(int sets, int groups, int Kb, int rows);
+int stamp_f8_route(int sets, int groups, int Kb, int rows, int wide_sums);
 hipError_t stamp_launch_f8_weights(stamp_fp8_plan* p, const void* W, const float* w_scales, hipStream_t st, uint32_t* flag);
 // row_of_slot != nullptr: row t's scales go to the places of its top_k slots (rows of the product, below nrows)
 hipError_t stamp_launch_f8_quant(const void* X, int x_bf16, int64_t ld_x, int rows, int d, int pow2, uint8_t* codes, float* scales, int64_t ld_s,
                                  const int32_t* row_of_slot, int top_k, int nrows, hipStream_t st);
 hipError_t stamp_launch_f8_rows(const StampF8Gemm& a, hipStream_t st);
 hipError_t stamp_launch_f8_tiles(const StampF8Gemm& a, int bm, hipStream_t st);
+
+// The FP8 matrix instructions align the 8 products of neighbouring channels to the largest of them and drop what lies 14 bits and more
+// below it (2^16 + 2^3 comes out, 2^16 + 2^2 does not): a product of random codes is 1e-5 to 6e-5 of its size off, while the bf16
+// instructions, which the codes fit exactly, keep 4e-8 at half the rate.  A bf16 Y cannot tell (its own rounding is 2e-3), so its layers
+// take the FP8 instructions.  An fp32 Y and the codes of the next layer (an error of 6e-5 moves one in 1000 of them to its neighbour) take
+// the bf16 instructions.
+inline int f8_wide_sums(const StampF8Gemm& a) { return a.gated || !a.y_bf16; }
 hipError_t stamp_launch_route(const stamp_routing_t& r, const void* logits, int bf16, int64_t ld, int renorm, void* ws, hipStream_t st);
 size_t stamp_route_ws(int tokens, int experts, int top_k);
 hipError_t stamp_launch_combine(const stamp_routing_t& r, const void* rows, int y_bf16, int64_t ld_rows, int nrows, void* Y, int64_t ld_y, int d,
@@ -119,8 +127,8 @@ __device__ __forceinline__ uint16_t to_bf16(float x) {
   return __builtin_bit_cast(uint16_t, b);
 }
 __device__ __forceinline__ uint32_t to_bf16x2(float x, float y) {
-  typedef __bf16 b2 __attribute__((ext_vector_type(2)));
-  const b2 v = {(__bf16)x, (__bf16)y};
+  typedef __bf16 bb __attribute__((ext_vector_type(2)));
+  const bb v = {(__bf16)x, (__bf16)y};
   return __builtin_bit_cast(uint32_t, v);
 }
 
@@ -169,6 +177,15 @@ __device__ __forceinline__ bool find_tile(const StampF8Gemm& a, int BM, int tile
     base += __shfl(incl, 63);
   }
   return false;
+}
+
+typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+// 8 codes as bf16: exact
+__device__ __forceinline__ b8 widen8(int lo, int hi) {
+  const b2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
+  const b2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
+  return b8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
 __device__ __forceinline__ float silu(float g) { return g / (1.0f + __expf(-g)); }

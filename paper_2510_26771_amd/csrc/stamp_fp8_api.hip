@@ -41,11 +41,12 @@ StampF8Gemm gemm_args(const stamp_fp8_plan* p) {
   a.pow2 = p->desc.scale_format == STAMP_SCALE_POW2;
   a.gated = p->desc.gated;
   a.y_bf16 = p->desc.y_dtype == STAMP_BF16;
+  a.wide_sums = f8_wide_sums(a);
   return a;
 }
 
 hipError_t product(const StampF8Gemm& a, hipStream_t st) {
-  switch (stamp_f8_route(a.sets, a.groups, a.Kb, a.rows)) {
+  switch (stamp_f8_route(a.sets, a.groups, a.Kb, a.rows, a.wide_sums)) {
     case STAMP_FP8_ROUTE_ROWS: return stamp_launch_f8_rows(a, st);
     case STAMP_FP8_ROUTE_TILES_64: return stamp_launch_f8_tiles(a, 64, st);
     case STAMP_FP8_ROUTE_TILES_128: return stamp_launch_f8_tiles(a, 128, st);
@@ -89,7 +90,8 @@ stamp_status_t check_ws(const void* ws, size_t bytes, size_t need) {
 // a matrix of `rows` rows of n elements, ld apart: element-aligned
 stamp_status_t check_matrix(const void* p, int32_t dtype, int64_t ld, int64_t n) {
   if (p == nullptr) return STAMP_ERR_NULL;
-  return ld < n || reinterpret_cast<uintptr_t>(p) % type_size(dtype) != 0 ? STAMP_ERR_SHAPE : STAMP_OK;
+  if (ld < n || reinterpret_cast<uintptr_t>(p) % type_size(dtype) != 0) return STAMP_ERR_SHAPE;
+  return ld > (1 << 21) ? STAMP_ERR_UNSUPPORTED : STAMP_OK;  // 256 rows within 32-bit offsets
 }
 
 stamp_status_t check_routing(const stamp_routing_t* r) {
@@ -134,11 +136,11 @@ stamp_status_t forward(const stamp_fp8_plan* p, int32_t rows, const int32_t* off
 }  // namespace
 
 // Kernel for a product of `rows` rows over `sets` weights.
-int stamp_f8_route(int sets, int groups, int Kb, int rows) {
+int stamp_f8_route(int sets, int groups, int Kb, int rows, int wide_sums) {
   const int avg = (int)(((int64_t)rows + sets - 1) / sets);
   if (avg <= 32) return STAMP_FP8_ROUTE_ROWS;
   if (avg <= 64) return STAMP_FP8_ROUTE_TILES_64;
-  if (avg <= 512) return STAMP_FP8_ROUTE_TILES_128;
+  if (avg <= 512 || wide_sums) return STAMP_FP8_ROUTE_TILES_128;  // the bf16 operands of 256 rows do not fit the registers
   return STAMP_FP8_ROUTE_TILES_256;
 }
 
@@ -282,7 +284,7 @@ stamp_status_t stamp_experts_forward(const stamp_fp8_plan_t* up, const stamp_fp8
     return STAMP_ERR_SHAPE;
   stamp_status_t s = check_routing(r);
   if (s != STAMP_OK) return s;
-  if ((int64_t)r->tokens * r->top_k > kMaxRows) return STAMP_ERR_UNSUPPORTED;
+  if ((int64_t)r->tokens * r->top_k > kMaxRows || (int64_t)r->tokens * up->Kp >= (int64_t)0xfffffff0u) return STAMP_ERR_UNSUPPORTED;
   if (r->tokens == 0) return STAMP_OK;
   s = check_matrix(X_dev, up->desc.x_dtype, ld_x, up->desc.d_in);
   if (s == STAMP_OK) s = check_matrix(Y_dev, down->desc.y_dtype, ld_y, down->desc.d_out);
@@ -354,7 +356,7 @@ stamp_status_t stamp_fp8_debug_weight_codes(const stamp_fp8_plan_t* p, uint8_t* 
 
 int32_t stamp_fp8_debug_route(const stamp_fp8_plan_t* p, int32_t rows) {
   if (p == nullptr || rows < 0) return 0;
-  return stamp_f8_route(p->sets, p->groups, p->Kb, rows);
+  return stamp_f8_route(p->sets, p->groups, p->Kb, rows, gemm_args(p).wide_sums);
 }
 
 }  // extern "C"

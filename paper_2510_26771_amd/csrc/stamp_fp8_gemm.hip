@@ -1,21 +1,43 @@
 // Product of the 8-bit floating point layers in tiles of BM rows x 256 places.
 //
-// Eight waves, 2 x 4, of BM / 2 x 64 each; the operands of a block of 128 channels are one stage in LDS, two stages, the next one filled
-// by asynchronous 16-byte loads while this one is multiplied.  The weights' stage is a copy of the operand image.  The rows' stage is
-// [row][8 pieces of 16 bytes], piece p at p ^ (row / 2 % 8): the 16 lanes of a read then hit all 64 banks once.
+// Eight waves, 2 x 4, of BM / 2 x 64 each; the operands of a block of 128 channels are one stage in LDS, two stages.  The weights' stage is
+// a copy of the operand image.  The rows' stage is [row][8 pieces of 16 bytes], piece p at p ^ (row / 2 % 8): the 16 lanes of a read then
+// hit all 64 banks once.
+//
+// A wave's turn from one stage to the next lies before its last row block of the stage: all its reads of this stage have returned, its
+// loads into the next have landed; behind the barrier it asks for the stage after the next (into this one's place) and reads the next
+// one's first operands under the last block's matrix instructions.
+//
+// STAMP_SCALE_F32: an instruction's sum over the block of channels (its addend is 0) goes to the accumulators by a multiplication with
+// both scales, 4 fused multiply-adds per instruction, one row block behind, so that the matrix pipe (32 cycles an instruction) runs on.
 #include "stamp_fp8.h"
 
 namespace {
 using namespace f8;
 
 typedef __attribute__((address_space(3))) void* LdsPtr;
-typedef const __attribute__((address_space(1))) void* GlobalPtr;
 
-template <int BM, bool POW2, bool GATED>
+#if defined(__HIP_DEVICE_COMPILE__)
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
+// buffer over 4 GB from a uniform address on; an access at kNowhere is dropped
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void* p) {
+  const uint64_t u = reinterpret_cast<uint64_t>(p);
+  const uint64_t v = (uint64_t)uniform((uint32_t)(u >> 32)) << 32 | uniform((uint32_t)u);
+  return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(v), 0, (int)0xfffffff0u, 0x00027000);
+}
+constexpr uint32_t kNowhere = 0xfffffff0u;
+#endif
+
+// How the products are summed: FP8 instructions with the scales by multiplication or as their own, or bf16 instructions (f8_wide_sums).
+enum Sums { kScaled, kPow2, kWide };
+
+template <int BM, Sums SUMS, bool GATED>
 __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
+#if defined(__HIP_DEVICE_COMPILE__)
   constexpr int kStageA = BM * 128, kStageB = 4 * kF8GroupBytes;
-  constexpr int MI = BM / 32;  // instructions along the rows, per wave
+  constexpr int MI = BM / 32;  // row blocks of 16 per wave
   constexpr int LA = BM / 64;  // 16-byte pieces of the rows' stage per thread
+  constexpr bool POW2 = SUMS == kPow2, WIDE = SUMS == kWide;
   // two variables, not one array of two: the compiler then knows that a read of one stage does not wait for the loads into the other
   __shared__ __attribute__((aligned(1024))) uint8_t stage0[kStageA + kStageB + BM * 4];
   __shared__ __attribute__((aligned(1024))) uint8_t stage1[kStageA + kStageB + BM * 4];
@@ -24,88 +46,165 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
   const int ncol = (a.groups + 3) / 4, col = blockIdx.x % ncol;  // consecutive workgroups share the rows' operand
   int set, row0, nrows;
   if (!find_tile(a, BM, blockIdx.x / ncol, &set, &row0, &nrows)) return;
+  set = __builtin_amdgcn_readfirstlane(set);
+  row0 = __builtin_amdgcn_readfirstlane(row0);
+  nrows = __builtin_amdgcn_readfirstlane(nrows);
   const int g0 = col * 4, Kb = a.Kb, Kp = Kb * 128;
 
-  const uint8_t* asrc[LA];
+  // 32-bit offsets from a scalar base: the tile's first row, or with an index all rows of A (below 4 GB, checked by the host)
+  uint32_t aoff[LA], boff[4];
 #pragma unroll
   for (int i = 0; i < LA; ++i) {
     const int p = i * 512 + t, row = p >> 3, piece = (p & 7) ^ ((row >> 1) & 7);
-    int r = row0 + min(row, nrows - 1);
-    if (a.index != nullptr) r = min(max(a.index[r], 0), a.a_rows - 1);
-    asrc[i] = a.A + (size_t)r * Kp + piece * 16;
+    uint32_t r = min(row, nrows - 1);
+    if (a.index != nullptr) r = min(max(a.index[row0 + r], 0), a.a_rows - 1);
+    aoff[i] = r * (uint32_t)Kp + piece * 16;
   }
-  const uint8_t* bsrc[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) bsrc[i] = a.W + ((size_t)set * a.groups + min(g0 + i, a.groups - 1)) * Kb * kF8GroupBytes + t * 16;
-  const float* ssrc = a.SA + row0 + min(t, nrows - 1);
+  for (int i = 0; i < 4; ++i) boff[i] = uniform((uint32_t)(min(g0 + i, a.groups - 1) - g0) * (uint32_t)Kb * kF8GroupBytes);
+  const __amdgpu_buffer_rsrc_t ra = buffer(a.A + (a.index != nullptr ? (size_t)0 : (size_t)row0 * Kp));
+  const __amdgpu_buffer_rsrc_t rb = buffer(a.W + ((size_t)set * a.groups + g0) * Kb * kF8GroupBytes);
+  const uint32_t soff = (uint32_t)min(t, nrows - 1);
 
   auto load = [&](uint8_t* S, int kb) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < LA; ++i)
-      __builtin_amdgcn_global_load_lds((GlobalPtr)(asrc[i] + (size_t)kb * 128), (LdsPtr)(S + i * 8192 + wave * 1024), 16, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (LdsPtr)(S + i * 8192 + wave * 1024), 16, aoff[i], kb * 128, 0, 0);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      __builtin_amdgcn_global_load_lds((GlobalPtr)(bsrc[i] + (size_t)kb * kF8GroupBytes), (LdsPtr)(S + kStageA + i * 8192 + wave * 1024), 16, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (LdsPtr)(S + kStageA + i * 8192 + wave * 1024), 16, t * 16, boff[i] + kb * kF8GroupBytes, 0, 0);
     if (wave < BM / 64)
-      __builtin_amdgcn_global_load_lds((GlobalPtr)(ssrc + (int64_t)kb * a.ld_sa), (LdsPtr)(S + kStageA + kStageB + wave * 256), 4, 0, 0);
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(a.SA + row0 + (int64_t)kb * a.ld_sa + soff),
+                                       (LdsPtr)(S + kStageA + kStageB + wave * 256), 4, 0, 0);
   };
 
-  f4 acc[MI][4];
+  f4 acc[MI][4], P[4];
 #pragma unroll
   for (int mi = 0; mi < MI; ++mi)
 #pragma unroll
     for (int b = 0; b < 4; ++b) acc[mi][b] = f4{0, 0, 0, 0};
+#pragma unroll
+  for (int b = 0; b < 4; ++b) P[b] = f4{0, 0, 0, 0};
   const int gw = min(g0 + wn, a.groups - 1);
   const float* sw0 = a.SW + (size_t)set * (GATED ? 2 : 1) * a.nblk * Kb + (size_t)(GATED ? gw >> 2 : gw >> 1) * Kb;
   const int x = ((lane & 15) >> 1) & 7, f = lane >> 4;
-  const int abase = (wm * (BM / 2) + (lane & 15)) * 128, p0 = ((2 * f) ^ x) * 16, p1 = ((2 * f + 1) ^ x) * 16;
+  const int abase = (wm * (BM / 2) + (lane & 15)) * 128, p0 = abase + ((2 * f) ^ x) * 16, p1 = abase + ((2 * f + 1) ^ x) * 16;
+  const int wbase = kStageA + wn * kF8GroupBytes + lane * 16, sbase = kStageA + kStageB + (wm * (BM / 2) + (lane & 15)) * 4;
 
-  auto multiply = [&](const uint8_t* S, int kb) __attribute__((always_inline)) {
-    v8i W[4];
-#pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      const uint8_t* s = S + kStageA + wn * kF8GroupBytes + b * 2048 + lane * 16;
-      W[b] = __builtin_shufflevector(*reinterpret_cast<const v4i*>(s), *reinterpret_cast<const v4i*>(s + 1024), 0, 1, 2, 3, 4, 5, 6, 7);
-    }
-    const float sw = sw0[kb], su = GATED ? sw0[(size_t)a.nblk * Kb + kb] : 0.0f;
-    const float* SA = reinterpret_cast<const float*>(S + kStageA + kStageB) + wm * (BM / 2) + (lane & 15);
-#pragma unroll
-    for (int mi = 0; mi < MI; ++mi) {
-      const uint8_t* s = S + abase + mi * 2048;
-      const v8i X = __builtin_shufflevector(*reinterpret_cast<const v4i*>(s + p0), *reinterpret_cast<const v4i*>(s + p1), 0, 1, 2, 3, 4, 5, 6, 7);
-      const float sx = SA[16 * mi];
-#pragma unroll
-      for (int b = 0; b < 4; ++b) {
-        const float sc = GATED && (b & 1) ? su : sw;
-        if constexpr (POW2) {
-          acc[mi][b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(W[b], X, acc[mi][b], 0, 0, 0, (int)(__float_as_uint(sc) >> 23), 0,
-                                                                       (int)(__float_as_uint(sx) >> 23));
-        } else {
-          const f4 z = {0, 0, 0, 0};
-          const f4 p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(W[b], X, z, 0, 0, 0, 0, 0, 0);
-          const float fs = sx * sc;
-#pragma unroll
-          for (int r = 0; r < 4; ++r) acc[mi][b][r] = __builtin_fmaf(p[r], fs, acc[mi][b][r]);
-        }
-      }
-    }
+  // weight scales of 64 blocks of channels at a time, lane kb % 64
+  float swv = 0.0f, suv = 0.0f;
+  auto weight_scales = [&](int kb) __attribute__((always_inline)) {
+    swv = sw0[min(kb + lane, Kb - 1)];
+    if (GATED) suv = sw0[(size_t)a.nblk * Kb + min(kb + lane, Kb - 1)];
   };
-  // the own loads have landed, the own reads returned; then everyone's
+  auto lane_of = [&](float v, int kb) __attribute__((always_inline)) {
+    return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), kb & 63));
+  };
+  auto read_w = [&](const uint8_t* S, int b) __attribute__((always_inline)) -> v8i {
+    const uint8_t* s = S + wbase + b * 2048;
+    return __builtin_shufflevector(*reinterpret_cast<const v4i*>(s), *reinterpret_cast<const v4i*>(s + 1024), 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  auto read_x = [&](const uint8_t* S, int mi) __attribute__((always_inline)) -> v8i {
+    return __builtin_shufflevector(*reinterpret_cast<const v4i*>(S + p0 + mi * 2048), *reinterpret_cast<const v4i*>(S + p1 + mi * 2048), 0, 1, 2, 3, 4, 5, 6,
+                                   7);
+  };
+  auto read_s = [&](const uint8_t* S, int mi) __attribute__((always_inline)) { return *reinterpret_cast<const float*>(S + sbase + mi * 64); };
+  // the own loads have landed and the own reads returned; then everyone's
   auto turn = [&]() __attribute__((always_inline)) {
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
+  auto add = [&](f4& c, const f4& p, float fs) __attribute__((always_inline)) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) c[r] = __builtin_fmaf(p[r], fs, c[r]);
+    asm volatile("" : "+v"(c));  // here, not where the value is next used: the products would pile up
+  };
 
+  v8i W[4], X;
+  b8 Wb[4][4];  // WIDE: of the step
+  float sx, fg = 0.0f, fu = 0.0f;  // of the row block before: its factors
+  // the step of stage S; N: the next one's stage
+  auto step = [&](uint8_t* S, uint8_t* N, int kb) __attribute__((always_inline)) {
+    const float sw = lane_of(swv, kb), su = GATED ? lane_of(suv, kb) : 0.0f;
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) {
+      if constexpr (POW2) {
+#pragma unroll
+        for (int b = 0; b < 4; ++b) asm volatile("" : "+v"(acc[(mi + MI / 2) % MI][b]));
+      }
+      v8i Xn;
+      float sn;
+      if (mi < MI - 1) {
+        Xn = read_x(S, mi + 1);
+        sn = read_s(S, mi + 1);
+      } else {
+        turn();
+        if (kb + 2 < Kb) load(S, kb + 2);
+        Xn = read_x(N, 0);
+        sn = read_s(N, 0);
+      }
+      const float f0 = sx * sw, f1 = GATED ? sx * su : 0.0f;
+      const int before = mi == 0 ? MI - 1 : mi - 1;
+      b8 Xb[4];
+      if constexpr (WIDE) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) Xb[k] = widen8(X[2 * k], X[2 * k + 1]);
+      }
+#pragma unroll
+      for (int b = 0; b < 4; ++b) {
+        if constexpr (WIDE) {
+          if (mi == 0) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) Wb[b][k] = widen8(W[b][2 * k], W[b][2 * k + 1]);
+          }
+          add(acc[before][b], P[b], GATED && (b & 1) ? fu : fg);
+          const f4 z = {0, 0, 0, 0};
+          P[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(Wb[b][0], Xb[0], z, 0, 0, 0);
+        } else if constexpr (POW2) {
+          acc[mi][b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(W[b], X, acc[mi][b], 0, 0, 0, (int)(__float_as_uint(GATED && (b & 1) ? su : sw) >> 23),
+                                                                       0, (int)(__float_as_uint(sx) >> 23));
+        } else {
+          add(acc[before][b], P[b], GATED && (b & 1) ? fu : fg);
+          const f4 z = {0, 0, 0, 0};
+          P[b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(W[b], X, z, 0, 0, 0, 0, 0, 0);
+        }
+        if (mi == MI - 1) W[b] = read_w(N, b);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if constexpr (WIDE) {
+#pragma unroll
+        for (int k = 1; k < 4; ++k) {
+#pragma unroll
+          for (int b = 0; b < 4; ++b) P[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(Wb[b][k], Xb[k], P[b], 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+      X = Xn;
+      sx = sn;
+      fg = f0;
+      fu = f1;
+    }
+    if (((kb + 1) & 63) == 0) weight_scales(kb + 1);
+  };
+
+  weight_scales(0);
   load(stage0, 0);
-  for (int kb = 0; kb < Kb; kb += 2) {
-    turn();
-    if (kb + 1 < Kb) load(stage1, kb + 1);
-    multiply(stage0, kb);
-    if (kb + 1 >= Kb) break;
-    turn();
-    if (kb + 2 < Kb) load(stage0, kb + 2);
-    multiply(stage1, kb + 1);
+  turn();
+  if (Kb > 1) load(stage1, 1);
+#pragma unroll
+  for (int b = 0; b < 4; ++b) W[b] = read_w(stage0, b);
+  X = read_x(stage0, 0);
+  sx = read_s(stage0, 0);
+  int kb = 0;
+  for (; kb + 1 < Kb; kb += 2) {
+    step(stage0, stage1, kb);
+    step(stage1, stage0, kb + 1);
+  }
+  if (kb < Kb) step(stage0, stage1, kb);
+  if constexpr (!POW2) {
+#pragma unroll
+    for (int b = 0; b < 4; ++b) add(acc[MI - 1][b], P[b], GATED && (b & 1) ? fu : fg);
   }
 
   const int g = g0 + wn;
@@ -114,39 +213,40 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
     float bias[16];
 #pragma unroll
     for (int j = 0; j < 16; ++j) bias[j] = a.bias != nullptr && n0 + j < a.N ? a.bias[(size_t)set * a.N + n0 + j] : 0.0f;
-    const int size = a.y_bf16 ? 2 : 4;
-    const bool wide = n0 + 16 <= a.N && (reinterpret_cast<uintptr_t>(a.Y) | (uintptr_t)(a.ld_y * size)) % 16 == 0;
+    const uint32_t size = a.y_bf16 ? 2 : 4, ld = (uint32_t)a.ld_y * size;
+    char* const y = static_cast<char*>(a.Y) + ((int64_t)row0 * a.ld_y) * size;  // 256 rows are below 4 GB, checked by the host
+    const bool wide = (reinterpret_cast<uintptr_t>(a.Y) | ld) % 16 == 0 && g * 64 + 64 <= a.N;
+    const __amdgpu_buffer_rsrc_t ry = buffer(y);
 #pragma unroll
     for (int mi = 0; mi < MI; ++mi) {
       const int m = wm * (BM / 2) + 16 * mi + (lane & 15);
-      if (m >= nrows) continue;
-      const int64_t o = (int64_t)(row0 + m) * a.ld_y + n0;
+      const uint32_t o = m < nrows ? (uint32_t)m * ld + (uint32_t)n0 * size : kNowhere;
       float v[16];
 #pragma unroll
       for (int j = 0; j < 16; ++j) v[j] = acc[mi][j >> 2][j & 3] + bias[j];
-      if (a.y_bf16) {
-        uint16_t* y = static_cast<uint16_t*>(a.Y) + o;
-        if (wide) {
-          u4 w[2];
+      if (wide) {
+        if (a.y_bf16) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) w[j >> 2][j & 3] = to_bf16x2(v[2 * j], v[2 * j + 1]);
-          reinterpret_cast<u4*>(y)[0] = w[0];
-          reinterpret_cast<u4*>(y)[1] = w[1];
+          for (int q = 0; q < 2; ++q) {
+            u4 w;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = to_bf16x2(v[8 * q + 2 * j], v[8 * q + 2 * j + 1]);
+            __builtin_amdgcn_raw_buffer_store_b128(w, ry, m < nrows ? o + 16 * q : kNowhere, 0, 0);
+          }
         } else {
 #pragma unroll
-          for (int j = 0; j < 16; ++j)
-            if (n0 + j < a.N) y[j] = to_bf16(v[j]);
+          for (int q = 0; q < 4; ++q) {
+            const u4 w = {__float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]), __float_as_uint(v[4 * q + 2]), __float_as_uint(v[4 * q + 3])};
+            __builtin_amdgcn_raw_buffer_store_b128(w, ry, m < nrows ? o + 16 * q : kNowhere, 0, 0);
+          }
         }
+      } else if (a.y_bf16) {
+#pragma unroll
+        for (int j = 0; j < 16; ++j) __builtin_amdgcn_raw_buffer_store_b16(to_bf16(v[j]), ry, m < nrows && n0 + j < a.N ? o + 2 * j : kNowhere, 0, 0);
       } else {
-        float* y = static_cast<float*>(a.Y) + o;
-        if (wide) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) reinterpret_cast<f4*>(y)[j] = f4{v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]};
-        } else {
-#pragma unroll
-          for (int j = 0; j < 16; ++j)
-            if (n0 + j < a.N) y[j] = v[j];
-        }
+        for (int j = 0; j < 16; ++j)
+          __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[j]), ry, m < nrows && n0 + j < a.N ? o + 4 * j : kNowhere, 0, 0);
       }
     }
   } else {
@@ -176,7 +276,7 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
 #pragma unroll
       for (int w = 0; w < 4; ++w) amax = max(amax, __float_as_uint(part[w * BM + m]));
       float scale, inv;
-      scale_of(amax, POW2, &scale, &inv);
+      scale_of(amax, a.pow2, &scale, &inv);
       if (m >= nrows) continue;
       u2 o;
       o[0] = pack4(acc[mi][0][0] * inv, acc[mi][0][1] * inv, acc[mi][0][2] * inv, acc[mi][0][3] * inv);
@@ -185,6 +285,7 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
       if (wn == 0 && f == 0) a.SH[(int64_t)col * a.ld_sh + row0 + m] = scale;
     }
   }
+#endif
 }
 
 template <int BM>
@@ -192,11 +293,13 @@ hipError_t go(const StampF8Gemm& a, hipStream_t st) {
   const int64_t tiles = a.offsets == nullptr ? ((int64_t)a.rows + BM - 1) / BM : (int64_t)a.rows / BM + (a.sets < a.rows ? a.sets : a.rows);
   const uint32_t grid = (uint32_t)(tiles * ((a.groups + 3) / 4));
   if (a.gated) {
-    if (a.pow2) k_f8_tiles<BM, true, true><<<grid, 512, 0, st>>>(a);
-    else k_f8_tiles<BM, false, true><<<grid, 512, 0, st>>>(a);
+    k_f8_tiles<BM, kWide, true><<<grid, 512, 0, st>>>(a);
+  } else if (a.wide_sums) {
+    k_f8_tiles<BM, kWide, false><<<grid, 512, 0, st>>>(a);
+  } else if (a.pow2) {
+    k_f8_tiles<BM, kPow2, false><<<grid, 512, 0, st>>>(a);
   } else {
-    if (a.pow2) k_f8_tiles<BM, true, false><<<grid, 512, 0, st>>>(a);
-    else k_f8_tiles<BM, false, false><<<grid, 512, 0, st>>>(a);
+    k_f8_tiles<BM, kScaled, false><<<grid, 512, 0, st>>>(a);
   }
   return hipGetLastError();
 }

@@ -2,7 +2,7 @@
 //
 // Bound by the weights' bytes: every byte is read once and feeds one matrix instruction per 16 rows.  So nothing is staged: a wave takes
 // some 16-place blocks of a group and a part of the depth, and reads its operand straight into registers in runs of 1 KB; the parts of
-// the depth are summed in LDS in a fixed order.
+// the depth are summed in LDS in a fixed order.  Always on the bf16 matrix instructions (f8_wide_sums): the pipe is idle most of the time.
 #include "stamp_fp8.h"
 
 namespace {
@@ -11,7 +11,7 @@ using namespace f8;
 constexpr int kWaves = 8;
 
 // MT: tiles of 16 rows held at once.  NB: blocks of 16 places per wave.  S: parts of the depth; kWaves / S waves lie side by side.
-template <int MT, int NB, int S, bool POW2, bool GATED>
+template <int MT, int NB, int S, bool GATED>
 __global__ __launch_bounds__(kWaves * 64) void k_f8_rows(StampF8Gemm a) {
   constexpr int kSide = kWaves / S;           // waves side by side
   constexpr int kPlaces = kSide * NB * 16;    // places of the workgroup
@@ -71,16 +71,13 @@ __global__ __launch_bounds__(kWaves * 64) void k_f8_rows(StampF8Gemm a) {
 #pragma unroll
           for (int b = 0; b < NB; ++b) {
             const float s = GATED && ((b0 + b) & 1) ? su : sw;
-            if constexpr (POW2) {
-              acc[mi][b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(B[b], X[mi], acc[mi][b], 0, 0, 0, (int)(__float_as_uint(s) >> 23), 0,
-                                                                           (int)(__float_as_uint(sx[mi]) >> 23));
-            } else {
-              const f4 z = {0, 0, 0, 0};
-              const f4 p = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(B[b], X[mi], z, 0, 0, 0, 0, 0, 0);
-              const float f = sx[mi] * s;
+            f4 p = {0, 0, 0, 0};
 #pragma unroll
-              for (int r = 0; r < 4; ++r) acc[mi][b][r] = __builtin_fmaf(p[r], f, acc[mi][b][r]);
-            }
+            for (int k = 0; k < 4; ++k)
+              p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(B[b][2 * k], B[b][2 * k + 1]), widen8(X[mi][2 * k], X[mi][2 * k + 1]), p, 0, 0, 0);
+            const float f = sx[mi] * s;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[mi][b][r] = __builtin_fmaf(p[r], f, acc[mi][b][r]);
           }
         }
       }
@@ -127,7 +124,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_f8_rows(StampF8Gemm a) {
         }
         amax = max8(amax);
         float scale, inv;
-        scale_of(amax, POW2, &scale, &inv);
+        scale_of(amax, a.pow2, &scale, &inv);
         u4 o;
 #pragma unroll
         for (int j = 0; j < 4; ++j) o[j] = pack4(hv[4 * j] * inv, hv[4 * j + 1] * inv, hv[4 * j + 2] * inv, hv[4 * j + 3] * inv);
@@ -144,8 +141,7 @@ template <int MT, int NB, int S, bool GATED>
 hipError_t go(const StampF8Gemm& a, hipStream_t st) {
   const int places = kWaves / S * NB * 16;
   const dim3 grid((a.groups * 64 + places - 1) / places, a.sets);
-  if (a.pow2) k_f8_rows<MT, NB, S, true, GATED><<<grid, kWaves * 64, 0, st>>>(a);
-  else k_f8_rows<MT, NB, S, false, GATED><<<grid, kWaves * 64, 0, st>>>(a);
+  k_f8_rows<MT, NB, S, GATED><<<grid, kWaves * 64, 0, st>>>(a);
   return hipGetLastError();
 }
 }  // namespace
