@@ -1,0 +1,514 @@
+"""8-bit floating point layers with block scales on the GPU: quantizer, dense and grouped products, router, experts' MLP, against the
+plain definition in 64 bits (fp8_reference.py)."""
+import numpy as np
+import pytest
+
+import fp8_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def st():
+    import paper_2510_26771_amd as st
+    st.load_library()
+    return st
+
+
+def _dt(name):
+    import torch
+    return {"f32": torch.float32, "bf16": torch.bfloat16}[name]
+
+
+def _code(st, name):
+    return {"f32": st.STAMP_F32, "bf16": st.STAMP_BF16}[name]
+
+
+def _gpu(a):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def _activations(rng, rows, d, dtype):
+    """fp32 values that `dtype` holds, outlier channels and rows of unlike size among them, and the same on the GPU."""
+    import torch
+    x = rng.standard_normal((rows, d)) * np.where(rng.random(d) < 0.03, 30.0, 1.0) * 2.0 ** rng.integers(-6, 7, (rows, 1))
+    t = torch.from_numpy(x.astype(np.float32)).to(_dt(dtype))
+    return t.float().numpy(), t.cuda()
+
+
+def _weights(rng, lead, n, d, pow2):
+    """Codes and scales as a checkpoint has them, magnitudes over the whole range."""
+    codes = rng.integers(0, 256, (*lead, n, d), dtype=np.uint8)
+    codes = np.where((codes & 0x7F) == 0x7F, 0x3A, codes).astype(np.uint8)
+    codes = np.where(rng.random(codes.shape) < 0.5, ref.encode(rng.standard_normal(codes.shape).astype(np.float32) * 40), codes)
+    shape = (*lead, -(-n // 128), -(-d // 128))
+    scales = np.ldexp(1.0, rng.integers(-12, -4, shape)) if pow2 else 2.0 ** rng.uniform(-12, -4, shape)
+    return codes, scales.astype(np.float32)
+
+
+def _strided(rows, cols, dtype, pad, offset=0):
+    """A [rows, cols] view with distant rows inside a buffer of a known pattern, and the buffer."""
+    import torch
+    buf = torch.full((rows * (cols + pad) + offset + 64,), -7.0, dtype=_dt(dtype), device="cuda")
+    return buf[offset:offset + rows * (cols + pad)].view(rows, cols + pad)[:, :cols], buf
+
+
+def _check(y, want, S, G, d_in, wide, bf16, what):
+    y = y.float().cpu().numpy().astype(np.float64)
+    tol = ref.slack(S, G, d_in, wide) + (2.0 ** -8 * np.abs(want) if bf16 else 2.0 ** -23 * np.abs(want)) + 1e-37
+    bad = np.abs(y - want) > tol
+    assert np.isfinite(y).all() and not bad.any(), (
+        f"{what}: {bad.sum()} of {bad.size} beyond the tolerance, worst {np.max(np.abs(y - want) / tol):.3g} times it, first at {np.argwhere(bad)[:1]}")
+
+
+# ---- the quantizer ----
+
+@pytest.mark.parametrize("pow2", [0, 1])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rows,d,pad", [(1, 1, 0), (3, 127, 0), (5, 128, 8), (17, 129, 3), (33, 1000, 0), (2, 4097, 1)])
+def test_codes_and_scales_are_the_definitions(st, rows, d, pad, dtype, pow2):
+    import torch
+    rng = np.random.default_rng(rows * 1000 + d)
+    x, xg = _activations(rng, rows, d, dtype)
+    special = [0.0, -0.0, 1e-45, 1e-38, -1.2e-36, 448.0, 449.0, 447.9, 7e-7, 3.3e38, -1e30]
+    for i, v in enumerate(special):  # blocks of few values: of one magnitude, of the smallest ones, zeros
+        x[i % rows, (131 * i) % d] = v
+    x[0, : min(d, 128)] = special[rows % len(special)] if d < 128 else 0.0
+    x = torch.from_numpy(x).to(_dt(dtype)).float().numpy()
+    view, _ = _strided(rows, d, dtype, pad)
+    view.copy_(torch.from_numpy(x))
+    desc = st.Fp8Desc(d_in=d, d_out=8, x_dtype=_code(st, dtype), scale_format=pow2)
+    w, ws = _weights(rng, (), 8, d, pow2)
+    plan = st.Fp8Plan(desc, _gpu(w), _gpu(ws))
+    codes, scales = plan.alloc_act_buffers(rows)
+    scales.fill_(-3.0)
+    plan.quantize_act(view, codes, scales)
+    want, wscale = ref.quantize(x, pow2)
+    got = codes.cpu().numpy()
+    assert np.array_equal(got, want), f"{np.count_nonzero(got != want)} codes differ"
+    assert np.array_equal(scales[:, :rows].cpu().numpy().T, wscale)
+    assert (scales[:, rows:] == -3.0).all()
+    plan.destroy()
+
+
+@pytest.mark.parametrize("pow2", [0, 1])
+def test_every_largest_magnitude_of_a_binade(st, pow2):
+    """Blocks whose largest magnitude is each bf16 value of a binade, and the first and last binades: the scale's rule at its edges."""
+    import torch
+    a = np.concatenate([np.float32(1.0 + np.arange(128) / 128.0), np.float32(2.0 ** -118) * np.float32(1.0 + np.arange(128) / 128.0),
+                        np.float32(2.0 ** 127) * np.float32(1.0 + np.arange(128) / 128.0), np.float32(2.0 ** -126) * np.arange(1, 9, dtype=np.float32) / 8])
+    rng = np.random.default_rng(5)
+    x = (a[:, None] * np.float32(1) * rng.uniform(-1, 1, (a.size, 128)).astype(np.float32)).astype(np.float32)
+    x[np.arange(a.size), rng.integers(0, 128, a.size)] = a
+    x = np.minimum(np.maximum(torch.from_numpy(x).to(torch.bfloat16).float().numpy(), -a[:, None]), a[:, None])
+    plan = st.Fp8Plan(st.Fp8Desc(d_in=128, d_out=1, x_dtype=st.STAMP_F32, scale_format=pow2), _gpu(np.zeros((1, 128), np.uint8)), _gpu(np.ones((1, 1), np.float32)))
+    codes, scales = plan.alloc_act_buffers(a.size)
+    plan.quantize_act(_gpu(x), codes, scales)
+    want, wscale = ref.quantize(x, pow2)
+    assert np.array_equal(scales[0, :a.size].cpu().numpy(), wscale[:, 0])
+    assert np.array_equal(codes.cpu().numpy(), want)
+    plan.destroy()
+
+
+@pytest.mark.parametrize("pow2", [0, 1])
+@pytest.mark.parametrize("rows", [5, 90, 700])
+@pytest.mark.parametrize("y", ["f32", "bf16"])
+def test_a_row_with_infinity_or_nan_is_nan_and_no_other(st, rows, y, pow2):
+    import torch
+    rng = np.random.default_rng(rows)
+    d, n = 300, 200
+    x, _ = _activations(rng, rows, d, "f32")
+    bad = {1: np.inf, 3: np.nan, rows - 1: -np.inf}
+    clean = x.copy()
+    for r, v in bad.items():
+        x[r, 7 * r % d] = v
+    w, ws = _weights(rng, (), n, d, pow2)
+    plan = st.Fp8Plan(st.Fp8Desc(d_in=d, d_out=n, x_dtype=st.STAMP_F32, y_dtype=_code(st, y), scale_format=pow2), _gpu(w), _gpu(ws))
+    a, b = (torch.empty((rows, n), dtype=_dt(y), device="cuda") for _ in range(2))
+    workspace = plan.alloc_workspace(rows)
+    plan.linear_forward(_gpu(x), a, workspace)
+    plan.linear_forward(_gpu(clean), b, workspace)
+    a, b = a.float().cpu().numpy(), b.float().cpu().numpy()
+    for r in range(rows):
+        if r in bad:
+            assert np.isnan(a[r]).all(), r
+        else:
+            assert np.array_equal(a[r], b[r]), r
+    assert np.isfinite(b).all()
+    plan.destroy()
+
+
+# ---- weights ----
+
+@pytest.mark.parametrize("pow2", [0, 1])
+@pytest.mark.parametrize("w_dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("out_by_in", [0, 1])
+@pytest.mark.parametrize("n,d,lead", [(1, 1, ()), (130, 257, ()), (70, 40, (3,)), (129, 128, (2, 2))])
+def test_weights_are_quantized_by_blocks(st, n, d, lead, out_by_in, w_dtype, pow2):
+    import torch
+    rng = np.random.default_rng(n + d)
+    w = rng.standard_normal((*lead, n, d)).astype(np.float32) * 2.0 ** rng.integers(-9, 9, (*lead, 1, 1)).astype(np.float32)
+    t = torch.from_numpy(w).to(_dt(w_dtype))
+    gated = len(lead) == 2
+    desc = st.Fp8Desc(d_in=d, d_out=n, experts=lead[0] if lead else 0, gated=int(gated), w_dtype=_code(st, w_dtype), w_is_out_by_in=out_by_in, scale_format=pow2)
+    plan = st.Fp8Plan(desc, (t if out_by_in else t.transpose(-1, -2)).contiguous().cuda())
+    codes, scales = plan.debug_weight_codes()
+    flat = t.float().numpy().reshape(-1, n, d)
+    for i, m in enumerate(flat):
+        c, s = ref.quantize_weights(m, pow2)
+        assert np.array_equal(scales.reshape(len(flat), *s.shape)[i], s)
+        assert np.array_equal(codes.reshape(len(flat), n, d)[i], c)
+    plan.destroy()
+
+
+def test_given_codes_come_back(st):
+    rng = np.random.default_rng(3)
+    w, ws = _weights(rng, (2, 2), 75, 200, 0)
+    plan = st.Fp8Plan(st.Fp8Desc(d_in=200, d_out=75, experts=2, gated=1), _gpu(w), _gpu(ws))
+    codes, scales = plan.debug_weight_codes()
+    assert np.array_equal(codes, w) and np.array_equal(scales, ws)
+    plan.destroy()
+
+
+# ---- the product ----
+
+# every kernel, its edges: one row, ends inside a tile of 16, 64, 128, 256 rows, more than one tile; widths below, at and above a
+# group of 64 and a tile of 256 columns; depths of one channel, one block, an odd and an even number of blocks, many
+SIZES = [(1, 1, 1), (1, 128, 64), (1, 5000, 77), (2, 129, 300), (15, 640, 33), (16, 256, 512), (17, 1000, 65), (32, 384, 257), (33, 130, 1000),
+         (48, 8500, 64), (64, 512, 256), (65, 896, 255), (100, 1100, 520), (127, 256, 1), (129, 384, 700), (200, 2000, 320), (257, 640, 2048), (520, 128, 129),
+         (700, 1281, 513), (1024, 512, 1536), (1300, 260, 4608)]
+
+
+@pytest.mark.parametrize("rows,d,n", SIZES)
+@pytest.mark.parametrize("x,y,pow2,bias", [("bf16", "bf16", 0, 0), ("f32", "f32", 0, 1), ("bf16", "f32", 1, 0), ("f32", "bf16", 1, 1)])
+def test_linear_against_the_definition(st, rows, d, n, x, y, pow2, bias):
+    import torch
+    rng = np.random.default_rng(rows * 31 + d * 7 + n)
+    xv, xg = _activations(rng, rows, d, x)
+    w, ws = _weights(rng, (), n, d, pow2)
+    b = rng.standard_normal(n).astype(np.float32) * 100 if bias else None
+    desc = st.Fp8Desc(d_in=d, d_out=n, x_dtype=_code(st, x), y_dtype=_code(st, y), scale_format=pow2)
+    plan = st.Fp8Plan(desc, _gpu(w), _gpu(ws), _gpu(b) if bias else None)
+    # rows apart, off the 16-byte grid for some sizes
+    pad, off = [(0, 0), (8, 0), (3, 1), (5, 8)][(rows + n) % 4]
+    X, _ = _strided(rows, d, x, pad, off)
+    X.copy_(xg)
+    Y, buf = _strided(rows, n, y, pad, off)
+    workspace = plan.alloc_workspace(rows)
+    plan.linear_forward(X, Y, workspace)
+    codes, scales = ref.quantize(xv, pow2)
+    want, S, G = ref.product(codes, scales, w, ws)
+    wide = y == "f32" or plan.route(rows) == "rows"
+    if bias:
+        want, S = want + b, S + np.abs(b)
+    _check(Y, want, S, G, d, wide, y == "bf16", f"{plan.route(rows)}")
+    first = Y.clone()
+    Y.fill_(-7.0)
+    assert (buf == -7.0).all(), "something outside of Y was written"
+    # the same from the quantizer's own call, and again: bit for bit
+    c, s = plan.alloc_act_buffers(rows)
+    plan.quantize_act(X, c, s)
+    plan.linear_forward_q(c, s, Y, workspace)
+    assert torch.equal(Y, first)
+    plan.destroy()
+
+
+def test_every_kernel_is_reached(st):
+    plan = st.Fp8Plan(st.Fp8Desc(d_in=512, d_out=1536), _gpu(np.zeros((1536, 512), np.uint8)), _gpu(np.ones((12, 4), np.float32)))
+    assert {plan.route(rows) for rows, _, _ in SIZES} == {"rows", "tiles_64", "tiles_128", "tiles_256"}
+    plan.destroy()
+
+
+def test_offsets_beyond_32_bits(st):
+    """Rows of X and Y so far apart that the last ones lie beyond 2^32 bytes."""
+    import torch
+    rng = np.random.default_rng(8)
+    rows, d, n, ld = 1100, 256, 320, 1 << 21
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("needs 24 GB of free GPU memory")
+    xv, xg = _activations(rng, rows, d, "bf16")
+    X = torch.empty(rows * ld, dtype=torch.bfloat16, device="cuda").view(rows, ld)[:, :d]
+    Y = torch.empty(rows * ld, dtype=torch.float32, device="cuda").view(rows, ld)[:, :n]
+    X.copy_(xg)
+    w, ws = _weights(rng, (), n, d, 0)
+    for y in ("f32", "bf16"):
+        plan = st.Fp8Plan(st.Fp8Desc(d_in=d, d_out=n, y_dtype=_code(st, y)), _gpu(w), _gpu(ws))
+        Yv = Y if y == "f32" else torch.empty(rows * ld, dtype=torch.bfloat16, device="cuda").view(rows, ld)[:, :n]
+        plan.linear_forward(X, Yv, plan.alloc_workspace(rows))
+        want, S, G = ref.product(*ref.quantize(xv, 0), w, ws)
+        _check(Yv, want, S, G, d, y == "f32", y == "bf16", y)
+        plan.destroy()
+
+
+# ---- by expert ----
+
+GROUPED = [([0, 0, 1], 1, 128, 64), ([5], 5, 200, 130), ([0, 33, 1, 0, 16, 17], 67, 640, 300), ([3] * 40, 120, 384, 70), ([0, 0, 300, 0], 300, 256, 257),
+           ([70, 129, 0, 64, 65, 1], 329, 1000, 520), ([256, 0, 257, 511, 1], 1025, 512, 320), ([600, 700, 0], 1310, 390, 600), ([0, 0, 0], 40, 128, 32),
+           ([1] * 130 + [200], 330, 256, 96), ([2, 0, 40, 90], 150, 1152, 256)]
+
+
+@pytest.mark.parametrize("case", range(len(GROUPED)))
+@pytest.mark.parametrize("x,y,pow2,bias", [("bf16", "bf16", 0, 1), ("f32", "f32", 1, 0), ("bf16", "bf16", 1, 0), ("f32", "f32", 0, 1)])
+def test_grouped_against_the_definition(st, case, x, y, pow2, bias):
+    counts, rows, d, n = GROUPED[case]
+    rng = np.random.default_rng(case)
+    E, total = len(counts), sum(counts)
+    xv, xg = _activations(rng, rows, d, x)
+    w, ws = _weights(rng, (E,), n, d, pow2)
+    b = rng.standard_normal((E, n)).astype(np.float32) * 100 if bias else None
+    plan = st.Fp8Plan(st.Fp8Desc(d_in=d, d_out=n, experts=E, x_dtype=_code(st, x), y_dtype=_code(st, y), scale_format=pow2), _gpu(w), _gpu(ws),
+                      _gpu(b) if bias else None)
+    Y, buf = _strided(rows, n, y, case % 3 * 4, 8 * (case % 2))
+    offsets = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+    plan.grouped_forward(xg, _gpu(offsets), Y, plan.alloc_workspace(rows))
+    codes, scales = ref.quantize(xv, pow2)
+    wide = y == "f32" or plan.route(rows) == "rows"
+    for e in range(E):
+        lo, hi = offsets[e], offsets[e + 1]
+        if lo == hi:
+            continue
+        want, S, G = ref.product(codes[lo:hi], scales[lo:hi], w[e], ws[e])
+        if bias:
+            want, S = want + b[e], S + np.abs(b[e])
+        _check(Y[lo:hi], want, S, G, d, wide, y == "bf16", f"expert {e}, {plan.route(rows)}")
+    Y[:total].fill_(-7.0)
+    assert (buf == -7.0).all(), "a row behind the last expert's, or something outside of Y, was written"
+    plan.destroy()
+
+
+@pytest.mark.parametrize("offsets", [[-5, 10, 20, 1000], [0, 50, 20, 90], [100, 200, 300, 400], [2 ** 31 - 1, -2 ** 31, 0, 7], [0, 90, 0, 90]])
+@pytest.mark.parametrize("rows", [90, 900])
+def test_offsets_that_break_the_rules_stay_in_bounds(st, offsets, rows):
+    import torch
+    rng = np.random.default_rng(1)
+    _, xg = _activations(rng, rows, 256, "bf16")
+    w, ws = _weights(rng, (3,), 200, 256, 0)
+    plan = st.Fp8Plan(st.Fp8Desc(d_in=256, d_out=200, experts=3), _gpu(w), _gpu(ws))
+    Y, buf = _strided(rows, 200, "bf16", 8, 8)
+    plan.grouped_forward(xg, torch.tensor(offsets, dtype=torch.int32, device="cuda"), Y, plan.alloc_workspace(rows))
+    torch.cuda.synchronize()
+    Y.fill_(-7.0)
+    assert (buf == -7.0).all()
+    plan.destroy()
+
+
+# ---- the router ----
+
+def _logits(rng, tokens, experts, dtype, kind):
+    import torch
+    l = rng.standard_normal((tokens, experts)).astype(np.float32)
+    if kind == "masked":
+        l[rng.random(l.shape) < 0.7] = -np.inf
+        l[rng.random(l.shape) < 0.1] = np.nan
+        l[tokens // 2] = -np.inf
+        l[0] = np.nan
+    if kind == "ties":
+        l = rng.integers(-1, 2, l.shape).astype(np.float32) * np.where(rng.random(l.shape) < 0.5, -1, 1).astype(np.float32)  # -0 among them
+    if kind == "extreme":
+        low = np.float32(np.finfo(np.float32).min)
+        l[rng.random(l.shape) < 0.3] = low
+        l[rng.random(l.shape) < 0.1] = np.float32(3e38)
+        l[tokens // 3] = low
+        l[tokens // 2, : experts // 2 + 1] = np.inf
+    t = torch.from_numpy(l).to(_dt(dtype))
+    return t.float().numpy(), t.cuda()
+
+
+@pytest.mark.parametrize("kind", ["plain", "masked", "ties", "extreme"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("renormalize", [0, 1])
+@pytest.mark.parametrize("tokens,experts,top_k", [(1, 1, 1), (1, 8, 2), (3, 5, 8), (64, 64, 6), (128, 65, 4), (129, 130, 3), (700, 256, 8), (260, 1000, 32), (1000, 16, 1),
+                                                  (300, 300, 9)])
+def test_router_against_the_definition(st, tokens, experts, top_k, renormalize, dtype, kind):
+    import torch
+    rng = np.random.default_rng(tokens + experts)
+    l, lg = _logits(rng, tokens, experts, dtype, kind)
+    wide = torch.full((tokens, experts + 3), 9e9, dtype=lg.dtype, device="cuda")
+    wide[:, :experts] = lg
+    r = st.Routing(tokens, experts, top_k)
+    for t in (r.ids, r.offsets, r.token_of_row, r.row_of_slot):
+        t.fill_(-77)
+    st.route_topk(wide[:, :experts], r, renormalize=renormalize)
+    ids, weights, offsets, token, row = ref.route(l, top_k, renormalize)
+    assert np.array_equal(r.ids.cpu().numpy(), ids)
+    assert np.array_equal(r.offsets.cpu().numpy(), offsets)
+    assert np.array_equal(r.token_of_row.cpu().numpy(), token)
+    assert np.array_equal(r.row_of_slot.cpu().numpy(), row)
+    # exp of a difference of up to 16 (rounded: 16 * 2^-24), its own error, and the sum's roundings
+    w = r.weights.cpu().numpy().astype(np.float64)
+    assert np.all(np.abs(w - weights) <= (32 + experts / 64 + 8) * 2.0 ** -23 * weights + 1e-37)
+
+
+def test_router_without_tokens(st):
+    r = st.Routing(0, 7, 2)
+    import torch
+    r.offsets.fill_(-1)
+    st.route_topk(torch.empty((0, 7), device="cuda"), r)
+    assert r.offsets.tolist() == [0] * 8
+
+
+# ---- the experts ----
+
+def _experts_reference(x, l, w_up, s_up, w_down, s_down, top_k, renormalize, pow2, bias):
+    """(Y, slack) in 64 bits.  A code of h may be its neighbour where h, off by its own sums' slack, lies that near to the middle of two
+    codes; the slack of Y then has that step times the weight."""
+    ids, weights, offsets, token, row = ref.route(l, top_k, renormalize)
+    t, d = x.shape
+    ff = w_up.shape[2]
+    codes, scales = ref.quantize(x, pow2)
+    y, tol = np.zeros((t, w_down.shape[1])), np.zeros((t, w_down.shape[1]))
+    for e in range(len(offsets) - 1):
+        rows = np.arange(offsets[e], offsets[e + 1])
+        if not rows.size:
+            continue
+        tk = token[rows]
+        g, gS, gG = ref.product(codes[tk], scales[tk], w_up[e, 0], s_up[e, 0])
+        u, uS, uG = ref.product(codes[tk], scales[tk], w_up[e, 1], s_up[e, 1])
+        sg = 1 / (1 + np.exp(-np.clip(g, -700, 700)))
+        h = g * sg * u
+        # silu's slope is at most 1.1; its evaluation is good to 2^-20
+        dh = 1.1 * ref.slack(gS, gG, d, True) * np.abs(u) + np.abs(g * sg) * ref.slack(uS, uG, d, True) + 2.0 ** -20 * np.abs(h)
+        hq, hs = ref.quantize(h.astype(np.float32), pow2)
+        v = ref.values(hq, hs, ff)
+        sc = np.repeat(hs.astype(np.float64), 128, 1)[:, :ff]
+        lo, hi = (ref.values(ref.quantize_like(h + s * (dh + 2.0 ** -21 * np.abs(h)), sc), np.ones((len(h), hq.shape[1] // 128)), ff) * sc for s in (-1, 1))
+        step = np.maximum(np.abs(hi - v), np.abs(lo - v)) + 2.0 ** -20 * np.abs(v)
+        # pow2 scales double where the largest magnitude passes 448: the tests' inputs keep clear of that (asserted)
+        if pow2:
+            a = np.abs(np.pad(h, ((0, 0), (0, -ff % 128)))).reshape(len(h), -1, 128).max(-1)
+            near = np.abs(a / (448 * hs.astype(np.float64)) - 1) < 1e-5
+            assert not (near & (a > 0)).any()
+        r, S, G = ref.product(hq, hs, w_down[e], s_down[e])
+        wv = np.abs(ref.weight_values(w_down[e], s_down[e]))
+        dr = ref.slack(S, G, ff, False) + step @ wv.T
+        if bias is not None:
+            r = r + bias[e]
+        for i, rr in enumerate(rows):
+            tt = token[rr]
+            j = np.flatnonzero(row[tt] == rr)[0]
+            y[tt] += weights[tt, j] * r[i]
+            tol[tt] += weights[tt, j] * (dr[i] + 2.0 ** -8 * np.abs(r[i])) + 2.0 ** -18 * np.abs(weights[tt, j] * r[i])
+    return y, tol
+
+
+@pytest.mark.parametrize("tokens,experts,top_k,d,ff,x,y,pow2,bias,masked", [
+    (1, 4, 2, 128, 128, "bf16", "bf16", 0, 0, 0), (1, 1, 1, 40, 24, "f32", "f32", 0, 1, 0), (4, 16, 6, 256, 200, "bf16", "bf16", 0, 0, 0),
+    (33, 8, 3, 300, 384, "bf16", "f32", 1, 1, 1), (70, 5, 2, 257, 129, "f32", "bf16", 0, 1, 1), (200, 4, 4, 384, 256, "bf16", "bf16", 1, 0, 0),
+    (300, 3, 2, 640, 520, "bf16", "bf16", 0, 1, 1), (700, 2, 2, 256, 384, "bf16", "bf16", 0, 0, 1), (600, 1, 1, 512, 1100, "bf16", "f32", 0, 0, 0),
+    (5, 40, 8, 512, 1000, "bf16", "bf16", 1, 0, 1)])
+def test_experts_against_the_definition(st, tokens, experts, top_k, d, ff, x, y, pow2, bias, masked):
+    import torch
+    rng = np.random.default_rng(tokens * 7 + experts)
+    l, lg = _logits(rng, tokens, experts, "f32", "masked" if masked else "plain")
+    xv, xg = _activations(rng, tokens, d, x)
+    w_up, s_up = _weights(rng, (experts, 2), ff, d, pow2)
+    w_down, s_down = _weights(rng, (experts,), d, ff, pow2)
+    s_up = (s_up * np.float32(2.0 ** -6)).astype(np.float32)  # gates of a size where silu is curved
+    b = rng.standard_normal((experts, d)).astype(np.float32) if bias else None
+    up = st.Fp8Plan(st.Fp8Desc(d_in=d, d_out=ff, experts=experts, gated=1, x_dtype=_code(st, x), scale_format=pow2), _gpu(w_up), _gpu(s_up))
+    down = st.Fp8Plan(st.Fp8Desc(d_in=ff, d_out=d, experts=experts, y_dtype=_code(st, y), scale_format=pow2), _gpu(w_down), _gpu(s_down), _gpu(b) if bias else None)
+    r = st.Routing(tokens, experts, top_k)
+    st.route_topk(lg, r)
+    Y, buf = _strided(tokens, d, y, 3, 1)
+    ws = st.experts_workspace(up, down, tokens, top_k)
+    ws.fill_(255)  # NaN wherever something is read that was not written
+    st.experts_forward(up, down, xg, r, Y, ws)
+    want, tol = _experts_reference(xv, l, w_up, s_up, w_down, s_down, top_k, 1, pow2, b)
+    got = Y.float().cpu().numpy().astype(np.float64)
+    tol = tol + 2.0 ** -8 * np.abs(want) + 1e-37
+    assert np.isfinite(got).all()
+    bad = np.abs(got - want) > tol
+    assert not bad.any(), f"{bad.sum()} of {bad.size}, worst {np.max(np.abs(got - want) / tol):.3g}"
+    first = Y.clone()
+    st.experts_forward(up, down, xg, r, Y, ws)
+    assert torch.equal(first, Y)
+    Y.fill_(-7.0)
+    assert (buf == -7.0).all()
+    up.destroy()
+    down.destroy()
+
+
+# ---- streams, graphs, refusals ----
+
+def test_on_another_stream_and_in_a_graph(st):
+    """Router and experts captured once, replayed on new inputs between eager calls."""
+    import torch
+    rng = np.random.default_rng(4)
+    T, E, k, d, ff = 150, 6, 2, 256, 256
+    w_up, s_up = _weights(rng, (E, 2), ff, d, 0)
+    w_down, s_down = _weights(rng, (E,), d, ff, 0)
+    up = st.Fp8Plan(st.Fp8Desc(d_in=d, d_out=ff, experts=E, gated=1), _gpu(w_up), _gpu(s_up))
+    down = st.Fp8Plan(st.Fp8Desc(d_in=ff, d_out=d, experts=E), _gpu(w_down), _gpu(s_down))
+    X, L = torch.empty((T, d), dtype=torch.bfloat16, device="cuda"), torch.empty((T, E), device="cuda")
+    Y, r, ws = torch.empty_like(X), st.Routing(T, E, k), st.experts_workspace(up, down, T, k)
+    Y2, r2, ws2 = torch.empty_like(X), st.Routing(T, E, k), st.experts_workspace(up, down, T, k)
+    X.normal_()
+    L.normal_()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        st.route_topk(L, r)
+        st.experts_forward(up, down, X, r, Y, ws)
+    torch.cuda.current_stream().wait_stream(side)
+    st.route_topk(L, r2)
+    st.experts_forward(up, down, X, r2, Y2, ws2)
+    assert torch.equal(Y, Y2)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        st.route_topk(L, r)
+        st.experts_forward(up, down, X, r, Y, ws)
+    for i in range(3):
+        X.normal_()
+        L.normal_()
+        Y.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        st.route_topk(L, r2)
+        st.experts_forward(up, down, X, r2, Y2, ws2)
+        assert torch.equal(Y, Y2) and torch.equal(r.ids, r2.ids), i
+    up.destroy()
+    down.destroy()
+
+
+def test_refusals(st):
+    import torch
+    d, n = 256, 128
+    w, ws = _weights(np.random.default_rng(0), (), n, d, 0)
+    plan = st.Fp8Plan(st.Fp8Desc(d_in=d, d_out=n), _gpu(w), _gpu(ws))
+    grouped = st.Fp8Plan(st.Fp8Desc(d_in=d, d_out=n, experts=2), _gpu(np.stack([w, w])), _gpu(np.stack([ws, ws])))
+    gated = st.Fp8Plan(st.Fp8Desc(d_in=d, d_out=n, experts=2, gated=1), _gpu(np.stack([w] * 4)), _gpu(np.stack([ws] * 4)))
+    X, Y = torch.zeros((4, d), dtype=torch.bfloat16, device="cuda"), torch.zeros((4, n), dtype=torch.bfloat16, device="cuda")
+    wsp, off = plan.alloc_workspace(4), torch.zeros(3, dtype=torch.int32, device="cuda")
+
+    def status(code, f):
+        with pytest.raises(st.StampError) as e:
+            f()
+        assert e.value.status == code
+    status(4, lambda: plan.linear_forward(X, Y, wsp[:64]))                 # workspace too small
+    status(4, lambda: plan.linear_forward(X, Y, torch.empty(wsp.numel() + 300, dtype=torch.uint8, device="cuda")[1:]))  # misaligned
+    status(3, lambda: grouped.linear_forward(X, Y, wsp))                   # a plan by expert has no dense call
+    status(3, lambda: gated.grouped_forward(X, off, Y, wsp))               # a gated plan serves experts_forward alone
+    for bad in (lambda: plan.linear_forward(X[:, :-1], Y, wsp), lambda: plan.linear_forward(X.float(), Y, wsp), lambda: plan.linear_forward(X, Y[:3], wsp),
+                lambda: plan.linear_forward(X.cpu(), Y, wsp), lambda: plan.linear_forward(X.t(), Y, wsp),
+                lambda: grouped.grouped_forward(X, off[:2], Y, wsp), lambda: grouped.grouped_forward(X, off.long(), Y, wsp),
+                lambda: st.route_topk(torch.zeros((4, 3), device="cuda"), st.Routing(4, 2, 1)),
+                lambda: st.Fp8Plan(st.Fp8Desc(d_in=d, d_out=n), _gpu(w[:-1]), _gpu(ws)), lambda: st.Fp8Plan(st.Fp8Desc(d_in=d, d_out=n), _gpu(w), _gpu(ws[:, :1])),
+                lambda: st.Routing(4, 2000, 1), lambda: st.Routing(4, 8, 40)):
+        with pytest.raises(ValueError):
+            bad()
+    status(1, lambda: st.Fp8Plan(st.Fp8Desc(d_in=d, d_out=n), _gpu(w)))    # codes without scales
+    status(3, lambda: st.Fp8Plan(st.Fp8Desc(d_in=d, d_out=n, scale_format=1), _gpu(w), _gpu(np.full_like(ws, 0.3))))  # no powers of two
+    for s in (0.0, -0.5, np.inf, np.nan, 2.0 ** -140):
+        bad = np.full_like(ws, 0.5)
+        bad[0, 1] = s
+        status(3, lambda: st.Fp8Plan(st.Fp8Desc(d_in=d, d_out=n, scale_format=1), _gpu(w), _gpu(bad)))
+    r, small = st.Routing(4, 2, 1), torch.empty(256, dtype=torch.uint8, device="cuda")
+    status(4, lambda: st.experts_forward(gated, st.Fp8Plan(st.Fp8Desc(d_in=n, d_out=d, experts=2), _gpu(np.stack([w.T, w.T])), _gpu(np.stack([ws.T, ws.T]))), X, r,
+                                         torch.zeros_like(X), small))
+    status(3, lambda: st.experts_forward(grouped, grouped, X, r, Y, small))
+    # nothing to do
+    plan.linear_forward(X[:0], Y[:0], wsp)
+    grouped.grouped_forward(X[:0], off, Y[:0], wsp)
+    for p in (plan, grouped, gated):
+        p.destroy()
