@@ -26,7 +26,7 @@ EXPORTS = ["stamp_plan_create", "stamp_plan_destroy", "stamp_plan_workspace_byte
            "stamp_debug_gemm_acc", "stamp_debug_weight_codes", "stamp_debug_run_stage", "stamp_plan_set_unfused", "stamp_plan_set_gemm_engine",
            "stamp_debug_set_choice", "stamp_debug_routes", "stamp_debug_layout", "stamp_debug_mfma_rate", "stamp_status_string",
            "stamp_fp8_plan_create", "stamp_fp8_plan_destroy", "stamp_fp8_workspace_bytes", "stamp_fp8_quantize_act", "stamp_fp8_linear_forward",
-           "stamp_fp8_linear_forward_q", "stamp_fp8_grouped_forward", "stamp_fp8_debug_weight_codes", "stamp_fp8_debug_route",
+           "stamp_fp8_linear_forward_q", "stamp_fp8_grouped_forward", "stamp_fp8_debug_weight_codes", "stamp_fp8_debug_route", "stamp_fp8_debug_set_route",
            "stamp_route_workspace_bytes", "stamp_route_topk", "stamp_experts_workspace_bytes", "stamp_experts_forward"]
 
 # stamp_choice_t and stamp_route_t (include/stamp.h)

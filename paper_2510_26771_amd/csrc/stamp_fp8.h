@@ -27,6 +27,7 @@ struct stamp_fp8_plan {
   int32_t Kb, Kp;      // blocks of the input channels, bytes of a row of codes
   int32_t groups;      // of a set
   int32_t nblk;        // blocks of 128 output columns of one matrix
+  int32_t forced;      // stamp_fp8_debug_set_route
   uint8_t* w_dev;      // operand image
   float* sw_dev;       // [sets][2 if gated][nblk][Kb]
   float* bias_dev;     // [sets][d_out] or nullptr
@@ -53,6 +54,7 @@ struct StampF8Gemm {
   const float* SW;
   const float* bias;
   int32_t sets, groups, Kb, nblk, N, pow2, gated, y_bf16;
+  int32_t forced;          // stamp_fp8_route_t, 0: by rule
   int32_t wide_sums;       // products on the bf16 matrix instructions (f8_wide_sums)
   void* Y;                 // rows of N values; gated: codes [rows][ld_y] and scales [ld_y / 128][ld_sh]
   int64_t ld_y;
@@ -144,39 +146,50 @@ __device__ __forceinline__ void rows_of(const StampF8Gemm& a, int e, int* lo, in
   *hi = min(max(a.offsets[e + 1], l), a.rows);
 }
 
-// The tile-th tile of BM rows, counted over the sets: its set and rows; false where there is none.  Every wave finds it by itself.
-__device__ __forceinline__ bool find_tile(const StampF8Gemm& a, int BM, int tile, int* set, int* row0, int* nrows) {
-  if (a.offsets == nullptr) {
-    *set = 0;
-    *row0 = tile * BM;
-    *nrows = min(BM, a.rows - *row0);
-    return *nrows > 0;
-  }
+// Tiles of BM rows, counted over the sets.  Every wave counts by itself.
+__device__ __forceinline__ int tiles_of(const StampF8Gemm& a, int e, int BM, int* lo, int* hi) {
+  *lo = *hi = 0;
+  if (e < a.sets) rows_of(a, e, lo, hi);
+  return (*hi - *lo + BM - 1) / BM;
+}
+__device__ __forceinline__ int wave_scan(int v) {  // inclusive
   const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int o = __shfl_up(v, d);
+    if (lane >= d) v += o;
+  }
+  return v;
+}
+__device__ __forceinline__ int count_tiles(const StampF8Gemm& a, int BM) {
+  if (a.offsets == nullptr) return (a.rows + BM - 1) / BM;
+  int n = 0, lo, hi;
+  for (int e = threadIdx.x & 63; e < a.sets; e += 64) n += tiles_of(a, e, BM, &lo, &hi);
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) n += __shfl_xor(n, d);
+  return __builtin_amdgcn_readfirstlane(n);
+}
+// set and rows of a tile that there is
+__device__ __forceinline__ void find_tile(const StampF8Gemm& a, int BM, int tile, int* set, int* row0, int* nrows) {
+  *set = 0;
+  *row0 = tile * BM;
+  *nrows = min(BM, a.rows - *row0);
+  if (a.offsets == nullptr) return;
   int base = 0;
   for (int e0 = 0; e0 < a.sets; e0 += 64) {
-    int lo = 0, hi = 0;
-    if (e0 + lane < a.sets) rows_of(a, e0 + lane, &lo, &hi);
-    int incl = (hi - lo + BM - 1) / BM;
-    const int own = incl;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int o = __shfl_up(incl, d);
-      if (lane >= d) incl += o;
-    }
+    int lo, hi;
+    const int own = tiles_of(a, e0 + (threadIdx.x & 63), BM, &lo, &hi), incl = wave_scan(own);
     const uint64_t past = __ballot(base + incl > tile);
     if (past != 0) {
-      const int src = __builtin_ctzll(past);
-      const int first = base + __shfl(incl - own, src);
+      const int src = __builtin_ctzll(past), first = base + __shfl(incl - own, src);
       const int l = __shfl(lo, src), h = __shfl(hi, src);
       *set = __builtin_amdgcn_readfirstlane(e0 + src);
       *row0 = __builtin_amdgcn_readfirstlane(l + (tile - first) * BM);
       *nrows = __builtin_amdgcn_readfirstlane(min(BM, h - *row0));
-      return true;
+      return;
     }
     base += __shfl(incl, 63);
   }
-  return false;
 }
 
 typedef __bf16 b2 __attribute__((ext_vector_type(2)));

@@ -42,11 +42,12 @@ StampF8Gemm gemm_args(const stamp_fp8_plan* p) {
   a.gated = p->desc.gated;
   a.y_bf16 = p->desc.y_dtype == STAMP_BF16;
   a.wide_sums = f8_wide_sums(a);
+  a.forced = p->forced;
   return a;
 }
 
 hipError_t product(const StampF8Gemm& a, hipStream_t st) {
-  switch (stamp_f8_route(a.sets, a.groups, a.Kb, a.rows, a.wide_sums)) {
+  switch (a.forced ? a.forced : stamp_f8_route(a.sets, a.groups, a.Kb, a.rows, a.wide_sums)) {
     case STAMP_FP8_ROUTE_ROWS: return stamp_launch_f8_rows(a, st);
     case STAMP_FP8_ROUTE_TILES_64: return stamp_launch_f8_tiles(a, 64, st);
     case STAMP_FP8_ROUTE_TILES_128: return stamp_launch_f8_tiles(a, 128, st);
@@ -163,6 +164,7 @@ stamp_status_t stamp_fp8_plan_create(const stamp_fp8_desc_t* desc, const void* W
   const int per_group = desc->gated ? kF8Group / 2 : kF8Group;
   p->groups = (desc->d_out + per_group - 1) / per_group;
   p->nblk = (desc->d_out + kF8Block - 1) / kF8Block;
+  p->forced = 0;
   p->w_dev = nullptr;
   p->sw_dev = p->bias_dev = nullptr;
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
@@ -356,7 +358,15 @@ stamp_status_t stamp_fp8_debug_weight_codes(const stamp_fp8_plan_t* p, uint8_t* 
 
 int32_t stamp_fp8_debug_route(const stamp_fp8_plan_t* p, int32_t rows) {
   if (p == nullptr || rows < 0) return 0;
-  return stamp_f8_route(p->sets, p->groups, p->Kb, rows, gemm_args(p).wide_sums);
+  return p->forced ? p->forced : stamp_f8_route(p->sets, p->groups, p->Kb, rows, gemm_args(p).wide_sums);
+}
+
+stamp_status_t stamp_fp8_debug_set_route(stamp_fp8_plan_t* p, int32_t route) {
+  if (p == nullptr) return STAMP_ERR_NULL;
+  if (route < 0 || route > STAMP_FP8_ROUTE_TILES_256) return STAMP_ERR_SHAPE;
+  if (route == STAMP_FP8_ROUTE_TILES_256 && gemm_args(p).wide_sums) return STAMP_ERR_UNSUPPORTED;
+  p->forced = route;
+  return STAMP_OK;
 }
 
 }  // extern "C"

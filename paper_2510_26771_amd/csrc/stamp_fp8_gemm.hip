@@ -43,9 +43,16 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
   __shared__ __attribute__((aligned(1024))) uint8_t stage1[kStageA + kStageB + BM * 4];
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int wm = wave >> 2, wn = wave & 3;
-  const int ncol = (a.groups + 3) / 4, col = blockIdx.x % ncol;  // consecutive workgroups share the rows' operand
+  // Workgroups go to the 8 XCDs in turn: an XCD takes a run of the tiles in an order in which 32 neighbours (its CUs) are 8 x 4 tiles, so
+  // that its L2 has 12 panels of operands to fetch for them and not 33.
+  constexpr int kXcd = 8, kBand = 8;
+  const int ncol = (a.groups + 3) / 4, nrow = count_tiles(a, BM), ntile = nrow * ncol, run = (ntile + kXcd - 1) / kXcd;
+  const int order = (int)(blockIdx.x % kXcd) * run + (int)(blockIdx.x / kXcd);
+  if ((int)(blockIdx.x / kXcd) >= run || order >= ntile) return;
+  const int band = order / (kBand * ncol), in_band = order - band * kBand * ncol, height = min(kBand, nrow - band * kBand);
+  const int col = in_band / height;
   int set, row0, nrows;
-  if (!find_tile(a, BM, blockIdx.x / ncol, &set, &row0, &nrows)) return;
+  find_tile(a, BM, band * kBand + in_band % height, &set, &row0, &nrows);
   set = __builtin_amdgcn_readfirstlane(set);
   row0 = __builtin_amdgcn_readfirstlane(row0);
   nrows = __builtin_amdgcn_readfirstlane(nrows);
@@ -66,16 +73,18 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
   const __amdgpu_buffer_rsrc_t rb = buffer(a.W + ((size_t)set * a.groups + g0) * Kb * kF8GroupBytes);
   const uint32_t soff = (uint32_t)min(t, nrows - 1);
 
-  auto load = [&](uint8_t* S, int kb) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < LA; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (LdsPtr)(S + i * 8192 + wave * 1024), 16, aoff[i], kb * 128, 0, 0);
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (LdsPtr)(S + kStageA + i * 8192 + wave * 1024), 16, t * 16, boff[i] + kb * kF8GroupBytes, 0, 0);
-    if (wave < BM / 64)
+  // the q-th of a stage's loads; behind the last block of channels that one again, which nobody reads
+  constexpr int kLoads = 4 + LA + 1;
+  auto load = [&](uint8_t* S, int kb, int q) __attribute__((always_inline)) {
+    kb = min(kb, Kb - 1);
+    if (q < 4) {
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (LdsPtr)(S + kStageA + q * 8192 + wave * 1024), 16, t * 16, boff[q] + kb * kF8GroupBytes, 0, 0);
+    } else if (q < 4 + LA) {
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (LdsPtr)(S + (q - 4) * 8192 + wave * 1024), 16, aoff[q - 4], kb * 128, 0, 0);
+    } else if (wave < BM / 64) {
       __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(a.SA + row0 + (int64_t)kb * a.ld_sa + soff),
                                        (LdsPtr)(S + kStageA + kStageB + wave * 256), 4, 0, 0);
+    }
   };
 
   f4 acc[MI][4], P[4];
@@ -140,7 +149,6 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
         sn = read_s(S, mi + 1);
       } else {
         turn();
-        if (kb + 2 < Kb) load(S, kb + 2);
         Xn = read_x(N, 0);
         sn = read_s(N, 0);
       }
@@ -169,7 +177,15 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
           const f4 z = {0, 0, 0, 0};
           P[b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(W[b], X, z, 0, 0, 0, 0, 0, 0);
         }
-        if (mi == MI - 1) W[b] = read_w(N, b);
+        // the stage's loads one by one: all at once they would keep the address unit busy, and the matrix pipe waiting
+        if (mi == MI - 1) {
+          W[b] = read_w(N, b);
+          load(S, kb + 2, b);
+        }
+        if (mi == 0) {
+#pragma unroll
+          for (int q = 4 + b; q < kLoads; q += 4) load(N, kb + 1, q);
+        }
         __builtin_amdgcn_sched_barrier(0);
       }
       if constexpr (WIDE) {
@@ -189,9 +205,11 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
   };
 
   weight_scales(0);
-  load(stage0, 0);
+#pragma unroll
+  for (int q = 0; q < kLoads; ++q) load(stage0, 0, q);
   turn();
-  if (Kb > 1) load(stage1, 1);
+#pragma unroll
+  for (int q = 0; q < 4; ++q) load(stage1, 1, q);
 #pragma unroll
   for (int b = 0; b < 4; ++b) W[b] = read_w(stage0, b);
   X = read_x(stage0, 0);
@@ -291,7 +309,7 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
 template <int BM>
 hipError_t go(const StampF8Gemm& a, hipStream_t st) {
   const int64_t tiles = a.offsets == nullptr ? ((int64_t)a.rows + BM - 1) / BM : (int64_t)a.rows / BM + (a.sets < a.rows ? a.sets : a.rows);
-  const uint32_t grid = (uint32_t)(tiles * ((a.groups + 3) / 4));
+  const uint32_t grid = (uint32_t)((tiles * ((a.groups + 3) / 4) + 7) / 8 * 8);
   if (a.gated) {
     k_f8_tiles<BM, kWide, true><<<grid, 512, 0, st>>>(a);
   } else if (a.wide_sums) {

@@ -108,6 +108,11 @@ class Fp8Plan:
         """Name (FP8_ROUTES) of the kernel that a call with so many rows runs."""
         return FP8_ROUTES[int(self.lib.stamp_fp8_debug_route(self._h, int(rows)))]
 
+    def set_route(self, route: str = ""):
+        """For tests and measurements: that kernel for every call ("": by rule)."""
+        code = {n: c for c, n in FP8_ROUTES.items()}[route] if route else 0
+        _check(self.lib.stamp_fp8_debug_set_route(self._h, code), "stamp_fp8_debug_set_route")
+
     # -- compute (asynchronous on the stream) --
     def alloc_act_buffers(self, rows: int, device="cuda"):
         """Codes [rows, d_in rounded up to 128] and scales [blocks, rows rounded up to 4] for quantize_act."""
