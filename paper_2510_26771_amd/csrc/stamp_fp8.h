@@ -9,7 +9,7 @@
 //          of 128 of the next layer's input
 //
 // Operand image of the weights, [matrix set e][group][block of 128 channels][b][h][lane][16 bytes]: lane 16 f + i's parts h = 0, 1 are
-// channels 32 f + 16 h .. + 15 of row i (any dealing of the channels is right that is the same for both operands).  A wave reads 1 KB of
+// channels 64 h + 16 f .. + 15 of row i (any dealing of the channels is right that is the same for both operands).  A wave reads 1 KB of
 // consecutive addresses, from memory or LDS.  Activations stay in rows: [row][Kp] bytes.
 #ifndef STAMP_FP8_H_
 #define STAMP_FP8_H_

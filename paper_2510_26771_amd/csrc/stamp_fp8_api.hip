@@ -348,7 +348,7 @@ stamp_status_t stamp_fp8_debug_weight_codes(const stamp_fp8_plan_t* p, uint8_t* 
           const size_t mat = d.gated ? 2 * (size_t)set + (b & 1) : (size_t)set;
           uint8_t* row = codes_host + (mat * d.d_out + n) * d.d_in;
           for (int c = 0; c < d.d_in; c += 16) {
-            const uint8_t* s = h + f8_w_offset(p->groups, p->Kb, set, g, c >> 7, b, (c >> 4) & 1, 16 * ((c >> 5) & 3) + i);
+            const uint8_t* s = h + f8_w_offset(p->groups, p->Kb, set, g, c >> 7, b, (c >> 6) & 1, 16 * ((c >> 4) & 3) + i);
             memcpy(row + c, s, d.d_in - c < 16 ? d.d_in - c : 16);
           }
         }

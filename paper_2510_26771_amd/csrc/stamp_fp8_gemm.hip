@@ -1,8 +1,8 @@
 // Product of the 8-bit floating point layers in tiles of BM rows x 256 places.
 //
 // Eight waves, 2 x 4, of BM / 2 x 64 each; the operands of a block of 128 channels are one stage in LDS, two stages.  The weights' stage is
-// a copy of the operand image.  The rows' stage is [row][8 pieces of 16 bytes], piece p at p ^ (row / 2 % 8): the 16 lanes of a read then
-// hit all 64 banks once.
+// a copy of the operand image.  The rows' stage is [row][8 pieces of 16 bytes], piece p at p ^ (row / 2 % 8): the 16 lanes that are
+// read at a time then hit all 64 banks once (also where they are lanes 0-3, 12-15 and 20-27, which take pieces f and f + 1 of 8 rows each).
 //
 // A wave's turn from one stage to the next lies before its last row block of the stage: all its reads of this stage have returned, its
 // loads into the next have landed; behind the barrier it asks for the stage after the next (into this one's place) and reads the next
@@ -97,7 +97,7 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
   const int gw = min(g0 + wn, a.groups - 1);
   const float* sw0 = a.SW + (size_t)set * (GATED ? 2 : 1) * a.nblk * Kb + (size_t)(GATED ? gw >> 2 : gw >> 1) * Kb;
   const int x = ((lane & 15) >> 1) & 7, f = lane >> 4;
-  const int abase = (wm * (BM / 2) + (lane & 15)) * 128, p0 = abase + ((2 * f) ^ x) * 16, p1 = abase + ((2 * f + 1) ^ x) * 16;
+  const int abase = (wm * (BM / 2) + (lane & 15)) * 128, p0 = abase + (f ^ x) * 16, p1 = abase + ((f + 4) ^ x) * 16;
   const int wbase = kStageA + wn * kF8GroupBytes + lane * 16, sbase = kStageA + kStageB + (wm * (BM / 2) + (lane & 15)) * 4;
 
   // weight scales of 64 blocks of channels at a time, lane kb % 64

@@ -114,7 +114,7 @@ __global__ __launch_bounds__(256) void k_f8_w_image(const void* W, int dtype, in
   const int64_t sg = gk / Kb;
   const int g = (int)(sg % groups);
   const int64_t set = sg / groups, mat = gated ? 2 * set + (b & 1) : set;
-  const int n = f8_column(gated, g, b, lane & 15), c0 = kb * 128 + 32 * (lane >> 4) + 16 * h;
+  const int n = f8_column(gated, g, b, lane & 15), c0 = kb * 128 + 64 * h + 16 * (lane >> 4);
   u4 o = {0, 0, 0, 0};
   if (n < N && c0 < d) {
     if (dtype == STAMP_E4M3) {

@@ -46,7 +46,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_f8_rows(StampF8Gemm a) {
       const int r = min(r0 + 16 * mi + (lane & 15), hi - 1);
       int ar = r;
       if (a.index != nullptr) ar = min(max(a.index[r], 0), a.a_rows - 1);
-      arow[mi] = a.A + (size_t)ar * Kp + 32 * (lane >> 4);
+      arow[mi] = a.A + (size_t)ar * Kp + 16 * (lane >> 4);
       srow[mi] = r;
     }
     if (in) {
@@ -62,7 +62,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_f8_rows(StampF8Gemm a) {
 #pragma unroll
         for (int mi = 0; mi < MT; ++mi) {
           const v4i* s = reinterpret_cast<const v4i*>(arow[mi] + (size_t)kb * 128);
-          X[mi] = __builtin_shufflevector(s[0], s[1], 0, 1, 2, 3, 4, 5, 6, 7);
+          X[mi] = __builtin_shufflevector(s[0], s[4], 0, 1, 2, 3, 4, 5, 6, 7);
           sx[mi] = a.SA[(int64_t)kb * a.ld_sa + srow[mi]];
         }
         const float sw = sw0[kb], su = GATED ? sw0[(size_t)a.nblk * a.Kb + kb] : 0.0f;
