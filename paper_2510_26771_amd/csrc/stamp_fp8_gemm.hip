@@ -1,15 +1,18 @@
 // Product of the 8-bit floating point layers in tiles of BM rows x 256 places.
 //
-// Eight waves, 2 x 4, of BM / 2 x 64 each; the operands of a block of 128 channels are one stage in LDS, two stages.  The weights' stage is
+// Eight waves, 2 x 4, of BM / 2 x 64 each; the operands of a block of 128 channels are one stage in LDS, two stages of 256 rows or three of
+// fewer (a step of 128 rows takes 0.5 us, less than a load does).  The weights' stage is
 // a copy of the operand image.  The rows' stage is [row][8 pieces of 16 bytes], piece p at p ^ (row / 2 % 8): the 16 lanes that are
 // read at a time then hit all 64 banks once (also where they are lanes 0-3, 12-15 and 20-27, which take pieces f and f + 1 of 8 rows each).
 //
 // A wave's turn from one stage to the next lies before its last row block of the stage: all its reads of this stage have returned, its
-// loads into the next have landed; behind the barrier it asks for the stage after the next (into this one's place) and reads the next
-// one's first operands under the last block's matrix instructions.
+// loads into the next have landed; behind the barrier it asks for the stage that takes this one's place and reads the next one's first
+// operands under the last block's matrix instructions.
 //
 // STAMP_SCALE_F32: an instruction's sum over the block of channels (its addend is 0) goes to the accumulators by a multiplication with
 // both scales, 4 fused multiply-adds per instruction, one row block behind, so that the matrix pipe (32 cycles an instruction) runs on.
+#include <type_traits>
+
 #include "stamp_fp8.h"
 
 namespace {
@@ -31,6 +34,8 @@ constexpr uint32_t kNowhere = 0xfffffff0u;
 // How the products are summed: FP8 instructions with the scales by multiplication or as their own, or bf16 instructions (f8_wide_sums).
 enum Sums { kScaled, kPow2, kWide };
 
+[[maybe_unused]] constexpr int kMaxBlocks = 65536 / kF8Block;
+
 template <int BM, Sums SUMS, bool GATED>
 __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -38,9 +43,13 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
   constexpr int MI = BM / 32;  // row blocks of 16 per wave
   constexpr int LA = BM / 64;  // 16-byte pieces of the rows' stage per thread
   constexpr bool POW2 = SUMS == kPow2, WIDE = SUMS == kWide;
-  // two variables, not one array of two: the compiler then knows that a read of one stage does not wait for the loads into the other
-  __shared__ __attribute__((aligned(1024))) uint8_t stage0[kStageA + kStageB + BM * 4];
-  __shared__ __attribute__((aligned(1024))) uint8_t stage1[kStageA + kStageB + BM * 4];
+  constexpr int NS = BM == 256 ? 2 : 3;                       // stages
+  constexpr int kStage = kStageA + kStageB + 8 * 256;         // with 64 row scales per wave (those of the first BM / 64 waves are used)
+  // variables of their own, not one array: the compiler then knows that a read of one stage does not wait for the loads into the others
+  __shared__ __attribute__((aligned(1024))) uint8_t stage0[kStage];
+  __shared__ __attribute__((aligned(1024))) uint8_t stage1[kStage];
+  __shared__ __attribute__((aligned(1024))) uint8_t stage2[NS > 2 ? kStage : 16];
+  __shared__ float wscale[2][kMaxBlocks];
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int wm = wave >> 2, wn = wave & 3;
   // Workgroups go to the 8 XCDs in turn: an XCD takes a run of the tiles in an order in which 32 neighbours (its CUs) are 8 x 4 tiles, so
@@ -81,7 +90,7 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (LdsPtr)(S + kStageA + q * 8192 + wave * 1024), 16, t * 16, boff[q] + kb * kF8GroupBytes, 0, 0);
     } else if (q < 4 + LA) {
       __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (LdsPtr)(S + (q - 4) * 8192 + wave * 1024), 16, aoff[q - 4], kb * 128, 0, 0);
-    } else if (wave < BM / 64) {
+    } else {
       __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(a.SA + row0 + (int64_t)kb * a.ld_sa + soff),
                                        (LdsPtr)(S + kStageA + kStageB + wave * 256), 4, 0, 0);
     }
@@ -94,21 +103,18 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
     for (int b = 0; b < 4; ++b) acc[mi][b] = f4{0, 0, 0, 0};
 #pragma unroll
   for (int b = 0; b < 4; ++b) P[b] = f4{0, 0, 0, 0};
-  const int gw = min(g0 + wn, a.groups - 1);
-  const float* sw0 = a.SW + (size_t)set * (GATED ? 2 : 1) * a.nblk * Kb + (size_t)(GATED ? gw >> 2 : gw >> 1) * Kb;
   const int x = ((lane & 15) >> 1) & 7, f = lane >> 4;
   const int abase = (wm * (BM / 2) + (lane & 15)) * 128, p0 = abase + (f ^ x) * 16, p1 = abase + ((f + 4) ^ x) * 16;
   const int wbase = kStageA + wn * kF8GroupBytes + lane * 16, sbase = kStageA + kStageB + (wm * (BM / 2) + (lane & 15)) * 4;
 
-  // weight scales of 64 blocks of channels at a time, lane kb % 64
-  float swv = 0.0f, suv = 0.0f;
-  auto weight_scales = [&](int kb) __attribute__((always_inline)) {
-    swv = sw0[min(kb + lane, Kb - 1)];
-    if (GATED) suv = sw0[(size_t)a.nblk * Kb + min(kb + lane, Kb - 1)];
-  };
-  auto lane_of = [&](float v, int kb) __attribute__((always_inline)) {
-    return __uint_as_float((uint32_t)__builtin_amdgcn_readlane((int)__float_as_uint(v), kb & 63));
-  };
+  // weight scales of the tile's two blocks of 128 columns (gated: of its gate and up columns): a register that now and then is loaded
+  // anew would make every use of it wait for the loads in flight
+  for (int i = t; i < 2 * Kb; i += 512) {
+    const int which = i >= Kb, kb = i - which * Kb;
+    const int blk = GATED ? which * a.nblk + (min(g0, a.groups - 1) >> 2) : min((g0 >> 1) + which, a.nblk - 1);
+    wscale[which][kb] = a.SW[((size_t)set * (GATED ? 2 : 1) * a.nblk + blk) * Kb + kb];
+  }
+  const float* const sw_of = wscale[GATED ? 0 : wn >> 1];
   auto read_w = [&](const uint8_t* S, int b) __attribute__((always_inline)) -> v8i {
     const uint8_t* s = S + wbase + b * 2048;
     return __builtin_shufflevector(*reinterpret_cast<const v4i*>(s), *reinterpret_cast<const v4i*>(s + 1024), 0, 1, 2, 3, 4, 5, 6, 7);
@@ -118,9 +124,9 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
                                    7);
   };
   auto read_s = [&](const uint8_t* S, int mi) __attribute__((always_inline)) { return *reinterpret_cast<const float*>(S + sbase + mi * 64); };
-  // the own loads have landed and the own reads returned; then everyone's
-  auto turn = [&]() __attribute__((always_inline)) {
-    __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
+  // all but the youngest `left` of the own loads have landed and the own reads returned; then everyone's
+  auto turn = [&](auto left) __attribute__((always_inline)) {
+    __builtin_amdgcn_s_waitcnt(0x0070 | decltype(left)::value);  // vmcnt(left) lgkmcnt(0)
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
   };
@@ -132,10 +138,13 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
 
   v8i W[4], X;
   b8 Wb[4][4];  // WIDE: of the step
-  float sx, fg = 0.0f, fu = 0.0f;  // of the row block before: its factors
-  // the step of stage S; N: the next one's stage
-  auto step = [&](uint8_t* S, uint8_t* N, int kb) __attribute__((always_inline)) {
-    const float sw = lane_of(swv, kb), su = GATED ? lane_of(suv, kb) : 0.0f;
+  float sx, sw, su, fg = 0.0f, fu = 0.0f;  // fg, fu: factors of the row block before
+  constexpr std::integral_constant<int, 0> none;
+  constexpr std::integral_constant<int, (NS - 2) * kLoads> later;  // the loads of the stages behind the next
+  static_assert(later <= 15, "one field of the wait");
+  // the step of stage S; N: the next one's stage; B: the one of the step before, which is being filled again
+  auto step = [&](uint8_t* S, uint8_t* N, uint8_t* B, int kb) __attribute__((always_inline)) {
+    float next_w = 0.0f, next_u = 0.0f;
 #pragma unroll
     for (int mi = 0; mi < MI; ++mi) {
       if constexpr (POW2) {
@@ -148,9 +157,11 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
         Xn = read_x(S, mi + 1);
         sn = read_s(S, mi + 1);
       } else {
-        turn();
+        turn(later);
         Xn = read_x(N, 0);
         sn = read_s(N, 0);
+        next_w = sw_of[min(kb + 1, Kb - 1)];
+        if (GATED) next_u = wscale[1][min(kb + 1, Kb - 1)];
       }
       const float f0 = sx * sw, f1 = GATED ? sx * su : 0.0f;
       const int before = mi == 0 ? MI - 1 : mi - 1;
@@ -180,11 +191,11 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
         // the stage's loads one by one: all at once they would keep the address unit busy, and the matrix pipe waiting
         if (mi == MI - 1) {
           W[b] = read_w(N, b);
-          load(S, kb + 2, b);
+          load(S, kb + NS, b);
         }
         if (mi == 0) {
 #pragma unroll
-          for (int q = 4 + b; q < kLoads; q += 4) load(N, kb + 1, q);
+          for (int q = 4 + b; q < kLoads; q += 4) load(B, kb - 1 + NS, q);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -201,29 +212,47 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
       fg = f0;
       fu = f1;
     }
-    if (((kb + 1) & 63) == 0) weight_scales(kb + 1);
+    sw = next_w;
+    su = next_u;
   };
 
-  weight_scales(0);
 #pragma unroll
   for (int q = 0; q < kLoads; ++q) load(stage0, 0, q);
-  turn();
+  if constexpr (NS == 3) {
 #pragma unroll
-  for (int q = 0; q < 4; ++q) load(stage1, 1, q);
+    for (int q = 0; q < kLoads; ++q) load(stage1, 1, q);
+  }
+  turn(later);
+#pragma unroll
+  for (int q = 0; q < 4; ++q) load(NS == 3 ? stage2 : stage1, NS - 1, q);
 #pragma unroll
   for (int b = 0; b < 4; ++b) W[b] = read_w(stage0, b);
   X = read_x(stage0, 0);
   sx = read_s(stage0, 0);
+  sw = sw_of[0];
+  su = wscale[1][0];
   int kb = 0;
-  for (; kb + 1 < Kb; kb += 2) {
-    step(stage0, stage1, kb);
-    step(stage1, stage0, kb + 1);
+  if constexpr (NS == 2) {
+    for (; kb + 1 < Kb; kb += 2) {
+      step(stage0, stage1, stage1, kb);
+      step(stage1, stage0, stage0, kb + 1);
+    }
+    if (kb < Kb) step(stage0, stage1, stage1, kb);
+  } else {
+    for (; kb + 2 < Kb; kb += 3) {
+      step(stage0, stage1, stage2, kb);
+      step(stage1, stage2, stage0, kb + 1);
+      step(stage2, stage0, stage1, kb + 2);
+    }
+    if (kb < Kb) step(stage0, stage1, stage2, kb);
+    if (kb + 1 < Kb) step(stage1, stage2, stage0, kb + 1);
   }
-  if (kb < Kb) step(stage0, stage1, kb);
   if constexpr (!POW2) {
 #pragma unroll
     for (int b = 0; b < 4; ++b) add(acc[MI - 1][b], P[b], GATED && (b & 1) ? fu : fg);
   }
+
+  __builtin_amdgcn_s_waitcnt(0x0070);  // no load into LDS may outlive the workgroup
 
   const int g = g0 + wn;
   if constexpr (!GATED) {
@@ -271,7 +300,7 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
     // a lane has 8 neighbouring columns of gate and up; the tile's 128 columns are a block of the next layer's input
     float* part = reinterpret_cast<float*>(stage0);  // [4][BM] largest magnitudes of the waves' 32 columns, as bits
     const int n0 = 32 * g + 8 * f;
-    turn();
+    turn(none);
 #pragma unroll
     for (int mi = 0; mi < MI; ++mi) {
       uint32_t amax = 0;
@@ -286,7 +315,7 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
       amax = max(amax, (uint32_t)__shfl_xor((int)amax, 32));
       if (f == 0) part[wn * BM + wm * (BM / 2) + 16 * mi + lane] = __uint_as_float(amax);
     }
-    turn();
+    turn(none);
 #pragma unroll
     for (int mi = 0; mi < MI; ++mi) {
       const int m = wm * (BM / 2) + 16 * mi + (lane & 15);
