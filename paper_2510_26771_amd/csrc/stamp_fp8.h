@@ -10,7 +10,7 @@
 //
 // Operand image of the weights, [matrix set e][group][block of 128 channels][b][h][lane][16 bytes]: lane 16 f + i's parts h = 0, 1 are
 // channels 64 h + 16 f .. + 15 of row i (any dealing of the channels is right that is the same for both operands).  A wave reads 1 KB of
-// consecutive addresses, from memory or LDS.  Activations stay in rows: [row][Kp] bytes.
+// consecutive addresses, from memory or LDS.  Activations stay in rows: [row][Kp] bytes (or bf16).
 #ifndef STAMP_FP8_H_
 #define STAMP_FP8_H_
 
@@ -43,7 +43,7 @@ STAMP_HD size_t f8_w_offset(int groups, int Kb, int set, int g, int kb, int b, i
 
 // The product's arguments.
 struct StampF8Gemm {
-  const uint8_t* A;        // codes [a_rows][Kp]
+  const uint8_t* A;        // codes [a_rows][Kp], for tiles of wide_sums as bf16
   const float* SA;         // scales [Kb][ld_sa], by row of the product
   int64_t ld_sa;
   const int32_t* index;    // row of A of every row of the product, or nullptr: the same
@@ -65,7 +65,9 @@ struct StampF8Gemm {
 int stamp_f8_route(int sets, int groups, int Kb, int rows, int wide_sums);
 hipError_t stamp_launch_f8_weights(stamp_fp8_plan* p, const void* W, const float* w_scales, hipStream_t st, uint32_t* flag);
 // row_of_slot != nullptr: row t's scales go to the places of its top_k slots (rows of the product, below nrows)
-hipError_t stamp_launch_f8_quant(const void* X, int x_bf16, int64_t ld_x, int rows, int d, int pow2, uint8_t* codes, float* scales, int64_t ld_s,
+// wide: the codes as bf16
+hipError_t stamp_launch_f8_widen(const uint8_t* codes, int64_t bytes, uint8_t* out, hipStream_t st);
+hipError_t stamp_launch_f8_quant(const void* X, int x_bf16, int64_t ld_x, int rows, int d, int pow2, int wide, uint8_t* codes, float* scales, int64_t ld_s,
                                  const int32_t* row_of_slot, int top_k, int nrows, hipStream_t st);
 hipError_t stamp_launch_f8_rows(const StampF8Gemm& a, hipStream_t st);
 hipError_t stamp_launch_f8_tiles(const StampF8Gemm& a, int bm, hipStream_t st);

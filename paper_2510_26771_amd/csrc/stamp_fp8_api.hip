@@ -46,8 +46,12 @@ StampF8Gemm gemm_args(const stamp_fp8_plan* p) {
   return a;
 }
 
+int route_of(const StampF8Gemm& a, int rows) { return a.forced ? a.forced : stamp_f8_route(a.sets, a.groups, a.Kb, rows, a.wide_sums); }
+// the codes are wanted as bf16
+bool wide_codes(const StampF8Gemm& a, int rows) { return a.wide_sums && route_of(a, rows) != STAMP_FP8_ROUTE_ROWS; }
+
 hipError_t product(const StampF8Gemm& a, hipStream_t st) {
-  switch (a.forced ? a.forced : stamp_f8_route(a.sets, a.groups, a.Kb, a.rows, a.wide_sums)) {
+  switch (route_of(a, a.rows)) {
     case STAMP_FP8_ROUTE_ROWS: return stamp_launch_f8_rows(a, st);
     case STAMP_FP8_ROUTE_TILES_64: return stamp_launch_f8_tiles(a, 64, st);
     case STAMP_FP8_ROUTE_TILES_128: return stamp_launch_f8_tiles(a, 128, st);
@@ -55,31 +59,36 @@ hipError_t product(const StampF8Gemm& a, hipStream_t st) {
   }
 }
 
+// room for a code of the activations: as bf16 where some route wants that
+int code_bytes(const stamp_fp8_plan* p) { return gemm_args(p).wide_sums ? 2 : 1; }
+
 struct LinearWs {
   size_t codes, scales, total;
 };
 LinearWs linear_ws(const stamp_fp8_plan* p, int32_t rows) {
   LinearWs w;
   w.codes = 0;
-  w.scales = align256((size_t)rows * p->Kp);
+  w.scales = align256((size_t)rows * p->Kp * code_bytes(p));
   w.total = w.scales + align256((size_t)p->Kb * scales_ld(rows) * sizeof(float));
   return w;
 }
 
 struct ExpertsWs {
-  size_t codes, scales, h, sh, rows, total;
+  size_t codes, scales, h, sh, rows, wide, total;
   int64_t ld_rows;
 };
 ExpertsWs experts_ws(const stamp_fp8_plan* up, const stamp_fp8_plan* down, int32_t tokens, int32_t top_k) {
   ExpertsWs w;
   const int64_t slots = (int64_t)tokens * top_k, ld = scales_ld((int32_t)slots);
   w.codes = 0;
-  w.scales = align256((size_t)tokens * up->Kp);
+  w.scales = align256((size_t)tokens * up->Kp * code_bytes(up));
   w.h = w.scales + align256((size_t)up->Kb * ld * sizeof(float));
   w.sh = w.h + align256((size_t)slots * down->Kp);
   w.rows = w.sh + align256((size_t)down->Kb * ld * sizeof(float));
   w.ld_rows = (down->desc.d_out + 7) / 8 * 8;
-  w.total = w.rows + align256((size_t)slots * w.ld_rows * type_size(down->desc.y_dtype));
+  // the up product writes codes of one byte; a down product that wants them as bf16 has them widened here
+  w.wide = w.rows + align256((size_t)slots * w.ld_rows * type_size(down->desc.y_dtype));
+  w.total = w.wide + (code_bytes(down) == 2 ? align256((size_t)slots * down->Kp * 2) : 0);
   return w;
 }
 
@@ -122,7 +131,8 @@ stamp_status_t forward(const stamp_fp8_plan* p, int32_t rows, const int32_t* off
   uint8_t* codes = static_cast<uint8_t*>(ws) + w.codes;
   float* scales = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + w.scales);
   StampF8Gemm a = gemm_args(p);
-  hipError_t e = stamp_launch_f8_quant(X, p->desc.x_dtype == STAMP_BF16, ld_x, rows, p->desc.d_in, a.pow2, codes, scales, scales_ld(rows), nullptr, 0, 0, st);
+  hipError_t e = stamp_launch_f8_quant(X, p->desc.x_dtype == STAMP_BF16, ld_x, rows, p->desc.d_in, a.pow2, wide_codes(a, rows), codes, scales,
+                                       scales_ld(rows), nullptr, 0, 0, st);
   if (e != hipSuccess) return STAMP_ERR_DEVICE;
   a.A = codes;
   a.SA = scales;
@@ -220,7 +230,7 @@ stamp_status_t stamp_fp8_quantize_act(const stamp_fp8_plan_t* p, int32_t rows, c
   if (s != STAMP_OK) return s;
   if (codes_dev == nullptr || scales_dev == nullptr) return STAMP_ERR_NULL;
   if (ld_scales < rows || ld_scales % 4 != 0 || (reinterpret_cast<uintptr_t>(codes_dev) | reinterpret_cast<uintptr_t>(scales_dev)) % 16 != 0) return STAMP_ERR_SHAPE;
-  return done(stamp_launch_f8_quant(X_dev, p->desc.x_dtype == STAMP_BF16, ld_x, rows, p->desc.d_in, p->desc.scale_format == STAMP_SCALE_POW2, codes_dev,
+  return done(stamp_launch_f8_quant(X_dev, p->desc.x_dtype == STAMP_BF16, ld_x, rows, p->desc.d_in, p->desc.scale_format == STAMP_SCALE_POW2, 0, codes_dev,
                                     scales_dev, ld_scales, nullptr, 0, 0, reinterpret_cast<hipStream_t>(hip_stream)));
 }
 
@@ -240,14 +250,20 @@ stamp_status_t stamp_fp8_linear_forward_q(const stamp_fp8_plan_t* p, int32_t row
   stamp_status_t s = check_matrix(Y_dev, p->desc.y_dtype, ld_y, p->desc.d_out);
   if (s == STAMP_OK) s = check_ws(workspace_dev, workspace_bytes, linear_ws(p, rows).total);
   if (s != STAMP_OK) return s;
+  hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
   StampF8Gemm a = gemm_args(p);
   a.A = codes_dev;
+  if (wide_codes(a, rows)) {
+    uint8_t* wide = static_cast<uint8_t*>(workspace_dev);
+    if (stamp_launch_f8_widen(codes_dev, (int64_t)rows * p->Kp, wide, st) != hipSuccess) return STAMP_ERR_DEVICE;
+    a.A = wide;
+  }
   a.SA = scales_dev;
   a.ld_sa = ld_scales;
   a.a_rows = a.rows = rows;
   a.Y = Y_dev;
   a.ld_y = ld_y;
-  return done(product(a, reinterpret_cast<hipStream_t>(hip_stream)));
+  return done(product(a, st));
 }
 
 stamp_status_t stamp_fp8_grouped_forward(const stamp_fp8_plan_t* p, int32_t rows, const int32_t* offsets_dev, const void* X_dev, int64_t ld_x, void* Y_dev,
@@ -286,7 +302,7 @@ stamp_status_t stamp_experts_forward(const stamp_fp8_plan_t* up, const stamp_fp8
     return STAMP_ERR_SHAPE;
   stamp_status_t s = check_routing(r);
   if (s != STAMP_OK) return s;
-  if ((int64_t)r->tokens * r->top_k > kMaxRows || (int64_t)r->tokens * up->Kp >= (int64_t)0xfffffff0u) return STAMP_ERR_UNSUPPORTED;
+  if ((int64_t)r->tokens * r->top_k > kMaxRows || (int64_t)r->tokens * up->Kp * 2 >= (int64_t)0xfffffff0u) return STAMP_ERR_UNSUPPORTED;
   if (r->tokens == 0) return STAMP_OK;
   s = check_matrix(X_dev, up->desc.x_dtype, ld_x, up->desc.d_in);
   if (s == STAMP_OK) s = check_matrix(Y_dev, down->desc.y_dtype, ld_y, down->desc.d_out);
@@ -300,7 +316,8 @@ stamp_status_t stamp_experts_forward(const stamp_fp8_plan_t* up, const stamp_fp8
 
   StampF8Gemm a = gemm_args(up);
   float* scales = reinterpret_cast<float*>(ws + w.scales);
-  if (stamp_launch_f8_quant(X_dev, up->desc.x_dtype == STAMP_BF16, ld_x, r->tokens, up->desc.d_in, a.pow2, ws + w.codes, scales, ld, r->row_of_slot_dev,
+  if (stamp_launch_f8_quant(X_dev, up->desc.x_dtype == STAMP_BF16, ld_x, r->tokens, up->desc.d_in, a.pow2, wide_codes(a, slots), ws + w.codes, scales,
+                            ld, r->row_of_slot_dev,
                             r->top_k, slots, st) != hipSuccess)
     return STAMP_ERR_DEVICE;
   a.A = ws + w.codes;
@@ -318,6 +335,10 @@ stamp_status_t stamp_experts_forward(const stamp_fp8_plan_t* up, const stamp_fp8
 
   StampF8Gemm b = gemm_args(down);
   b.A = ws + w.h;
+  if (wide_codes(b, slots)) {
+    if (stamp_launch_f8_widen(b.A, (int64_t)slots * down->Kp, ws + w.wide, st) != hipSuccess) return STAMP_ERR_DEVICE;
+    b.A = ws + w.wide;
+  }
   b.SA = a.SH;
   b.ld_sa = ld;
   b.a_rows = b.rows = slots;

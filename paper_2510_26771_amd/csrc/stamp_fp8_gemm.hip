@@ -9,6 +9,10 @@
 // loads into the next have landed; behind the barrier it asks for the stage that takes this one's place and reads the next one's first
 // operands under the last block's matrix instructions.
 //
+// Sums in fp32 (kWide): the rows come as bf16 (the quantizer widens the codes, or k_f8_widen: half of the kernel's conversions otherwise, and
+// the vector ALU its bound), 256 bytes a row, piece p of 16 at p ^ (row % 16); the weights are widened once per step and wave
+// (conversions among the matrix instructions, see wide_step: in a row of their own they leave the matrix pipe idle in both waves of a SIMD).
+//
 // STAMP_SCALE_F32: an instruction's sum over the block of channels (its addend is 0) goes to the accumulators by a multiplication with
 // both scales, 4 fused multiply-adds per instruction, one row block behind, so that the matrix pipe (32 cycles an instruction) runs on.
 #include <type_traits>
@@ -39,11 +43,12 @@ enum Sums { kScaled, kPow2, kWide };
 template <int BM, Sums SUMS, bool GATED>
 __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  constexpr int kStageA = BM * 128, kStageB = 4 * kF8GroupBytes;
-  constexpr int MI = BM / 32;  // row blocks of 16 per wave
-  constexpr int LA = BM / 64;  // 16-byte pieces of the rows' stage per thread
   constexpr bool POW2 = SUMS == kPow2, WIDE = SUMS == kWide;
-  constexpr int NS = BM == 256 ? 2 : 3;                       // stages
+  constexpr int kRowBytes = WIDE ? 256 : 128;
+  constexpr int kStageA = BM * kRowBytes, kStageB = 4 * kF8GroupBytes;
+  constexpr int MI = BM / 32;         // row blocks of 16 per wave
+  constexpr int LA = kStageA / 8192;  // 16-byte pieces of the rows' stage per thread
+  constexpr int NS = kStageA > 16384 ? 2 : 3;                 // stages
   constexpr int kStage = kStageA + kStageB + 8 * 256;         // with 64 row scales per wave (those of the first BM / 64 waves are used)
   // variables of their own, not one array: the compiler then knows that a read of one stage does not wait for the loads into the others
   __shared__ __attribute__((aligned(1024))) uint8_t stage0[kStage];
@@ -65,20 +70,20 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
   set = __builtin_amdgcn_readfirstlane(set);
   row0 = __builtin_amdgcn_readfirstlane(row0);
   nrows = __builtin_amdgcn_readfirstlane(nrows);
-  const int g0 = col * 4, Kb = a.Kb, Kp = Kb * 128;
+  const int g0 = col * 4, Kb = a.Kb;
 
   // 32-bit offsets from a scalar base: the tile's first row, or with an index all rows of A (below 4 GB, checked by the host)
   uint32_t aoff[LA], boff[4];
 #pragma unroll
   for (int i = 0; i < LA; ++i) {
-    const int p = i * 512 + t, row = p >> 3, piece = (p & 7) ^ ((row >> 1) & 7);
+    const int p = i * 512 + t, row = WIDE ? p >> 4 : p >> 3, piece = WIDE ? (p & 15) ^ (row & 15) : (p & 7) ^ ((row >> 1) & 7);
     uint32_t r = min(row, nrows - 1);
     if (a.index != nullptr) r = min(max(a.index[row0 + r], 0), a.a_rows - 1);
-    aoff[i] = r * (uint32_t)Kp + piece * 16;
+    aoff[i] = r * (uint32_t)(Kb * kRowBytes) + piece * 16;
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) boff[i] = uniform((uint32_t)(min(g0 + i, a.groups - 1) - g0) * (uint32_t)Kb * kF8GroupBytes);
-  const __amdgpu_buffer_rsrc_t ra = buffer(a.A + (a.index != nullptr ? (size_t)0 : (size_t)row0 * Kp));
+  const __amdgpu_buffer_rsrc_t ra = buffer(a.A + (a.index != nullptr ? (size_t)0 : (size_t)row0 * Kb * kRowBytes));
   const __amdgpu_buffer_rsrc_t rb = buffer(a.W + ((size_t)set * a.groups + g0) * Kb * kF8GroupBytes);
   const uint32_t soff = (uint32_t)min(t, nrows - 1);
 
@@ -89,7 +94,7 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
     if (q < 4) {
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (LdsPtr)(S + kStageA + q * 8192 + wave * 1024), 16, t * 16, boff[q] + kb * kF8GroupBytes, 0, 0);
     } else if (q < 4 + LA) {
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (LdsPtr)(S + (q - 4) * 8192 + wave * 1024), 16, aoff[q - 4], kb * 128, 0, 0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (LdsPtr)(S + (q - 4) * 8192 + wave * 1024), 16, aoff[q - 4], kb * kRowBytes, 0, 0);
     } else {
       __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(a.SA + row0 + (int64_t)kb * a.ld_sa + soff),
                                        (LdsPtr)(S + kStageA + kStageB + wave * 256), 4, 0, 0);
@@ -104,7 +109,7 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
 #pragma unroll
   for (int b = 0; b < 4; ++b) P[b] = f4{0, 0, 0, 0};
   const int x = ((lane & 15) >> 1) & 7, f = lane >> 4;
-  const int abase = (wm * (BM / 2) + (lane & 15)) * 128, p0 = abase + (f ^ x) * 16, p1 = abase + ((f + 4) ^ x) * 16;
+  const int abase = (wm * (BM / 2) + (lane & 15)) * kRowBytes, p0 = abase + (f ^ x) * 16, p1 = abase + ((f + 4) ^ x) * 16;
   const int wbase = kStageA + wn * kF8GroupBytes + lane * 16, sbase = kStageA + kStageB + (wm * (BM / 2) + (lane & 15)) * 4;
 
   // weight scales of the tile's two blocks of 128 columns (gated: of its gate and up columns): a register that now and then is loaded
@@ -118,6 +123,9 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
   auto read_w = [&](const uint8_t* S, int b) __attribute__((always_inline)) -> v8i {
     const uint8_t* s = S + wbase + b * 2048;
     return __builtin_shufflevector(*reinterpret_cast<const v4i*>(s), *reinterpret_cast<const v4i*>(s + 1024), 0, 1, 2, 3, 4, 5, 6, 7);
+  };
+  auto read_x1 = [&](const uint8_t* S, int mi, int k) __attribute__((always_inline)) -> b8 {
+    return *reinterpret_cast<const b8*>(S + abase + mi * 16 * kRowBytes + ((8 * (k >> 1) + 2 * f + (k & 1)) ^ (lane & 15)) * 16);
   };
   auto read_x = [&](const uint8_t* S, int mi) __attribute__((always_inline)) -> v8i {
     return __builtin_shufflevector(*reinterpret_cast<const v4i*>(S + p0 + mi * 2048), *reinterpret_cast<const v4i*>(S + p1 + mi * 2048), 0, 1, 2, 3, 4, 5, 6,
@@ -137,7 +145,6 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
   };
 
   v8i W[4], X;
-  b8 Wb[4][4];  // WIDE: of the step
   float sx, sw, su, fg = 0.0f, fu = 0.0f;  // fg, fu: factors of the row block before
   constexpr std::integral_constant<int, 0> none;
   constexpr std::integral_constant<int, (NS - 2) * kLoads> later;  // the loads of the stages behind the next
@@ -165,22 +172,9 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
       }
       const float f0 = sx * sw, f1 = GATED ? sx * su : 0.0f;
       const int before = mi == 0 ? MI - 1 : mi - 1;
-      b8 Xb[4];
-      if constexpr (WIDE) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) Xb[k] = widen8(X[2 * k], X[2 * k + 1]);
-      }
 #pragma unroll
       for (int b = 0; b < 4; ++b) {
-        if constexpr (WIDE) {
-          if (mi == 0) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k) Wb[b][k] = widen8(W[b][2 * k], W[b][2 * k + 1]);
-          }
-          add(acc[before][b], P[b], GATED && (b & 1) ? fu : fg);
-          const f4 z = {0, 0, 0, 0};
-          P[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(Wb[b][0], Xb[0], z, 0, 0, 0);
-        } else if constexpr (POW2) {
+        if constexpr (POW2) {
           acc[mi][b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(W[b], X, acc[mi][b], 0, 0, 0, (int)(__float_as_uint(GATED && (b & 1) ? su : sw) >> 23),
                                                                        0, (int)(__float_as_uint(sx) >> 23));
         } else {
@@ -199,14 +193,6 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
         }
         __builtin_amdgcn_sched_barrier(0);
       }
-      if constexpr (WIDE) {
-#pragma unroll
-        for (int k = 1; k < 4; ++k) {
-#pragma unroll
-          for (int b = 0; b < 4; ++b) P[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(Wb[b][k], Xb[k], P[b], 0, 0, 0);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-      }
       X = Xn;
       sx = sn;
       fg = f0;
@@ -214,6 +200,69 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
     }
     sw = next_w;
     su = next_u;
+  };
+
+  // kWide: by blocks of 16 places, so that the conversions of a block's weights lie among the 4 MI matrix instructions of the block before;
+  // all rows of the stage are in registers, and the turn lies before the last block.
+  b8 XW[MI][4];
+  b8 Wb[2][4];
+  v8i raw;
+  f4 PW[MI];
+  float sxw[MI], f0[MI], f1[MI];  // f0, f1: this step's factors (of the gate and the up columns)
+  float fold[MI];                 // of the block before
+  auto widen_w = [&](b8(&w)[4], const v8i& r) __attribute__((always_inline)) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) w[k] = widen8(r[2 * k], r[2 * k + 1]);
+  };
+  auto wide_step = [&](uint8_t* S, uint8_t* N, uint8_t* B, int kb) __attribute__((always_inline)) {
+    float next_w = 0.0f, next_u = 0.0f, sn[MI];
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) {
+      f0[mi] = sxw[mi] * sw;
+      f1[mi] = GATED ? sxw[mi] * su : 0.0f;
+    }
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      if (b == 3) {
+        turn(later);
+        next_w = sw_of[min(kb + 1, Kb - 1)];
+        if (GATED) next_u = wscale[1][min(kb + 1, Kb - 1)];
+      }
+      raw = b < 3 ? read_w(S, b + 1) : read_w(N, 0);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+#pragma unroll
+        for (int mi = 0; mi < MI; ++mi) {
+          if (k == 0) add(acc[mi][(b + 3) & 3], PW[mi], fold[mi]);
+          const f4 z = {0, 0, 0, 0};
+          PW[mi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(Wb[b & 1][k], XW[mi][k], k == 0 ? z : PW[mi], 0, 0, 0);
+          if (b == 3) XW[mi][k] = read_x1(N, mi, k);
+        }
+        if (b == 3) {
+          load(S, kb + NS, k);
+          if (k == 0) {
+#pragma unroll
+            for (int mi = 0; mi < MI; ++mi) sn[mi] = read_s(N, mi);
+          }
+        }
+        if (b == 0) {
+#pragma unroll
+          for (int q = 4 + k; q < kLoads; q += 4) load(B, kb - 1 + NS, q);
+        }
+        if (k == 1) widen_w(Wb[(b + 1) & 1], raw);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int mi = 0; mi < MI; ++mi) fold[mi] = GATED && (b & 1) ? f1[mi] : f0[mi];
+    }
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) sxw[mi] = sn[mi];
+    sw = next_w;
+    su = next_u;
+  };
+  auto any_step = [&](uint8_t* S, uint8_t* N, uint8_t* B, int kb) __attribute__((always_inline)) {
+    if constexpr (WIDE) wide_step(S, N, B, kb);
+    else step(S, N, B, kb);
   };
 
 #pragma unroll
@@ -225,29 +274,44 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
   turn(later);
 #pragma unroll
   for (int q = 0; q < 4; ++q) load(NS == 3 ? stage2 : stage1, NS - 1, q);
+  if constexpr (WIDE) {
+    widen_w(Wb[0], read_w(stage0, 0));
 #pragma unroll
-  for (int b = 0; b < 4; ++b) W[b] = read_w(stage0, b);
-  X = read_x(stage0, 0);
-  sx = read_s(stage0, 0);
+    for (int mi = 0; mi < MI; ++mi) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) XW[mi][k] = read_x1(stage0, mi, k);
+      sxw[mi] = read_s(stage0, mi);
+      PW[mi] = f4{0, 0, 0, 0};
+      fold[mi] = 0.0f;
+    }
+  } else {
+#pragma unroll
+    for (int b = 0; b < 4; ++b) W[b] = read_w(stage0, b);
+    X = read_x(stage0, 0);
+    sx = read_s(stage0, 0);
+  }
   sw = sw_of[0];
   su = wscale[1][0];
   int kb = 0;
   if constexpr (NS == 2) {
     for (; kb + 1 < Kb; kb += 2) {
-      step(stage0, stage1, stage1, kb);
-      step(stage1, stage0, stage0, kb + 1);
+      any_step(stage0, stage1, stage1, kb);
+      any_step(stage1, stage0, stage0, kb + 1);
     }
-    if (kb < Kb) step(stage0, stage1, stage1, kb);
+    if (kb < Kb) any_step(stage0, stage1, stage1, kb);
   } else {
     for (; kb + 2 < Kb; kb += 3) {
-      step(stage0, stage1, stage2, kb);
-      step(stage1, stage2, stage0, kb + 1);
-      step(stage2, stage0, stage1, kb + 2);
+      any_step(stage0, stage1, stage2, kb);
+      any_step(stage1, stage2, stage0, kb + 1);
+      any_step(stage2, stage0, stage1, kb + 2);
     }
-    if (kb < Kb) step(stage0, stage1, stage2, kb);
-    if (kb + 1 < Kb) step(stage1, stage2, stage0, kb + 1);
+    if (kb < Kb) any_step(stage0, stage1, stage2, kb);
+    if (kb + 1 < Kb) any_step(stage1, stage2, stage0, kb + 1);
   }
-  if constexpr (!POW2) {
+  if constexpr (WIDE) {
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) add(acc[mi][3], PW[mi], fold[mi]);
+  } else if constexpr (!POW2) {
 #pragma unroll
     for (int b = 0; b < 4; ++b) add(acc[MI - 1][b], P[b], GATED && (b & 1) ? fu : fg);
   }
@@ -335,15 +399,28 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
 #endif
 }
 
+__global__ __launch_bounds__(256) void k_f8_widen(const uint8_t* codes, int64_t n16, uint8_t* out) {
+  const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (u >= n16) return;
+  const u4 c = reinterpret_cast<const u4*>(codes)[u];
+  reinterpret_cast<b8*>(out)[2 * u] = widen8((int)c[0], (int)c[1]);
+  reinterpret_cast<b8*>(out)[2 * u + 1] = widen8((int)c[2], (int)c[3]);
+}
+
 template <int BM>
 hipError_t go(const StampF8Gemm& a, hipStream_t st) {
   const int64_t tiles = a.offsets == nullptr ? ((int64_t)a.rows + BM - 1) / BM : (int64_t)a.rows / BM + (a.sets < a.rows ? a.sets : a.rows);
   const uint32_t grid = (uint32_t)((tiles * ((a.groups + 3) / 4) + 7) / 8 * 8);
-  if (a.gated) {
+  if constexpr (BM == 256) {
+    if (a.wide_sums) return hipErrorInvalidValue;  // its registers do not hold the bf16 operands: never chosen
+  } else if (a.gated) {
     k_f8_tiles<BM, kWide, true><<<grid, 512, 0, st>>>(a);
+    return hipGetLastError();
   } else if (a.wide_sums) {
     k_f8_tiles<BM, kWide, false><<<grid, 512, 0, st>>>(a);
-  } else if (a.pow2) {
+    return hipGetLastError();
+  }
+  if (a.pow2) {
     k_f8_tiles<BM, kPow2, false><<<grid, 512, 0, st>>>(a);
   } else {
     k_f8_tiles<BM, kScaled, false><<<grid, 512, 0, st>>>(a);
@@ -351,6 +428,11 @@ hipError_t go(const StampF8Gemm& a, hipStream_t st) {
   return hipGetLastError();
 }
 }  // namespace
+
+hipError_t stamp_launch_f8_widen(const uint8_t* codes, int64_t bytes, uint8_t* out, hipStream_t st) {
+  k_f8_widen<<<(uint32_t)((bytes / 16 + 255) / 256), 256, 0, st>>>(codes, bytes / 16, out);
+  return hipGetLastError();
+}
 
 hipError_t stamp_launch_f8_tiles(const StampF8Gemm& a, int bm, hipStream_t st) {
   return bm == 64 ? go<64>(a, st) : bm == 128 ? go<128>(a, st) : go<256>(a, st);

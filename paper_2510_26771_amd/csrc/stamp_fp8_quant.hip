@@ -37,8 +37,8 @@ __device__ __forceinline__ void load16(const void* row, int c, int d, bool wide,
 }
 
 // A thread has 16 channels, 8 lanes a block.  Bound by memory: 2 (4) bytes read, 1.03 written per element.
-template <bool BF16>
-__global__ __launch_bounds__(256) void k_f8_quant(const void* X, int64_t ld_x, int rows, int d, int Kp, int pow2, int wide, uint8_t* codes, float* scales,
+template <bool BF16, bool WIDE>
+__global__ __launch_bounds__(256) void k_f8_quant(const void* X, int64_t ld_x, int rows, int d, int Kp, int pow2, int aligned, uint8_t* codes, float* scales,
                                                   int64_t ld_s, const int32_t* row_of_slot, int top_k, int nrows) {
   const int per = Kp >> 4;
   const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -46,7 +46,7 @@ __global__ __launch_bounds__(256) void k_f8_quant(const void* X, int64_t ld_x, i
   const int c = (int)(u - m * per) * 16;
   if (m >= rows) return;  // whole groups of 8 lanes: per is a multiple of 8
   float v[16];
-  load16<BF16>(static_cast<const char*>(X) + m * ld_x * (BF16 ? 2 : 4), c, d, wide, v);
+  load16<BF16>(static_cast<const char*>(X) + m * ld_x * (BF16 ? 2 : 4), c, d, aligned, v);
   uint32_t a = 0;
 #pragma unroll
   for (int j = 0; j < 16; ++j) a = max(a, abs_bits(v[j]));
@@ -57,7 +57,13 @@ __global__ __launch_bounds__(256) void k_f8_quant(const void* X, int64_t ld_x, i
 #pragma unroll
   for (int j = 0; j < 4; ++j)
     o[j] = pack4(__fmul_rn(v[4 * j], inv), __fmul_rn(v[4 * j + 1], inv), __fmul_rn(v[4 * j + 2], inv), __fmul_rn(v[4 * j + 3], inv));
-  *reinterpret_cast<u4*>(codes + m * Kp + c) = o;
+  if constexpr (WIDE) {
+    b8* p = reinterpret_cast<b8*>(codes + (m * Kp + c) * 2);
+    p[0] = widen8((int)o[0], (int)o[1]);
+    p[1] = widen8((int)o[2], (int)o[3]);
+  } else {
+    *reinterpret_cast<u4*>(codes + m * Kp + c) = o;
+  }
   if ((threadIdx.x & 7) != 0) return;
   float* s = scales + (int64_t)(c >> 7) * ld_s;
   if (row_of_slot == nullptr) {
@@ -140,15 +146,13 @@ __global__ __launch_bounds__(256) void k_f8_check_pow2(const float* s, int64_t n
 }
 }  // namespace
 
-hipError_t stamp_launch_f8_quant(const void* X, int x_bf16, int64_t ld_x, int rows, int d, int pow2, uint8_t* codes, float* scales, int64_t ld_s,
+hipError_t stamp_launch_f8_quant(const void* X, int x_bf16, int64_t ld_x, int rows, int d, int pow2, int wide, uint8_t* codes, float* scales, int64_t ld_s,
                                  const int32_t* row_of_slot, int top_k, int nrows, hipStream_t st) {
   const int Kp = (d + 127) / 128 * 128, size = x_bf16 ? 2 : 4;
-  const int wide = reinterpret_cast<uintptr_t>(X) % 16 == 0 && ld_x * size % 16 == 0;
-  const int64_t blocks = ((int64_t)rows * (Kp / 16) + 255) / 256;
-  if (x_bf16)
-    k_f8_quant<true><<<(uint32_t)blocks, 256, 0, st>>>(X, ld_x, rows, d, Kp, pow2, wide, codes, scales, ld_s, row_of_slot, top_k, nrows);
-  else
-    k_f8_quant<false><<<(uint32_t)blocks, 256, 0, st>>>(X, ld_x, rows, d, Kp, pow2, wide, codes, scales, ld_s, row_of_slot, top_k, nrows);
+  const int aligned = reinterpret_cast<uintptr_t>(X) % 16 == 0 && ld_x * size % 16 == 0;
+  const uint32_t blocks = (uint32_t)(((int64_t)rows * (Kp / 16) + 255) / 256);
+  auto* kernel = x_bf16 ? (wide ? k_f8_quant<true, true> : k_f8_quant<true, false>) : (wide ? k_f8_quant<false, true> : k_f8_quant<false, false>);
+  kernel<<<blocks, 256, 0, st>>>(X, ld_x, rows, d, Kp, pow2, aligned, codes, scales, ld_s, row_of_slot, top_k, nrows);
   return hipGetLastError();
 }
 
