@@ -50,6 +50,16 @@ int route_of(const StampF8Gemm& a, int rows) { return a.forced ? a.forced : stam
 // the codes are wanted as bf16
 bool wide_codes(const StampF8Gemm& a, int rows) { return a.wide_sums && route_of(a, rows) != STAMP_FP8_ROUTE_ROWS; }
 
+// the kernel quantizes the rows itself
+bool takes_x(const StampF8Gemm& a, int rows) { return route_of(a, rows) == STAMP_FP8_ROUTE_ROWS && stamp_f8_rows_quantize(a, rows); }
+void give_x(StampF8Gemm* a, const stamp_fp8_desc_t& d, const void* X, int64_t ld_x) {
+  a->X = X;
+  a->ld_x = ld_x;
+  a->x_bf16 = d.x_dtype == STAMP_BF16;
+  a->d = d.d_in;
+  a->aligned = (reinterpret_cast<uintptr_t>(X) | (uintptr_t)(ld_x * (a->x_bf16 ? 2 : 4))) % 16 == 0;
+}
+
 hipError_t product(const StampF8Gemm& a, hipStream_t st) {
   switch (route_of(a, a.rows)) {
     case STAMP_FP8_ROUTE_ROWS: return stamp_launch_f8_rows(a, st);
@@ -131,9 +141,12 @@ stamp_status_t forward(const stamp_fp8_plan* p, int32_t rows, const int32_t* off
   uint8_t* codes = static_cast<uint8_t*>(ws) + w.codes;
   float* scales = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + w.scales);
   StampF8Gemm a = gemm_args(p);
-  hipError_t e = stamp_launch_f8_quant(X, p->desc.x_dtype == STAMP_BF16, ld_x, rows, p->desc.d_in, a.pow2, wide_codes(a, rows), codes, scales,
-                                       scales_ld(rows), nullptr, 0, 0, st);
-  if (e != hipSuccess) return STAMP_ERR_DEVICE;
+  if (takes_x(a, rows)) {
+    give_x(&a, p->desc, X, ld_x);
+  } else if (stamp_launch_f8_quant(X, p->desc.x_dtype == STAMP_BF16, ld_x, rows, p->desc.d_in, a.pow2, wide_codes(a, rows), codes, scales, scales_ld(rows),
+                                   nullptr, 0, 0, st) != hipSuccess) {
+    return STAMP_ERR_DEVICE;
+  }
   a.A = codes;
   a.SA = scales;
   a.ld_sa = scales_ld(rows);
@@ -316,10 +329,12 @@ stamp_status_t stamp_experts_forward(const stamp_fp8_plan_t* up, const stamp_fp8
 
   StampF8Gemm a = gemm_args(up);
   float* scales = reinterpret_cast<float*>(ws + w.scales);
-  if (stamp_launch_f8_quant(X_dev, up->desc.x_dtype == STAMP_BF16, ld_x, r->tokens, up->desc.d_in, a.pow2, wide_codes(a, slots), ws + w.codes, scales,
-                            ld, r->row_of_slot_dev,
-                            r->top_k, slots, st) != hipSuccess)
+  if (takes_x(a, slots)) {
+    give_x(&a, up->desc, X_dev, ld_x);
+  } else if (stamp_launch_f8_quant(X_dev, up->desc.x_dtype == STAMP_BF16, ld_x, r->tokens, up->desc.d_in, a.pow2, wide_codes(a, slots), ws + w.codes, scales,
+                                   ld, r->row_of_slot_dev, r->top_k, slots, st) != hipSuccess) {
     return STAMP_ERR_DEVICE;
+  }
   a.A = ws + w.codes;
   a.SA = scales;
   a.ld_sa = ld;

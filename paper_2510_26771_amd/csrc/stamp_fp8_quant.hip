@@ -4,38 +4,6 @@
 namespace {
 using namespace f8;
 
-// 16 channels of a row from c on, zeros from d on.  wide: 16-byte loads are aligned.
-template <bool BF16>
-__device__ __forceinline__ void load16(const void* row, int c, int d, bool wide, float (&v)[16]) {
-  if (wide && c + 16 <= d) {
-    if constexpr (BF16) {
-      const u4* s = reinterpret_cast<const u4*>(static_cast<const uint16_t*>(row) + c);
-#pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        const u4 w = s[q];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[8 * q + 2 * j] = bf16_lo(w[j]), v[8 * q + 2 * j + 1] = bf16_hi(w[j]);
-      }
-    } else {
-      const f4* s = reinterpret_cast<const f4*>(static_cast<const float*>(row) + c);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const f4 w = s[q];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[4 * q + j] = w[j];
-      }
-    }
-    return;
-  }
-#pragma unroll
-  for (int j = 0; j < 16; ++j) {
-    if constexpr (BF16)
-      v[j] = c + j < d ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(row)[c + j] << 16) : 0.0f;
-    else
-      v[j] = c + j < d ? static_cast<const float*>(row)[c + j] : 0.0f;
-  }
-}
-
 // A thread has 16 channels, 8 lanes a block.  Bound by memory: 2 (4) bytes read, 1.03 written per element.
 template <bool BF16, bool WIDE>
 __global__ __launch_bounds__(256) void k_f8_quant(const void* X, int64_t ld_x, int rows, int d, int Kp, int pow2, int aligned, uint8_t* codes, float* scales,

@@ -1,8 +1,12 @@
 // Product of the 8-bit floating point layers for few rows (on average per expert).
 //
 // Bound by the weights' bytes: every byte is read once and feeds one matrix instruction per 16 rows.  So nothing is staged: a wave takes
-// some 16-place blocks of a group and a part of the depth, and reads its operand straight into registers in runs of 1 KB; the parts of
-// the depth are summed in LDS in a fixed order.  Always on the bf16 matrix instructions (f8_wide_sums): the pipe is idle most of the time.
+// blocks of 16 places and a part of the depth, and reads its operand straight into registers in runs of 1 KB; the parts of the depth
+// are summed in LDS in a fixed order.  Always on the bf16 matrix instructions (f8_wide_sums): the pipe is idle most of the time.
+//
+// Up to 16 rows the kernel quantizes the rows itself: the 4 lanes that share a row hold a block of its channels in the operand's order, so
+// its largest magnitude takes two exchanges and the codes never leave the registers.  Every workgroup does that again for its rows, in
+// the shadow of the weights on their way, and a launch of its own (2.6 us for one row, more than a quarter of the product) is saved.
 #include "stamp_fp8.h"
 
 namespace {
@@ -10,25 +14,30 @@ using namespace f8;
 
 constexpr int kWaves = 8;
 
+// where the rows come from: codes, or X in its type
+enum Rows { kCodes, kBf16, kF32 };
+
 // MT: tiles of 16 rows held at once.  NB: blocks of 16 places per wave.  S: parts of the depth; kWaves / S waves lie side by side.
-template <int MT, int NB, int S, bool GATED>
+template <int MT, int NB, int S, bool GATED, Rows IN>
 __global__ __launch_bounds__(kWaves * 64) void k_f8_rows(StampF8Gemm a) {
-  constexpr int kSide = kWaves / S;           // waves side by side
-  constexpr int kPlaces = kSide * NB * 16;    // places of the workgroup
-  constexpr int kLd = kPlaces + 4;            // floats of a row of partial sums
+  constexpr int kSide = kWaves / S;             // waves side by side
+  constexpr int kPlaces = kSide * NB * 16;      // places of the workgroup
+  constexpr int kLd = kPlaces + 4;              // floats of a row of partial sums
   constexpr int kRows = 16 * MT;
+  constexpr int U = MT == 1 ? 8 / NB : 1;       // blocks of channels whose weights are asked for at once: 64 registers
   __shared__ float red[S][kRows][kLd];
-  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
+  const int t = threadIdx.x, lane = t & 63, f = lane >> 4, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int side = wave % kSide, part = wave / kSide;
   const int set = blockIdx.y;
   int lo, hi;
   rows_of(a, set, &lo, &hi);
   lo = __builtin_amdgcn_readfirstlane(lo);
   hi = __builtin_amdgcn_readfirstlane(hi);
+  if (lo >= hi) return;
   const int blk0 = (blockIdx.x * kSide + side) * NB;  // first of the wave's blocks, counted over the groups
   const int g = blk0 >> 2, b0 = blk0 & 3;
   const bool in = g < a.groups;
-  const int kb0 = (int)((int64_t)a.Kb * part / S), kb1 = (int)((int64_t)a.Kb * (part + 1) / S);
+  const int kb0 = (int)((int64_t)a.Kb * part / S), kb1 = in ? (int)((int64_t)a.Kb * (part + 1) / S) : kb0;
   const uint8_t* w0 = a.W + (((size_t)set * a.groups + (in ? g : 0)) * a.Kb) * kF8GroupBytes + b0 * 2048 + lane * 16;
   const float* sw0 = a.SW + (size_t)set * (GATED ? 2 : 1) * a.nblk * a.Kb + (size_t)(GATED ? (in ? g : 0) >> 2 : (in ? g : 0) >> 1) * a.Kb;
   const int Kp = a.Kb * 128;
@@ -39,47 +48,99 @@ __global__ __launch_bounds__(kWaves * 64) void k_f8_rows(StampF8Gemm a) {
     for (int mi = 0; mi < MT; ++mi)
 #pragma unroll
       for (int b = 0; b < NB; ++b) acc[mi][b] = f4{0, 0, 0, 0};
-    const uint8_t* arow[MT];
+    const char* arow[MT];
     int srow[MT];
 #pragma unroll
     for (int mi = 0; mi < MT; ++mi) {
       const int r = min(r0 + 16 * mi + (lane & 15), hi - 1);
       int ar = r;
       if (a.index != nullptr) ar = min(max(a.index[r], 0), a.a_rows - 1);
-      arow[mi] = a.A + (size_t)ar * Kp + 16 * (lane >> 4);
+      if constexpr (IN == kCodes) arow[mi] = reinterpret_cast<const char*>(a.A) + (size_t)ar * Kp + 16 * f;
+      else arow[mi] = static_cast<const char*>(a.X) + (int64_t)ar * a.ld_x * (IN == kBf16 ? 2 : 4);
       srow[mi] = r;
     }
-    if (in) {
+
+    struct Step {
+      v8i W[NB];
+      v8i X[IN == kCodes ? MT : 1];
+      float sx[MT], sw, su;
+    };
+    auto fetch = [&](Step& s, int kb) __attribute__((always_inline)) {
+      const uint8_t* w = w0 + (size_t)kb * kF8GroupBytes;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+        s.W[b] = __builtin_shufflevector(*reinterpret_cast<const v4i*>(w + b * 2048), *reinterpret_cast<const v4i*>(w + b * 2048 + 1024), 0, 1, 2, 3, 4, 5, 6, 7);
+      if constexpr (IN == kCodes) {
+#pragma unroll
+        for (int mi = 0; mi < MT; ++mi) {
+          const v4i* p = reinterpret_cast<const v4i*>(arow[mi] + (size_t)kb * 128);
+          s.X[mi] = __builtin_shufflevector(p[0], p[4], 0, 1, 2, 3, 4, 5, 6, 7);
+          s.sx[mi] = a.SA[(int64_t)kb * a.ld_sa + srow[mi]];
+        }
+      }
+      s.sw = sw0[kb];
+      s.su = GATED ? sw0[(size_t)a.nblk * a.Kb + kb] : 0.0f;
+    };
+    auto multiply = [&](Step& s, int kb) __attribute__((always_inline)) {
+      if constexpr (IN != kCodes) {  // the lane's channels 64 h + 16 f .. + 15 of the block
+        float v[2][16];
+        uint32_t am = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          load16<IN == kBf16>(arow[0], kb * 128 + 64 * h + 16 * f, a.d, a.aligned, v[h]);
+#pragma unroll
+          for (int j = 0; j < 16; ++j) am = max(am, abs_bits(v[h][j]));
+        }
+        am = max(am, (uint32_t)__shfl_xor((int)am, 16));
+        am = max(am, (uint32_t)__shfl_xor((int)am, 32));
+        float inv;
+        scale_of(am, a.pow2, &s.sx[0], &inv);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            s.X[0][4 * h + j] = (int)pack4(__fmul_rn(v[h][4 * j], inv), __fmul_rn(v[h][4 * j + 1], inv), __fmul_rn(v[h][4 * j + 2], inv), __fmul_rn(v[h][4 * j + 3], inv));
+      }
+      b8 X[MT][4];
+#pragma unroll
+      for (int mi = 0; mi < MT; ++mi)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) X[mi][k] = widen8(s.X[mi][2 * k], s.X[mi][2 * k + 1]);
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        f4 p[MT];
+#pragma unroll
+        for (int mi = 0; mi < MT; ++mi) p[mi] = f4{0, 0, 0, 0};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          const b8 w = widen8(s.W[b][2 * k], s.W[b][2 * k + 1]);
+#pragma unroll
+          for (int mi = 0; mi < MT; ++mi) p[mi] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, X[mi][k], p[mi], 0, 0, 0);
+        }
+#pragma unroll
+        for (int mi = 0; mi < MT; ++mi) {
+          const float fs = s.sx[mi] * (GATED && ((b0 + b) & 1) ? s.su : s.sw);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) acc[mi][b][r] = __builtin_fmaf(p[mi][r], fs, acc[mi][b][r]);
+        }
+      }
+    };
+    if constexpr (MT == 1) {
+      for (int kb = kb0; kb < kb1; kb += U) {
+        Step s[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) fetch(s[u], min(kb + u, kb1 - 1));
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+          if (kb + u < kb1) multiply(s[u], kb + u);
+      }
+    } else if (kb0 < kb1) {
+      Step s, n;
+      fetch(s, kb0);
       for (int kb = kb0; kb < kb1; ++kb) {
-        const uint8_t* w = w0 + (size_t)kb * kF8GroupBytes;
-        v8i B[NB], X[MT];
-        float sx[MT];
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          const v4i l = *reinterpret_cast<const v4i*>(w + b * 2048), h = *reinterpret_cast<const v4i*>(w + b * 2048 + 1024);
-          B[b] = __builtin_shufflevector(l, h, 0, 1, 2, 3, 4, 5, 6, 7);
-        }
-#pragma unroll
-        for (int mi = 0; mi < MT; ++mi) {
-          const v4i* s = reinterpret_cast<const v4i*>(arow[mi] + (size_t)kb * 128);
-          X[mi] = __builtin_shufflevector(s[0], s[4], 0, 1, 2, 3, 4, 5, 6, 7);
-          sx[mi] = a.SA[(int64_t)kb * a.ld_sa + srow[mi]];
-        }
-        const float sw = sw0[kb], su = GATED ? sw0[(size_t)a.nblk * a.Kb + kb] : 0.0f;
-#pragma unroll
-        for (int mi = 0; mi < MT; ++mi) {
-#pragma unroll
-          for (int b = 0; b < NB; ++b) {
-            const float s = GATED && ((b0 + b) & 1) ? su : sw;
-            f4 p = {0, 0, 0, 0};
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-              p = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(B[b][2 * k], B[b][2 * k + 1]), widen8(X[mi][2 * k], X[mi][2 * k + 1]), p, 0, 0, 0);
-            const float f = sx[mi] * s;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) acc[mi][b][r] = __builtin_fmaf(p[r], f, acc[mi][b][r]);
-          }
-        }
+        fetch(n, min(kb + 1, kb1 - 1));
+        multiply(s, kb);
+        s = n;
       }
     }
     // partial sums: element r of block b is row 4 f + r of the instruction, token lane % 16
@@ -87,16 +148,15 @@ __global__ __launch_bounds__(kWaves * 64) void k_f8_rows(StampF8Gemm a) {
 #pragma unroll
     for (int mi = 0; mi < MT; ++mi)
 #pragma unroll
-      for (int b = 0; b < NB; ++b)
-        *reinterpret_cast<f4*>(&red[part][16 * mi + (lane & 15)][(side * NB + b) * 16 + 4 * (lane >> 4)]) = acc[mi][b];
+      for (int b = 0; b < NB; ++b) *reinterpret_cast<f4*>(&red[part][16 * mi + (lane & 15)][(side * NB + b) * 16 + 4 * f]) = acc[mi][b];
     __syncthreads();
     const int nr = min(kRows, hi - r0);
     if constexpr (!GATED) {
-      for (int u = t; u < kRows * kPlaces; u += kWaves * 64) {
+      for (int u = t; u < nr * kPlaces; u += kWaves * 64) {
         const int m = u / kPlaces, pl = u % kPlaces;
         const int blk = blockIdx.x * (kSide * NB) + (pl >> 4);
         const int n = f8_column(0, blk >> 2, blk & 3, pl & 15);
-        if (m >= nr || n >= a.N) continue;
+        if (n >= a.N) continue;
         float v = red[0][m][pl];
 #pragma unroll
         for (int s = 1; s < S; ++s) v += red[s][m][pl];
@@ -114,7 +174,7 @@ __global__ __launch_bounds__(kWaves * 64) void k_f8_rows(StampF8Gemm a) {
         uint32_t amax = 0;
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-          const int c = c0 + j, ch = blockIdx.x * 128 + c;  // of group c / 32: f = c / 8 % 4, pair c / 4 % 2
+          const int c = c0 + j, ch = blockIdx.x * 128 + c;  // of group c / 32: lanes c / 8 % 4, pair c / 4 % 2
           const int pl = (c >> 5) * 64 + ((c >> 2) & 1) * 32 + ((c >> 3) & 3) * 4 + (c & 3);
           float gt = red[0][m][pl], up = red[0][m][pl + 16];
 #pragma unroll
@@ -141,13 +201,29 @@ template <int MT, int NB, int S, bool GATED>
 hipError_t go(const StampF8Gemm& a, hipStream_t st) {
   const int places = kWaves / S * NB * 16;
   const dim3 grid((a.groups * 64 + places - 1) / places, a.sets);
-  k_f8_rows<MT, NB, S, GATED><<<grid, kWaves * 64, 0, st>>>(a);
+  if (a.X == nullptr) {
+    k_f8_rows<MT, NB, S, GATED, kCodes><<<grid, kWaves * 64, 0, st>>>(a);
+  } else if constexpr (MT == 1) {
+    if (a.x_bf16) k_f8_rows<MT, NB, S, GATED, kBf16><<<grid, kWaves * 64, 0, st>>>(a);
+    else k_f8_rows<MT, NB, S, GATED, kF32><<<grid, kWaves * 64, 0, st>>>(a);
+  } else {
+    return hipErrorInvalidValue;
+  }
   return hipGetLastError();
 }
+int average(const StampF8Gemm& a, int rows) { return (int)(((int64_t)rows + a.sets - 1) / a.sets); }
 }  // namespace
 
+bool stamp_f8_rows_quantize(const StampF8Gemm& a, int rows) { return average(a, rows) <= 16; }
+
 hipError_t stamp_launch_f8_rows(const StampF8Gemm& a, hipStream_t st) {
-  const int avg = (a.rows + a.sets - 1) / a.sets;
+  const int avg = average(a, a.rows), busy = a.sets < a.rows ? a.sets : a.rows;
   if (a.gated) return avg <= 16 ? go<1, 4, 2, true>(a, st) : go<2, 4, 2, true>(a, st);
-  return avg <= 16 ? go<1, 1, 8, false>(a, st) : go<2, 1, 8, false>(a, st);
+  // blocks per wave: as many as leave a workgroup for every CU; fewer workgroups read (and quantize) the rows less often
+  const int64_t groups = (int64_t)a.groups * busy;
+  const int cus = stamp_device_cus();
+  const int nb = groups >= cus ? 4 : 2 * groups >= cus ? 2 : 1;
+  if (avg <= 16) return nb == 4 ? go<1, 4, 8, false>(a, st) : nb == 2 ? go<1, 2, 8, false>(a, st) : go<1, 1, 8, false>(a, st);
+  if (avg <= 32) return nb == 4 ? go<2, 4, 8, false>(a, st) : nb == 2 ? go<2, 2, 8, false>(a, st) : go<2, 1, 8, false>(a, st);
+  return nb >= 2 ? go<4, 2, 8, false>(a, st) : go<4, 1, 8, false>(a, st);
 }

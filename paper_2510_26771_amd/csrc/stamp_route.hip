@@ -14,7 +14,7 @@ struct RouteArgs {
   int64_t ld;
   int32_t bf16, renorm;
   int32_t per_block;   // tokens of a workgroup
-  uint16_t* hist;      // [workgroups][experts] rows that a workgroup's tokens give an expert
+  uint16_t* hist;      // [workgroups][experts, an even number] rows that a workgroup's tokens give an expert
 };
 
 // order of floats as unsigned integers; 0 for what is masked.  -0 counts as 0.
@@ -24,78 +24,115 @@ __device__ __forceinline__ uint32_t order_key(float l) {
   return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? k & 0x7fffffffu : ~k); }
-// exp(l - top), where both may be +infinity: then they are equal
-__device__ __forceinline__ float share(float l, float top) { return l == top ? 1.0f : expf(l - top); }
-
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
-  return v;
+// exp(l - top) to 2 ulp, where both may be +infinity: then they are equal.  The product with log2 e in two parts.
+__device__ __forceinline__ float share(float l, float top) {
+  if (l == top) return 1.0f;
+  const float x = l - top, t = x * 1.44269502162933349609f;
+  const float rest = __builtin_fmaf(x, 1.44269502162933349609f, -t) + x * 1.92596299112661746887e-8f;
+  const float p = __builtin_amdgcn_exp2f(t);
+  return p > 0.0f ? __builtin_fmaf(p, rest * 0.693147180559945f, p) : 0.0f;  // (rest is no number where x is -infinity)
 }
 
-// One wave per token at a time, lane l has experts l + 64 j.  The largest (key, lower index first) is taken k times.
-template <int NV>
+// over the LANES lanes of a token, in all of them
+template <int CTRL>
+__device__ __forceinline__ uint32_t turn(uint32_t v) {
+  return (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, 0xf, 0xf, false);
+}
+template <int LANES, typename F>
+__device__ __forceinline__ uint32_t over_lanes(uint32_t v, F f) {
+  v = f(v, turn<0x128>(v));  // the row of 16 turned by 8, 4, 2, 1
+  v = f(v, turn<0x124>(v));
+  v = f(v, turn<0x122>(v));
+  v = f(v, turn<0x121>(v));
+  if constexpr (LANES == 64) {
+    v = f(v, (uint32_t)__shfl_xor((int)v, 16));
+    v = f(v, (uint32_t)__shfl_xor((int)v, 32));
+  }
+  return v;
+}
+template <int LANES>
+__device__ __forceinline__ float sum_lanes(float v) {
+  return __uint_as_float(over_lanes<LANES>(__float_as_uint(v), [](uint32_t x, uint32_t y) { return __float_as_uint(__uint_as_float(x) + __uint_as_float(y)); }));
+}
+
+// LANES lanes have a token, lane l of them experts l + LANES j: 4 tokens a wave up to 256 experts (the vector ALU is the bound, and the
+// steps over lanes cost the same for 1 and for 4 tokens).  The largest key, of the lowest expert, is taken top_k times.
+template <int LANES, int NV>
 __device__ void top_tokens(const RouteArgs& a, int tok0, int tok1, int wave, int lane, uint32_t* count) {
-  const int E = a.r.experts, K = a.r.top_k;
-  for (int t = tok0 + wave; t < tok1; t += kRtWaves) {
+  constexpr int kTokens = 64 / LANES, kMine = LANES == 16 ? 2 : 1;  // top_k <= 32 = kMine * LANES (or less)
+  const int E = a.r.experts, K = a.r.top_k, l0 = lane % LANES;
+  for (int tb = tok0 + wave * kTokens; tb < tok1; tb += kRtWaves * kTokens) {
+    const int t = tb + lane / LANES;
+    const bool in = t < tok1;
     uint32_t key[NV];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int e = lane + 64 * j;
+      const int e = l0 + LANES * j;
       float l = -__builtin_inff();
-      if (e < E)
+      if (in && e < E)
         l = a.bf16 ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(a.logits)[(int64_t)t * a.ld + e] << 16)
                    : static_cast<const float*>(a.logits)[(int64_t)t * a.ld + e];
       key[j] = order_key(l);
     }
-    uint32_t mine = 0;  // lane j: key of the j-th chosen
-    int id = -1;
+    uint32_t mine[kMine] = {};  // lane l: key of the chosen l, l + 16
+    int id[kMine];
+#pragma unroll
+    for (int q = 0; q < kMine; ++q) id[q] = -1;
     float top = 0.0f, sum = 0.0f;
     for (int k = 0; k < K; ++k) {
-      uint64_t best = 0;
+      uint32_t best = key[0];
 #pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        const uint64_t c = (uint64_t)key[j] << 32 | (uint32_t)~(lane + 64 * j);
-        best = c > best ? c : best;
-      }
+      for (int j = 1; j < NV; ++j) best = max(best, key[j]);
+      best = over_lanes<LANES>(best, [](uint32_t x, uint32_t y) { return max(x, y); });
+      uint32_t at = 0xffffffffu;
 #pragma unroll
-      for (int d = 1; d < 64; d <<= 1) {
-        const uint64_t o = __shfl_xor((unsigned long long)best, d);
-        best = o > best ? o : best;
-      }
-      const uint32_t bk = (uint32_t)(best >> 32);
-      if (bk == 0) break;
-      const int e = (int)~(uint32_t)best;
+      for (int j = NV - 1; j >= 0; --j) at = key[j] == best ? (uint32_t)(LANES * j) : at;
+      const uint32_t e = over_lanes<LANES>(at == 0xffffffffu ? at : at + l0, [](uint32_t x, uint32_t y) { return min(x, y); });
       if (k == 0) {
-        top = key_value(bk);
+        top = key_value(best);
         if (!a.renorm) {
           float s = 0.0f;
 #pragma unroll
           for (int j = 0; j < NV; ++j) s += key[j] != 0 ? share(key_value(key[j]), top) : 0.0f;
-          sum = wave_sum(s);
+          sum = sum_lanes<LANES>(s);
         }
       }
-      if (lane == k) mine = bk, id = e;
+      if (best == 0) continue;  // nothing left of this token (the wave's others may go on)
+      if (l0 == k % LANES) {
 #pragma unroll
-      for (int j = 0; j < NV; ++j)
-        if (e == lane + 64 * j) key[j] = 0;
+        for (int q = 0; q < kMine; ++q)
+          if (k / LANES == q) mine[q] = best, id[q] = (int)e;
+      }
+      const uint32_t gone = e - l0;  // LANES j where the chosen one is this lane's
+#pragma unroll
+      for (int j = 0; j < NV; ++j) key[j] = gone == (uint32_t)(LANES * j) ? 0 : key[j];
     }
-    const float sh = id >= 0 ? share(key_value(mine), top) : 0.0f;
-    if (a.renorm) sum = wave_sum(sh);
-    if (lane < K) {
-      a.r.ids_dev[(int64_t)t * K + lane] = id;
-      a.r.weights_dev[(int64_t)t * K + lane] = id >= 0 ? sh / sum : 0.0f;
-      if (id >= 0) atomicAdd(&count[id], 1u);
+    float sh[kMine], s = 0.0f;
+#pragma unroll
+    for (int q = 0; q < kMine; ++q) {
+      sh[q] = id[q] >= 0 ? share(key_value(mine[q]), top) : 0.0f;
+      s += sh[q];
+    }
+    if (a.renorm) sum = sum_lanes<LANES>(s);
+#pragma unroll
+    for (int q = 0; q < kMine; ++q) {
+      const int k = l0 + q * LANES;
+      if (in && k < K) {
+        a.r.ids_dev[(int64_t)t * K + k] = id[q];
+        a.r.weights_dev[(int64_t)t * K + k] = id[q] >= 0 ? sh[q] / sum : 0.0f;
+        if (id[q] >= 0) atomicAdd(&count[id[q]], 1u);
+      }
     }
   }
 }
 __device__ __forceinline__ void top_tokens_of(const RouteArgs& a, int tok0, int tok1, int wave, int lane, uint32_t* count) {
   const int E = a.r.experts;
-  if (E <= 64) top_tokens<1>(a, tok0, tok1, wave, lane, count);
-  else if (E <= 128) top_tokens<2>(a, tok0, tok1, wave, lane, count);
-  else if (E <= 256) top_tokens<4>(a, tok0, tok1, wave, lane, count);
-  else if (E <= 512) top_tokens<8>(a, tok0, tok1, wave, lane, count);
-  else top_tokens<16>(a, tok0, tok1, wave, lane, count);
+  if (E <= 32) top_tokens<16, 2>(a, tok0, tok1, wave, lane, count);
+  else if (E <= 64) top_tokens<16, 4>(a, tok0, tok1, wave, lane, count);
+  else if (E <= 128) top_tokens<16, 8>(a, tok0, tok1, wave, lane, count);
+  else if (E <= 256) top_tokens<16, 16>(a, tok0, tok1, wave, lane, count);
+  else if (E <= 512) top_tokens<64, 8>(a, tok0, tok1, wave, lane, count);
+  else top_tokens<64, 16>(a, tok0, tok1, wave, lane, count);
 }
 
 // Order of the workgroup's slots by expert: every wave has a run of them.  cnt [waves][E].
@@ -104,7 +141,7 @@ __device__ void place_rows(const RouteArgs& a, int tok0, int tok1, int wave, int
   const int64_t s0 = (int64_t)tok0 * K;
   const int n = (tok1 - tok0) * K;
   const int run = ((n + kRtWaves - 1) / kRtWaves + 63) / 64 * 64;
-  for (int i = t; i < kRtWaves * kF8MaxExperts; i += kRtWaves * 64) (&cnt[0][0])[i] = 0;
+  for (int e = lane; e < E; e += 64) cnt[wave][e] = 0;
   __syncthreads();
   const int r0 = min(wave * run, n), r1 = min(r0 + run, n);
   for (int i = r0 + lane; i < r1; i += 64) {
@@ -178,7 +215,8 @@ __global__ __launch_bounds__(kRtWaves * 64) void k_route_top(RouteArgs a) {
   __threadfence_block();
   __syncthreads();
   if constexpr (!ONE) {
-    for (int e = t; e < E; e += kRtWaves * 64) a.hist[(size_t)blockIdx.x * E + e] = (uint16_t)count[e];
+    const int stride = (E + 1) & ~1;
+    for (int e = t; e < stride; e += kRtWaves * 64) a.hist[(size_t)blockIdx.x * stride + e] = e < E ? (uint16_t)count[e] : (uint16_t)0;
   } else {
     __shared__ uint32_t cnt[kRtWaves][kF8MaxExperts];
     __shared__ uint32_t base[kF8MaxExperts];
@@ -196,15 +234,29 @@ __global__ __launch_bounds__(kRtWaves * 64) void k_route_place(RouteArgs a) {
   __shared__ uint32_t tmp[kRtWaves];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, E = a.r.experts, nb = gridDim.x;
   const int tok0 = min((int)blockIdx.x * a.per_block, a.r.tokens), tok1 = min(tok0 + a.per_block, a.r.tokens);
-  for (int e = t; e < E; e += kRtWaves * 64) {
-    uint32_t all = 0, before = 0;
-    for (int b = 0; b < nb; ++b) {
-      const uint32_t h = a.hist[(size_t)b * E + e];
-      all += h;
-      before += b < (int)blockIdx.x ? h : 0;
+  // all workgroups' counts, two experts and a part of the workgroups a thread: `parts` threads side by side have the same experts
+  const int pairs = (E + 1) / 2, parts = max(1, kRtWaves * 64 / pairs), stride = (E + 1) & ~1;
+  for (int e = t; e < E; e += kRtWaves * 64) total[e] = mine[e] = 0;
+  __syncthreads();
+  for (int u = t; u < pairs * parts; u += kRtWaves * 64) {
+    const int pair = u % pairs, part = u / pairs, b1 = nb * (part + 1) / parts;
+    const uint32_t* h = reinterpret_cast<const uint32_t*>(a.hist) + pair;
+    uint32_t all0 = 0, all1 = 0, before0 = 0, before1 = 0;
+#pragma unroll 16
+    for (int b = nb * part / parts; b < b1; ++b) {
+      const uint32_t v = h[(size_t)b * (stride / 2)];
+      const uint32_t mask = b < (int)blockIdx.x ? 0xffffffffu : 0;
+      all0 += v & 0xffff;
+      all1 += v >> 16;
+      before0 += v & 0xffff & mask;
+      before1 += (v & mask) >> 16;
     }
-    total[e] = all;
-    mine[e] = before;
+    atomicAdd(&total[2 * pair], all0);
+    atomicAdd(&mine[2 * pair], before0);
+    if (2 * pair + 1 < E) {
+      atomicAdd(&total[2 * pair + 1], all1);
+      atomicAdd(&mine[2 * pair + 1], before1);
+    }
   }
   __syncthreads();
   const uint32_t all = scan_experts(total, base, E, tmp);
@@ -232,18 +284,44 @@ __global__ __launch_bounds__(256) void k_combine(stamp_routing_t r, const void* 
   const int c = (int)(u - t * per) * 8;
   if (t >= r.tokens) return;
   float y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-  for (int j = 0; j < r.top_k; ++j) {
-    const int row = r.row_of_slot_dev[t * r.top_k + j];
-    if ((uint32_t)row >= (uint32_t)nrows) continue;
-    const float w = r.weights_dev[t * r.top_k + j];
+  const int32_t* slot = r.row_of_slot_dev + t * r.top_k;
+  const float* weight = r.weights_dev + t * r.top_k;
+  for (int j0 = 0; j0 < r.top_k; j0 += 8) {  // 8 rows in flight
+    int row[8];
+    float w[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const int jj = min(j0 + j, r.top_k - 1);
+      row[j] = slot[jj];
+      w[j] = weight[jj];
+      if (j0 + j >= r.top_k) row[j] = -1;
+    }
     if constexpr (BF16) {
-      const u4 v = *reinterpret_cast<const u4*>(static_cast<const uint16_t*>(rows) + row * ld_rows + c);
+      u4 v[8];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) y[2 * i] = __builtin_fmaf(w, bf16_lo(v[i]), y[2 * i]), y[2 * i + 1] = __builtin_fmaf(w, bf16_hi(v[i]), y[2 * i + 1]);
+      for (int j = 0; j < 8; ++j)
+        v[j] = (uint32_t)row[j] < (uint32_t)nrows ? *reinterpret_cast<const u4*>(static_cast<const uint16_t*>(rows) + row[j] * ld_rows + c) : u4{0, 0, 0, 0};
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float f = (uint32_t)row[j] < (uint32_t)nrows ? w[j] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) y[2 * i] = __builtin_fmaf(f, bf16_lo(v[j][i]), y[2 * i]), y[2 * i + 1] = __builtin_fmaf(f, bf16_hi(v[j][i]), y[2 * i + 1]);
+      }
     } else {
-      const f4* s = reinterpret_cast<const f4*>(static_cast<const float*>(rows) + row * ld_rows + c);
+      f4 v[8][2];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) y[i] = __builtin_fmaf(w, s[i >> 2][i & 3], y[i]);
+      for (int j = 0; j < 8; ++j) {
+        const f4* s = reinterpret_cast<const f4*>(static_cast<const float*>(rows) + row[j] * ld_rows + c);
+        const bool on = (uint32_t)row[j] < (uint32_t)nrows;
+        v[j][0] = on ? s[0] : f4{0, 0, 0, 0};
+        v[j][1] = on ? s[1] : f4{0, 0, 0, 0};
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float f = (uint32_t)row[j] < (uint32_t)nrows ? w[j] : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = __builtin_fmaf(f, v[j][i >> 2][i & 3], y[i]);
+      }
     }
   }
   const int64_t o = t * ld_y + c;
@@ -268,7 +346,7 @@ __global__ __launch_bounds__(256) void k_combine(stamp_routing_t r, const void* 
 size_t stamp_route_ws(int tokens, int experts, int) {
   const int per = tokens_per_block(tokens);
   const size_t nb = ((size_t)tokens + per - 1) / per;
-  return (nb * experts * sizeof(uint16_t) + 255) / 256 * 256 + 256;
+  return (nb * ((size_t)experts + 1) * sizeof(uint16_t) + 255) / 256 * 256 + 256;
 }
 
 hipError_t stamp_launch_route(const stamp_routing_t& r, const void* logits, int bf16, int64_t ld, int renorm, void* ws, hipStream_t st) {
