@@ -51,6 +51,7 @@ struct StampF8Gemm {
   const void* X;           // not nullptr: A's rows before Q8, quantized by the product itself (few rows)
   int64_t ld_x;
   int32_t x_bf16, d, aligned;  // channels; rows of X on the 16-byte grid
+  int32_t chunk;           // rows quantized at a time
   int32_t rows;
   const int32_t* offsets;  // [sets + 1] or nullptr (one set)
   const uint8_t* W;
@@ -72,7 +73,7 @@ hipError_t stamp_launch_f8_weights(stamp_fp8_plan* p, const void* W, const float
 hipError_t stamp_launch_f8_widen(const uint8_t* codes, int64_t bytes, uint8_t* out, hipStream_t st);
 hipError_t stamp_launch_f8_quant(const void* X, int x_bf16, int64_t ld_x, int rows, int d, int pow2, int wide, uint8_t* codes, float* scales, int64_t ld_s,
                                  const int32_t* row_of_slot, int top_k, int nrows, hipStream_t st);
-bool stamp_f8_rows_quantize(const StampF8Gemm& a, int rows);  // the kernel for few rows would take X itself
+int stamp_f8_rows_quantize(const StampF8Gemm& a, int rows);  // rows that the kernel for few rows quantizes at a time, 0: it takes codes
 hipError_t stamp_launch_f8_rows(const StampF8Gemm& a, hipStream_t st);
 hipError_t stamp_launch_f8_tiles(const StampF8Gemm& a, int bm, hipStream_t st);
 
@@ -198,37 +199,46 @@ __device__ __forceinline__ void find_tile(const StampF8Gemm& a, int BM, int tile
   }
 }
 
-// 16 channels of a row from c on, zeros from d on.  aligned: 16-byte loads are.
+// 16 channels of a row from c on as they are stored, zeros from d on.  aligned: 16-byte loads are.
 template <bool BF16>
-__device__ __forceinline__ void load16(const void* row, int c, int d, bool aligned, float (&v)[16]) {
-  if (aligned && c + 16 <= d) {
-    if constexpr (BF16) {
-      const u4* s = reinterpret_cast<const u4*>(static_cast<const uint16_t*>(row) + c);
+struct Raw16 {
+  u4 w[BF16 ? 2 : 4];
+  __device__ __forceinline__ void load(const void* row, int c, int d, bool aligned) {
+    if (aligned && c + 16 <= d) {
+      const u4* s = reinterpret_cast<const u4*>(static_cast<const char*>(row) + (size_t)c * (BF16 ? 2 : 4));
 #pragma unroll
-      for (int q = 0; q < 2; ++q) {
-        const u4 w = s[q];
+      for (int q = 0; q < (BF16 ? 2 : 4); ++q) w[q] = s[q];
+      return;
+    }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) v[8 * q + 2 * j] = bf16_lo(w[j]), v[8 * q + 2 * j + 1] = bf16_hi(w[j]);
-      }
-    } else {
-      const f4* s = reinterpret_cast<const f4*>(static_cast<const float*>(row) + c);
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const f4 w = s[q];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) v[4 * q + j] = w[j];
+    for (int j = 0; j < 16; ++j) {
+      if constexpr (BF16) {
+        const uint32_t x = c + j < d ? static_cast<const uint16_t*>(row)[c + j] : 0u;
+        if (j & 1) w[j >> 3][(j >> 1) & 3] |= x << 16;
+        else w[j >> 3][(j >> 1) & 3] = x;
+      } else {
+        w[j >> 2][j & 3] = c + j < d ? static_cast<const uint32_t*>(row)[c + j] : 0u;
       }
     }
-    return;
   }
+  __device__ __forceinline__ float at(int j) const {
+    if constexpr (BF16) return (j & 1) ? bf16_hi(w[j >> 3][(j >> 1) & 3]) : bf16_lo(w[j >> 3][(j >> 1) & 3]);
+    else return __uint_as_float(w[j >> 2][j & 3]);
+  }
+  __device__ __forceinline__ uint32_t amax() const {
+    uint32_t a = 0;
 #pragma unroll
-  for (int j = 0; j < 16; ++j) {
-    if constexpr (BF16)
-      v[j] = c + j < d ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(row)[c + j] << 16) : 0.0f;
-    else
-      v[j] = c + j < d ? static_cast<const float*>(row)[c + j] : 0.0f;
+    for (int j = 0; j < 16; ++j) a = max(a, abs_bits(at(j)));
+    return a;
   }
-}
+  __device__ __forceinline__ u4 codes(float inv) const {
+    u4 o;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      o[j] = pack4(__fmul_rn(at(4 * j), inv), __fmul_rn(at(4 * j + 1), inv), __fmul_rn(at(4 * j + 2), inv), __fmul_rn(at(4 * j + 3), inv));
+    return o;
+  }
+};
 
 typedef __bf16 b2 __attribute__((ext_vector_type(2)));
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));

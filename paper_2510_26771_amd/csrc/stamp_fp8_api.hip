@@ -51,9 +51,10 @@ int route_of(const StampF8Gemm& a, int rows) { return a.forced ? a.forced : stam
 bool wide_codes(const StampF8Gemm& a, int rows) { return a.wide_sums && route_of(a, rows) != STAMP_FP8_ROUTE_ROWS; }
 
 // the kernel quantizes the rows itself
-bool takes_x(const StampF8Gemm& a, int rows) { return route_of(a, rows) == STAMP_FP8_ROUTE_ROWS && stamp_f8_rows_quantize(a, rows); }
-void give_x(StampF8Gemm* a, const stamp_fp8_desc_t& d, const void* X, int64_t ld_x) {
+bool takes_x(const StampF8Gemm& a, int rows) { return route_of(a, rows) == STAMP_FP8_ROUTE_ROWS && stamp_f8_rows_quantize(a, rows) > 0; }
+void give_x(StampF8Gemm* a, const stamp_fp8_desc_t& d, int rows, const void* X, int64_t ld_x) {
   a->X = X;
+  a->chunk = stamp_f8_rows_quantize(*a, rows);
   a->ld_x = ld_x;
   a->x_bf16 = d.x_dtype == STAMP_BF16;
   a->d = d.d_in;
@@ -142,7 +143,7 @@ stamp_status_t forward(const stamp_fp8_plan* p, int32_t rows, const int32_t* off
   float* scales = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + w.scales);
   StampF8Gemm a = gemm_args(p);
   if (takes_x(a, rows)) {
-    give_x(&a, p->desc, X, ld_x);
+    give_x(&a, p->desc, rows, X, ld_x);
   } else if (stamp_launch_f8_quant(X, p->desc.x_dtype == STAMP_BF16, ld_x, rows, p->desc.d_in, a.pow2, wide_codes(a, rows), codes, scales, scales_ld(rows),
                                    nullptr, 0, 0, st) != hipSuccess) {
     return STAMP_ERR_DEVICE;
@@ -160,12 +161,32 @@ stamp_status_t forward(const stamp_fp8_plan* p, int32_t rows, const int32_t* off
 }  // namespace
 
 // Kernel for a product of `rows` rows over `sets` weights.
+//
+// Few rows: the weights' time, and some 5 us more per 16 rows and 700 groups; tiles of 64 rows hold the time up to 64 rows but take one
+// workgroup per 256 columns and set.  Whole calls, us (rows kernel / tiles of 64), 4096 -> 11008, bf16 Y: 17 rows 15.2 / 19.2,
+// 32 18.3 / 19.6, 33 21.2 / 19.6, 64 28.4 / 20.5; 4096 -> 4096: 64 15.3 / 19.2, 128 26 / 19.4; fp32 Y (sums in fp32), 4096 -> 11008:
+// 64 28.5 / 34.8, 96 43.7 / 35.2; 4096 -> 4096: 128 26.9 / 34.4.
+//
+// Tiles of 64, 128, 256 rows: a workgroup a CU, so rounds of `cus` tiles, each of Kb steps and a start and end.  us per step and
+// per round, measured on full rounds: 0.53 + 3.5, 0.9 + 4.5, 1.45 + 6; with sums in fp32 1.05 + 4, 1.75 + 6.  (2048 x 4096 -> 11008: 120, 98
+// and 100 us; 8192 x 1152 -> 4608: 77, 64 and 60; 512 x 4096 -> 11008: 39, 30 and 45.)
 int stamp_f8_route(int sets, int groups, int Kb, int rows, int wide_sums) {
-  const int avg = (int)(((int64_t)rows + sets - 1) / sets);
-  if (avg <= 32) return STAMP_FP8_ROUTE_ROWS;
-  if (avg <= 64) return STAMP_FP8_ROUTE_TILES_64;
-  if (avg <= 512 || wide_sums) return STAMP_FP8_ROUTE_TILES_128;  // the bf16 operands of 256 rows do not fit the registers
-  return STAMP_FP8_ROUTE_TILES_256;
+  const int busy = sets < rows ? sets : rows > 0 ? rows : 1, avg = (int)(((int64_t)rows + busy - 1) / busy);
+  const int64_t ncol = (groups + 3) / 4;
+  int few = ncol * busy < 32 ? 64 : 32;
+  if (wide_sums) few *= 2;
+  if (avg <= few) return STAMP_FP8_ROUTE_ROWS;
+  const int cus = stamp_device_cus();
+  static const float step[2][3] = {{0.53f, 0.9f, 1.45f}, {1.05f, 1.75f, 0.0f}}, ends[2][3] = {{3.5f, 4.5f, 6.0f}, {4.0f, 6.0f, 0.0f}};
+  int best = 0;
+  float best_us = 0.0f;
+  for (int i = 0; i < (wide_sums ? 2 : 3); ++i) {  // the bf16 operands of 256 rows do not fit the registers
+    const int bm = 64 << i;
+    const int64_t tiles = sets == 1 ? (rows + bm - 1) / bm : rows / bm + (busy + 1) / 2;  // half of the last tile of a set is empty
+    const float us = (float)((tiles * ncol + cus - 1) / cus) * ((float)Kb * step[wide_sums != 0][i] + ends[wide_sums != 0][i]);
+    if (best == 0 || us < best_us) best = STAMP_FP8_ROUTE_TILES_64 + i, best_us = us;
+  }
+  return best;
 }
 
 extern "C" {
@@ -330,7 +351,7 @@ stamp_status_t stamp_experts_forward(const stamp_fp8_plan_t* up, const stamp_fp8
   StampF8Gemm a = gemm_args(up);
   float* scales = reinterpret_cast<float*>(ws + w.scales);
   if (takes_x(a, slots)) {
-    give_x(&a, up->desc, X_dev, ld_x);
+    give_x(&a, up->desc, slots, X_dev, ld_x);
   } else if (stamp_launch_f8_quant(X_dev, up->desc.x_dtype == STAMP_BF16, ld_x, r->tokens, up->desc.d_in, a.pow2, wide_codes(a, slots), ws + w.codes, scales,
                                    ld, r->row_of_slot_dev, r->top_k, slots, st) != hipSuccess) {
     return STAMP_ERR_DEVICE;

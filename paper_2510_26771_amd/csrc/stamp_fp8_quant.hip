@@ -13,18 +13,11 @@ __global__ __launch_bounds__(256) void k_f8_quant(const void* X, int64_t ld_x, i
   const int64_t m = u / per;
   const int c = (int)(u - m * per) * 16;
   if (m >= rows) return;  // whole groups of 8 lanes: per is a multiple of 8
-  float v[16];
-  load16<BF16>(static_cast<const char*>(X) + m * ld_x * (BF16 ? 2 : 4), c, d, aligned, v);
-  uint32_t a = 0;
-#pragma unroll
-  for (int j = 0; j < 16; ++j) a = max(a, abs_bits(v[j]));
-  a = max8(a);
+  Raw16<BF16> x;
+  x.load(static_cast<const char*>(X) + m * ld_x * (BF16 ? 2 : 4), c, d, aligned);
   float scale, inv;
-  scale_of(a, pow2, &scale, &inv);
-  u4 o;
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-    o[j] = pack4(__fmul_rn(v[4 * j], inv), __fmul_rn(v[4 * j + 1], inv), __fmul_rn(v[4 * j + 2], inv), __fmul_rn(v[4 * j + 3], inv));
+  scale_of(max8(x.amax()), pow2, &scale, &inv);
+  const u4 o = x.codes(inv);
   if constexpr (WIDE) {
     b8* p = reinterpret_cast<b8*>(codes + (m * Kp + c) * 2);
     p[0] = widen8((int)o[0], (int)o[1]);
@@ -37,9 +30,13 @@ __global__ __launch_bounds__(256) void k_f8_quant(const void* X, int64_t ld_x, i
   if (row_of_slot == nullptr) {
     s[m] = scale;
   } else {
-    for (int j = 0; j < top_k; ++j) {
-      const int r = row_of_slot[m * top_k + j];
-      if ((uint32_t)r < (uint32_t)nrows) s[r] = scale;
+    for (int j0 = 0; j0 < top_k; j0 += 8) {
+      int r[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) r[j] = j0 + j < top_k ? row_of_slot[m * top_k + j0 + j] : -1;
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if ((uint32_t)r[j] < (uint32_t)nrows) s[r[j]] = scale;
     }
   }
 }

@@ -4,28 +4,32 @@
 // blocks of 16 places and a part of the depth, and reads its operand straight into registers in runs of 1 KB; the parts of the depth
 // are summed in LDS in a fixed order.  Always on the bf16 matrix instructions (f8_wide_sums): the pipe is idle most of the time.
 //
-// Up to 16 rows the kernel quantizes the rows itself: the 4 lanes that share a row hold a block of its channels in the operand's order, so
-// its largest magnitude takes two exchanges and the codes never leave the registers.  Every workgroup does that again for its rows, in
-// the shadow of the weights on their way, and a launch of its own (2.6 us for one row, more than a quarter of the product) is saved.
+// Few rows the kernel quantizes itself, into LDS: X is asked for first, then the weights, and the codes are made while those are on their
+// way (loads return in order).  Every workgroup does that again for its rows; a launch of its own is saved (2.6 us for one row, more than a
+// quarter of the product).
 #include "stamp_fp8.h"
 
 namespace {
 using namespace f8;
 
-constexpr int kWaves = 8;
-
 // where the rows come from: codes, or X in its type
 enum Rows { kCodes, kBf16, kF32 };
 
 // MT: tiles of 16 rows held at once.  NB: blocks of 16 places per wave.  S: parts of the depth; kWaves / S waves lie side by side.
-template <int MT, int NB, int S, bool GATED, Rows IN>
-__global__ __launch_bounds__(kWaves * 64) void k_f8_rows(StampF8Gemm a) {
+template <int MT, int NB, int S, int kWaves, bool GATED, Rows IN>
+__global__ __launch_bounds__(kWaves * 64, IN == kCodes ? 2 : 4) void k_f8_rows(StampF8Gemm a) {
   constexpr int kSide = kWaves / S;             // waves side by side
   constexpr int kPlaces = kSide * NB * 16;      // places of the workgroup
   constexpr int kLd = kPlaces + 4;              // floats of a row of partial sums
   constexpr int kRows = 16 * MT;
-  constexpr int U = MT == 1 ? 8 / NB : 1;       // blocks of channels whose weights are asked for at once: 64 registers
-  __shared__ float red[S][kRows][kLd];
+  // blocks of channels whose weights are asked for at once: 64 registers, 32 beside the rows' (two workgroups a CU then)
+  constexpr int U = MT > 1 ? 1 : IN == kCodes ? 8 / NB : 4 / NB;
+  // one after the other: codes [rows][Kp + 16] and scales [rows][Kb] of the rows quantized here; partial sums
+  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+  float(*red)[kRows][kLd] = reinterpret_cast<float(*)[kRows][kLd]>(lds);
+  const int chunk = IN == kCodes ? kRows : a.chunk;
+  const int ldc = a.Kb * 128 + 16;
+  float* lds_scale = reinterpret_cast<float*>(lds + chunk * ldc);
   const int t = threadIdx.x, lane = t & 63, f = lane >> 4, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int side = wave % kSide, part = wave / kSide;
   const int set = blockIdx.y;
@@ -42,65 +46,52 @@ __global__ __launch_bounds__(kWaves * 64) void k_f8_rows(StampF8Gemm a) {
   const float* sw0 = a.SW + (size_t)set * (GATED ? 2 : 1) * a.nblk * a.Kb + (size_t)(GATED ? (in ? g : 0) >> 2 : (in ? g : 0) >> 1) * a.Kb;
   const int Kp = a.Kb * 128;
 
-  for (int r0 = lo; r0 < hi; r0 += kRows) {
+  for (int r0 = lo; r0 < hi; r0 += chunk) {
+    const int nr = min(chunk, hi - r0);
     f4 acc[MT][NB];
 #pragma unroll
     for (int mi = 0; mi < MT; ++mi)
 #pragma unroll
       for (int b = 0; b < NB; ++b) acc[mi][b] = f4{0, 0, 0, 0};
-    const char* arow[MT];
+    const uint8_t* arow[MT];
     int srow[MT];
 #pragma unroll
     for (int mi = 0; mi < MT; ++mi) {
-      const int r = min(r0 + 16 * mi + (lane & 15), hi - 1);
-      int ar = r;
-      if (a.index != nullptr) ar = min(max(a.index[r], 0), a.a_rows - 1);
-      if constexpr (IN == kCodes) arow[mi] = reinterpret_cast<const char*>(a.A) + (size_t)ar * Kp + 16 * f;
-      else arow[mi] = static_cast<const char*>(a.X) + (int64_t)ar * a.ld_x * (IN == kBf16 ? 2 : 4);
-      srow[mi] = r;
+      const int m = min(16 * mi + (lane & 15), nr - 1);
+      srow[mi] = IN == kCodes ? r0 + m : m * a.Kb;
+      if constexpr (IN == kCodes) {
+        int ar = r0 + m;
+        if (a.index != nullptr) ar = min(max(a.index[ar], 0), a.a_rows - 1);
+        arow[mi] = a.A + (size_t)ar * Kp + 16 * f;
+      } else {
+        arow[mi] = lds + m * ldc + 16 * f;
+      }
     }
 
     struct Step {
       v8i W[NB];
-      v8i X[IN == kCodes ? MT : 1];
+      v8i X[MT];
       float sx[MT], sw, su;
+    };
+    auto fetch_rows = [&](Step& s, int kb) __attribute__((always_inline)) {
+#pragma unroll
+      for (int mi = 0; mi < MT; ++mi) {
+        const v4i* p = reinterpret_cast<const v4i*>(arow[mi] + (size_t)kb * 128);
+        s.X[mi] = __builtin_shufflevector(p[0], p[4], 0, 1, 2, 3, 4, 5, 6, 7);
+        s.sx[mi] = IN == kCodes ? a.SA[(int64_t)kb * a.ld_sa + srow[mi]] : lds_scale[srow[mi] + kb];
+      }
     };
     auto fetch = [&](Step& s, int kb) __attribute__((always_inline)) {
       const uint8_t* w = w0 + (size_t)kb * kF8GroupBytes;
 #pragma unroll
       for (int b = 0; b < NB; ++b)
         s.W[b] = __builtin_shufflevector(*reinterpret_cast<const v4i*>(w + b * 2048), *reinterpret_cast<const v4i*>(w + b * 2048 + 1024), 0, 1, 2, 3, 4, 5, 6, 7);
-      if constexpr (IN == kCodes) {
-#pragma unroll
-        for (int mi = 0; mi < MT; ++mi) {
-          const v4i* p = reinterpret_cast<const v4i*>(arow[mi] + (size_t)kb * 128);
-          s.X[mi] = __builtin_shufflevector(p[0], p[4], 0, 1, 2, 3, 4, 5, 6, 7);
-          s.sx[mi] = a.SA[(int64_t)kb * a.ld_sa + srow[mi]];
-        }
-      }
+      if constexpr (IN == kCodes) fetch_rows(s, kb);
       s.sw = sw0[kb];
       s.su = GATED ? sw0[(size_t)a.nblk * a.Kb + kb] : 0.0f;
     };
     auto multiply = [&](Step& s, int kb) __attribute__((always_inline)) {
-      if constexpr (IN != kCodes) {  // the lane's channels 64 h + 16 f .. + 15 of the block
-        float v[2][16];
-        uint32_t am = 0;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          load16<IN == kBf16>(arow[0], kb * 128 + 64 * h + 16 * f, a.d, a.aligned, v[h]);
-#pragma unroll
-          for (int j = 0; j < 16; ++j) am = max(am, abs_bits(v[h][j]));
-        }
-        am = max(am, (uint32_t)__shfl_xor((int)am, 16));
-        am = max(am, (uint32_t)__shfl_xor((int)am, 32));
-        float inv;
-        scale_of(am, a.pow2, &s.sx[0], &inv);
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            s.X[0][4 * h + j] = (int)pack4(__fmul_rn(v[h][4 * j], inv), __fmul_rn(v[h][4 * j + 1], inv), __fmul_rn(v[h][4 * j + 2], inv), __fmul_rn(v[h][4 * j + 3], inv));
-      }
+      if constexpr (IN != kCodes) fetch_rows(s, kb);
       b8 X[MT][4];
 #pragma unroll
       for (int mi = 0; mi < MT; ++mi)
@@ -126,10 +117,44 @@ __global__ __launch_bounds__(kWaves * 64) void k_f8_rows(StampF8Gemm a) {
       }
     };
     if constexpr (MT == 1) {
-      for (int kb = kb0; kb < kb1; kb += U) {
-        Step s[U];
+      Step s[U];
+      if constexpr (IN != kCodes) {
+        // a unit: 16 channels of a row, 8 lanes a block
+        const int units = nr * a.Kb * 8, per = a.Kb * 8;
+        auto row_of = [&](int u) __attribute__((always_inline)) {
+          const int r = r0 + u / per;
+          const int ar = a.index != nullptr ? min(max(a.index[r], 0), a.a_rows - 1) : r;
+          return static_cast<const char*>(a.X) + (int64_t)ar * a.ld_x * (IN == kBf16 ? 2 : 4);
+        };
+        auto make = [&](int u, const Raw16<IN == kBf16>& x) __attribute__((always_inline)) {
+          float scale, inv;
+          scale_of(max8(x.amax()), a.pow2, &scale, &inv);
+          const int m = u / per, c = (u - m * per) * 16;
+          *reinterpret_cast<u4*>(lds + m * ldc + c) = x.codes(inv);
+          if ((t & 7) == 0) lds_scale[m * a.Kb + (c >> 7)] = scale;
+        };
+        Raw16<IN == kBf16> x0, x1;
+        const bool two = t + kWaves * 64 < units;
+        if (t < units) x0.load(row_of(t), t % per * 16, a.d, a.aligned);
+        if (two) x1.load(row_of(t + kWaves * 64), (t + kWaves * 64) % per * 16, a.d, a.aligned);
+        if (kb0 < kb1) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) fetch(s[u], min(kb + u, kb1 - 1));
+          for (int u = 0; u < U; ++u) fetch(s[u], min(kb0 + u, kb1 - 1));
+        }
+        __syncthreads();  // the partial sums of the rows before have been read
+        if (t < units) make(t, x0);
+        if (two) make(t + kWaves * 64, x1);
+        for (int u = t + 2 * kWaves * 64; u < units; u += kWaves * 64) {
+          x0.load(row_of(u), u % per * 16, a.d, a.aligned);
+          make(u, x0);
+        }
+        __syncthreads();
+      }
+      for (int kb = kb0; kb < kb1; kb += U) {
+        if (IN == kCodes || kb > kb0) {
+#pragma unroll
+          for (int u = 0; u < U; ++u) fetch(s[u], min(kb + u, kb1 - 1));
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u)
           if (kb + u < kb1) multiply(s[u], kb + u);
@@ -150,7 +175,6 @@ __global__ __launch_bounds__(kWaves * 64) void k_f8_rows(StampF8Gemm a) {
 #pragma unroll
       for (int b = 0; b < NB; ++b) *reinterpret_cast<f4*>(&red[part][16 * mi + (lane & 15)][(side * NB + b) * 16 + 4 * f]) = acc[mi][b];
     __syncthreads();
-    const int nr = min(kRows, hi - r0);
     if constexpr (!GATED) {
       for (int u = t; u < nr * kPlaces; u += kWaves * 64) {
         const int m = u / kPlaces, pl = u % kPlaces;
@@ -197,33 +221,49 @@ __global__ __launch_bounds__(kWaves * 64) void k_f8_rows(StampF8Gemm a) {
   }
 }
 
-template <int MT, int NB, int S, bool GATED>
+int row_bytes(int Kb) { return Kb * 128 + 16 + Kb * 4; }  // of a row quantized here
+constexpr int kCodesLds = 68 << 10;                       // 16 rows of 4096 channels, two workgroups a CU
+
+template <int MT, int NB, int S, int WV, bool GATED, Rows IN>
 hipError_t go(const StampF8Gemm& a, hipStream_t st) {
-  const int places = kWaves / S * NB * 16;
-  const dim3 grid((a.groups * 64 + places - 1) / places, a.sets);
-  if (a.X == nullptr) {
-    k_f8_rows<MT, NB, S, GATED, kCodes><<<grid, kWaves * 64, 0, st>>>(a);
-  } else if constexpr (MT == 1) {
-    if (a.x_bf16) k_f8_rows<MT, NB, S, GATED, kBf16><<<grid, kWaves * 64, 0, st>>>(a);
-    else k_f8_rows<MT, NB, S, GATED, kF32><<<grid, kWaves * 64, 0, st>>>(a);
-  } else {
-    return hipErrorInvalidValue;
-  }
+  const int places = WV / S * NB * 16, sums = S * 16 * MT * (places + 4) * 4, codes = IN == kCodes ? 0 : a.chunk * row_bytes(a.Kb);
+  const int lds = codes > sums ? codes : sums;
+  static size_t done[kStampMaxDevices];
+  const hipError_t e = stamp_allow_lds(reinterpret_cast<const void*>(&k_f8_rows<MT, NB, S, WV, GATED, IN>), (size_t)lds, done);
+  if (e != hipSuccess) return e;
+  k_f8_rows<MT, NB, S, WV, GATED, IN><<<dim3((a.groups * 64 + places - 1) / places, a.sets), WV * 64, lds, st>>>(a);
   return hipGetLastError();
+}
+template <Rows IN>
+hipError_t quantizing(const StampF8Gemm& a, int nb, hipStream_t st) {
+  if (a.gated) return go<1, 2, 2, 16, true, IN>(a, st);
+  return nb >= 2 ? go<1, 2, 8, 8, false, IN>(a, st) : go<1, 1, 8, 8, false, IN>(a, st);
 }
 int average(const StampF8Gemm& a, int rows) { return (int)(((int64_t)rows + a.sets - 1) / a.sets); }
 }  // namespace
 
-bool stamp_f8_rows_quantize(const StampF8Gemm& a, int rows) { return average(a, rows) <= 16; }
+// Where all workgroups run at once and the rows are few: 1 x 4096 -> 11008 9.9 us, with a launch for the codes 12.1; with more workgroups
+// than that the registers of the quantizer cost more than the launch (1 x 8192 -> 28672: 49 us and 38.5; 96 rows over 24 of 32 experts,
+// 4096 -> 1536: 29.9 and 29.8; 24 rows over 24 experts, gated 2048 -> 1408: 33 and 29).
+int stamp_f8_rows_quantize(const StampF8Gemm& a, int rows) {
+  const int fit = kCodesLds / row_bytes(a.Kb), busy = a.sets < rows ? a.sets : rows;
+  const int chunk = fit > 16 ? 16 : fit;  // 65536 channels: one row
+  const int64_t workgroups = (int64_t)busy * (a.gated ? (a.groups + 3) / 4 : a.groups);  // gated: one a CU; else two, of half a group at least
+  return workgroups <= stamp_device_cus() && average(a, rows) <= (chunk < 4 ? chunk : 4) ? chunk : 0;
+}
 
 hipError_t stamp_launch_f8_rows(const StampF8Gemm& a, hipStream_t st) {
   const int avg = average(a, a.rows), busy = a.sets < a.rows ? a.sets : a.rows;
-  if (a.gated) return avg <= 16 ? go<1, 4, 2, true>(a, st) : go<2, 4, 2, true>(a, st);
-  // blocks per wave: as many as leave a workgroup for every CU; fewer workgroups read (and quantize) the rows less often
+  // blocks per wave: as many as leave a workgroup for every CU; fewer workgroups read (and quantize) the rows less often.  Four do not fit
+  // the registers beside the quantizer's.
   const int64_t groups = (int64_t)a.groups * busy;
   const int cus = stamp_device_cus();
   const int nb = groups >= cus ? 4 : 2 * groups >= cus ? 2 : 1;
-  if (avg <= 16) return nb == 4 ? go<1, 4, 8, false>(a, st) : nb == 2 ? go<1, 2, 8, false>(a, st) : go<1, 1, 8, false>(a, st);
-  if (avg <= 32) return nb == 4 ? go<2, 4, 8, false>(a, st) : nb == 2 ? go<2, 2, 8, false>(a, st) : go<2, 1, 8, false>(a, st);
-  return nb >= 2 ? go<4, 2, 8, false>(a, st) : go<4, 1, 8, false>(a, st);
+  if (a.X != nullptr) return a.x_bf16 ? quantizing<kBf16>(a, nb, st) : quantizing<kF32>(a, nb, st);
+  if (a.gated) return avg <= 16 ? go<1, 4, 2, 8, true, kCodes>(a, st) : go<2, 4, 2, 8, true, kCodes>(a, st);
+  if (avg <= 16)
+    return nb == 4 ? go<1, 4, 8, 8, false, kCodes>(a, st) : nb == 2 ? go<1, 2, 8, 8, false, kCodes>(a, st) : go<1, 1, 8, 8, false, kCodes>(a, st);
+  if (avg <= 32)
+    return nb == 4 ? go<2, 4, 8, 8, false, kCodes>(a, st) : nb == 2 ? go<2, 2, 8, 8, false, kCodes>(a, st) : go<2, 1, 8, 8, false, kCodes>(a, st);
+  return nb >= 2 ? go<4, 2, 8, 8, false, kCodes>(a, st) : go<4, 1, 8, 8, false, kCodes>(a, st);
 }

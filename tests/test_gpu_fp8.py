@@ -214,10 +214,74 @@ def test_linear_against_the_definition(st, rows, d, n, x, y, pow2, bias):
     plan.destroy()
 
 
-def test_every_kernel_is_reached(st):
+def test_every_kernel_is_reached_by_rule(st):
     plan = st.Fp8Plan(st.Fp8Desc(d_in=512, d_out=1536), _gpu(np.zeros((1536, 512), np.uint8)), _gpu(np.ones((12, 4), np.float32)))
-    assert {plan.route(rows) for rows, _, _ in SIZES} == {"rows", "tiles_64", "tiles_128", "tiles_256"}
+    assert {plan.route(rows) for rows in (1, 100, 600, 2000, 5000, 40000)} == {"rows", "tiles_64", "tiles_128", "tiles_256"}
     plan.destroy()
+
+
+@pytest.mark.parametrize("route", ["rows", "tiles_64", "tiles_128", "tiles_256"])
+@pytest.mark.parametrize("y,pow2", [("bf16", 0), ("bf16", 1), ("f32", 0), ("f32", 1)])
+@pytest.mark.parametrize("experts", [0, 4])
+def test_every_kernel_on_sizes_off_its_tiles(st, route, y, pow2, experts):
+    import torch
+    if route == "tiles_256" and y == "f32":
+        plan = st.Fp8Plan(st.Fp8Desc(d_in=128, d_out=1, y_dtype=st.STAMP_F32), _gpu(np.zeros((1, 128), np.uint8)), _gpu(np.ones((1, 1), np.float32)))
+        with pytest.raises(st.StampError):
+            plan.set_route(route)
+        return
+    for rows, d, n in ((1, 100, 70), (70, 640, 300), (140, 257, 64), (300, 1290, 530), (530, 384, 1030)):
+        rng = np.random.default_rng(rows)
+        xv, xg = _activations(rng, rows, d, "bf16")
+        lead = (experts,) if experts else ()
+        w, ws = _weights(rng, lead, n, d, pow2)
+        plan = st.Fp8Plan(st.Fp8Desc(d_in=d, d_out=n, experts=experts, y_dtype=_code(st, y), scale_format=pow2), _gpu(w), _gpu(ws))
+        plan.set_route(route)
+        Y, buf = _strided(rows, n, y, 5, 3)
+        codes, scales = ref.quantize(xv, pow2)
+        if experts:
+            cut = np.sort(rng.integers(0, rows + 1, experts - 1))
+            cut[0] = 0
+            offsets = np.concatenate([[0], cut, [rows]]).astype(np.int32)
+            plan.grouped_forward(xg, _gpu(offsets), Y, plan.alloc_workspace(rows))
+        else:
+            offsets = [0, rows]
+            plan.linear_forward(xg, Y, plan.alloc_workspace(rows))
+        for e in range(len(offsets) - 1):
+            lo, hi = offsets[e], offsets[e + 1]
+            if lo == hi:
+                continue
+            want, S, G = ref.product(codes[lo:hi], scales[lo:hi], *((w[e], ws[e]) if experts else (w, ws)))
+            _check(Y[lo:hi], want, S, G, d, y == "f32" or route == "rows", y == "bf16", f"{route} {rows} {d} {n} {e}")
+        Y.fill_(-7.0)
+        assert (buf == -7.0).all()
+        plan.destroy()
+
+
+@pytest.mark.parametrize("up_route", ["rows", "tiles_64", "tiles_128"])
+@pytest.mark.parametrize("pow2", [0, 1])
+@pytest.mark.parametrize("tokens,experts,top_k", [(3, 2, 1), (40, 6, 2), (150, 3, 2)])
+def test_gated_products_of_every_kernel(st, up_route, pow2, tokens, experts, top_k):
+    import torch
+    rng = np.random.default_rng(tokens)
+    d, ff = 300, 270
+    l, lg = _logits(rng, tokens, experts, "f32", "plain")
+    xv, xg = _activations(rng, tokens, d, "bf16")
+    w_up, s_up = _weights(rng, (experts, 2), ff, d, pow2)
+    s_up = (s_up * np.float32(2.0 ** -6)).astype(np.float32)
+    w_down, s_down = _weights(rng, (experts,), d, ff, pow2)
+    up = st.Fp8Plan(st.Fp8Desc(d_in=d, d_out=ff, experts=experts, gated=1, scale_format=pow2), _gpu(w_up), _gpu(s_up))
+    down = st.Fp8Plan(st.Fp8Desc(d_in=ff, d_out=d, experts=experts, y_dtype=st.STAMP_F32, scale_format=pow2), _gpu(w_down), _gpu(s_down))
+    up.set_route(up_route)
+    r = st.Routing(tokens, experts, top_k)
+    st.route_topk(lg, r)
+    Y = torch.empty((tokens, d), device="cuda")
+    st.experts_forward(up, down, xg, r, Y, st.experts_workspace(up, down, tokens, top_k))
+    want, tol = _experts_reference(xv, l, w_up, s_up, w_down, s_down, top_k, 1, pow2, None)
+    bad = np.abs(Y.cpu().numpy() - want) > tol + 2.0 ** -22 * np.abs(want) + 1e-37
+    assert not bad.any()
+    up.destroy()
+    down.destroy()
 
 
 def test_offsets_beyond_32_bits(st):
