@@ -168,27 +168,38 @@ __device__ __forceinline__ int wave_scan(int v) {  // inclusive
   }
   return v;
 }
-__device__ __forceinline__ int count_tiles(const StampF8Gemm& a, int BM) {
-  if (a.offsets == nullptr) return (a.rows + BM - 1) / BM;
-  int n = 0, lo, hi;
-  for (int e = threadIdx.x & 63; e < a.sets; e += 64) n += tiles_of(a, e, BM, &lo, &hi);
+// The sets 0 .. 63 stay in the lanes: their rows and the tiles up to and including theirs.
+struct Tiles {
+  int lo, hi, incl, total;
+};
+__device__ __forceinline__ Tiles count_tiles(const StampF8Gemm& a, int BM) {
+  Tiles t;
+  t.lo = t.hi = t.incl = 0;
+  t.total = (a.rows + BM - 1) / BM;
+  if (a.offsets == nullptr) return t;
+  t.incl = wave_scan(tiles_of(a, threadIdx.x & 63, BM, &t.lo, &t.hi));
+  int n = __shfl(t.incl, 63), more = 0, lo, hi;
+  if (a.sets > 64) {
+    for (int e = 64 + (threadIdx.x & 63); e < a.sets; e += 64) more += tiles_of(a, e, BM, &lo, &hi);
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) n += __shfl_xor(n, d);
-  return __builtin_amdgcn_readfirstlane(n);
+    for (int d = 1; d < 64; d <<= 1) more += __shfl_xor(more, d);
+  }
+  t.total = __builtin_amdgcn_readfirstlane(n + more);
+  return t;
 }
-// set and rows of a tile that there is
-__device__ __forceinline__ void find_tile(const StampF8Gemm& a, int BM, int tile, int* set, int* row0, int* nrows) {
+// set and rows of a tile below total
+__device__ __forceinline__ void find_tile(const StampF8Gemm& a, const Tiles& t, int BM, int tile, int* set, int* row0, int* nrows) {
   *set = 0;
   *row0 = tile * BM;
   *nrows = min(BM, a.rows - *row0);
   if (a.offsets == nullptr) return;
   int base = 0;
   for (int e0 = 0; e0 < a.sets; e0 += 64) {
-    int lo, hi;
-    const int own = tiles_of(a, e0 + (threadIdx.x & 63), BM, &lo, &hi), incl = wave_scan(own);
+    int lo = t.lo, hi = t.hi, incl = t.incl;
+    if (e0 > 0) incl = wave_scan(tiles_of(a, e0 + (threadIdx.x & 63), BM, &lo, &hi));
     const uint64_t past = __ballot(base + incl > tile);
     if (past != 0) {
-      const int src = __builtin_ctzll(past), first = base + __shfl(incl - own, src);
+      const int src = __builtin_ctzll(past), first = base + __shfl(incl, src) - (__shfl(hi, src) - __shfl(lo, src) + BM - 1) / BM;
       const int l = __shfl(lo, src), h = __shfl(hi, src);
       *set = __builtin_amdgcn_readfirstlane(e0 + src);
       *row0 = __builtin_amdgcn_readfirstlane(l + (tile - first) * BM);

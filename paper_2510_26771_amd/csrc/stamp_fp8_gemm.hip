@@ -55,18 +55,20 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
   __shared__ __attribute__((aligned(1024))) uint8_t stage1[kStage];
   __shared__ __attribute__((aligned(1024))) uint8_t stage2[NS > 2 ? kStage : 16];
   __shared__ float wscale[2][kMaxBlocks];
+  __shared__ float bias_of[GATED ? 1 : 256];
   const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6);
   const int wm = wave >> 2, wn = wave & 3;
   // Workgroups go to the 8 XCDs in turn: an XCD takes a run of the tiles in an order in which 32 neighbours (its CUs) are 8 x 4 tiles, so
   // that its L2 has 12 panels of operands to fetch for them and not 33.
   constexpr int kXcd = 8, kBand = 8;
-  const int ncol = (a.groups + 3) / 4, nrow = count_tiles(a, BM), ntile = nrow * ncol, run = (ntile + kXcd - 1) / kXcd;
+  const Tiles tiles = count_tiles(a, BM);
+  const int ncol = (a.groups + 3) / 4, nrow = tiles.total, ntile = nrow * ncol, run = (ntile + kXcd - 1) / kXcd;
   const int order = (int)(blockIdx.x % kXcd) * run + (int)(blockIdx.x / kXcd);
   if ((int)(blockIdx.x / kXcd) >= run || order >= ntile) return;
   const int band = order / (kBand * ncol), in_band = order - band * kBand * ncol, height = min(kBand, nrow - band * kBand);
   const int col = in_band / height;
   int set, row0, nrows;
-  find_tile(a, BM, band * kBand + in_band % height, &set, &row0, &nrows);
+  find_tile(a, tiles, BM, band * kBand + in_band % height, &set, &row0, &nrows);
   set = __builtin_amdgcn_readfirstlane(set);
   row0 = __builtin_amdgcn_readfirstlane(row0);
   nrows = __builtin_amdgcn_readfirstlane(nrows);
@@ -114,11 +116,6 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
 
   // weight scales of the tile's two blocks of 128 columns (gated: of its gate and up columns): a register that now and then is loaded
   // anew would make every use of it wait for the loads in flight
-  for (int i = t; i < 2 * Kb; i += 512) {
-    const int which = i >= Kb, kb = i - which * Kb;
-    const int blk = GATED ? which * a.nblk + (min(g0, a.groups - 1) >> 2) : min((g0 >> 1) + which, a.nblk - 1);
-    wscale[which][kb] = a.SW[((size_t)set * (GATED ? 2 : 1) * a.nblk + blk) * Kb + kb];
-  }
   const float* const sw_of = wscale[GATED ? 0 : wn >> 1];
   auto read_w = [&](const uint8_t* S, int b) __attribute__((always_inline)) -> v8i {
     const uint8_t* s = S + wbase + b * 2048;
@@ -271,7 +268,19 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
 #pragma unroll
     for (int q = 0; q < kLoads; ++q) load(stage1, 1, q);
   }
-  turn(later);
+  // behind the stages' loads, on whose way they are
+  for (int i = t; i < 2 * Kb; i += 512) {
+    const int which = i >= Kb, kb = i - which * Kb;
+    const int blk = GATED ? which * a.nblk + (min(g0, a.groups - 1) >> 2) : min((g0 >> 1) + which, a.nblk - 1);
+    wscale[which][kb] = a.SW[((size_t)set * (GATED ? 2 : 1) * a.nblk + blk) * Kb + kb];
+  }
+  if constexpr (!GATED) {
+    if (t < 256) {
+      const int n = g0 * 64 + t;
+      bias_of[t] = a.bias != nullptr && n < a.N ? a.bias[(size_t)set * a.N + n] : 0.0f;
+    }
+  }
+  turn(none);
 #pragma unroll
   for (int q = 0; q < 4; ++q) load(NS == 3 ? stage2 : stage1, NS - 1, q);
   if constexpr (WIDE) {
@@ -323,7 +332,7 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
     const int n0 = 64 * g + 16 * f;
     float bias[16];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) bias[j] = a.bias != nullptr && n0 + j < a.N ? a.bias[(size_t)set * a.N + n0 + j] : 0.0f;
+    for (int j = 0; j < 16; ++j) bias[j] = bias_of[64 * wn + 16 * f + j];
     const uint32_t size = a.y_bf16 ? 2 : 4, ld = (uint32_t)a.ld_y * size;
     char* const y = static_cast<char*>(a.Y) + ((int64_t)row0 * a.ld_y) * size;  // 256 rows are below 4 GB, checked by the host
     const bool wide = (reinterpret_cast<uintptr_t>(a.Y) | ld) % 16 == 0 && g * 64 + 64 <= a.N;
