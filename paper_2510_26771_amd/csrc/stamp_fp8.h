@@ -4,7 +4,7 @@
 // one row.  The weights are the first operand of v_mfma_f32_16x16x128_f8f6f4, a block of 128 input channels in one instruction: lane
 // 16 f + i gives row i of it, and element r of lane 16 f + m of the result is row 4 f + r of column m.  With the tokens as columns a lane
 // has one token, whose scale it then needs once, and rows 4 f .. 4 f + 3 of every instruction b = 0 .. 3 of a group:
-//   plain  column 64 g + 16 f + 4 b + r: 16 neighbours
+//   plain  column 64 g + 32 (b / 2) + 8 f + 4 (b % 2) + r: twice 8 neighbours; the 4 lanes of a row have 32, stored at once
 //   gated  column 32 g + 8 f + 4 (b / 2) + r of the gate (b even) or the up matrix (b odd): 8 neighbours of both; four groups are a block
 //          of 128 of the next layer's input
 //
@@ -35,7 +35,7 @@ struct stamp_fp8_plan {
 
 // column of place (b, row i of the instruction) in group g; gated: of the gate matrix for even b
 STAMP_HD int f8_column(int gated, int g, int b, int i) {
-  return gated ? 32 * g + 8 * (i >> 2) + 4 * (b >> 1) + (i & 3) : 64 * g + 16 * (i >> 2) + 4 * b + (i & 3);
+  return gated ? 32 * g + 8 * (i >> 2) + 4 * (b >> 1) + (i & 3) : 64 * g + 32 * (b >> 1) + 8 * (i >> 2) + 4 * (b & 1) + (i & 3);
 }
 STAMP_HD size_t f8_w_offset(int groups, int Kb, int set, int g, int kb, int b, int h, int lane) {
   return ((((size_t)set * groups + g) * Kb + kb) * 8 + b * 2 + h) * 1024 + (size_t)lane * 16;

@@ -329,14 +329,15 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
 
   const int g = g0 + wn;
   if constexpr (!GATED) {
-    const int n0 = 64 * g + 16 * f;
+    const int n0 = 64 * g + 8 * f;  // and 32 further on
     float bias[16];
 #pragma unroll
-    for (int j = 0; j < 16; ++j) bias[j] = bias_of[64 * wn + 16 * f + j];
+    for (int j = 0; j < 16; ++j) bias[j] = bias_of[64 * wn + 32 * (j >> 3) + 8 * f + (j & 7)];
     const uint32_t size = a.y_bf16 ? 2 : 4, ld = (uint32_t)a.ld_y * size;
     char* const y = static_cast<char*>(a.Y) + ((int64_t)row0 * a.ld_y) * size;  // 256 rows are below 4 GB, checked by the host
     const bool wide = (reinterpret_cast<uintptr_t>(a.Y) | ld) % 16 == 0 && g * 64 + 64 <= a.N;
     const __amdgpu_buffer_rsrc_t ry = buffer(y);
+    auto col_of = [](int j) { return 32 * (j >> 3) + (j & 7); };
 #pragma unroll
     for (int mi = 0; mi < MI; ++mi) {
       const int m = wm * (BM / 2) + 16 * mi + (lane & 15);
@@ -351,22 +352,22 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
             u4 w;
 #pragma unroll
             for (int j = 0; j < 4; ++j) w[j] = to_bf16x2(v[8 * q + 2 * j], v[8 * q + 2 * j + 1]);
-            __builtin_amdgcn_raw_buffer_store_b128(w, ry, m < nrows ? o + 16 * q : kNowhere, 0, 0);
+            __builtin_amdgcn_raw_buffer_store_b128(w, ry, m < nrows ? o + 64 * q : kNowhere, 0, 0);
           }
         } else {
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             const u4 w = {__float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]), __float_as_uint(v[4 * q + 2]), __float_as_uint(v[4 * q + 3])};
-            __builtin_amdgcn_raw_buffer_store_b128(w, ry, m < nrows ? o + 16 * q : kNowhere, 0, 0);
+            __builtin_amdgcn_raw_buffer_store_b128(w, ry, m < nrows ? o + 128 * (q >> 1) + 16 * (q & 1) : kNowhere, 0, 0);
           }
         }
       } else if (a.y_bf16) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) __builtin_amdgcn_raw_buffer_store_b16(to_bf16(v[j]), ry, m < nrows && n0 + j < a.N ? o + 2 * j : kNowhere, 0, 0);
+        for (int j = 0; j < 16; ++j) __builtin_amdgcn_raw_buffer_store_b16(to_bf16(v[j]), ry, m < nrows && n0 + col_of(j) < a.N ? o + 2 * col_of(j) : kNowhere, 0, 0);
       } else {
 #pragma unroll
         for (int j = 0; j < 16; ++j)
-          __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[j]), ry, m < nrows && n0 + j < a.N ? o + 4 * j : kNowhere, 0, 0);
+          __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[j]), ry, m < nrows && n0 + col_of(j) < a.N ? o + 4 * col_of(j) : kNowhere, 0, 0);
       }
     }
   } else {
