@@ -44,9 +44,9 @@ STAMP_HD size_t f8_w_offset(int groups, int Kb, int set, int g, int kb, int b, i
 // The product's arguments.
 struct StampF8Gemm {
   const uint8_t* A;        // codes [a_rows][Kp], for tiles of wide_sums as bf16
-  const float* SA;         // scales [Kb][ld_sa], by row of the product
+  const float* SA;         // scales [Kb][ld_sa], by row of A
   int64_t ld_sa;
-  const int32_t* index;    // row of A of every row of the product, or nullptr: the same
+  const int32_t* index;    // gated: row of A of every row of the product (else the same)
   int32_t a_rows;
   const void* X;           // not nullptr: A's rows before Q8, quantized by the product itself (few rows)
   int64_t ld_x;
@@ -68,11 +68,10 @@ struct StampF8Gemm {
 
 int stamp_f8_route(int sets, int groups, int Kb, int rows, int wide_sums);
 hipError_t stamp_launch_f8_weights(stamp_fp8_plan* p, const void* W, const float* w_scales, hipStream_t st, uint32_t* flag);
-// row_of_slot != nullptr: row t's scales go to the places of its top_k slots (rows of the product, below nrows)
 // wide: the codes as bf16
 hipError_t stamp_launch_f8_widen(const uint8_t* codes, int64_t bytes, uint8_t* out, hipStream_t st);
 hipError_t stamp_launch_f8_quant(const void* X, int x_bf16, int64_t ld_x, int rows, int d, int pow2, int wide, uint8_t* codes, float* scales, int64_t ld_s,
-                                 const int32_t* row_of_slot, int top_k, int nrows, hipStream_t st);
+                                 hipStream_t st);
 int stamp_f8_rows_quantize(const StampF8Gemm& a, int rows);  // rows that the kernel for few rows quantizes at a time, 0: it takes codes
 hipError_t stamp_launch_f8_rows(const StampF8Gemm& a, hipStream_t st);
 hipError_t stamp_launch_f8_tiles(const StampF8Gemm& a, int bm, hipStream_t st);

@@ -93,7 +93,7 @@ ExpertsWs experts_ws(const stamp_fp8_plan* up, const stamp_fp8_plan* down, int32
   const int64_t slots = (int64_t)tokens * top_k, ld = scales_ld((int32_t)slots);
   w.codes = 0;
   w.scales = align256((size_t)tokens * up->Kp * code_bytes(up));
-  w.h = w.scales + align256((size_t)up->Kb * ld * sizeof(float));
+  w.h = w.scales + align256((size_t)up->Kb * scales_ld(tokens) * sizeof(float));
   w.sh = w.h + align256((size_t)slots * down->Kp);
   w.rows = w.sh + align256((size_t)down->Kb * ld * sizeof(float));
   w.ld_rows = (down->desc.d_out + 7) / 8 * 8;
@@ -145,7 +145,7 @@ stamp_status_t forward(const stamp_fp8_plan* p, int32_t rows, const int32_t* off
   if (takes_x(a, rows)) {
     give_x(&a, p->desc, rows, X, ld_x);
   } else if (stamp_launch_f8_quant(X, p->desc.x_dtype == STAMP_BF16, ld_x, rows, p->desc.d_in, a.pow2, wide_codes(a, rows), codes, scales, scales_ld(rows),
-                                   nullptr, 0, 0, st) != hipSuccess) {
+                                   st) != hipSuccess) {
     return STAMP_ERR_DEVICE;
   }
   a.A = codes;
@@ -265,7 +265,7 @@ stamp_status_t stamp_fp8_quantize_act(const stamp_fp8_plan_t* p, int32_t rows, c
   if (codes_dev == nullptr || scales_dev == nullptr) return STAMP_ERR_NULL;
   if (ld_scales < rows || ld_scales % 4 != 0 || (reinterpret_cast<uintptr_t>(codes_dev) | reinterpret_cast<uintptr_t>(scales_dev)) % 16 != 0) return STAMP_ERR_SHAPE;
   return done(stamp_launch_f8_quant(X_dev, p->desc.x_dtype == STAMP_BF16, ld_x, rows, p->desc.d_in, p->desc.scale_format == STAMP_SCALE_POW2, 0, codes_dev,
-                                    scales_dev, ld_scales, nullptr, 0, 0, reinterpret_cast<hipStream_t>(hip_stream)));
+                                    scales_dev, ld_scales, reinterpret_cast<hipStream_t>(hip_stream)));
 }
 
 stamp_status_t stamp_fp8_linear_forward(const stamp_fp8_plan_t* p, int32_t rows, const void* X_dev, int64_t ld_x, void* Y_dev, int64_t ld_y,
@@ -353,12 +353,12 @@ stamp_status_t stamp_experts_forward(const stamp_fp8_plan_t* up, const stamp_fp8
   if (takes_x(a, slots)) {
     give_x(&a, up->desc, slots, X_dev, ld_x);
   } else if (stamp_launch_f8_quant(X_dev, up->desc.x_dtype == STAMP_BF16, ld_x, r->tokens, up->desc.d_in, a.pow2, wide_codes(a, slots), ws + w.codes, scales,
-                                   ld, r->row_of_slot_dev, r->top_k, slots, st) != hipSuccess) {
+                                   scales_ld(r->tokens), st) != hipSuccess) {
     return STAMP_ERR_DEVICE;
   }
   a.A = ws + w.codes;
   a.SA = scales;
-  a.ld_sa = ld;
+  a.ld_sa = scales_ld(r->tokens);
   a.index = r->token_of_row_dev;
   a.a_rows = r->tokens;
   a.rows = slots;

@@ -74,20 +74,22 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
   nrows = __builtin_amdgcn_readfirstlane(nrows);
   const int g0 = col * 4, Kb = a.Kb;
 
-  // 32-bit offsets from a scalar base: the tile's first row, or with an index all rows of A (below 4 GB, checked by the host)
+  // 32-bit offsets from a scalar base: the tile's first row, or (gated, by index) all rows of A, below 4 GB
   uint32_t aoff[LA], boff[4];
 #pragma unroll
   for (int i = 0; i < LA; ++i) {
     const int p = i * 512 + t, row = WIDE ? p >> 4 : p >> 3, piece = WIDE ? (p & 15) ^ (row & 15) : (p & 7) ^ ((row >> 1) & 7);
     uint32_t r = min(row, nrows - 1);
-    if (a.index != nullptr) r = min(max(a.index[row0 + r], 0), a.a_rows - 1);
+    if constexpr (GATED) r = min(max(a.index[row0 + r], 0), a.a_rows - 1);
     aoff[i] = r * (uint32_t)(Kb * kRowBytes) + piece * 16;
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) boff[i] = uniform((uint32_t)(min(g0 + i, a.groups - 1) - g0) * (uint32_t)Kb * kF8GroupBytes);
-  const __amdgpu_buffer_rsrc_t ra = buffer(a.A + (a.index != nullptr ? (size_t)0 : (size_t)row0 * Kb * kRowBytes));
+  const __amdgpu_buffer_rsrc_t ra = buffer(a.A + (GATED ? (size_t)0 : (size_t)row0 * Kb * kRowBytes));
   const __amdgpu_buffer_rsrc_t rb = buffer(a.W + ((size_t)set * a.groups + g0) * Kb * kF8GroupBytes);
-  const uint32_t soff = (uint32_t)min(t, nrows - 1);
+  uint32_t soff = (uint32_t)min(t, nrows - 1);  // of the rows' scales, which lie by row of A
+  if constexpr (GATED) soff = (uint32_t)min(max(a.index[row0 + soff], 0), a.a_rows - 1);
+  const float* const sa = a.SA + (GATED ? 0 : row0);
 
   // the q-th of a stage's loads; behind the last block of channels that one again, which nobody reads
   constexpr int kLoads = 4 + LA + 1;
@@ -98,7 +100,7 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
     } else if (q < 4 + LA) {
       __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (LdsPtr)(S + (q - 4) * 8192 + wave * 1024), 16, aoff[q - 4], kb * kRowBytes, 0, 0);
     } else {
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(a.SA + row0 + (int64_t)kb * a.ld_sa + soff),
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(sa + (int64_t)kb * a.ld_sa + soff),
                                        (LdsPtr)(S + kStageA + kStageB + wave * 256), 4, 0, 0);
     }
   };

@@ -7,7 +7,7 @@ using namespace f8;
 // A thread has 16 channels, 8 lanes a block.  Bound by memory: 2 (4) bytes read, 1.03 written per element.
 template <bool BF16, bool WIDE>
 __global__ __launch_bounds__(256) void k_f8_quant(const void* X, int64_t ld_x, int rows, int d, int Kp, int pow2, int aligned, uint8_t* codes, float* scales,
-                                                  int64_t ld_s, const int32_t* row_of_slot, int top_k, int nrows) {
+                                                  int64_t ld_s) {
   const int per = Kp >> 4;
   const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int64_t m = u / per;
@@ -25,20 +25,7 @@ __global__ __launch_bounds__(256) void k_f8_quant(const void* X, int64_t ld_x, i
   } else {
     *reinterpret_cast<u4*>(codes + m * Kp + c) = o;
   }
-  if ((threadIdx.x & 7) != 0) return;
-  float* s = scales + (int64_t)(c >> 7) * ld_s;
-  if (row_of_slot == nullptr) {
-    s[m] = scale;
-  } else {
-    for (int j0 = 0; j0 < top_k; j0 += 8) {
-      int r[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) r[j] = j0 + j < top_k ? row_of_slot[m * top_k + j0 + j] : -1;
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if ((uint32_t)r[j] < (uint32_t)nrows) s[r[j]] = scale;
-    }
-  }
+  if ((threadIdx.x & 7) == 0) scales[(int64_t)(c >> 7) * ld_s + m] = scale;
 }
 
 // ---- weights, once per plan ----
@@ -112,12 +99,12 @@ __global__ __launch_bounds__(256) void k_f8_check_pow2(const float* s, int64_t n
 }  // namespace
 
 hipError_t stamp_launch_f8_quant(const void* X, int x_bf16, int64_t ld_x, int rows, int d, int pow2, int wide, uint8_t* codes, float* scales, int64_t ld_s,
-                                 const int32_t* row_of_slot, int top_k, int nrows, hipStream_t st) {
+                                 hipStream_t st) {
   const int Kp = (d + 127) / 128 * 128, size = x_bf16 ? 2 : 4;
   const int aligned = reinterpret_cast<uintptr_t>(X) % 16 == 0 && ld_x * size % 16 == 0;
   const uint32_t blocks = (uint32_t)(((int64_t)rows * (Kp / 16) + 255) / 256);
   auto* kernel = x_bf16 ? (wide ? k_f8_quant<true, true> : k_f8_quant<true, false>) : (wide ? k_f8_quant<false, true> : k_f8_quant<false, false>);
-  kernel<<<blocks, 256, 0, st>>>(X, ld_x, rows, d, Kp, pow2, aligned, codes, scales, ld_s, row_of_slot, top_k, nrows);
+  kernel<<<blocks, 256, 0, st>>>(X, ld_x, rows, d, Kp, pow2, aligned, codes, scales, ld_s);
   return hipGetLastError();
 }
 

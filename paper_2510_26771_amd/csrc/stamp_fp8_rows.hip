@@ -58,13 +58,14 @@ __global__ __launch_bounds__(kWaves * 64, IN == kCodes ? 2 : 4) void k_f8_rows(S
 #pragma unroll
     for (int mi = 0; mi < MT; ++mi) {
       const int m = min(16 * mi + (lane & 15), nr - 1);
-      srow[mi] = IN == kCodes ? r0 + m : m * a.Kb;
       if constexpr (IN == kCodes) {
         int ar = r0 + m;
-        if (a.index != nullptr) ar = min(max(a.index[ar], 0), a.a_rows - 1);
+        if constexpr (GATED) ar = min(max(a.index[ar], 0), a.a_rows - 1);
         arow[mi] = a.A + (size_t)ar * Kp + 16 * f;
+        srow[mi] = ar;
       } else {
         arow[mi] = lds + m * ldc + 16 * f;
+        srow[mi] = m * a.Kb;
       }
     }
 
@@ -123,7 +124,7 @@ __global__ __launch_bounds__(kWaves * 64, IN == kCodes ? 2 : 4) void k_f8_rows(S
         const int units = nr * a.Kb * 8, per = a.Kb * 8;
         auto row_of = [&](int u) __attribute__((always_inline)) {
           const int r = r0 + u / per;
-          const int ar = a.index != nullptr ? min(max(a.index[r], 0), a.a_rows - 1) : r;
+          const int ar = GATED ? min(max(a.index[r], 0), a.a_rows - 1) : r;
           return static_cast<const char*>(a.X) + (int64_t)ar * a.ld_x * (IN == kBf16 ? 2 : 4);
         };
         auto make = [&](int u, const Raw16<IN == kBf16>& x) __attribute__((always_inline)) {

@@ -5,7 +5,7 @@
 namespace {
 using namespace f8;
 
-constexpr int kRtWaves = 8;
+constexpr int kRtWaves = 16;  // of a workgroup
 constexpr int kRtMaxBlocks = 256;
 
 struct RouteArgs {
@@ -179,7 +179,7 @@ __device__ void place_rows(const RouteArgs& a, int tok0, int tok1, int wave, int
   }
 }
 
-// Exclusive sums of total[0 .. E) -> base; returns the whole.  E <= 1024 = 2 * threads.
+// Exclusive sums of total[0 .. E) -> base; returns the whole.  E <= 1024, two experts a thread.
 __device__ uint32_t scan_experts(const uint32_t* total, uint32_t* base, int E, uint32_t* tmp) {
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   const uint32_t x = 2 * t < E ? total[2 * t] : 0, y = 2 * t + 1 < E ? total[2 * t + 1] : 0;
