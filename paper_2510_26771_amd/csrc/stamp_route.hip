@@ -5,14 +5,14 @@
 namespace {
 using namespace f8;
 
-constexpr int kRtWaves = 16;  // of a workgroup
+constexpr int kTopWaves = 16, kPlaceWaves = 8;  // of a workgroup
 constexpr int kRtMaxBlocks = 256;
 
 struct RouteArgs {
   stamp_routing_t r;
   const void* logits;
   int64_t ld;
-  int32_t bf16, renorm;
+  int32_t renorm;
   int32_t per_block;   // tokens of a workgroup
   uint16_t* hist;      // [workgroups][experts, an even number] rows that a workgroup's tokens give an expert
 };
@@ -23,7 +23,6 @@ __device__ __forceinline__ uint32_t order_key(float l) {
   const uint32_t b = __float_as_uint(l + 0.0f);
   return (b & 0x80000000u) ? ~b : b | 0x80000000u;
 }
-__device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float((k & 0x80000000u) ? k & 0x7fffffffu : ~k); }
 // exp(l - top) to 2 ulp, where both may be +infinity: then they are equal.  The product with log2 e in two parts.
 __device__ __forceinline__ float share(float l, float top) {
   if (l == top) return 1.0f;
@@ -56,12 +55,18 @@ __device__ __forceinline__ float sum_lanes(float v) {
 }
 
 // LANES lanes have a token, lane l of them experts l + LANES j: 4 tokens a wave up to 256 experts (the vector ALU is the bound, and the
-// steps over lanes cost the same for 1 and for 4 tokens).  The largest key, of the lowest expert, is taken top_k times.
-template <int LANES, int NV>
-__device__ void top_tokens(const RouteArgs& a, int tok0, int tok1, int wave, int lane, uint32_t* count) {
+// steps over lanes cost the same for 1 and for 4 tokens).  The largest key, of the lowest expert, is taken top_k times.  A bf16 logit's key
+// has 16 bits: with the expert below it in one word the largest word is the choice, and no two are equal.
+// slot_id: where not nullptr, the ids go there as well.
+template <int W, int LANES, int NV, bool BF16>
+__device__ void top_tokens(const RouteArgs& a, int tok0, int tok1, int wave, int lane, uint32_t* count, int* slot_id) {
   constexpr int kTokens = 64 / LANES, kMine = LANES == 16 ? 2 : 1;  // top_k <= 32 = kMine * LANES (or less)
   const int E = a.r.experts, K = a.r.top_k, l0 = lane % LANES;
-  for (int tb = tok0 + wave * kTokens; tb < tok1; tb += kRtWaves * kTokens) {
+  auto value = [](uint32_t k) {
+    if constexpr (BF16) return __uint_as_float(((k & 0x80000000u) ? k & 0x7fff0000u : ~k & 0xffff0000u));
+    else return __uint_as_float((k & 0x80000000u) ? k & 0x7fffffffu : ~k);
+  };
+  for (int tb = tok0 + wave * kTokens; tb < tok1; tb += W * kTokens) {
     const int t = tb + lane / LANES;
     const bool in = t < tok1;
     uint32_t key[NV];
@@ -69,10 +74,12 @@ __device__ void top_tokens(const RouteArgs& a, int tok0, int tok1, int wave, int
     for (int j = 0; j < NV; ++j) {
       const int e = l0 + LANES * j;
       float l = -__builtin_inff();
-      if (in && e < E)
-        l = a.bf16 ? __uint_as_float((uint32_t)static_cast<const uint16_t*>(a.logits)[(int64_t)t * a.ld + e] << 16)
-                   : static_cast<const float*>(a.logits)[(int64_t)t * a.ld + e];
+      if (in && e < E) {
+        if constexpr (BF16) l = __uint_as_float((uint32_t)static_cast<const uint16_t*>(a.logits)[(int64_t)t * a.ld + e] << 16);
+        else l = static_cast<const float*>(a.logits)[(int64_t)t * a.ld + e];
+      }
       key[j] = order_key(l);
+      if constexpr (BF16) key[j] = key[j] == 0 ? 0 : (key[j] & 0xffff0000u) | (uint32_t)(0xffff - e);
     }
     uint32_t mine[kMine] = {};  // lane l: key of the chosen l, l + 16
     int id[kMine];
@@ -84,16 +91,21 @@ __device__ void top_tokens(const RouteArgs& a, int tok0, int tok1, int wave, int
 #pragma unroll
       for (int j = 1; j < NV; ++j) best = max(best, key[j]);
       best = over_lanes<LANES>(best, [](uint32_t x, uint32_t y) { return max(x, y); });
-      uint32_t at = 0xffffffffu;
+      uint32_t e;
+      if constexpr (BF16) {
+        e = 0xffffu - (best & 0xffffu);
+      } else {
+        uint32_t at = 0xffffffffu;
 #pragma unroll
-      for (int j = NV - 1; j >= 0; --j) at = key[j] == best ? (uint32_t)(LANES * j) : at;
-      const uint32_t e = over_lanes<LANES>(at == 0xffffffffu ? at : at + l0, [](uint32_t x, uint32_t y) { return min(x, y); });
+        for (int j = NV - 1; j >= 0; --j) at = key[j] == best ? (uint32_t)(LANES * j) : at;
+        e = over_lanes<LANES>(at == 0xffffffffu ? at : at + l0, [](uint32_t x, uint32_t y) { return min(x, y); });
+      }
       if (k == 0) {
-        top = key_value(best);
+        top = value(best);
         if (!a.renorm) {
           float s = 0.0f;
 #pragma unroll
-          for (int j = 0; j < NV; ++j) s += key[j] != 0 ? share(key_value(key[j]), top) : 0.0f;
+          for (int j = 0; j < NV; ++j) s += key[j] != 0 ? share(value(key[j]), top) : 0.0f;
           sum = sum_lanes<LANES>(s);
         }
       }
@@ -105,12 +117,12 @@ __device__ void top_tokens(const RouteArgs& a, int tok0, int tok1, int wave, int
       }
       const uint32_t gone = e - l0;  // LANES j where the chosen one is this lane's
 #pragma unroll
-      for (int j = 0; j < NV; ++j) key[j] = gone == (uint32_t)(LANES * j) ? 0 : key[j];
+      for (int j = 0; j < NV; ++j) key[j] = (BF16 ? key[j] == best : gone == (uint32_t)(LANES * j)) ? 0 : key[j];
     }
     float sh[kMine], s = 0.0f;
 #pragma unroll
     for (int q = 0; q < kMine; ++q) {
-      sh[q] = id[q] >= 0 ? share(key_value(mine[q]), top) : 0.0f;
+      sh[q] = id[q] >= 0 ? share(value(mine[q]), top) : 0.0f;
       s += sh[q];
     }
     if (a.renorm) sum = sum_lanes<LANES>(s);
@@ -120,38 +132,40 @@ __device__ void top_tokens(const RouteArgs& a, int tok0, int tok1, int wave, int
       if (in && k < K) {
         a.r.ids_dev[(int64_t)t * K + k] = id[q];
         a.r.weights_dev[(int64_t)t * K + k] = id[q] >= 0 ? sh[q] / sum : 0.0f;
+        if (slot_id != nullptr) slot_id[(t - tok0) * K + k] = id[q];
         if (id[q] >= 0) atomicAdd(&count[id[q]], 1u);
       }
     }
   }
 }
-__device__ __forceinline__ void top_tokens_of(const RouteArgs& a, int tok0, int tok1, int wave, int lane, uint32_t* count) {
+template <bool BF16>
+__device__ __forceinline__ void top_tokens_of(const RouteArgs& a, int tok0, int tok1, int wave, int lane, uint32_t* count, int* slot_id) {
   const int E = a.r.experts;
-  if (E <= 32) top_tokens<16, 2>(a, tok0, tok1, wave, lane, count);
-  else if (E <= 64) top_tokens<16, 4>(a, tok0, tok1, wave, lane, count);
-  else if (E <= 128) top_tokens<16, 8>(a, tok0, tok1, wave, lane, count);
-  else if (E <= 256) top_tokens<16, 16>(a, tok0, tok1, wave, lane, count);
-  else if (E <= 512) top_tokens<64, 8>(a, tok0, tok1, wave, lane, count);
-  else top_tokens<64, 16>(a, tok0, tok1, wave, lane, count);
+  if (E <= 32) top_tokens<kTopWaves, 16, 2, BF16>(a, tok0, tok1, wave, lane, count, slot_id);
+  else if (E <= 64) top_tokens<kTopWaves, 16, 4, BF16>(a, tok0, tok1, wave, lane, count, slot_id);
+  else if (E <= 128) top_tokens<kTopWaves, 16, 8, BF16>(a, tok0, tok1, wave, lane, count, slot_id);
+  else if (E <= 256) top_tokens<kTopWaves, 16, 16, BF16>(a, tok0, tok1, wave, lane, count, slot_id);
+  else if (E <= 512) top_tokens<kTopWaves, 64, 8, BF16>(a, tok0, tok1, wave, lane, count, slot_id);
+  else top_tokens<kTopWaves, 64, 16, BF16>(a, tok0, tok1, wave, lane, count, slot_id);
 }
 
-// Order of the workgroup's slots by expert: every wave has a run of them.  cnt [waves][E].
-__device__ void place_rows(const RouteArgs& a, int tok0, int tok1, int wave, int lane, uint32_t (*cnt)[kF8MaxExperts], const uint32_t* base) {
+template <int W>
+__device__ void place_rows(const RouteArgs& a, const int* ids, int tok0, int tok1, int wave, int lane, uint32_t (*cnt)[kF8MaxExperts], const uint32_t* base) {
   const int E = a.r.experts, K = a.r.top_k, t = threadIdx.x;
   const int64_t s0 = (int64_t)tok0 * K;
   const int n = (tok1 - tok0) * K;
-  const int run = ((n + kRtWaves - 1) / kRtWaves + 63) / 64 * 64;
+  const int run = ((n + W - 1) / W + 63) / 64 * 64;
   for (int e = lane; e < E; e += 64) cnt[wave][e] = 0;
   __syncthreads();
   const int r0 = min(wave * run, n), r1 = min(r0 + run, n);
   for (int i = r0 + lane; i < r1; i += 64) {
-    const int e = a.r.ids_dev[s0 + i];
+    const int e = ids[i];
     if (e >= 0) atomicAdd(&cnt[wave][e], 1u);
   }
   __syncthreads();
-  for (int e = t; e < E; e += kRtWaves * 64) {
+  for (int e = t; e < E; e += W * 64) {
     uint32_t b = base[e];
-    for (int w = 0; w < kRtWaves; ++w) {
+    for (int w = 0; w < W; ++w) {
       const uint32_t c = cnt[w][e];
       cnt[w][e] = b;
       b += c;
@@ -161,7 +175,7 @@ __device__ void place_rows(const RouteArgs& a, int tok0, int tok1, int wave, int
   const int bits = 32 - __builtin_clz((unsigned)E);
   for (int i0 = r0; i0 < r1; i0 += 64) {
     const int i = i0 + lane;
-    const int e = i < r1 ? a.r.ids_dev[s0 + i] : -1;
+    const int e = i < r1 ? ids[i] : -1;
     uint64_t same = ~0ull;
     for (int b = 0; b <= bits; ++b) {  // one bit more: -1 has none in common with the others
       const bool on = (e >> b) & 1;
@@ -179,7 +193,8 @@ __device__ void place_rows(const RouteArgs& a, int tok0, int tok1, int wave, int
   }
 }
 
-// Exclusive sums of total[0 .. E) -> base; returns the whole.  E <= 1024, two experts a thread.
+// Exclusive sums of total[0 .. E) -> base; returns the whole.  E <= 1024, two experts a thread (512 threads or more).
+template <int W>
 __device__ uint32_t scan_experts(const uint32_t* total, uint32_t* base, int E, uint32_t* tmp) {
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   const uint32_t x = 2 * t < E ? total[2 * t] : 0, y = 2 * t + 1 < E ? total[2 * t + 1] : 0;
@@ -192,7 +207,7 @@ __device__ uint32_t scan_experts(const uint32_t* total, uint32_t* base, int E, u
   if (lane == 63) tmp[wave] = incl;
   __syncthreads();
   uint32_t before = 0, all = 0;
-  for (int w = 0; w < kRtWaves; ++w) {
+  for (int w = 0; w < W; ++w) {
     before += w < wave ? tmp[w] : 0;
     all += tmp[w];
   }
@@ -204,41 +219,41 @@ __device__ uint32_t scan_experts(const uint32_t* total, uint32_t* base, int E, u
 }
 
 // ONE: a single workgroup does all.
-template <bool ONE>
-__global__ __launch_bounds__(kRtWaves * 64) void k_route_top(RouteArgs a) {
+template <bool ONE, bool BF16>
+__global__ __launch_bounds__(kTopWaves * 64) void k_route_top(RouteArgs a) {
   __shared__ uint32_t count[kF8MaxExperts];
+  __shared__ int slot_id[ONE ? kTopWaves * 4 * 32 : 1];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, E = a.r.experts;
   const int tok0 = min((int)blockIdx.x * a.per_block, a.r.tokens), tok1 = min(tok0 + a.per_block, a.r.tokens);
-  for (int e = t; e < E; e += kRtWaves * 64) count[e] = 0;
+  for (int e = t; e < E; e += kTopWaves * 64) count[e] = 0;
   __syncthreads();
-  top_tokens_of(a, tok0, tok1, wave, lane, count);
-  __threadfence_block();
+  top_tokens_of<BF16>(a, tok0, tok1, wave, lane, count, ONE ? slot_id : nullptr);
   __syncthreads();
   if constexpr (!ONE) {
     const int stride = (E + 1) & ~1;
-    for (int e = t; e < stride; e += kRtWaves * 64) a.hist[(size_t)blockIdx.x * stride + e] = e < E ? (uint16_t)count[e] : (uint16_t)0;
+    for (int e = t; e < stride; e += kTopWaves * 64) a.hist[(size_t)blockIdx.x * stride + e] = e < E ? (uint16_t)count[e] : (uint16_t)0;
   } else {
-    __shared__ uint32_t cnt[kRtWaves][kF8MaxExperts];
+    __shared__ uint32_t cnt[kTopWaves][kF8MaxExperts];
     __shared__ uint32_t base[kF8MaxExperts];
-    __shared__ uint32_t tmp[kRtWaves];
-    const uint32_t all = scan_experts(count, base, E, tmp);
-    for (int e = t; e <= E; e += kRtWaves * 64) a.r.offsets_dev[e] = (int)(e < E ? base[e] : all);
-    place_rows(a, tok0, tok1, wave, lane, cnt, base);
-    for (int i = (int)all + t; i < a.r.tokens * a.r.top_k; i += kRtWaves * 64) a.r.token_of_row_dev[i] = -1;
+    __shared__ uint32_t tmp[kTopWaves];
+    const uint32_t all = scan_experts<kTopWaves>(count, base, E, tmp);
+    for (int e = t; e <= E; e += kTopWaves * 64) a.r.offsets_dev[e] = (int)(e < E ? base[e] : all);
+    place_rows<kTopWaves>(a, slot_id, tok0, tok1, wave, lane, cnt, base);
+    for (int i = (int)all + t; i < a.r.tokens * a.r.top_k; i += kTopWaves * 64) a.r.token_of_row_dev[i] = -1;
   }
 }
 
-__global__ __launch_bounds__(kRtWaves * 64) void k_route_place(RouteArgs a) {
-  __shared__ uint32_t cnt[kRtWaves][kF8MaxExperts];
+__global__ __launch_bounds__(kPlaceWaves * 64) void k_route_place(RouteArgs a) {
+  __shared__ uint32_t cnt[kPlaceWaves][kF8MaxExperts];
   __shared__ uint32_t total[kF8MaxExperts], base[kF8MaxExperts], mine[kF8MaxExperts];
-  __shared__ uint32_t tmp[kRtWaves];
+  __shared__ uint32_t tmp[kPlaceWaves];
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, E = a.r.experts, nb = gridDim.x;
   const int tok0 = min((int)blockIdx.x * a.per_block, a.r.tokens), tok1 = min(tok0 + a.per_block, a.r.tokens);
   // all workgroups' counts, two experts and a part of the workgroups a thread: `parts` threads side by side have the same experts
-  const int pairs = (E + 1) / 2, parts = max(1, kRtWaves * 64 / pairs), stride = (E + 1) & ~1;
-  for (int e = t; e < E; e += kRtWaves * 64) total[e] = mine[e] = 0;
+  const int pairs = (E + 1) / 2, parts = max(1, kPlaceWaves * 64 / pairs), stride = (E + 1) & ~1;
+  for (int e = t; e < E; e += kPlaceWaves * 64) total[e] = mine[e] = 0;
   __syncthreads();
-  for (int u = t; u < pairs * parts; u += kRtWaves * 64) {
+  for (int u = t; u < pairs * parts; u += kPlaceWaves * 64) {
     const int pair = u % pairs, part = u / pairs, b1 = nb * (part + 1) / parts;
     const uint32_t* h = reinterpret_cast<const uint32_t*>(a.hist) + pair;
     uint32_t all0 = 0, all1 = 0, before0 = 0, before1 = 0;
@@ -259,20 +274,23 @@ __global__ __launch_bounds__(kRtWaves * 64) void k_route_place(RouteArgs a) {
     }
   }
   __syncthreads();
-  const uint32_t all = scan_experts(total, base, E, tmp);
+  const uint32_t all = scan_experts<kPlaceWaves>(total, base, E, tmp);
   if (blockIdx.x == 0)
-    for (int e = t; e <= E; e += kRtWaves * 64) a.r.offsets_dev[e] = (int)(e < E ? base[e] : all);
+    for (int e = t; e <= E; e += kPlaceWaves * 64) a.r.offsets_dev[e] = (int)(e < E ? base[e] : all);
   __syncthreads();
-  for (int e = t; e < E; e += kRtWaves * 64) base[e] += mine[e];
+  for (int e = t; e < E; e += kPlaceWaves * 64) base[e] += mine[e];
   __syncthreads();
-  place_rows(a, tok0, tok1, wave, lane, cnt, base);
+  place_rows<kPlaceWaves>(a, a.r.ids_dev + (int64_t)tok0 * a.r.top_k, tok0, tok1, wave, lane, cnt, base);
   const int64_t slots = (int64_t)a.r.tokens * a.r.top_k;
-  for (int64_t i = (int64_t)all + (int64_t)blockIdx.x * (kRtWaves * 64) + t; i < slots; i += (int64_t)nb * (kRtWaves * 64)) a.r.token_of_row_dev[i] = -1;
+  for (int64_t i = (int64_t)all + (int64_t)blockIdx.x * (kPlaceWaves * 64) + t; i < slots; i += (int64_t)nb * (kPlaceWaves * 64)) a.r.token_of_row_dev[i] = -1;
 }
 
-int tokens_per_block(int tokens) {
+// Tokens of a workgroup: what its waves take at once, or more where that would be over 256 workgroups (each of which adds up the counts of
+// all).  One workgroup does all in one launch.
+int tokens_per_block(int tokens, int experts) {
+  const int once = kTopWaves * (experts <= 256 ? 4 : 1);
   const int per = (tokens + kRtMaxBlocks - 1) / kRtMaxBlocks;
-  return per < 128 ? 128 : per;
+  return per < once ? once : per;
 }
 
 // Y[t] = sum of a token's rows times their weights, slots in order.  A thread has 8 columns.
@@ -344,7 +362,7 @@ __global__ __launch_bounds__(256) void k_combine(stamp_routing_t r, const void* 
 }  // namespace
 
 size_t stamp_route_ws(int tokens, int experts, int) {
-  const int per = tokens_per_block(tokens);
+  const int per = tokens_per_block(tokens, experts);
   const size_t nb = ((size_t)tokens + per - 1) / per;
   return (nb * ((size_t)experts + 1) * sizeof(uint16_t) + 255) / 256 * 256 + 256;
 }
@@ -354,16 +372,17 @@ hipError_t stamp_launch_route(const stamp_routing_t& r, const void* logits, int 
   a.r = r;
   a.logits = logits;
   a.ld = ld;
-  a.bf16 = bf16;
   a.renorm = renorm;
-  a.per_block = tokens_per_block(r.tokens);
+  a.per_block = tokens_per_block(r.tokens, r.experts);
   a.hist = static_cast<uint16_t*>(ws);
   const int nb = (r.tokens + a.per_block - 1) / a.per_block;
   if (nb <= 1) {
-    k_route_top<true><<<1, kRtWaves * 64, 0, st>>>(a);
+    if (bf16) k_route_top<true, true><<<1, kTopWaves * 64, 0, st>>>(a);
+    else k_route_top<true, false><<<1, kTopWaves * 64, 0, st>>>(a);
   } else {
-    k_route_top<false><<<nb, kRtWaves * 64, 0, st>>>(a);
-    k_route_place<<<nb, kRtWaves * 64, 0, st>>>(a);
+    if (bf16) k_route_top<false, true><<<nb, kTopWaves * 64, 0, st>>>(a);
+    else k_route_top<false, false><<<nb, kTopWaves * 64, 0, st>>>(a);
+    k_route_place<<<nb, kPlaceWaves * 64, 0, st>>>(a);
   }
   return hipGetLastError();
 }
