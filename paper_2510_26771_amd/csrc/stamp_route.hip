@@ -12,7 +12,7 @@ struct RouteArgs {
   stamp_routing_t r;
   const void* logits;
   int64_t ld;
-  int32_t renorm;
+  int32_t renorm, aligned;  // rows of logits on the 16-byte grid
   int32_t per_block;   // tokens of a workgroup
   uint16_t* hist;      // [workgroups][experts, an even number] rows that a workgroup's tokens give an expert
 };
@@ -54,7 +54,7 @@ __device__ __forceinline__ float sum_lanes(float v) {
   return __uint_as_float(over_lanes<LANES>(__float_as_uint(v), [](uint32_t x, uint32_t y) { return __float_as_uint(__uint_as_float(x) + __uint_as_float(y)); }));
 }
 
-// LANES lanes have a token, lane l of them experts l + LANES j: 4 tokens a wave up to 256 experts (the vector ALU is the bound, and the
+// LANES lanes have a token, lane l of them experts NV l + j: 4 tokens a wave up to 256 experts (the vector ALU is the bound, and the
 // steps over lanes cost the same for 1 and for 4 tokens).  The largest key, of the lowest expert, is taken top_k times.  A bf16 logit's key
 // has 16 bits: with the expert below it in one word the largest word is the choice, and no two are equal.
 // slot_id: where not nullptr, the ids go there as well.
@@ -70,16 +70,30 @@ __device__ void top_tokens(const RouteArgs& a, int tok0, int tok1, int wave, int
     const int t = tb + lane / LANES;
     const bool in = t < tok1;
     uint32_t key[NV];
+    constexpr int kSize = BF16 ? 2 : 4, kWords = NV * kSize / 16;
+    const char* const row = static_cast<const char*>(a.logits) + ((int64_t)(in ? t : tok0) * a.ld + l0 * NV) * kSize;
+    uint32_t raw[NV];  // the logits as fp32
+    if (kWords > 0 && a.aligned && (l0 + 1) * NV <= E) {
+#pragma unroll
+      for (int w = 0; w < kWords; ++w) {
+        const u4 v = reinterpret_cast<const u4*>(row)[w];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if constexpr (BF16) raw[8 * w + 2 * i] = v[i] << 16, raw[8 * w + 2 * i + 1] = v[i] & 0xffff0000u;
+          else raw[4 * w + i] = v[i];
+        }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        raw[j] = 0xff800000u;
+        if (l0 * NV + j < E) raw[j] = BF16 ? (uint32_t)reinterpret_cast<const uint16_t*>(row)[j] << 16 : reinterpret_cast<const uint32_t*>(row)[j];
+      }
+    }
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      const int e = l0 + LANES * j;
-      float l = -__builtin_inff();
-      if (in && e < E) {
-        if constexpr (BF16) l = __uint_as_float((uint32_t)static_cast<const uint16_t*>(a.logits)[(int64_t)t * a.ld + e] << 16);
-        else l = static_cast<const float*>(a.logits)[(int64_t)t * a.ld + e];
-      }
-      key[j] = order_key(l);
-      if constexpr (BF16) key[j] = key[j] == 0 ? 0 : (key[j] & 0xffff0000u) | (uint32_t)(0xffff - e);
+      key[j] = in ? order_key(__uint_as_float(raw[j])) : 0;
+      if constexpr (BF16) key[j] = key[j] == 0 ? 0 : (key[j] & 0xffff0000u) | (uint32_t)(0xffff - (l0 * NV + j));
     }
     uint32_t mine[kMine] = {};  // lane l: key of the chosen l, l + 16
     int id[kMine];
@@ -97,8 +111,8 @@ __device__ void top_tokens(const RouteArgs& a, int tok0, int tok1, int wave, int
       } else {
         uint32_t at = 0xffffffffu;
 #pragma unroll
-        for (int j = NV - 1; j >= 0; --j) at = key[j] == best ? (uint32_t)(LANES * j) : at;
-        e = over_lanes<LANES>(at == 0xffffffffu ? at : at + l0, [](uint32_t x, uint32_t y) { return min(x, y); });
+        for (int j = NV - 1; j >= 0; --j) at = key[j] == best ? (uint32_t)j : at;
+        e = over_lanes<LANES>(at == 0xffffffffu ? at : at + l0 * NV, [](uint32_t x, uint32_t y) { return min(x, y); });
       }
       if (k == 0) {
         top = value(best);
@@ -115,9 +129,9 @@ __device__ void top_tokens(const RouteArgs& a, int tok0, int tok1, int wave, int
         for (int q = 0; q < kMine; ++q)
           if (k / LANES == q) mine[q] = best, id[q] = (int)e;
       }
-      const uint32_t gone = e - l0;  // LANES j where the chosen one is this lane's
+      const uint32_t gone = e - l0 * NV;  // j where the chosen one is this lane's
 #pragma unroll
-      for (int j = 0; j < NV; ++j) key[j] = (BF16 ? key[j] == best : gone == (uint32_t)(LANES * j)) ? 0 : key[j];
+      for (int j = 0; j < NV; ++j) key[j] = (BF16 ? key[j] == best : gone == (uint32_t)j) ? 0 : key[j];
     }
     float sh[kMine], s = 0.0f;
 #pragma unroll
@@ -373,6 +387,7 @@ hipError_t stamp_launch_route(const stamp_routing_t& r, const void* logits, int 
   a.logits = logits;
   a.ld = ld;
   a.renorm = renorm;
+  a.aligned = (reinterpret_cast<uintptr_t>(logits) | (uintptr_t)(ld * (bf16 ? 2 : 4))) % 16 == 0;
   a.per_block = tokens_per_block(r.tokens, r.experts);
   a.hist = static_cast<uint16_t*>(ws);
   const int nb = (r.tokens + a.per_block - 1) / a.per_block;
