@@ -170,9 +170,11 @@ def _ptr(t) -> Optional[int]:
 
 
 def _stream(stream) -> Optional[int]:
+    if stream is not None:
+        return stream.cuda_stream or None
     import torch
-    s = stream if stream is not None else torch.cuda.current_stream()
-    return s.cuda_stream or None
+    # torch.cuda.current_stream() builds a Stream object: 2.8 us, more than a third of a small layer's call
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) or None
 
 
 def mfma_rate(engine) -> float:

@@ -401,6 +401,10 @@ def test_router_against_the_definition(st, tokens, experts, top_k, renormalize, 
     assert np.array_equal(r.row_of_slot.cpu().numpy(), row)
     # exp of a difference of up to 16 (rounded: 16 * 2^-24), its own error, and the sum's roundings
     w = r.weights.cpu().numpy().astype(np.float64)
+    # rows side by side (16-byte loads where they are on that grid): the same bits
+    r2 = st.Routing(tokens, experts, top_k)
+    st.route_topk(lg, r2, renormalize=renormalize)
+    assert all(torch.equal(getattr(r, n), getattr(r2, n)) for n in ("ids", "weights", "offsets", "token_of_row", "row_of_slot"))
     assert np.all(np.abs(w - weights) <= (32 + experts / 64 + 8) * 2.0 ** -23 * weights + 1e-37)
 
 
