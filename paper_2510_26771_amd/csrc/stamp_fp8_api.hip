@@ -46,7 +46,9 @@ StampF8Gemm gemm_args(const stamp_fp8_plan* p) {
   return a;
 }
 
-int route_of(const StampF8Gemm& a, int rows) { return a.forced ? a.forced : stamp_f8_route(a.sets, a.groups, a.Kb, rows, a.wide_sums); }
+int route_of(const StampF8Gemm& a, int rows, int* parts = nullptr) {
+  return stamp_f8_route(a.sets, a.groups, a.Kb, rows, a.wide_sums, a.gated, a.forced, parts);
+}
 // the codes are wanted as bf16
 bool wide_codes(const StampF8Gemm& a, int rows) { return a.wide_sums && route_of(a, rows) != STAMP_FP8_ROUTE_ROWS; }
 
@@ -62,30 +64,29 @@ void give_x(StampF8Gemm* a, const stamp_fp8_desc_t& d, int rows, const void* X, 
 }
 
 hipError_t product(const StampF8Gemm& a, hipStream_t st) {
-  switch (route_of(a, a.rows)) {
-    case STAMP_FP8_ROUTE_ROWS: return stamp_launch_f8_rows(a, st);
-    case STAMP_FP8_ROUTE_TILES_64: return stamp_launch_f8_tiles(a, 64, st);
-    case STAMP_FP8_ROUTE_TILES_128: return stamp_launch_f8_tiles(a, 128, st);
-    default: return stamp_launch_f8_tiles(a, 256, st);
-  }
+  int parts = 1;
+  const int route = route_of(a, a.rows, &parts);
+  if (route == STAMP_FP8_ROUTE_ROWS) return stamp_launch_f8_rows(a, st);
+  return stamp_launch_f8_tiles(a, 64 << (route - STAMP_FP8_ROUTE_TILES_64), parts, st);
 }
 
 // room for a code of the activations: as bf16 where some route wants that
 int code_bytes(const stamp_fp8_plan* p) { return gemm_args(p).wide_sums ? 2 : 1; }
 
 struct LinearWs {
-  size_t codes, scales, total;
+  size_t codes, scales, partial, total;
 };
 LinearWs linear_ws(const stamp_fp8_plan* p, int32_t rows) {
   LinearWs w;
   w.codes = 0;
   w.scales = align256((size_t)rows * p->Kp * code_bytes(p));
-  w.total = w.scales + align256((size_t)p->Kb * scales_ld(rows) * sizeof(float));
+  w.partial = w.scales + align256((size_t)p->Kb * scales_ld(rows) * sizeof(float));
+  w.total = w.partial + align256(stamp_f8_partial_bytes(p->groups, rows));
   return w;
 }
 
 struct ExpertsWs {
-  size_t codes, scales, h, sh, rows, wide, total;
+  size_t codes, scales, h, sh, rows, wide, partial, total;
   int64_t ld_rows;
 };
 ExpertsWs experts_ws(const stamp_fp8_plan* up, const stamp_fp8_plan* down, int32_t tokens, int32_t top_k) {
@@ -99,7 +100,8 @@ ExpertsWs experts_ws(const stamp_fp8_plan* up, const stamp_fp8_plan* down, int32
   w.ld_rows = (down->desc.d_out + 7) / 8 * 8;
   // the up product writes codes of one byte; a down product that wants them as bf16 has them widened here
   w.wide = w.rows + align256((size_t)slots * w.ld_rows * type_size(down->desc.y_dtype));
-  w.total = w.wide + (code_bytes(down) == 2 ? align256((size_t)slots * down->Kp * 2) : 0);
+  w.partial = w.wide + (code_bytes(down) == 2 ? align256((size_t)slots * down->Kp * 2) : 0);
+  w.total = w.partial + align256(stamp_f8_partial_bytes(down->groups, (int32_t)slots));
   return w;
 }
 
@@ -149,6 +151,7 @@ stamp_status_t forward(const stamp_fp8_plan* p, int32_t rows, const int32_t* off
     return STAMP_ERR_DEVICE;
   }
   a.A = codes;
+  a.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + w.partial);
   a.SA = scales;
   a.ld_sa = scales_ld(rows);
   a.a_rows = a.rows = rows;
@@ -162,31 +165,52 @@ stamp_status_t forward(const stamp_fp8_plan* p, int32_t rows, const int32_t* off
 
 // Kernel for a product of `rows` rows over `sets` weights.
 //
-// Few rows: the weights' time, and some 5 us more per 16 rows and 700 groups; tiles of 64 rows hold the time up to 64 rows but take one
-// workgroup per 256 columns and set.  Whole calls, us (rows kernel / tiles of 64), 4096 -> 11008, bf16 Y: 17 rows 15.2 / 19.2,
-// 32 18.3 / 19.6, 33 21.2 / 19.6, 64 28.4 / 20.5; 4096 -> 4096: 64 15.3 / 19.2, 128 26 / 19.4; fp32 Y (sums in fp32), 4096 -> 11008:
-// 64 28.5 / 34.8, 96 43.7 / 35.2; 4096 -> 4096: 128 26.9 / 34.4.
+// Few rows: the weights' time, and some 5 us more per 16 rows and 700 blocks of 16 columns; tiles of 64 rows hold the time up to 64 rows.
+// Whole calls, us (rows kernel / tiles of 64), bf16 Y: 4096 -> 11008 32 rows 17.9 / 17.4, 48 24.1 / 18.2; 4096 -> 4096 32 rows 10.1 / 12.6,
+// 48 13.6 / 13.8, 96 22.5 / 16.6; 1152 -> 4608 32 rows 8.8 / 9.4, 48 11.7 / 9.8.  fp32 Y (sums in fp32): 1152 -> 4608 64 rows 13.5 / 15.1,
+// 96 19.1 / 15.2; 1185 -> 2305 64 rows 11.0 / 16.1; 8192 -> 1024 32 rows 13.7 / 16.3, 64 22.4 / 18.4.
 //
 // Tiles of 64, 128, 256 rows: a workgroup a CU, so rounds of `cus` tiles, each of Kb steps and a start and end.  us per step and
 // per round, measured on full rounds: 0.53 + 3.5, 0.9 + 4.5, 1.45 + 6; with sums in fp32 1.05 + 4, 1.75 + 6.  (2048 x 4096 -> 11008: 120, 98
 // and 100 us; 8192 x 1152 -> 4608: 77, 64 and 60; 512 x 4096 -> 11008: 39, 30 and 45.)
-int stamp_f8_route(int sets, int groups, int Kb, int rows, int wide_sums) {
+//
+// Few tiles: the depth in up to 8 parts, at least 4 blocks each, while the workgroups fit the CUs; 3.5 us for the pass that adds them up,
+// and the parts' rows at 3 TB/s.  A step takes 0.43, 0.7, 1.1 us while most CUs are idle (sums in fp32: 0.9, 1.3).
+int stamp_f8_route(int sets, int groups, int Kb, int rows, int wide_sums, int gated, int forced, int* parts_out) {
   const int busy = sets < rows ? sets : rows > 0 ? rows : 1, avg = (int)(((int64_t)rows + busy - 1) / busy);
   const int64_t ncol = (groups + 3) / 4;
-  int few = ncol * busy < 32 ? 64 : 32;
-  if (wide_sums) few *= 2;
-  if (avg <= few) return STAMP_FP8_ROUTE_ROWS;
+  const int few = wide_sums ? 64 : 32;
+  if (parts_out) *parts_out = 1;
+  if (forced == STAMP_FP8_ROUTE_ROWS || (forced == 0 && avg <= few)) return STAMP_FP8_ROUTE_ROWS;
   const int cus = stamp_device_cus();
-  static const float step[2][3] = {{0.53f, 0.9f, 1.45f}, {1.05f, 1.75f, 0.0f}}, ends[2][3] = {{3.5f, 4.5f, 6.0f}, {4.0f, 6.0f, 0.0f}};
+  static const float step[2][3] = {{0.53f, 0.9f, 1.45f}, {1.05f, 1.75f, 0.0f}}, idle[2][3] = {{0.43f, 0.7f, 1.1f}, {0.9f, 1.3f, 0.0f}},
+                     ends[2][3] = {{3.5f, 4.5f, 6.0f}, {4.0f, 6.0f, 0.0f}};
+  const int w = wide_sums != 0;
   int best = 0;
   float best_us = 0.0f;
-  for (int i = 0; i < (wide_sums ? 2 : 3); ++i) {  // the bf16 operands of 256 rows do not fit the registers
+  for (int i = 0; i < (w ? 2 : 3); ++i) {  // the bf16 operands of 256 rows do not fit the registers
+    if (forced != 0 && forced != STAMP_FP8_ROUTE_TILES_64 + i) continue;
     const int bm = 64 << i;
-    const int64_t tiles = sets == 1 ? (rows + bm - 1) / bm : rows / bm + (busy + 1) / 2;  // half of the last tile of a set is empty
-    const float us = (float)((tiles * ncol + cus - 1) / cus) * ((float)Kb * step[wide_sums != 0][i] + ends[wide_sums != 0][i]);
-    if (best == 0 || us < best_us) best = STAMP_FP8_ROUTE_TILES_64 + i, best_us = us;
+    const int64_t tiles = (sets == 1 ? (rows + bm - 1) / bm : rows / bm + (busy + 1) / 2) * ncol;  // half of the last tile of a set is empty
+    float us = (float)((tiles + cus - 1) / cus) * ((float)Kb * (2 * tiles <= cus ? idle : step)[w][i] + ends[w][i]);
+    int parts = 1;
+    for (int n = 2; !gated && n <= kF8MaxParts && n * tiles <= cus && 4 * n <= Kb; ++n) {
+      const float split = (float)((Kb + n - 1) / n) * idle[w][i] + ends[w][i] + 3.5f + (float)n * rows * groups * 64 * 8 * 1e-6f / 3.0f;
+      if (split < us) us = split, parts = n;
+    }
+    if (best == 0 || us < best_us) {
+      best = STAMP_FP8_ROUTE_TILES_64 + i;
+      best_us = us;
+      if (parts_out) *parts_out = parts;
+    }
   }
   return best;
+}
+
+// parts * tiles <= CUs, and the rows are at most the tiles' (a set's half tile is counted, and one more)
+size_t stamp_f8_partial_bytes(int groups, int rows) {
+  const size_t whole = (size_t)kF8MaxParts * rows * groups * 64, fit = (size_t)stamp_device_cus() * 256 * 256;
+  return (whole < fit ? whole : fit) * sizeof(float);
 }
 
 extern "C" {
@@ -286,6 +310,7 @@ stamp_status_t stamp_fp8_linear_forward_q(const stamp_fp8_plan_t* p, int32_t row
   if (s != STAMP_OK) return s;
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
   StampF8Gemm a = gemm_args(p);
+  a.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace_dev) + linear_ws(p, rows).partial);
   a.A = codes_dev;
   if (wide_codes(a, rows)) {
     uint8_t* wide = static_cast<uint8_t*>(workspace_dev);
@@ -370,6 +395,7 @@ stamp_status_t stamp_experts_forward(const stamp_fp8_plan_t* up, const stamp_fp8
   if (product(a, st) != hipSuccess) return STAMP_ERR_DEVICE;
 
   StampF8Gemm b = gemm_args(down);
+  b.partial = reinterpret_cast<float*>(ws + w.partial);
   b.A = ws + w.h;
   if (wide_codes(b, slots)) {
     if (stamp_launch_f8_widen(b.A, (int64_t)slots * down->Kp, ws + w.wide, st) != hipSuccess) return STAMP_ERR_DEVICE;
@@ -415,7 +441,7 @@ stamp_status_t stamp_fp8_debug_weight_codes(const stamp_fp8_plan_t* p, uint8_t* 
 
 int32_t stamp_fp8_debug_route(const stamp_fp8_plan_t* p, int32_t rows) {
   if (p == nullptr || rows < 0) return 0;
-  return p->forced ? p->forced : stamp_f8_route(p->sets, p->groups, p->Kb, rows, gemm_args(p).wide_sums);
+  return route_of(gemm_args(p), rows);
 }
 
 stamp_status_t stamp_fp8_debug_set_route(stamp_fp8_plan_t* p, int32_t route) {

@@ -13,6 +13,8 @@
 // the vector ALU its bound), 256 bytes a row, piece p of 16 at p ^ (row % 16); the weights are widened once per step and wave
 // (conversions among the matrix instructions, see wide_step: in a row of their own they leave the matrix pipe idle in both waves of a SIMD).
 //
+// Few tiles: the depth in parts, each tile by as many workgroups, whose fp32 rows k_f8_join adds up in order.
+//
 // STAMP_SCALE_F32: an instruction's sum over the block of channels (its addend is 0) goes to the accumulators by a multiplication with
 // both scales, 4 fused multiply-adds per instruction, one row block behind, so that the matrix pipe (32 cycles an instruction) runs on.
 #include <type_traits>
@@ -72,7 +74,9 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
   set = __builtin_amdgcn_readfirstlane(set);
   row0 = __builtin_amdgcn_readfirstlane(row0);
   nrows = __builtin_amdgcn_readfirstlane(nrows);
-  const int g0 = col * 4, Kb = a.Kb;
+  // its part of the depth: blocks kb0 .. kb0 + Kb - 1
+  const int g0 = col * 4, depth = a.Kb, parts = gridDim.y, part_no = blockIdx.y;
+  const int kb0 = depth * part_no / parts, Kb = depth * (part_no + 1) / parts - kb0;
 
   // 32-bit offsets from a scalar base: the tile's first row, or (gated, by index) all rows of A, below 4 GB
   uint32_t aoff[LA], boff[4];
@@ -81,15 +85,15 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
     const int p = i * 512 + t, row = WIDE ? p >> 4 : p >> 3, piece = WIDE ? (p & 15) ^ (row & 15) : (p & 7) ^ ((row >> 1) & 7);
     uint32_t r = min(row, nrows - 1);
     if constexpr (GATED) r = min(max(a.index[row0 + r], 0), a.a_rows - 1);
-    aoff[i] = r * (uint32_t)(Kb * kRowBytes) + piece * 16;
+    aoff[i] = r * (uint32_t)(depth * kRowBytes) + piece * 16;
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) boff[i] = uniform((uint32_t)(min(g0 + i, a.groups - 1) - g0) * (uint32_t)Kb * kF8GroupBytes);
-  const __amdgpu_buffer_rsrc_t ra = buffer(a.A + (GATED ? (size_t)0 : (size_t)row0 * Kb * kRowBytes));
-  const __amdgpu_buffer_rsrc_t rb = buffer(a.W + ((size_t)set * a.groups + g0) * Kb * kF8GroupBytes);
+  for (int i = 0; i < 4; ++i) boff[i] = uniform((uint32_t)(min(g0 + i, a.groups - 1) - g0) * (uint32_t)depth * kF8GroupBytes);
+  const __amdgpu_buffer_rsrc_t ra = buffer(a.A + (GATED ? (size_t)0 : (size_t)row0 * depth * kRowBytes) + (size_t)kb0 * kRowBytes);
+  const __amdgpu_buffer_rsrc_t rb = buffer(a.W + (((size_t)set * a.groups + g0) * depth + kb0) * kF8GroupBytes);
   uint32_t soff = (uint32_t)min(t, nrows - 1);  // of the rows' scales, which lie by row of A
   if constexpr (GATED) soff = (uint32_t)min(max(a.index[row0 + soff], 0), a.a_rows - 1);
-  const float* const sa = a.SA + (GATED ? 0 : row0);
+  const float* const sa = a.SA + (GATED ? 0 : row0) + (int64_t)kb0 * a.ld_sa;
 
   // the q-th of a stage's loads; behind the last block of channels that one again, which nobody reads
   constexpr int kLoads = 4 + LA + 1;
@@ -274,12 +278,12 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
   for (int i = t; i < 2 * Kb; i += 512) {
     const int which = i >= Kb, kb = i - which * Kb;
     const int blk = GATED ? which * a.nblk + (min(g0, a.groups - 1) >> 2) : min((g0 >> 1) + which, a.nblk - 1);
-    wscale[which][kb] = a.SW[((size_t)set * (GATED ? 2 : 1) * a.nblk + blk) * Kb + kb];
+    wscale[which][kb] = a.SW[((size_t)set * (GATED ? 2 : 1) * a.nblk + blk) * depth + kb0 + kb];
   }
   if constexpr (!GATED) {
     if (t < 256) {
       const int n = g0 * 64 + t;
-      bias_of[t] = a.bias != nullptr && n < a.N ? a.bias[(size_t)set * a.N + n] : 0.0f;
+      bias_of[t] = a.bias != nullptr && n < a.N && part_no == 0 ? a.bias[(size_t)set * a.N + n] : 0.0f;
     }
   }
   turn(none);
@@ -335,9 +339,14 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
     float bias[16];
 #pragma unroll
     for (int j = 0; j < 16; ++j) bias[j] = bias_of[64 * wn + 32 * (j >> 3) + 8 * f + (j & 7)];
-    const uint32_t size = a.y_bf16 ? 2 : 4, ld = (uint32_t)a.ld_y * size;
-    char* const y = static_cast<char*>(a.Y) + ((int64_t)row0 * a.ld_y) * size;  // 256 rows are below 4 GB, checked by the host
-    const bool wide = (reinterpret_cast<uintptr_t>(a.Y) | ld) % 16 == 0 && g * 64 + 64 <= a.N;
+    // one of several parts: fp32 rows of all places into its own piece of the scratch memory, for k_f8_join
+    const bool whole = parts == 1, bf16 = whole && a.y_bf16;
+    const int N = whole ? a.N : a.groups * 64;
+    const int64_t ld_y = whole ? a.ld_y : N;
+    const uint32_t size = bf16 ? 2 : 4, ld = (uint32_t)ld_y * size;
+    char* const base = whole ? static_cast<char*>(a.Y) : reinterpret_cast<char*>(a.partial + (int64_t)part_no * a.rows * N);
+    char* const y = base + ((int64_t)row0 * ld_y) * size;  // 256 rows are below 4 GB, checked by the host
+    const bool wide = (reinterpret_cast<uintptr_t>(base) | ld) % 16 == 0 && g * 64 + 64 <= N;
     const __amdgpu_buffer_rsrc_t ry = buffer(y);
     auto col_of = [](int j) { return 32 * (j >> 3) + (j & 7); };
 #pragma unroll
@@ -348,7 +357,7 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
 #pragma unroll
       for (int j = 0; j < 16; ++j) v[j] = acc[mi][j >> 2][j & 3] + bias[j];
       if (wide) {
-        if (a.y_bf16) {
+        if (bf16) {
 #pragma unroll
           for (int q = 0; q < 2; ++q) {
             u4 w;
@@ -363,13 +372,13 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
             __builtin_amdgcn_raw_buffer_store_b128(w, ry, m < nrows ? o + 128 * (q >> 1) + 16 * (q & 1) : kNowhere, 0, 0);
           }
         }
-      } else if (a.y_bf16) {
+      } else if (bf16) {
 #pragma unroll
-        for (int j = 0; j < 16; ++j) __builtin_amdgcn_raw_buffer_store_b16(to_bf16(v[j]), ry, m < nrows && n0 + col_of(j) < a.N ? o + 2 * col_of(j) : kNowhere, 0, 0);
+        for (int j = 0; j < 16; ++j) __builtin_amdgcn_raw_buffer_store_b16(to_bf16(v[j]), ry, m < nrows && n0 + col_of(j) < N ? o + 2 * col_of(j) : kNowhere, 0, 0);
       } else {
 #pragma unroll
         for (int j = 0; j < 16; ++j)
-          __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[j]), ry, m < nrows && n0 + col_of(j) < a.N ? o + 4 * col_of(j) : kNowhere, 0, 0);
+          __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[j]), ry, m < nrows && n0 + col_of(j) < N ? o + 4 * col_of(j) : kNowhere, 0, 0);
       }
     }
   } else {
@@ -419,23 +428,68 @@ __global__ __launch_bounds__(256) void k_f8_widen(const uint8_t* codes, int64_t 
   reinterpret_cast<b8*>(out)[2 * u + 1] = widen8((int)c[2], (int)c[3]);
 }
 
+// Y = sum of the parts, in order.  A thread has 4 columns of a row.
+template <int PARTS>
+__global__ __launch_bounds__(256) void k_f8_join(StampF8Gemm a, int wide) {
+  const int N = a.groups * 64, per = (a.N + 3) / 4;
+  const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x, m = u / per;
+  const int c = (int)(u - m * per) * 4;
+  const int rows = a.offsets == nullptr ? a.rows : min(max(a.offsets[a.sets], 0), a.rows);
+  if (m >= rows) return;
+  const f4* p = reinterpret_cast<const f4*>(a.partial + m * N + c);
+  f4 v[PARTS];
+#pragma unroll
+  for (int i = 0; i < PARTS; ++i) v[i] = p[(int64_t)i * a.rows * (N / 4)];
+  f4 s = v[0];
+#pragma unroll
+  for (int i = 1; i < PARTS; ++i) s += v[i];
+  if (a.y_bf16) {
+    uint16_t* y = static_cast<uint16_t*>(a.Y) + m * a.ld_y + c;
+    if (wide && c + 4 <= a.N) {
+      *reinterpret_cast<u2*>(y) = u2{to_bf16x2(s[0], s[1]), to_bf16x2(s[2], s[3])};
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (c + j < a.N) y[j] = to_bf16(s[j]);
+    }
+  } else {
+    float* y = static_cast<float*>(a.Y) + m * a.ld_y + c;
+    if (wide && c + 4 <= a.N) {
+      *reinterpret_cast<f4*>(y) = s;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (c + j < a.N) y[j] = s[j];
+    }
+  }
+}
+
 template <int BM>
-hipError_t go(const StampF8Gemm& a, hipStream_t st) {
+hipError_t go(const StampF8Gemm& a, int parts, hipStream_t st) {
   const int64_t tiles = a.offsets == nullptr ? ((int64_t)a.rows + BM - 1) / BM : (int64_t)a.rows / BM + (a.sets < a.rows ? a.sets : a.rows);
-  const uint32_t grid = (uint32_t)((tiles * ((a.groups + 3) / 4) + 7) / 8 * 8);
+  const dim3 grid((uint32_t)((tiles * ((a.groups + 3) / 4) + 7) / 8 * 8), parts);
   if constexpr (BM == 256) {
     if (a.wide_sums) return hipErrorInvalidValue;  // its registers do not hold the bf16 operands: never chosen
-  } else if (a.gated) {
-    k_f8_tiles<BM, kWide, true><<<grid, 512, 0, st>>>(a);
-    return hipGetLastError();
-  } else if (a.wide_sums) {
-    k_f8_tiles<BM, kWide, false><<<grid, 512, 0, st>>>(a);
-    return hipGetLastError();
-  }
-  if (a.pow2) {
-    k_f8_tiles<BM, kPow2, false><<<grid, 512, 0, st>>>(a);
+    if (a.pow2) k_f8_tiles<BM, kPow2, false><<<grid, 512, 0, st>>>(a);
+    else k_f8_tiles<BM, kScaled, false><<<grid, 512, 0, st>>>(a);
   } else {
-    k_f8_tiles<BM, kScaled, false><<<grid, 512, 0, st>>>(a);
+    if (a.gated) k_f8_tiles<BM, kWide, true><<<grid, 512, 0, st>>>(a);
+    else if (a.wide_sums) k_f8_tiles<BM, kWide, false><<<grid, 512, 0, st>>>(a);
+    else if (a.pow2) k_f8_tiles<BM, kPow2, false><<<grid, 512, 0, st>>>(a);
+    else k_f8_tiles<BM, kScaled, false><<<grid, 512, 0, st>>>(a);
+  }
+  if (parts > 1) {
+    const int64_t n = (int64_t)a.rows * ((a.N + 3) / 4);
+    const int wide = (reinterpret_cast<uintptr_t>(a.Y) | (uintptr_t)(a.ld_y * (a.y_bf16 ? 2 : 4))) % (a.y_bf16 ? 8 : 16) == 0;
+    static_assert(kF8MaxParts == 8, "a kernel for every number of parts");
+    auto* const join = parts == 2   ? k_f8_join<2>
+                       : parts == 3 ? k_f8_join<3>
+                       : parts == 4 ? k_f8_join<4>
+                       : parts == 5 ? k_f8_join<5>
+                       : parts == 6 ? k_f8_join<6>
+                       : parts == 7 ? k_f8_join<7>
+                                    : k_f8_join<8>;
+    join<<<(uint32_t)((n + 255) / 256), 256, 0, st>>>(a, wide);
   }
   return hipGetLastError();
 }
@@ -446,6 +500,6 @@ hipError_t stamp_launch_f8_widen(const uint8_t* codes, int64_t bytes, uint8_t* o
   return hipGetLastError();
 }
 
-hipError_t stamp_launch_f8_tiles(const StampF8Gemm& a, int bm, hipStream_t st) {
-  return bm == 64 ? go<64>(a, st) : bm == 128 ? go<128>(a, st) : go<256>(a, st);
+hipError_t stamp_launch_f8_tiles(const StampF8Gemm& a, int bm, int parts, hipStream_t st) {
+  return bm == 64 ? go<64>(a, parts, st) : bm == 128 ? go<128>(a, parts, st) : go<256>(a, parts, st);
 }
