@@ -67,8 +67,13 @@ struct StampF8Gemm {
   float* partial;          // [parts][rows][groups * 64] where the depth is split
 };
 
-// kernel for a product of `rows` rows over `sets` weights, and (not nullptr) the parts its depth is split into
-int stamp_f8_route(int sets, int groups, int Kb, int rows, int wide_sums, int gated, int forced, int* parts);
+// stamp_fp8_route_t of a product of `rows` rows over `sets` weights
+int stamp_f8_route(int sets, int groups, int Kb, int rows, int wide_sums, int gated, int forced);
+// its tiles: 64 << size rows and the parts of the depth, of the first `groups` groups (0: of all), and of the rest
+struct F8Cut {
+  int groups, size, parts, rest_size, rest_parts;
+};
+F8Cut stamp_f8_cut(int sets, int groups, int Kb, int rows, int wide_sums, int gated, int forced);
 constexpr int kF8MaxParts = 8;
 // bytes of the parts' rows, at most
 size_t stamp_f8_partial_bytes(int groups, int rows);

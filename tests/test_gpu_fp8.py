@@ -220,6 +220,25 @@ def test_every_kernel_is_reached_by_rule(st):
     plan.destroy()
 
 
+# tiles of one and a bit rounds: the last columns in a launch of their own, its depth in one piece or in parts
+@pytest.mark.parametrize("rows,d,n,y,pow2", [(3000, 520, 5700, "bf16", 0), (3000, 520, 5700, "f32", 1), (2900, 300, 5643, "bf16", 1), (2900, 300, 5643, "f32", 0),
+                                             (324, 4725, 10849, "bf16", 0), (323, 2998, 10965, "f32", 1)])
+def test_columns_in_two_launches(st, rows, d, n, y, pow2):
+    rng = np.random.default_rng(n)
+    xv, xg = _activations(rng, rows, d, "bf16")
+    w, ws = _weights(rng, (), n, d, pow2)
+    bias = rng.standard_normal(n).astype(np.float32) * 100
+    plan = st.Fp8Plan(st.Fp8Desc(d_in=d, d_out=n, y_dtype=_code(st, y), scale_format=pow2), _gpu(w), _gpu(ws), _gpu(bias))
+    Y, buf = _strided(rows, n, y, 3, 1)
+    plan.linear_forward(xg, Y, plan.alloc_workspace(rows))
+    codes, scales = ref.quantize(xv, pow2)
+    want, S, G = ref.product(codes, scales, w, ws)
+    _check(Y, want + bias, S + np.abs(bias), G, d, y == "f32", y == "bf16", f"{rows} {d} {n} {y}")
+    Y.fill_(-7.0)
+    assert (buf == -7.0).all(), "something outside of Y was written"
+    plan.destroy()
+
+
 @pytest.mark.parametrize("route", ["rows", "tiles_64", "tiles_128", "tiles_256"])
 @pytest.mark.parametrize("y,pow2", [("bf16", 0), ("bf16", 1), ("f32", 0), ("f32", 1)])
 @pytest.mark.parametrize("experts", [0, 4])
