@@ -50,7 +50,7 @@ struct StampF8Gemm {
   int32_t a_rows;
   const void* X;           // not nullptr: A's rows before Q8, quantized by the product itself (few rows)
   int64_t ld_x;
-  int32_t x_bf16, d, aligned;  // channels; rows of X on the 16-byte grid
+  int32_t x_bf16, d;       // channels
   int32_t chunk;           // rows quantized at a time
   int32_t rows;
   const int32_t* offsets;  // [sets + 1] or nullptr (one set)
@@ -106,6 +106,10 @@ typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+// in rows of any stride and alignment: loads and stores of 8 and 16 bytes need none
+typedef f4 f4_any __attribute__((aligned(4)));
+typedef u4 u4_any __attribute__((aligned(2)));
+typedef u2 u2_any __attribute__((aligned(2)));
 
 constexpr uint32_t kSmallest = (127u - 118u) << 23 | 0x600000u;  // 1.75 * 2^-118
 constexpr uint32_t kInfBits = 0x7f800000u;
@@ -219,13 +223,13 @@ __device__ __forceinline__ void find_tile(const StampF8Gemm& a, const Tiles& t, 
   }
 }
 
-// 16 channels of a row from c on as they are stored, zeros from d on.  aligned: 16-byte loads are.
+// 16 channels of a row from c on as they are stored, zeros from d on
 template <bool BF16>
 struct Raw16 {
   u4 w[BF16 ? 2 : 4];
-  __device__ __forceinline__ void load(const void* row, int c, int d, bool aligned) {
-    if (aligned && c + 16 <= d) {
-      const u4* s = reinterpret_cast<const u4*>(static_cast<const char*>(row) + (size_t)c * (BF16 ? 2 : 4));
+  __device__ __forceinline__ void load(const void* row, int c, int d) {
+    if (c + 16 <= d) {
+      const u4_any* s = reinterpret_cast<const u4_any*>(static_cast<const char*>(row) + (size_t)c * (BF16 ? 2 : 4));
 #pragma unroll
       for (int q = 0; q < (BF16 ? 2 : 4); ++q) w[q] = s[q];
       return;

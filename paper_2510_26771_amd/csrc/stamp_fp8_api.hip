@@ -58,7 +58,6 @@ void give_x(StampF8Gemm* a, const stamp_fp8_desc_t& d, int rows, const void* X, 
   a->ld_x = ld_x;
   a->x_bf16 = d.x_dtype == STAMP_BF16;
   a->d = d.d_in;
-  a->aligned = (reinterpret_cast<uintptr_t>(X) | (uintptr_t)(ld_x * (a->x_bf16 ? 2 : 4))) % 16 == 0;
 }
 
 hipError_t product(const StampF8Gemm& a, hipStream_t st) {

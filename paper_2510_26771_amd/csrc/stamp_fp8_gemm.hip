@@ -28,13 +28,12 @@ typedef __attribute__((address_space(3))) void* LdsPtr;
 
 #if defined(__HIP_DEVICE_COMPILE__)
 __device__ __forceinline__ uint32_t uniform(uint32_t v) { return (uint32_t)__builtin_amdgcn_readfirstlane((int)v); }
-// buffer over 4 GB from a uniform address on; an access at kNowhere is dropped
+// buffer over 4 GB from a uniform address on
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void* p) {
   const uint64_t u = reinterpret_cast<uint64_t>(p);
   const uint64_t v = (uint64_t)uniform((uint32_t)(u >> 32)) << 32 | uniform((uint32_t)u);
   return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>(v), 0, (int)0xfffffff0u, 0x00027000);
 }
-constexpr uint32_t kNowhere = 0xfffffff0u;
 #endif
 
 // How the products are summed: FP8 instructions with the scales by multiplication or as their own, or bf16 instructions (f8_wide_sums).
@@ -346,39 +345,36 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
     const uint32_t size = bf16 ? 2 : 4, ld = (uint32_t)ld_y * size;
     char* const base = whole ? static_cast<char*>(a.Y) : reinterpret_cast<char*>(a.partial + (int64_t)part_no * a.rows * N);
     char* const y = base + ((int64_t)row0 * ld_y) * size;  // 256 rows are below 4 GB, checked by the host
-    const bool wide = (reinterpret_cast<uintptr_t>(base) | ld) % 16 == 0 && g * 64 + 64 <= N;
-    const __amdgpu_buffer_rsrc_t ry = buffer(y);
-    auto col_of = [](int j) { return 32 * (j >> 3) + (j & 7); };
 #pragma unroll
     for (int mi = 0; mi < MI; ++mi) {
       const int m = wm * (BM / 2) + 16 * mi + (lane & 15);
-      const uint32_t o = m < nrows ? (uint32_t)m * ld + (uint32_t)n0 * size : kNowhere;
-      float v[16];
+      if (m >= nrows) continue;
 #pragma unroll
-      for (int j = 0; j < 16; ++j) v[j] = acc[mi][j >> 2][j & 3] + bias[j];
-      if (wide) {
+      for (int h = 0; h < 2; ++h) {
+        const int n = n0 + 32 * h, left = N - n;
+        char* const o = y + ((uint32_t)m * ld + (uint32_t)n * size);
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = acc[mi][2 * h + (j >> 2)][j & 3] + bias[8 * h + j];
         if (bf16) {
+          const u4 w = {to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3]), to_bf16x2(v[4], v[5]), to_bf16x2(v[6], v[7])};
+          if (left >= 8) {
+            *reinterpret_cast<u4_any*>(o) = w;
+          } else {
 #pragma unroll
-          for (int q = 0; q < 2; ++q) {
-            u4 w;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = to_bf16x2(v[8 * q + 2 * j], v[8 * q + 2 * j + 1]);
-            __builtin_amdgcn_raw_buffer_store_b128(w, ry, m < nrows ? o + 64 * q : kNowhere, 0, 0);
+            for (int j = 0; j < 8; ++j)
+              if (j < left) reinterpret_cast<uint16_t*>(o)[j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
           }
+        } else if (left >= 8) {
+#pragma unroll
+          for (int q = 0; q < 2; ++q)
+            reinterpret_cast<u4_any*>(o)[q] =
+                u4{__float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]), __float_as_uint(v[4 * q + 2]), __float_as_uint(v[4 * q + 3])};
         } else {
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const u4 w = {__float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]), __float_as_uint(v[4 * q + 2]), __float_as_uint(v[4 * q + 3])};
-            __builtin_amdgcn_raw_buffer_store_b128(w, ry, m < nrows ? o + 128 * (q >> 1) + 16 * (q & 1) : kNowhere, 0, 0);
-          }
+          for (int j = 0; j < 8; ++j)
+            if (j < left) reinterpret_cast<float*>(o)[j] = v[j];
         }
-      } else if (bf16) {
-#pragma unroll
-        for (int j = 0; j < 16; ++j) __builtin_amdgcn_raw_buffer_store_b16(to_bf16(v[j]), ry, m < nrows && n0 + col_of(j) < N ? o + 2 * col_of(j) : kNowhere, 0, 0);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 16; ++j)
-          __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[j]), ry, m < nrows && n0 + col_of(j) < N ? o + 4 * col_of(j) : kNowhere, 0, 0);
       }
     }
   } else {
@@ -430,7 +426,7 @@ __global__ __launch_bounds__(256) void k_f8_widen(const uint8_t* codes, int64_t 
 
 // Y = sum of the parts, in order.  A thread has 4 columns of a row.
 template <int PARTS>
-__global__ __launch_bounds__(256) void k_f8_join(StampF8Gemm a, int wide) {
+__global__ __launch_bounds__(256) void k_f8_join(StampF8Gemm a) {
   const int N = a.groups * 64, per = (a.N + 3) / 4;
   const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x, m = u / per;
   const int c = (int)(u - m * per) * 4;
@@ -445,8 +441,8 @@ __global__ __launch_bounds__(256) void k_f8_join(StampF8Gemm a, int wide) {
   for (int i = 1; i < PARTS; ++i) s += v[i];
   if (a.y_bf16) {
     uint16_t* y = static_cast<uint16_t*>(a.Y) + m * a.ld_y + c;
-    if (wide && c + 4 <= a.N) {
-      *reinterpret_cast<u2*>(y) = u2{to_bf16x2(s[0], s[1]), to_bf16x2(s[2], s[3])};
+    if (c + 4 <= a.N) {
+      *reinterpret_cast<u2_any*>(y) = u2{to_bf16x2(s[0], s[1]), to_bf16x2(s[2], s[3])};
     } else {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
@@ -454,8 +450,8 @@ __global__ __launch_bounds__(256) void k_f8_join(StampF8Gemm a, int wide) {
     }
   } else {
     float* y = static_cast<float*>(a.Y) + m * a.ld_y + c;
-    if (wide && c + 4 <= a.N) {
-      *reinterpret_cast<f4*>(y) = s;
+    if (c + 4 <= a.N) {
+      *reinterpret_cast<f4_any*>(y) = s;
     } else {
 #pragma unroll
       for (int j = 0; j < 4; ++j)
@@ -480,7 +476,6 @@ hipError_t go(const StampF8Gemm& a, int parts, hipStream_t st) {
   }
   if (parts > 1) {
     const int64_t n = (int64_t)a.rows * ((a.N + 3) / 4);
-    const int wide = (reinterpret_cast<uintptr_t>(a.Y) | (uintptr_t)(a.ld_y * (a.y_bf16 ? 2 : 4))) % (a.y_bf16 ? 8 : 16) == 0;
     static_assert(kF8MaxParts == 8, "a kernel for every number of parts");
     auto* const join = parts == 2   ? k_f8_join<2>
                        : parts == 3 ? k_f8_join<3>
@@ -489,7 +484,7 @@ hipError_t go(const StampF8Gemm& a, int parts, hipStream_t st) {
                        : parts == 6 ? k_f8_join<6>
                        : parts == 7 ? k_f8_join<7>
                                     : k_f8_join<8>;
-    join<<<(uint32_t)((n + 255) / 256), 256, 0, st>>>(a, wide);
+    join<<<(uint32_t)((n + 255) / 256), 256, 0, st>>>(a);
   }
   return hipGetLastError();
 }

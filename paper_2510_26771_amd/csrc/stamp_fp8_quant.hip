@@ -6,7 +6,7 @@ using namespace f8;
 
 // A thread has 16 channels, 8 lanes a block.  Bound by memory: 2 (4) bytes read, 1.03 written per element.
 template <bool BF16, bool WIDE>
-__global__ __launch_bounds__(256) void k_f8_quant(const void* X, int64_t ld_x, int rows, int d, int Kp, int pow2, int aligned, uint8_t* codes, float* scales,
+__global__ __launch_bounds__(256) void k_f8_quant(const void* X, int64_t ld_x, int rows, int d, int Kp, int pow2, uint8_t* codes, float* scales,
                                                   int64_t ld_s) {
   const int per = Kp >> 4;
   const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -14,7 +14,7 @@ __global__ __launch_bounds__(256) void k_f8_quant(const void* X, int64_t ld_x, i
   const int c = (int)(u - m * per) * 16;
   if (m >= rows) return;  // whole groups of 8 lanes: per is a multiple of 8
   Raw16<BF16> x;
-  x.load(static_cast<const char*>(X) + m * ld_x * (BF16 ? 2 : 4), c, d, aligned);
+  x.load(static_cast<const char*>(X) + m * ld_x * (BF16 ? 2 : 4), c, d);
   float scale, inv;
   scale_of(max8(x.amax()), pow2, &scale, &inv);
   const u4 o = x.codes(inv);
@@ -100,11 +100,10 @@ __global__ __launch_bounds__(256) void k_f8_check_pow2(const float* s, int64_t n
 
 hipError_t stamp_launch_f8_quant(const void* X, int x_bf16, int64_t ld_x, int rows, int d, int pow2, int wide, uint8_t* codes, float* scales, int64_t ld_s,
                                  hipStream_t st) {
-  const int Kp = (d + 127) / 128 * 128, size = x_bf16 ? 2 : 4;
-  const int aligned = reinterpret_cast<uintptr_t>(X) % 16 == 0 && ld_x * size % 16 == 0;
+  const int Kp = (d + 127) / 128 * 128;
   const uint32_t blocks = (uint32_t)(((int64_t)rows * (Kp / 16) + 255) / 256);
   auto* kernel = x_bf16 ? (wide ? k_f8_quant<true, true> : k_f8_quant<true, false>) : (wide ? k_f8_quant<false, true> : k_f8_quant<false, false>);
-  kernel<<<blocks, 256, 0, st>>>(X, ld_x, rows, d, Kp, pow2, aligned, codes, scales, ld_s);
+  kernel<<<blocks, 256, 0, st>>>(X, ld_x, rows, d, Kp, pow2, codes, scales, ld_s);
   return hipGetLastError();
 }
 

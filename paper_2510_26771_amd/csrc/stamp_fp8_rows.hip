@@ -136,8 +136,8 @@ __global__ __launch_bounds__(kWaves * 64, IN == kCodes ? 2 : 4) void k_f8_rows(S
         };
         Raw16<IN == kBf16> x0, x1;
         const bool two = t + kWaves * 64 < units;
-        if (t < units) x0.load(row_of(t), t % per * 16, a.d, a.aligned);
-        if (two) x1.load(row_of(t + kWaves * 64), (t + kWaves * 64) % per * 16, a.d, a.aligned);
+        if (t < units) x0.load(row_of(t), t % per * 16, a.d);
+        if (two) x1.load(row_of(t + kWaves * 64), (t + kWaves * 64) % per * 16, a.d);
         if (kb0 < kb1) {
 #pragma unroll
           for (int u = 0; u < U; ++u) fetch(s[u], min(kb0 + u, kb1 - 1));
@@ -146,7 +146,7 @@ __global__ __launch_bounds__(kWaves * 64, IN == kCodes ? 2 : 4) void k_f8_rows(S
         if (t < units) make(t, x0);
         if (two) make(t + kWaves * 64, x1);
         for (int u = t + 2 * kWaves * 64; u < units; u += kWaves * 64) {
-          x0.load(row_of(u), u % per * 16, a.d, a.aligned);
+          x0.load(row_of(u), u % per * 16, a.d);
           make(u, x0);
         }
         __syncthreads();

@@ -12,7 +12,7 @@ struct RouteArgs {
   stamp_routing_t r;
   const void* logits;
   int64_t ld;
-  int32_t renorm, aligned;  // rows of logits on the 16-byte grid
+  int32_t renorm;
   int32_t per_block;   // tokens of a workgroup
   uint16_t* hist;      // [workgroups][experts, an even number] rows that a workgroup's tokens give an expert
 };
@@ -73,10 +73,10 @@ __device__ void top_tokens(const RouteArgs& a, int tok0, int tok1, int wave, int
     constexpr int kSize = BF16 ? 2 : 4, kWords = NV * kSize / 16;
     const char* const row = static_cast<const char*>(a.logits) + ((int64_t)(in ? t : tok0) * a.ld + l0 * NV) * kSize;
     uint32_t raw[NV];  // the logits as fp32
-    if (kWords > 0 && a.aligned && (l0 + 1) * NV <= E) {
+    if (kWords > 0 && (l0 + 1) * NV <= E) {
 #pragma unroll
       for (int w = 0; w < kWords; ++w) {
-        const u4 v = reinterpret_cast<const u4*>(row)[w];
+        const u4 v = reinterpret_cast<const u4_any*>(row)[w];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           if constexpr (BF16) raw[8 * w + 2 * i] = v[i] << 16, raw[8 * w + 2 * i + 1] = v[i] & 0xffff0000u;
@@ -309,7 +309,7 @@ int tokens_per_block(int tokens, int experts) {
 
 // Y[t] = sum of a token's rows times their weights, slots in order.  A thread has 8 columns.
 template <bool BF16>
-__global__ __launch_bounds__(256) void k_combine(stamp_routing_t r, const void* rows, int64_t ld_rows, int nrows, void* Y, int64_t ld_y, int d, int wide) {
+__global__ __launch_bounds__(256) void k_combine(stamp_routing_t r, const void* rows, int64_t ld_rows, int nrows, void* Y, int64_t ld_y, int d) {
   const int per = (d + 7) / 8;
   const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int64_t t = u / per;
@@ -359,8 +359,8 @@ __global__ __launch_bounds__(256) void k_combine(stamp_routing_t r, const void* 
   const int64_t o = t * ld_y + c;
   if constexpr (BF16) {
     uint16_t* p = static_cast<uint16_t*>(Y) + o;
-    if (wide && c + 8 <= d) {
-      *reinterpret_cast<u4*>(p) = u4{to_bf16x2(y[0], y[1]), to_bf16x2(y[2], y[3]), to_bf16x2(y[4], y[5]), to_bf16x2(y[6], y[7])};
+    if (c + 8 <= d) {
+      *reinterpret_cast<u4_any*>(p) = u4{to_bf16x2(y[0], y[1]), to_bf16x2(y[2], y[3]), to_bf16x2(y[4], y[5]), to_bf16x2(y[6], y[7])};
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
@@ -368,9 +368,14 @@ __global__ __launch_bounds__(256) void k_combine(stamp_routing_t r, const void* 
     }
   } else {
     float* p = static_cast<float*>(Y) + o;
+    if (c + 8 <= d) {
+      reinterpret_cast<f4_any*>(p)[0] = f4{y[0], y[1], y[2], y[3]};
+      reinterpret_cast<f4_any*>(p)[1] = f4{y[4], y[5], y[6], y[7]};
+    } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (c + i < d) p[i] = y[i];
+      for (int i = 0; i < 8; ++i)
+        if (c + i < d) p[i] = y[i];
+    }
   }
 }
 }  // namespace
@@ -387,7 +392,6 @@ hipError_t stamp_launch_route(const stamp_routing_t& r, const void* logits, int 
   a.logits = logits;
   a.ld = ld;
   a.renorm = renorm;
-  a.aligned = (reinterpret_cast<uintptr_t>(logits) | (uintptr_t)(ld * (bf16 ? 2 : 4))) % 16 == 0;
   a.per_block = tokens_per_block(r.tokens, r.experts);
   a.hist = static_cast<uint16_t*>(ws);
   const int nb = (r.tokens + a.per_block - 1) / a.per_block;
@@ -405,8 +409,7 @@ hipError_t stamp_launch_route(const stamp_routing_t& r, const void* logits, int 
 hipError_t stamp_launch_combine(const stamp_routing_t& r, const void* rows, int y_bf16, int64_t ld_rows, int nrows, void* Y, int64_t ld_y, int d,
                                 hipStream_t st) {
   const int64_t blocks = ((int64_t)r.tokens * ((d + 7) / 8) + 255) / 256;
-  const int wide = (reinterpret_cast<uintptr_t>(Y) | (uintptr_t)(ld_y * (y_bf16 ? 2 : 4))) % 16 == 0;
-  if (y_bf16) k_combine<true><<<(uint32_t)blocks, 256, 0, st>>>(r, rows, ld_rows, nrows, Y, ld_y, d, wide);
-  else k_combine<false><<<(uint32_t)blocks, 256, 0, st>>>(r, rows, ld_rows, nrows, Y, ld_y, d, wide);
+  if (y_bf16) k_combine<true><<<(uint32_t)blocks, 256, 0, st>>>(r, rows, ld_rows, nrows, Y, ld_y, d);
+  else k_combine<false><<<(uint32_t)blocks, 256, 0, st>>>(r, rows, ld_rows, nrows, Y, ld_y, d);
   return hipGetLastError();
 }
