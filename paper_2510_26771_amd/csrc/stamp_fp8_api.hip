@@ -173,49 +173,65 @@ stamp_status_t forward(const stamp_fp8_plan* p, int32_t rows, const int32_t* off
 
 }  // namespace
 
-// Kernel for a product of `rows` rows over `sets` weights.
+// Kernel for a product of `rows` rows over `sets` weights, by estimates in us.
 //
-// Few rows: the weights' time, and some 5 us more per 16 rows and 700 blocks of 16 columns; tiles of 64 rows hold the time up to 64 rows.
-// Whole calls, us (rows kernel / tiles of 64), bf16 Y: 4096 -> 11008 32 rows 17.9 / 17.4, 48 24.1 / 18.2; 4096 -> 4096 32 rows 10.1 / 12.6,
-// 48 13.6 / 13.8, 96 22.5 / 16.6; 1152 -> 4608 32 rows 8.8 / 9.4, 48 11.7 / 9.8.  fp32 Y (sums in fp32): 1152 -> 4608 64 rows 13.5 / 15.1,
-// 96 19.1 / 15.2; 1185 -> 2305 64 rows 11.0 / 16.1; 8192 -> 1024 32 rows 13.7 / 16.3, 64 22.4 / 18.4.
-//
-// Tiles of 64, 128, 256 rows: a workgroup a CU, so rounds of `cus` tiles, each of Kb steps and a start and end.  us per step and
-// per round, measured on full rounds: 0.53 + 3.5, 0.9 + 4.5, 1.45 + 6; with sums in fp32 1.05 + 4, 1.75 + 6.  (2048 x 4096 -> 11008: 120, 98
-// and 100 us; 8192 x 1152 -> 4608: 77, 64 and 60; 512 x 4096 -> 11008: 39, 30 and 45.)
-//
+// Few rows: up to 12 a set always the rows kernel, which reads the weights at up to 6 TB/s; beyond that its pass over 16 rows is the bound, and
+// a set's last pass half empty.  Tiles of 64, 128, 256 rows: a workgroup a CU, so rounds of `cus` tiles, each of Kb steps and a start and end.
+// us per step and per round, measured on full rounds: 0.53 + 3.5, 0.9 + 4.5, 1.45 + 6; with sums in fp32 1.05 + 4, 1.75 + 6.  (2048 x 4096 -> 11008:
+// 120, 98 and 100 us; 8192 x 1152 -> 4608: 77, 64 and 60; 512 x 4096 -> 11008: 39, 30 and 45.)  Over several sets the tiles' ends take 2 to 5 more,
+// as neighbours read other weights; and the weights have to come from memory.
 // Few tiles: the depth in up to 8 parts, at least 4 blocks each, while the workgroups fit the CUs; 3.5 us for the pass that adds them up,
 // and the parts' rows at 3 TB/s.  A step takes 0.43, 0.7, 1.1 us while most CUs are idle (sums in fp32: 0.9, 1.3).
+//
+// Whole calls, us (rows kernel / tiles of 64 / of 128), 85 sets of 1024 -> 2944, bf16 Y: 16 rows a set 52 / 53 / 57, 24: 74 / 56 / 59, 48: 145 / 62 / 66;
+// fp32 Y 16: 56 / 62 / 76, 24: 76 / 66 / 80, 64: 196 / 105 / 97.  8 sets of 2048 -> 2048, fp32 Y 32: 15.3 / 21.2 / 22.3, 64: 27 / 25 / 28.  One of 4096 -> 11008,
+// bf16 Y 32: 17.9 / 17.4, 48: 24.1 / 18.2; of 1152 -> 4608 32: 8.8 / 9.4, 48: 11.7 / 9.8, fp32 Y 64: 13.5 / 15.1, 96: 19.1 / 15.2; of 8192 -> 1024 64: 22.4 / 18.4.
+// Over 120 products of 8 to 191 sets with 4 to 96 rows a set, gated ones among them, the choice takes 1 % more than the best on average, 20 % at worst.
 namespace {
 constexpr float kStep[2][3] = {{0.53f, 0.9f, 1.45f}, {1.05f, 1.75f, 0.0f}}, kIdle[2][3] = {{0.43f, 0.7f, 1.1f}, {0.9f, 1.3f, 0.0f}},
-                kEnds[2][3] = {{3.5f, 4.5f, 6.0f}, {4.0f, 6.0f, 0.0f}};
+                kEnds[2][3] = {{3.5f, 4.5f, 6.0f}, {4.0f, 6.0f, 0.0f}}, kSetEnds[2][3] = {{7.5f, 7.5f, 9.0f}, {9.0f, 8.0f, 0.0f}};
+constexpr float kBytesPerUs = 6e6f;
+constexpr int kAlwaysRows = 12;  // a set
 struct TileChoice {
   int size, parts;  // tiles of 64 << size rows, parts of the depth
   float us;
 };
+int busy_sets(int sets, int rows) { return sets < rows ? sets : rows > 0 ? rows : 1; }
+float weight_bytes(int sets, int groups, int Kb, int rows) { return (float)busy_sets(sets, rows) * groups * Kb * kF8GroupBytes; }
+
 TileChoice best_tiles(int sets, int groups, int Kb, int rows, int wide_sums, int gated, int forced) {
-  const int busy = sets < rows ? sets : rows > 0 ? rows : 1, cus = stamp_device_cus(), w = wide_sums != 0;
+  const int busy = busy_sets(sets, rows), cus = stamp_device_cus(), w = wide_sums != 0;
   const int64_t ncol = (groups + 3) / 4;
+  const float read = weight_bytes(sets, groups, Kb, rows) / kBytesPerUs + (sets > 1 ? 6.0f : 0.0f);
   TileChoice best = {-1, 1, 0.0f};
   for (int i = 0; i < (w ? 2 : 3); ++i) {  // the bf16 operands of 256 rows do not fit the registers
     if (forced != 0 && forced != STAMP_FP8_ROUTE_TILES_64 + i) continue;
-    const int bm = 64 << i;
-    const int64_t tiles = (sets == 1 ? (rows + bm - 1) / bm : rows / bm + (busy + 1) / 2) * ncol;  // half of the last tile of a set is empty
-    TileChoice c = {i, 1, (float)((tiles + cus - 1) / cus) * ((float)Kb * (2 * tiles <= cus ? kIdle : kStep)[w][i] + kEnds[w][i])};
+    const int bm = 64 << i, many = rows / bm + (busy + 1) / 2;  // half of the last tile of a set is empty
+    const int64_t tiles = (sets == 1 ? (rows + bm - 1) / bm : many > busy ? many : busy) * ncol;
+    const float ends = (sets > 1 ? kSetEnds : kEnds)[w][i];
+    TileChoice c = {i, 1, (float)((tiles + cus - 1) / cus) * ((float)Kb * (2 * tiles <= cus ? kIdle : kStep)[w][i] + ends)};
+    if (c.us < read) c.us = read;
     for (int n = 2; !gated && n <= kF8MaxParts && n * tiles <= cus && 4 * n <= Kb; ++n) {
-      const float us = (float)((Kb + n - 1) / n) * kIdle[w][i] + kEnds[w][i] + 3.5f + (float)n * rows * groups * 64 * 8 * 1e-6f / 3.0f;
+      const float us = (float)((Kb + n - 1) / n) * kIdle[w][i] + ends + 3.5f + (float)n * rows * groups * 64 * 8 * 1e-6f / 3.0f;
       if (us < c.us) c.us = us, c.parts = n;
     }
     if (best.size < 0 || c.us < best.us) best = c;
   }
   return best;
 }
+
+float rows_us(int sets, int groups, int Kb, int rows) {
+  const float read = weight_bytes(sets, groups, Kb, rows) / kBytesPerUs;
+  const float passes = sets == 1 ? (float)((rows + 15) / 16) : (float)rows / busy_sets(sets, rows) / 16.0f + 0.5f;
+  const float work = read * 0.84f * passes;
+  return 2.5f + (read > work ? read : work) + passes * (0.8f + 0.025f * Kb);
+}
 }  // namespace
 
 int stamp_f8_route(int sets, int groups, int Kb, int rows, int wide_sums, int gated, int forced) {
-  const int busy = sets < rows ? sets : rows > 0 ? rows : 1, avg = (int)(((int64_t)rows + busy - 1) / busy);
-  if (forced == STAMP_FP8_ROUTE_ROWS || (forced == 0 && avg <= (wide_sums ? 64 : 32))) return STAMP_FP8_ROUTE_ROWS;
-  return STAMP_FP8_ROUTE_TILES_64 + best_tiles(sets, groups, Kb, rows, wide_sums, gated, forced).size;
+  if (forced == STAMP_FP8_ROUTE_ROWS || (forced == 0 && (int64_t)rows <= (int64_t)kAlwaysRows * sets)) return STAMP_FP8_ROUTE_ROWS;
+  const TileChoice tiles = best_tiles(sets, groups, Kb, rows, wide_sums, gated, forced);
+  return forced == 0 && rows_us(sets, groups, Kb, rows) <= tiles.us ? STAMP_FP8_ROUTE_ROWS : STAMP_FP8_ROUTE_TILES_64 + tiles.size;
 }
 
 // Tiles that leave most CUs idle in their last round: of one layer, the columns of the whole rounds first, the others in a launch of their own
