@@ -4,7 +4,8 @@
 namespace {
 using namespace f8;
 
-// A thread has 16 channels, 8 lanes a block.  Bound by memory: 2 (4) bytes read, 1.03 written per element.
+// A thread has 16 channels, 8 lanes a block: the largest magnitude takes three steps over lanes, and loads and stores are 16 bytes.  Bound by memory:
+// 2 (4) bytes read, 1.03 written per element (2.03 as bf16).  32768 x 4096 from bf16 66 us, 6.1 TB/s; 1 to 100 rows 3 to 5 us, the launch.
 template <bool BF16, bool WIDE>
 __global__ __launch_bounds__(256) void k_f8_quant(const void* X, int64_t ld_x, int rows, int d, int Kp, int pow2, uint8_t* codes, float* scales,
                                                   int64_t ld_s) {

@@ -4,6 +4,8 @@
 // blocks of 16 places and a part of the depth, and reads its operand straight into registers in runs of 1 KB; the parts of the depth
 // are summed in LDS in a fixed order.  Always on the bf16 matrix instructions (f8_wide_sums): the pipe is idle most of the time.
 //
+// 1 x 4096 -> 11008: 9.9 us, 4.5 TB/s of weights; 96 rows over 27 of 32 experts, 4096 -> 1536: 27 us, 6.2 TB/s.
+//
 // Few rows the kernel quantizes itself, into LDS: X is asked for first, then the weights, and the codes are made while those are on their
 // way (loads return in order).  Every workgroup does that again for its rows; a launch of its own is saved (2.6 us for one row, more than a
 // quarter of the product).

@@ -57,6 +57,7 @@ __device__ __forceinline__ float sum_lanes(float v) {
 // LANES lanes have a token, lane l of them experts NV l + j: 4 tokens a wave up to 256 experts (the vector ALU is the bound, and the
 // steps over lanes cost the same for 1 and for 4 tokens).  The largest key, of the lowest expert, is taken top_k times.  A bf16 logit's key
 // has 16 bits: with the expert below it in one word the largest word is the choice, and no two are equal.
+// 32768 tokens, 8 of 256 experts: 18 us (the logits alone 3); 64 tokens, 6 of 64, with the sort in the same workgroup 6.5.
 // slot_id: where not nullptr, the ids go there as well.
 template <int W, int LANES, int NV, bool BF16>
 __device__ void top_tokens(const RouteArgs& a, int tok0, int tok1, int wave, int lane, uint32_t* count, int* slot_id) {
@@ -257,6 +258,8 @@ __global__ __launch_bounds__(kTopWaves * 64) void k_route_top(RouteArgs a) {
   }
 }
 
+// Rows of several workgroups' tokens: each adds up the counts of all (integers, in any order) and places its own.  32768 tokens, 8 of 256 experts: 9.7 us,
+// the counts' two trips through the L2s.
 __global__ __launch_bounds__(kPlaceWaves * 64) void k_route_place(RouteArgs a) {
   __shared__ uint32_t cnt[kPlaceWaves][kF8MaxExperts];
   __shared__ uint32_t total[kF8MaxExperts], base[kF8MaxExperts], mine[kF8MaxExperts];
@@ -307,7 +310,8 @@ int tokens_per_block(int tokens, int experts) {
   return per < once ? once : per;
 }
 
-// Y[t] = sum of a token's rows times their weights, slots in order.  A thread has 8 columns.
+// Y[t] = sum of a token's rows times their weights, slots in order.  A thread has 8 columns and 8 rows in flight.  Bound by memory: 8192 tokens of
+// 4096 columns, 8 rows each, bf16: 122 us, 5 TB/s.
 template <bool BF16>
 __global__ __launch_bounds__(256) void k_combine(stamp_routing_t r, const void* rows, int64_t ld_rows, int nrows, void* Y, int64_t ld_y, int d) {
   const int per = (d + 7) / 8;
