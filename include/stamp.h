@@ -442,7 +442,7 @@ stamp_status_t stamp_experts_forward(const stamp_fp8_plan_t* up, const stamp_fp8
  * Synchronizes the device. */
 stamp_status_t stamp_fp8_debug_weight_codes(const stamp_fp8_plan_t* plan, uint8_t* codes_host, float* scales_host);
 
-/* Which kernel a call with that many rows runs: 0 for a NULL plan, else one of these. */
+/* Which kernel a call with that many rows runs: 0 for a NULL plan, else one of these (of columns in two launches: what one would take). */
 typedef enum {
   STAMP_FP8_ROUTE_ROWS = 1,      /* few rows (on average per expert): weights streamed past them */
   STAMP_FP8_ROUTE_TILES_64 = 2,  /* tiles of 64 rows x 256 columns */
