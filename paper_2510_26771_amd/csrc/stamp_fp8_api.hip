@@ -185,8 +185,10 @@ stamp_status_t forward(const stamp_fp8_plan* p, int32_t rows, const int32_t* off
 //
 // Whole calls, us (rows kernel / tiles of 64 / of 128), 85 sets of 1024 -> 2944, bf16 Y: 16 rows a set 52 / 53 / 57, 24: 74 / 56 / 59, 48: 145 / 62 / 66;
 // fp32 Y 16: 56 / 62 / 76, 24: 76 / 66 / 80, 64: 196 / 105 / 97.  8 sets of 2048 -> 2048, fp32 Y 32: 15.3 / 21.2 / 22.3, 64: 27 / 25 / 28.  One of 4096 -> 11008,
-// bf16 Y 32: 17.9 / 17.4, 48: 24.1 / 18.2; of 1152 -> 4608 32: 8.8 / 9.4, 48: 11.7 / 9.8, fp32 Y 64: 13.5 / 15.1, 96: 19.1 / 15.2; of 8192 -> 1024 64: 22.4 / 18.4.
-// Over 120 products of 8 to 191 sets with 4 to 96 rows a set, gated ones among them, the choice takes 1 % more than the best on average, 20 % at worst.
+// bf16 Y 32: 17.9 / 17.4, 48: 24.1 / 18.2; of 1152 -> 4608 32: 8.8 / 9.4, 48: 11.7 / 9.8, fp32 Y 64: 13.5 / 15.1, 96: 19.1 / 15.2; of 8192 -> 1024 64: 22.4 / 18.4;
+// of 590 -> 7231 58: 11.2 / 13.2.  Over 88 layers of 13 to 16000 rows, 100 to 9000 channels and 100 to 15000 columns the choice takes 0.3 % more than the
+// best on average, 6 % at worst.
+// Over 120 products of 8 to 191 sets with 4 to 96 rows a set, gated ones among them, the choice takes 0.6 % more than the best on average, 17 % at worst.
 namespace {
 constexpr float kStep[2][3] = {{0.53f, 0.9f, 1.45f}, {1.05f, 1.75f, 0.0f}}, kIdle[2][3] = {{0.43f, 0.7f, 1.1f}, {0.9f, 1.3f, 0.0f}},
                 kEnds[2][3] = {{3.5f, 4.5f, 6.0f}, {4.0f, 6.0f, 0.0f}}, kSetEnds[2][3] = {{7.5f, 7.5f, 9.0f}, {9.0f, 8.0f, 0.0f}};
@@ -202,7 +204,7 @@ float weight_bytes(int sets, int groups, int Kb, int rows) { return (float)busy_
 TileChoice best_tiles(int sets, int groups, int Kb, int rows, int wide_sums, int gated, int forced) {
   const int busy = busy_sets(sets, rows), cus = stamp_device_cus(), w = wide_sums != 0;
   const int64_t ncol = (groups + 3) / 4;
-  const float read = weight_bytes(sets, groups, Kb, rows) / kBytesPerUs + (sets > 1 ? 6.0f : 0.0f);
+  const float read = weight_bytes(sets, groups, Kb, rows) / kBytesPerUs;
   TileChoice best = {-1, 1, 0.0f};
   for (int i = 0; i < (w ? 2 : 3); ++i) {  // the bf16 operands of 256 rows do not fit the registers
     if (forced != 0 && forced != STAMP_FP8_ROUTE_TILES_64 + i) continue;
@@ -210,9 +212,11 @@ TileChoice best_tiles(int sets, int groups, int Kb, int rows, int wide_sums, int
     const int64_t tiles = (sets == 1 ? (rows + bm - 1) / bm : many > busy ? many : busy) * ncol;
     const float ends = (sets > 1 ? kSetEnds : kEnds)[w][i];
     TileChoice c = {i, 1, (float)((tiles + cus - 1) / cus) * ((float)Kb * (2 * tiles <= cus ? kIdle : kStep)[w][i] + ends)};
-    if (c.us < read) c.us = read;
+    const float least = read + (sets > 1 ? 6.0f : ends);  // the weights' way from memory
+    if (c.us < least) c.us = least;
     for (int n = 2; !gated && n <= kF8MaxParts && n * tiles <= cus && 4 * n <= Kb; ++n) {
-      const float us = (float)((Kb + n - 1) / n) * kIdle[w][i] + ends + 3.5f + (float)n * rows * groups * 64 * 8 * 1e-6f / 3.0f;
+      const float steps = (float)((Kb + n - 1) / n) * kIdle[w][i] + ends;
+      const float us = (steps > least ? steps : least) + 3.5f + (float)n * rows * groups * 64 * 8 * 1e-6f / 3.0f;
       if (us < c.us) c.us = us, c.parts = n;
     }
     if (best.size < 0 || c.us < best.us) best = c;
@@ -224,7 +228,8 @@ float rows_us(int sets, int groups, int Kb, int rows) {
   const float read = weight_bytes(sets, groups, Kb, rows) / kBytesPerUs;
   const float passes = sets == 1 ? (float)((rows + 15) / 16) : (float)rows / busy_sets(sets, rows) / 16.0f + 0.5f;
   const float work = read * 0.84f * passes;
-  return 2.5f + (read > work ? read : work) + passes * (0.8f + 0.025f * Kb);
+  const float pass = 0.3f + 0.09f * Kb, deep = 0.8f + 0.025f * Kb;  // its own chain of steps
+  return 2.5f + (read > work ? read : work) + passes * (pass < deep ? pass : deep);
 }
 }  // namespace
 
