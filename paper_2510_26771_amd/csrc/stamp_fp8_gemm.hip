@@ -369,35 +369,70 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
     const uint32_t size = bf16 ? 2 : 4, ld = (uint32_t)ld_y * size;
     char* const base = whole ? static_cast<char*>(a.Y) : reinterpret_cast<char*>(a.partial + (int64_t)part_no * a.rows * N);
     char* const y = base + ((int64_t)row0 * ld_y) * size;  // 256 rows are below 4 GB, checked by the host
+    // 8 columns at a time wherever the row begins, element by element in the last 8 only: 4742 x 576 -> 7644 (rows 8 bytes off the grid of 16)
+    // took 108 us with elements throughout, 44 so, and 7680 columns take 43.  bf16 rows that begin between two words are slow to store all the same
+    // (8192 x 1152 -> 4607 79 us, rows 4608 apart 58): there a lane stores its words from the second element on, the last one with the next lane's
+    // first element, and the ends of the wave's 64 columns one by one.
+    const bool between = bf16 && ((reinterpret_cast<uintptr_t>(base) | ld) & 2) != 0 && 64 * g + 64 <= N;
 #pragma unroll
     for (int mi = 0; mi < MI; ++mi) {
       const int m = wm * (BM / 2) + 16 * mi + (lane & 15);
+      char* const o = y + ((uint32_t)m * ld + (uint32_t)n0 * size);
+      float v[16];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) v[j] = acc[mi][j >> 2][j & 3] + bias[j];
+      u4 w[2];
+      if (bf16) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j >> 2][j & 3] = to_bf16x2(v[2 * j], v[2 * j + 1]);
+      }
+      if (between) {
+        // lanes f = 1, 2, 3 give their first word, f = 0 that of the second 32 columns
+        const uint32_t next0 = (uint32_t)__shfl((int)(f == 0 ? w[1][0] : w[0][0]), (lane + 16) & 63);
+        const uint32_t next1 = (uint32_t)__shfl((int)w[1][0], (lane + 16) & 63);
+        if (m >= nrows) continue;
+        const bool odd = (reinterpret_cast<uintptr_t>(o) & 2) != 0;
+        const uint16_t first = (uint16_t)w[0][0], last = (uint16_t)(w[1][3] >> 16);
+        if (odd) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[h][j] = __builtin_amdgcn_alignbit(j < 3 ? w[h][j + 1] : h == 0 ? next0 : next1, w[h][j], 16);
+        }
+        char* const p = o + (odd ? 2 : 0);
+        *reinterpret_cast<u4_any*>(p) = w[0];
+        if (odd && f == 3) {
+          *reinterpret_cast<u2_any*>(p + 64) = u2{w[1][0], w[1][1]};
+          *reinterpret_cast<uint32_t*>(p + 72) = w[1][2];
+          *reinterpret_cast<uint16_t*>(p + 76) = last;
+        } else {
+          *reinterpret_cast<u4_any*>(p + 64) = w[1];
+        }
+        if (odd && f == 0) *reinterpret_cast<uint16_t*>(o) = first;
+        continue;
+      }
       if (m >= nrows) continue;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int n = n0 + 32 * h, left = N - n;
-        char* const o = y + ((uint32_t)m * ld + (uint32_t)n * size);
-        float v[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = acc[mi][2 * h + (j >> 2)][j & 3] + bias[8 * h + j];
+        const int left = N - n0 - 32 * h;
+        char* const p = o + 32 * h * size;
         if (bf16) {
-          const u4 w = {to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3]), to_bf16x2(v[4], v[5]), to_bf16x2(v[6], v[7])};
           if (left >= 8) {
-            *reinterpret_cast<u4_any*>(o) = w;
+            *reinterpret_cast<u4_any*>(p) = w[h];
           } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-              if (j < left) reinterpret_cast<uint16_t*>(o)[j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+              if (j < left) reinterpret_cast<uint16_t*>(p)[j] = (uint16_t)(w[h][j >> 1] >> (16 * (j & 1)));
           }
         } else if (left >= 8) {
 #pragma unroll
           for (int q = 0; q < 2; ++q)
-            reinterpret_cast<u4_any*>(o)[q] =
-                u4{__float_as_uint(v[4 * q]), __float_as_uint(v[4 * q + 1]), __float_as_uint(v[4 * q + 2]), __float_as_uint(v[4 * q + 3])};
+            reinterpret_cast<u4_any*>(p)[q] = u4{__float_as_uint(v[8 * h + 4 * q]), __float_as_uint(v[8 * h + 4 * q + 1]), __float_as_uint(v[8 * h + 4 * q + 2]),
+                                                 __float_as_uint(v[8 * h + 4 * q + 3])};
         } else {
 #pragma unroll
           for (int j = 0; j < 8; ++j)
-            if (j < left) reinterpret_cast<float*>(o)[j] = v[j];
+            if (j < left) reinterpret_cast<float*>(p)[j] = v[8 * h + j];
         }
       }
     }
