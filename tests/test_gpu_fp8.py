@@ -220,6 +220,32 @@ def test_every_kernel_is_reached_by_rule(st):
     plan.destroy()
 
 
+@pytest.mark.parametrize("route", ["rows", "tiles_64", "tiles_128", "tiles_256"])
+@pytest.mark.parametrize("n", [64, 300, 321])
+def test_rows_at_any_place_hold_the_same(st, n, route):
+    """bf16 rows that begin on a word, between two, and on either in turn: the values of rows on the 16-byte grid, and nothing around them."""
+    import torch
+    rng = np.random.default_rng(n)
+    rows, d = 150, 300
+    _, xg = _activations(rng, rows, d, "bf16")
+    w, ws = _weights(rng, (), n, d, 0)
+    plan = st.Fp8Plan(st.Fp8Desc(d_in=d, d_out=n), _gpu(w), _gpu(ws), _gpu(rng.standard_normal(n).astype(np.float32)))
+    plan.set_route(route)
+    workspace = plan.alloc_workspace(rows)
+    want, _ = _strided(rows, n, "bf16", -n % 8)
+    plan.linear_forward(xg, want, workspace)
+    for pad in (0, 1, 2, 3, 7):
+        for offset in (0, 1, 2, 5):
+            X, _ = _strided(rows, d, "bf16", pad, offset)
+            X.copy_(xg)
+            Y, buf = _strided(rows, n, "bf16", pad, offset)
+            plan.linear_forward(X, Y, workspace)
+            assert torch.equal(Y, want), f"{pad} {offset}"
+            Y.fill_(-7.0)
+            assert (buf == -7.0).all(), f"{pad} {offset}: something outside of Y was written"
+    plan.destroy()
+
+
 # tiles of one and a bit rounds: the last columns in a launch of their own, its depth in one piece or in parts
 @pytest.mark.parametrize("rows,d,n,y,pow2", [(3000, 520, 5700, "bf16", 0), (3000, 520, 5700, "f32", 1), (2900, 300, 5643, "bf16", 1), (2900, 300, 5643, "f32", 0),
                                              (324, 4725, 10849, "bf16", 0), (323, 2998, 10965, "f32", 1)])
