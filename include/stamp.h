@@ -424,6 +424,7 @@ typedef struct {
   int32_t* token_of_row_dev;
   int32_t* row_of_slot_dev;
 } stamp_routing_t;
+/* Bytes of workspace (256-byte aligned pointer) for up to `tokens` tokens over that many experts; 0 for sizes out of range. */
 size_t stamp_route_workspace_bytes(int32_t tokens, int32_t experts, int32_t top_k);
 stamp_status_t stamp_route_topk(const stamp_routing_t* routing, const void* logits_dev, int32_t logits_dtype, int64_t ld,
                                 int32_t renormalize, void* workspace_dev, size_t workspace_bytes, void* hip_stream);

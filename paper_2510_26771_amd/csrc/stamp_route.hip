@@ -304,9 +304,9 @@ __global__ __launch_bounds__(kPlaceWaves * 64) void k_route_place(RouteArgs a) {
 
 // Tokens of a workgroup: what its waves take at once, or more where that would be over 256 workgroups (each of which adds up the counts of
 // all).  One workgroup does all in one launch.
+int tokens_at_once(int experts) { return kTopWaves * (experts <= 256 ? 4 : 1); }
 int tokens_per_block(int tokens, int experts) {
-  const int once = kTopWaves * (experts <= 256 ? 4 : 1);
-  const int per = (tokens + kRtMaxBlocks - 1) / kRtMaxBlocks;
+  const int once = tokens_at_once(experts), per = (tokens + kRtMaxBlocks - 1) / kRtMaxBlocks;
   return per < once ? once : per;
 }
 
@@ -384,9 +384,11 @@ __global__ __launch_bounds__(256) void k_combine(stamp_routing_t r, const void* 
 }
 }  // namespace
 
+// The counts of as many workgroups as any call of up to `tokens` tokens has: beyond 256 times the tokens at once a workgroup takes more, and
+// their number falls and rises again.
 size_t stamp_route_ws(int tokens, int experts, int) {
-  const int per = tokens_per_block(tokens, experts);
-  const size_t nb = ((size_t)tokens + per - 1) / per;
+  const int once = tokens_at_once(experts), blocks = (tokens + once - 1) / once;
+  const size_t nb = blocks < kRtMaxBlocks ? blocks : kRtMaxBlocks;
   return (nb * ((size_t)experts + 1) * sizeof(uint16_t) + 255) / 256 * 256 + 256;
 }
 
