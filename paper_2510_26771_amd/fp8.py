@@ -1,7 +1,7 @@
 """8-bit floating point layers with block scales, dense and by expert, the router and the experts' MLP (include/stamp.h).
 
-Like binding.StampPlan: argument checks and marshalling only, no fallback; tensors live on the GPU, calls are asynchronous on the
-given stream (default: torch's current one)."""
+Like binding.StampPlan: argument checks and marshalling only, no fallback; all tensors of a call live on the plan's (the routing's) GPU,
+which is the current one, and calls are asynchronous on the given stream of it (default: torch's current one)."""
 from __future__ import annotations
 
 import ctypes as C
@@ -45,10 +45,17 @@ def _torch_dtype(code):
     return torch.bfloat16 if code == STAMP_BF16 else torch.float32
 
 
-def _matrix(t, name, rows, cols, dtype):
-    """A [rows, cols] GPU tensor of that type whose rows are contiguous; returns the distance of its rows in elements."""
-    if not t.is_cuda or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
-        raise ValueError(f"{name} must be a GPU tensor of shape ({rows}, {cols})")
+def _current(device, stream):
+    """The kernels are launched on the current GPU: the plan has to be there, and the stream."""
+    import torch
+    if torch.cuda.current_device() != device.index or (stream is not None and stream.device != device):
+        raise ValueError(f"{device} must be the current GPU, and the stream one of it")
+
+
+def _matrix(t, name, rows, cols, dtype, device):
+    """A [rows, cols] tensor of that type on that GPU whose rows are contiguous; returns the distance of its rows in elements."""
+    if not t.is_cuda or t.device != device or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        raise ValueError(f"{name} must be a tensor of shape ({rows}, {cols}) on {device}")
     if t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
     if cols > 1 and t.stride(1) != 1:
@@ -56,9 +63,16 @@ def _matrix(t, name, rows, cols, dtype):
     return t.stride(0) if rows > 1 else cols
 
 
-def _flat(t, name, numel, dtype):
-    if not t.is_cuda or t.dtype != dtype or t.numel() != numel or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous GPU tensor of {numel} {dtype}")
+def _flat(t, name, numel, dtype, device):
+    if not t.is_cuda or t.device != device or t.dtype != dtype or t.numel() != numel or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous tensor of {numel} {dtype} on {device}")
+
+
+def _room(t, device):
+    """Bytes of a workspace."""
+    if t is None or not t.is_cuda or t.device != device or not t.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on {device}")
+    return t.numel() * t.element_size()
 
 
 class Fp8Plan:
@@ -77,10 +91,12 @@ class Fp8Plan:
             raise ValueError(f"W is {W.dtype}, the description says otherwise")
         if W.numel() != mats * d.d_in * d.d_out or W.dim() < 2 or tuple(W.shape[-2:]) != ((d.d_out, d.d_in) if d.w_is_out_by_in else (d.d_in, d.d_out)):
             raise ValueError("W's shape is not the description's")
+        self.device = W.device
         if w_scales is not None:
-            _flat(w_scales, "w_scales", mats * -(-d.d_out // BLOCK) * -(-d.d_in // BLOCK), torch.float32)
+            _flat(w_scales, "w_scales", mats * -(-d.d_out // BLOCK) * -(-d.d_in // BLOCK), torch.float32, self.device)
         if bias is not None:
-            _flat(bias, "bias", max(d.experts, 1) * d.d_out, torch.float32)
+            _flat(bias, "bias", max(d.experts, 1) * d.d_out, torch.float32, self.device)
+        _current(self.device, stream)
         _check(self.lib.stamp_fp8_plan_create(C.byref(d.to_c()), _ptr(W), _ptr(w_scales), _ptr(bias), _stream(stream), C.byref(self._h)),
                "stamp_fp8_plan_create")
         self._x_dtype, self._y_dtype = _torch_dtype(d.x_dtype), _torch_dtype(d.y_dtype)
@@ -124,37 +140,48 @@ class Fp8Plan:
     def _act_buffers(self, codes, scales, rows):
         import torch
         kb = -(-self.desc.d_in // BLOCK)
-        _flat(codes, "codes", rows * kb * BLOCK, torch.uint8)
-        if not scales.is_cuda or scales.dtype != torch.float32 or scales.dim() != 2 or scales.shape[0] != kb or not scales.is_contiguous():
-            raise ValueError(f"scales must be a contiguous GPU tensor of {kb} rows of float32")
+        _flat(codes, "codes", rows * kb * BLOCK, torch.uint8, self.device)
+        if (not scales.is_cuda or scales.device != self.device or scales.dtype != torch.float32 or scales.dim() != 2 or scales.shape[0] != kb
+                or not scales.is_contiguous()):
+            raise ValueError(f"scales must be a contiguous tensor of {kb} rows of float32 on {self.device}")
         return scales.shape[1]
 
+    def _x(self, X, rows):
+        return _matrix(X, "X", rows, self.desc.d_in, self._x_dtype, self.device)
+
+    def _y(self, Y, rows):
+        return _matrix(Y, "Y", rows, self.desc.d_out, self._y_dtype, self.device)
+
     def quantize_act(self, X, codes, scales, stream=None):
-        ld = _matrix(X, "X", X.shape[0], self.desc.d_in, self._x_dtype)
+        _current(self.device, stream)
+        ld = self._x(X, X.shape[0])
         lds = self._act_buffers(codes, scales, X.shape[0])
         _check(self.lib.stamp_fp8_quantize_act(self._h, X.shape[0], _ptr(X), ld, _ptr(codes), _ptr(scales), lds, _stream(stream)),
                "stamp_fp8_quantize_act")
 
     def linear_forward(self, X, Y, workspace, stream=None):
+        _current(self.device, stream)
         rows = X.shape[0]
-        ld_x, ld_y = _matrix(X, "X", rows, self.desc.d_in, self._x_dtype), _matrix(Y, "Y", rows, self.desc.d_out, self._y_dtype)
-        _check(self.lib.stamp_fp8_linear_forward(self._h, rows, _ptr(X), ld_x, _ptr(Y), ld_y, _ptr(workspace), workspace.numel(), _stream(stream)),
+        ld_x, ld_y, room = self._x(X, rows), self._y(Y, rows), _room(workspace, self.device)
+        _check(self.lib.stamp_fp8_linear_forward(self._h, rows, _ptr(X), ld_x, _ptr(Y), ld_y, _ptr(workspace), room, _stream(stream)),
                "stamp_fp8_linear_forward")
 
     def linear_forward_q(self, codes, scales, Y, workspace, stream=None):
+        _current(self.device, stream)
         rows = Y.shape[0]
-        lds, ld_y = self._act_buffers(codes, scales, rows), _matrix(Y, "Y", rows, self.desc.d_out, self._y_dtype)
+        lds, ld_y, room = self._act_buffers(codes, scales, rows), self._y(Y, rows), _room(workspace, self.device)
         _check(self.lib.stamp_fp8_linear_forward_q(self._h, rows, _ptr(codes), _ptr(scales), lds, _ptr(Y), ld_y, _ptr(workspace),
-                                                   workspace.numel(), _stream(stream)), "stamp_fp8_linear_forward_q")
+                                                   room, _stream(stream)), "stamp_fp8_linear_forward_q")
 
     def grouped_forward(self, X, offsets, Y, workspace, stream=None):
         """Rows offsets[e] .. offsets[e + 1] - 1 of X times expert e's weights."""
         import torch
+        _current(self.device, stream)
         rows = X.shape[0]
-        ld_x, ld_y = _matrix(X, "X", rows, self.desc.d_in, self._x_dtype), _matrix(Y, "Y", rows, self.desc.d_out, self._y_dtype)
-        _flat(offsets, "offsets", self.desc.experts + 1, torch.int32)
+        ld_x, ld_y, room = self._x(X, rows), self._y(Y, rows), _room(workspace, self.device)
+        _flat(offsets, "offsets", self.desc.experts + 1, torch.int32, self.device)
         _check(self.lib.stamp_fp8_grouped_forward(self._h, rows, _ptr(offsets), _ptr(X), ld_x, _ptr(Y), ld_y, _ptr(workspace),
-                                                  workspace.numel(), _stream(stream)), "stamp_fp8_grouped_forward")
+                                                  room, _stream(stream)), "stamp_fp8_grouped_forward")
 
     def debug_weight_codes(self):
         """Codes (bytes) [experts][2 if gated][d_out][d_in] and scales [..][blocks of d_out][blocks of d_in], on the host."""
@@ -172,6 +199,8 @@ class Routing:
 
     def __init__(self, tokens: int, experts: int, top_k: int, device="cuda"):
         import torch
+        if torch.device(device).type != "cuda":
+            raise ValueError("a routing lives on a GPU")
         self.lib = load_library()
         self.tokens, self.experts, self.top_k = int(tokens), int(experts), int(top_k)
         need = int(self.lib.stamp_route_workspace_bytes(self.tokens, self.experts, self.top_k))
@@ -184,6 +213,7 @@ class Routing:
         self.weights = torch.empty((tokens, top_k), dtype=torch.float32, device=device)
         self.offsets, self.token_of_row = ints(experts + 1), ints(tokens * top_k)
         self.workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        self.device = self.workspace.device
         self._c = _Routing(self.tokens, self.experts, self.top_k, _ptr(self.ids), _ptr(self.weights), _ptr(self.offsets), _ptr(self.token_of_row),
                            _ptr(self.row_of_slot))
 
@@ -193,7 +223,8 @@ def route_topk(logits, routing: Routing, renormalize: bool = True, stream=None):
     import torch
     if logits.dtype not in (torch.float32, torch.bfloat16):
         raise ValueError("logits must be float32 or bfloat16")
-    ld = _matrix(logits, "logits", routing.tokens, routing.experts, logits.dtype)
+    _current(routing.device, stream)
+    ld = _matrix(logits, "logits", routing.tokens, routing.experts, logits.dtype, routing.device)
     _check(routing.lib.stamp_route_topk(C.byref(routing._c), _ptr(logits), STAMP_BF16 if logits.dtype == torch.bfloat16 else STAMP_F32, ld,
                                         int(bool(renormalize)), _ptr(routing.workspace), routing.workspace.numel(), _stream(stream)), "stamp_route_topk")
 
@@ -206,7 +237,9 @@ def experts_workspace(up: Fp8Plan, down: Fp8Plan, tokens: int, top_k: int, devic
 
 def experts_forward(up: Fp8Plan, down: Fp8Plan, X, routing: Routing, Y, workspace, stream=None):
     """The gated MLP of the chosen experts of every token, summed with their weights."""
-    ld_x = _matrix(X, "X", routing.tokens, up.desc.d_in, up._x_dtype)
-    ld_y = _matrix(Y, "Y", routing.tokens, down.desc.d_out, down._y_dtype)
-    _check(up.lib.stamp_experts_forward(up._h, down._h, C.byref(routing._c), _ptr(X), ld_x, _ptr(Y), ld_y, _ptr(workspace), workspace.numel(),
+    _current(up.device, stream)
+    if down.device != up.device or routing.device != up.device:
+        raise ValueError("both plans and the routing must lie on one GPU")
+    ld_x, ld_y, room = up._x(X, routing.tokens), down._y(Y, routing.tokens), _room(workspace, up.device)
+    _check(up.lib.stamp_experts_forward(up._h, down._h, C.byref(routing._c), _ptr(X), ld_x, _ptr(Y), ld_y, _ptr(workspace), room,
                                         _stream(stream)), "stamp_experts_forward")
