@@ -166,7 +166,11 @@ def _check(status: int, where: str):
 
 
 def _ptr(t) -> Optional[int]:
-    return None if t is None else t.data_ptr()
+    if t is None:
+        return None
+    if not t.is_cuda and not t.is_pinned():  # a kernel that follows an address of ordinary host memory faults
+        raise ValueError("a tensor lies on the host: the library has no host path")
+    return t.data_ptr()
 
 
 def _stream(stream) -> Optional[int]:
