@@ -65,7 +65,21 @@ struct StampF8Gemm {
   float* SH;
   int64_t ld_sh;
   float* partial;          // [parts][rows][groups * 64] where the depth is split
+  uint32_t first;          // workgroups of the launches before this one (tiles)
 };
+
+// A launch of 2^32 threads or more is refused: units beyond that many workgroups are taken by further launches.
+constexpr int64_t kF8MaxThreads = (int64_t)1 << 31;
+template <typename F>
+hipError_t f8_launches(int64_t workgroups, int threads, F launch) {
+  const int64_t most = kF8MaxThreads / threads;
+  for (int64_t first = 0; first < workgroups; first += most) {
+    launch(first, (uint32_t)(workgroups - first < most ? workgroups - first : most));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
 
 // stamp_fp8_route_t of a product of `rows` rows over `sets` weights
 int stamp_f8_route(int sets, int groups, int Kb, int rows, int wide_sums, int gated, int forced);

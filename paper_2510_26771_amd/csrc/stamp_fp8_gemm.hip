@@ -68,8 +68,9 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
   constexpr int kXcd = 8, kBand = 8;
   const Tiles tiles = count_tiles(a, BM);
   const int ncol = (a.groups + 3) / 4, nrow = tiles.total, ntile = nrow * ncol, run = (ntile + kXcd - 1) / kXcd;
-  const int order = (int)(blockIdx.x % kXcd) * run + (int)(blockIdx.x / kXcd);
-  if ((int)(blockIdx.x / kXcd) >= run || order >= ntile) return;
+  const uint32_t group = a.first + blockIdx.x;
+  const int order = (int)(group % kXcd) * run + (int)(group / kXcd);
+  if ((int)(group / kXcd) >= run || order >= ntile) return;
   const int band = order / (kBand * ncol), in_band = order - band * kBand * ncol, height = min(kBand, nrow - band * kBand);
   const int col = in_band / height;
   int set, row0, nrows;
@@ -475,8 +476,8 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
 #endif
 }
 
-__global__ __launch_bounds__(256) void k_f8_widen(const uint8_t* codes, int64_t n16, uint8_t* out) {
-  const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x;
+__global__ __launch_bounds__(256) void k_f8_widen(const uint8_t* codes, int64_t n16, uint8_t* out, int64_t first) {
+  const int64_t u = (first + blockIdx.x) * 256 + threadIdx.x;
   if (u >= n16) return;
   const u4 c = reinterpret_cast<const u4*>(codes)[u];
   reinterpret_cast<b8*>(out)[2 * u] = widen8((int)c[0], (int)c[1]);
@@ -522,17 +523,23 @@ __global__ __launch_bounds__(256) void k_f8_join(StampF8Gemm a) {
 template <int BM>
 hipError_t go(const StampF8Gemm& a, int parts, hipStream_t st) {
   const int64_t tiles = a.offsets == nullptr ? ((int64_t)a.rows + BM - 1) / BM : (int64_t)a.rows / BM + (a.sets < a.rows ? a.sets : a.rows);
-  const dim3 grid((uint32_t)((tiles * ((a.groups + 3) / 4) + 7) / 8 * 8), parts);
-  if constexpr (BM == 256) {
-    if (a.wide_sums) return hipErrorInvalidValue;  // its registers do not hold the bf16 operands: never chosen
-    if (a.pow2) k_f8_tiles<BM, kPow2, false><<<grid, 512, 0, st>>>(a);
-    else k_f8_tiles<BM, kScaled, false><<<grid, 512, 0, st>>>(a);
-  } else {
-    if (a.gated) k_f8_tiles<BM, kWide, true><<<grid, 512, 0, st>>>(a);
-    else if (a.wide_sums) k_f8_tiles<BM, kWide, false><<<grid, 512, 0, st>>>(a);
-    else if (a.pow2) k_f8_tiles<BM, kPow2, false><<<grid, 512, 0, st>>>(a);
-    else k_f8_tiles<BM, kScaled, false><<<grid, 512, 0, st>>>(a);
-  }
+  if (BM == 256 && a.wide_sums) return hipErrorInvalidValue;  // its registers do not hold the bf16 operands: never chosen
+  // a launch's first workgroup is a multiple of 8: the XCDs keep their turn
+  const hipError_t e = f8_launches((tiles * ((a.groups + 3) / 4) + 7) / 8 * 8, 512, [&](int64_t first, uint32_t n) {
+    const dim3 grid(n, parts);
+    StampF8Gemm part = a;
+    part.first = (uint32_t)first;
+    if constexpr (BM == 256) {
+      if (a.pow2) k_f8_tiles<BM, kPow2, false><<<grid, 512, 0, st>>>(part);
+      else k_f8_tiles<BM, kScaled, false><<<grid, 512, 0, st>>>(part);
+    } else {
+      if (a.gated) k_f8_tiles<BM, kWide, true><<<grid, 512, 0, st>>>(part);
+      else if (a.wide_sums) k_f8_tiles<BM, kWide, false><<<grid, 512, 0, st>>>(part);
+      else if (a.pow2) k_f8_tiles<BM, kPow2, false><<<grid, 512, 0, st>>>(part);
+      else k_f8_tiles<BM, kScaled, false><<<grid, 512, 0, st>>>(part);
+    }
+  });
+  if (e != hipSuccess) return e;
   if (parts > 1) {
     const int64_t n = (int64_t)a.rows * ((a.N + 3) / 4);
     static_assert(kF8MaxParts == 8, "a kernel for every number of parts");
@@ -550,8 +557,8 @@ hipError_t go(const StampF8Gemm& a, int parts, hipStream_t st) {
 }  // namespace
 
 hipError_t stamp_launch_f8_widen(const uint8_t* codes, int64_t bytes, uint8_t* out, hipStream_t st) {
-  k_f8_widen<<<(uint32_t)((bytes / 16 + 255) / 256), 256, 0, st>>>(codes, bytes / 16, out);
-  return hipGetLastError();
+  return f8_launches((bytes / 16 + 255) / 256, 256,
+                     [&](int64_t first, uint32_t n) { k_f8_widen<<<n, 256, 0, st>>>(codes, bytes / 16, out, first); });
 }
 
 hipError_t stamp_launch_f8_tiles(const StampF8Gemm& a, int bm, int parts, hipStream_t st) {

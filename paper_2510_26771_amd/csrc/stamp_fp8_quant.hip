@@ -8,9 +8,9 @@ using namespace f8;
 // 2 (4) bytes read, 1.03 written per element (2.03 as bf16).  32768 x 4096 from bf16 66 us, 6.1 TB/s; 1 to 100 rows 3 to 5 us, the launch.
 template <bool BF16, bool WIDE>
 __global__ __launch_bounds__(256) void k_f8_quant(const void* X, int64_t ld_x, int rows, int d, int Kp, int pow2, uint8_t* codes, float* scales,
-                                                  int64_t ld_s) {
+                                                  int64_t ld_s, int64_t first) {
   const int per = Kp >> 4;
-  const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t u = (first + blockIdx.x) * 256 + threadIdx.x;
   const int64_t m = u / per;
   const int c = (int)(u - m * per) * 16;
   if (m >= rows) return;  // whole groups of 8 lanes: per is a multiple of 8
@@ -64,8 +64,8 @@ __global__ __launch_bounds__(256) void k_f8_w_scale(float* SW, int64_t n, int po
 
 // one thread per 16 bytes of the operand image; SW: the blocks' largest magnitudes, unless W holds codes
 __global__ __launch_bounds__(256) void k_f8_w_image(const void* W, int dtype, int out_by_in, int N, int d, int nblk, int Kb, int groups, int gated, int pow2,
-                                                    const float* SW, uint8_t* image, int64_t total) {
-  const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x;
+                                                    const float* SW, uint8_t* image, int64_t total, int64_t first) {
+  const int64_t u = (first + blockIdx.x) * 256 + threadIdx.x;
   if (u >= total) return;
   const int lane = (int)(u & 63), h = (int)(u >> 6) & 1, b = (int)(u >> 7) & 3;
   const int64_t gk = u >> 9;
@@ -102,10 +102,10 @@ __global__ __launch_bounds__(256) void k_f8_check_pow2(const float* s, int64_t n
 hipError_t stamp_launch_f8_quant(const void* X, int x_bf16, int64_t ld_x, int rows, int d, int pow2, int wide, uint8_t* codes, float* scales, int64_t ld_s,
                                  hipStream_t st) {
   const int Kp = (d + 127) / 128 * 128;
-  const uint32_t blocks = (uint32_t)(((int64_t)rows * (Kp / 16) + 255) / 256);
   auto* kernel = x_bf16 ? (wide ? k_f8_quant<true, true> : k_f8_quant<true, false>) : (wide ? k_f8_quant<false, true> : k_f8_quant<false, false>);
-  kernel<<<blocks, 256, 0, st>>>(X, ld_x, rows, d, Kp, pow2, codes, scales, ld_s);
-  return hipGetLastError();
+  return f8_launches(((int64_t)rows * (Kp / 16) + 255) / 256, 256, [&](int64_t first, uint32_t n) {
+    kernel<<<n, 256, 0, st>>>(X, ld_x, rows, d, Kp, pow2, codes, scales, ld_s, first);
+  });
 }
 
 hipError_t stamp_launch_f8_weights(stamp_fp8_plan* p, const void* W, const float* w_scales, hipStream_t st, uint32_t* flag) {
@@ -121,8 +121,10 @@ hipError_t stamp_launch_f8_weights(stamp_fp8_plan* p, const void* W, const float
                                                              reinterpret_cast<uint32_t*>(p->sw_dev));
   }
   const int64_t total = (int64_t)p->sets * p->groups * p->Kb * (kF8GroupBytes / 16);
-  k_f8_w_image<<<(uint32_t)((total + 255) / 256), 256, 0, st>>>(W, d.w_dtype, d.w_is_out_by_in, d.d_out, d.d_in, p->nblk, p->Kb, p->groups, d.gated, pow2,
-                                                               p->sw_dev, p->w_dev, total);
+  const hipError_t e = f8_launches((total + 255) / 256, 256, [&](int64_t first, uint32_t n) {
+    k_f8_w_image<<<n, 256, 0, st>>>(W, d.w_dtype, d.w_is_out_by_in, d.d_out, d.d_in, p->nblk, p->Kb, p->groups, d.gated, pow2, p->sw_dev, p->w_dev, total, first);
+  });
+  if (e != hipSuccess) return e;
   if (d.w_dtype != STAMP_E4M3) k_f8_w_scale<<<(uint32_t)((ns + 255) / 256), 256, 0, st>>>(p->sw_dev, ns, pow2);
   return hipGetLastError();
 }

@@ -1,0 +1,123 @@
+"""Calls of the 8-bit floating point layers, the router and the experts at the ends of their ranges, on the GPU."""
+import numpy as np
+import pytest
+
+import fp8_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def st():
+    import paper_2510_26771_amd as st
+    st.load_library()
+    return st
+
+
+def _gpu(a):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def _needs(gib):
+    import torch
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < gib << 30:
+        pytest.skip(f"needs {gib} GiB of free GPU memory")
+
+
+# ---- more units of work than one launch takes (2^32 threads) ----
+
+def test_quantizer_and_widening_of_the_most_rows(st):
+    """2^24 rows of 32 blocks: the first, the last, and the rows on both sides of every 2^31 units of 16 channels."""
+    import torch
+    _needs(214)
+    rows, d = 1 << 24, 3969
+    rng = np.random.default_rng(0)
+    w, ws = rng.integers(0, 120, (1, d), dtype=np.uint8), np.ones((1, 32), np.float32)
+    plan = st.Fp8Plan(st.Fp8Desc(d_in=d, d_out=1, y_dtype=st.STAMP_F32), _gpu(w), _gpu(ws))
+    X = torch.empty((rows, d), dtype=torch.bfloat16, device="cuda")
+    look = torch.tensor([0, 1, (1 << 23) - 1, 1 << 23, (1 << 23) + 1, 12345678, rows - 2, rows - 1], device="cuda")
+    x = torch.from_numpy(rng.standard_normal((look.numel(), d)).astype(np.float32)).to(torch.bfloat16)
+    X[look] = x.cuda()
+    codes, scales = plan.alloc_act_buffers(rows)
+    codes[look] = 0xEE
+    plan.quantize_act(X, codes, scales)
+    want, wscale = ref.quantize(x.float().numpy(), 0)
+    assert np.array_equal(codes[look].cpu().numpy(), want)
+    assert np.array_equal(scales[:, look].cpu().numpy().T, wscale)
+    del X
+    torch.cuda.empty_cache()
+    Y = torch.zeros((rows, 1), device="cuda")
+    assert plan.route(rows) != "rows"  # tiles: the codes are widened first
+    plan.linear_forward_q(codes, scales, Y, plan.alloc_workspace(rows))
+    y, S, G = ref.product(want, wscale, w, ws)
+    assert np.all(np.abs(Y[look].cpu().numpy() - y) <= ref.slack(S, G, d, True) + 2.0 ** -23 * np.abs(y))
+    plan.destroy()
+    del codes, scales, Y
+    torch.cuda.empty_cache()
+
+
+def test_weights_of_64_gib(st):
+    """1024 experts of 8192 x 8192: codes of the first, the last and those in the middle."""
+    import torch
+    _needs(140)
+    E, d, n = 1024, 8192, 8192
+    rng = np.random.default_rng(1)
+    w = torch.empty((E, n, d), dtype=torch.uint8, device="cuda")
+    ws = torch.ones((E, 64, 64), device="cuda")
+    look = [0, 511, 512, E - 1]
+    for e in look:
+        w[e] = torch.from_numpy(rng.integers(0, 120, (1, d), dtype=np.uint8)).cuda()  # every column of an expert alike
+    plan = st.Fp8Plan(st.Fp8Desc(d_in=d, d_out=n, experts=E), w, ws)
+    rows = len(look)
+    x = torch.from_numpy(rng.standard_normal((rows, d)).astype(np.float32)).to(torch.bfloat16)
+    counts = np.zeros(E, int)
+    counts[look] = 1
+    offsets = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+    Y = torch.empty((rows, n), dtype=torch.bfloat16, device="cuda")
+    plan.grouped_forward(x.cuda(), _gpu(offsets), Y, plan.alloc_workspace(rows))
+    codes, scales = ref.quantize(x.float().numpy(), 0)
+    got = Y.float().cpu().numpy()
+    for i, e in enumerate(look):
+        y, S, G = ref.product(codes[i:i + 1], scales[i:i + 1], w[e, :1].cpu().numpy(), np.ones((1, 64), np.float32))
+        assert np.all(np.abs(got[i] - y[0]) <= ref.slack(S, G, d, True)[0] + 2.0 ** -8 * np.abs(y[0]))
+    plan.destroy()
+    del w, ws
+    torch.cuda.empty_cache()
+
+
+def test_experts_of_the_most_slots(st):
+    """2^24 slots, 64 tiles of columns each: every token has the outputs that it has among a few, by the same kernels."""
+    import torch
+    _needs(150)
+    tokens, E, d, ff = 1 << 19, 32, 128, 8192
+    g = torch.Generator(device="cuda").manual_seed(2)
+    w_up = (torch.randn((E, 2, ff, d), device="cuda", generator=g) * d ** -0.5).to(torch.bfloat16)
+    w_down = (torch.randn((E, d, ff), device="cuda", generator=g) * ff ** -0.5).to(torch.bfloat16)
+    up = st.Fp8Plan(st.Fp8Desc(d_in=d, d_out=ff, experts=E, gated=1, w_dtype=st.STAMP_BF16), w_up)
+    down = st.Fp8Plan(st.Fp8Desc(d_in=ff, d_out=d, experts=E, w_dtype=st.STAMP_BF16), w_down)
+    up.set_route("tiles_128")
+    down.set_route("tiles_256")
+    X = torch.randn((tokens, d), device="cuda", generator=g).to(torch.bfloat16)
+    L = torch.randn((tokens, E), device="cuda", generator=g)
+    Y = torch.full((tokens, d), -7.0, dtype=torch.bfloat16, device="cuda")
+
+    def run(x, l, y):
+        r = st.Routing(x.shape[0], E, E)
+        st.route_topk(l, r)
+        st.experts_forward(up, down, x, r, y, st.experts_workspace(up, down, x.shape[0], E))
+    run(X, L, Y)
+    look = torch.tensor([0, 1, tokens // 2 - 1, tokens // 2, 400000, tokens - 2, tokens - 1], device="cuda")
+    few = torch.empty((look.numel(), d), dtype=torch.bfloat16, device="cuda")
+    run(X[look].contiguous(), L[look].contiguous(), few)
+    assert torch.isfinite(few).all() and torch.equal(Y[look], few)
+    # all tokens: from a second call on each quarter of them
+    Q = torch.empty((tokens // 4, d), dtype=torch.bfloat16, device="cuda")
+    for q in range(4):
+        part = slice(q * (tokens // 4), (q + 1) * (tokens // 4))
+        run(X[part], L[part], Q)
+        assert torch.equal(Y[part], Q), q
+    up.destroy()
+    down.destroy()
+    torch.cuda.empty_cache()
