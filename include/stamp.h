@@ -432,8 +432,9 @@ stamp_status_t stamp_route_topk(const stamp_routing_t* routing, const void* logi
 /* The experts' gated MLP on the rows of a routing (as stamp_route_topk wrote it; entries out of range are cut to the range):
  *     h = silu(Xq Wgate) * (Xq Wup)  in fp32, per row,   r = Q8(h) Wdown (+ bias),   Y[t] = sum over slots j of  weights[t, j] r[row(t, j)]
  * up: a gated plan [d -> ff], down: a plan [ff -> d] with as many experts and the same scale_format; X [tokens, d] in up's x_dtype
- * (tokens * d < 2^31 - 2^16, tokens * top_k <= 2^24), Y [tokens, d] in down's y_dtype.  A token without any row gets zeros.  Between the down product and the sum the rows are held in
- * down's y_dtype: for a bf16 Y that rounds every term once more, by what Y itself is rounded. */
+ * (tokens * d, d rounded up to 128, < 2^31; tokens * top_k <= 2^24), Y [tokens, d] in down's y_dtype.  A token without any row gets
+ * zeros.  Between the down product and the sum the rows are held in down's y_dtype: for a bf16 Y that rounds every term once more, by
+ * what Y itself is rounded. */
 size_t stamp_experts_workspace_bytes(const stamp_fp8_plan_t* up, const stamp_fp8_plan_t* down, int32_t tokens, int32_t top_k);
 stamp_status_t stamp_experts_forward(const stamp_fp8_plan_t* up, const stamp_fp8_plan_t* down, const stamp_routing_t* routing,
                                      const void* X_dev, int64_t ld_x, void* Y_dev, int64_t ld_y, void* workspace_dev,

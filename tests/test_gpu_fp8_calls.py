@@ -121,3 +121,23 @@ def test_experts_of_the_most_slots(st):
     up.destroy()
     down.destroy()
     torch.cuda.empty_cache()
+
+
+# ---- limits ----
+
+@pytest.mark.parametrize("d", [1, 128, 385, 512])
+def test_the_most_tokens_of_the_experts(st, d):
+    """tokens * (d rounded up to 128) < 2^31: one token fewer gets as far as the missing workspace, nothing is launched."""
+    import ctypes as C
+
+    from paper_2510_26771_amd import fp8
+    up = st.Fp8Plan(st.Fp8Desc(d_in=d, d_out=8, experts=1, gated=1), _gpu(np.zeros((1, 2, 8, d), np.uint8)), _gpu(np.ones((2, -(-d // 128)), np.float32)))
+    down = st.Fp8Plan(st.Fp8Desc(d_in=8, d_out=d, experts=1), _gpu(np.zeros((1, d, 8), np.uint8)), _gpu(np.ones((-(-d // 128), 1), np.float32)))
+    most = min((2 ** 31 - 1) // (-(-d // 128) * 128), 1 << 22)
+
+    def status(tokens):
+        r = fp8._Routing(tokens, 1, 1, 256, 256, 256, 256, 256)
+        return up.lib.stamp_experts_forward(up._h, down._h, C.byref(r), 256, d, 256, d, None, 0, None)
+    assert status(most) == 4 and status(most + 1) == 3
+    up.destroy()
+    down.destroy()
