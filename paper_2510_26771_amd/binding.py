@@ -173,12 +173,17 @@ def _ptr(t) -> Optional[int]:
     return t.data_ptr()
 
 
-def _stream(stream) -> Optional[int]:
-    if stream is not None:
+def _stream(stream, gpu: Optional[int] = None) -> Optional[int]:
+    """Handle of the stream (default: torch's current one).  gpu: the index of the GPU that a call's tensors lie on; the kernels are
+    launched on the current GPU, so that has to be the one, and the stream one of it."""
+    if stream is not None and gpu is None:
         return stream.cuda_stream or None
     import torch
     # torch.cuda.current_stream() builds a Stream object: 2.8 us, more than a third of a small layer's call
-    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) or None
+    here = torch._C._cuda_getDevice()
+    if gpu is not None and (here != gpu or (stream is not None and stream.device.index != gpu)):
+        raise ValueError(f"GPU {gpu} has to be the current one, and the stream one of it")
+    return (torch._C._cuda_getCurrentRawStream(here) if stream is None else stream.cuda_stream) or None
 
 
 def mfma_rate(engine) -> float:

@@ -45,17 +45,11 @@ def _torch_dtype(code):
     return torch.bfloat16 if code == STAMP_BF16 else torch.float32
 
 
-def _current(device, stream):
-    """The kernels are launched on the current GPU: the plan has to be there, and the stream."""
-    import torch
-    if torch.cuda.current_device() != device.index or (stream is not None and stream.device != device):
-        raise ValueError(f"{device} must be the current GPU, and the stream one of it")
-
-
-def _matrix(t, name, rows, cols, dtype, device):
+# gpu: index of the plan's (the routing's) GPU; get_device() is -1 for tensors of the host
+def _matrix(t, name, rows, cols, dtype, gpu):
     """A [rows, cols] tensor of that type on that GPU whose rows are contiguous; returns the distance of its rows in elements."""
-    if not t.is_cuda or t.device != device or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
-        raise ValueError(f"{name} must be a tensor of shape ({rows}, {cols}) on {device}")
+    if t.get_device() != gpu or t.shape != (rows, cols):
+        raise ValueError(f"{name} must be a tensor of shape ({rows}, {cols}) on GPU {gpu}")
     if t.dtype != dtype:
         raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
     if cols > 1 and t.stride(1) != 1:
@@ -63,16 +57,16 @@ def _matrix(t, name, rows, cols, dtype, device):
     return t.stride(0) if rows > 1 else cols
 
 
-def _flat(t, name, numel, dtype, device):
-    if not t.is_cuda or t.device != device or t.dtype != dtype or t.numel() != numel or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous tensor of {numel} {dtype} on {device}")
+def _flat(t, name, numel, dtype, gpu):
+    if t.get_device() != gpu or t.dtype != dtype or t.numel() != numel or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous tensor of {numel} {dtype} on GPU {gpu}")
 
 
-def _room(t, device):
+def _room(t, gpu):
     """Bytes of a workspace."""
-    if t is None or not t.is_cuda or t.device != device or not t.is_contiguous():
-        raise ValueError(f"workspace must be a contiguous tensor on {device}")
-    return t.numel() * t.element_size()
+    if t is None or t.get_device() != gpu or not t.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on GPU {gpu}")
+    return t.nbytes
 
 
 class Fp8Plan:
@@ -91,13 +85,12 @@ class Fp8Plan:
             raise ValueError(f"W is {W.dtype}, the description says otherwise")
         if W.numel() != mats * d.d_in * d.d_out or W.dim() < 2 or tuple(W.shape[-2:]) != ((d.d_out, d.d_in) if d.w_is_out_by_in else (d.d_in, d.d_out)):
             raise ValueError("W's shape is not the description's")
-        self.device = W.device
+        self.gpu = W.get_device()
         if w_scales is not None:
-            _flat(w_scales, "w_scales", mats * -(-d.d_out // BLOCK) * -(-d.d_in // BLOCK), torch.float32, self.device)
+            _flat(w_scales, "w_scales", mats * -(-d.d_out // BLOCK) * -(-d.d_in // BLOCK), torch.float32, self.gpu)
         if bias is not None:
-            _flat(bias, "bias", max(d.experts, 1) * d.d_out, torch.float32, self.device)
-        _current(self.device, stream)
-        _check(self.lib.stamp_fp8_plan_create(C.byref(d.to_c()), _ptr(W), _ptr(w_scales), _ptr(bias), _stream(stream), C.byref(self._h)),
+            _flat(bias, "bias", max(d.experts, 1) * d.d_out, torch.float32, self.gpu)
+        _check(self.lib.stamp_fp8_plan_create(C.byref(d.to_c()), _ptr(W), _ptr(w_scales), _ptr(bias), _stream(stream, self.gpu), C.byref(self._h)),
                "stamp_fp8_plan_create")
         self._x_dtype, self._y_dtype = _torch_dtype(d.x_dtype), _torch_dtype(d.y_dtype)
 
@@ -140,48 +133,43 @@ class Fp8Plan:
     def _act_buffers(self, codes, scales, rows):
         import torch
         kb = -(-self.desc.d_in // BLOCK)
-        _flat(codes, "codes", rows * kb * BLOCK, torch.uint8, self.device)
-        if (not scales.is_cuda or scales.device != self.device or scales.dtype != torch.float32 or scales.dim() != 2 or scales.shape[0] != kb
-                or not scales.is_contiguous()):
-            raise ValueError(f"scales must be a contiguous tensor of {kb} rows of float32 on {self.device}")
+        _flat(codes, "codes", rows * kb * BLOCK, torch.uint8, self.gpu)
+        if scales.get_device() != self.gpu or scales.dtype != torch.float32 or scales.dim() != 2 or scales.shape[0] != kb or not scales.is_contiguous():
+            raise ValueError(f"scales must be a contiguous tensor of {kb} rows of float32 on GPU {self.gpu}")
         return scales.shape[1]
 
     def _x(self, X, rows):
-        return _matrix(X, "X", rows, self.desc.d_in, self._x_dtype, self.device)
+        return _matrix(X, "X", rows, self.desc.d_in, self._x_dtype, self.gpu)
 
     def _y(self, Y, rows):
-        return _matrix(Y, "Y", rows, self.desc.d_out, self._y_dtype, self.device)
+        return _matrix(Y, "Y", rows, self.desc.d_out, self._y_dtype, self.gpu)
 
     def quantize_act(self, X, codes, scales, stream=None):
-        _current(self.device, stream)
         ld = self._x(X, X.shape[0])
         lds = self._act_buffers(codes, scales, X.shape[0])
-        _check(self.lib.stamp_fp8_quantize_act(self._h, X.shape[0], _ptr(X), ld, _ptr(codes), _ptr(scales), lds, _stream(stream)),
+        _check(self.lib.stamp_fp8_quantize_act(self._h, X.shape[0], _ptr(X), ld, _ptr(codes), _ptr(scales), lds, _stream(stream, self.gpu)),
                "stamp_fp8_quantize_act")
 
     def linear_forward(self, X, Y, workspace, stream=None):
-        _current(self.device, stream)
         rows = X.shape[0]
-        ld_x, ld_y, room = self._x(X, rows), self._y(Y, rows), _room(workspace, self.device)
-        _check(self.lib.stamp_fp8_linear_forward(self._h, rows, _ptr(X), ld_x, _ptr(Y), ld_y, _ptr(workspace), room, _stream(stream)),
+        ld_x, ld_y, room = self._x(X, rows), self._y(Y, rows), _room(workspace, self.gpu)
+        _check(self.lib.stamp_fp8_linear_forward(self._h, rows, _ptr(X), ld_x, _ptr(Y), ld_y, _ptr(workspace), room, _stream(stream, self.gpu)),
                "stamp_fp8_linear_forward")
 
     def linear_forward_q(self, codes, scales, Y, workspace, stream=None):
-        _current(self.device, stream)
         rows = Y.shape[0]
-        lds, ld_y, room = self._act_buffers(codes, scales, rows), self._y(Y, rows), _room(workspace, self.device)
+        lds, ld_y, room = self._act_buffers(codes, scales, rows), self._y(Y, rows), _room(workspace, self.gpu)
         _check(self.lib.stamp_fp8_linear_forward_q(self._h, rows, _ptr(codes), _ptr(scales), lds, _ptr(Y), ld_y, _ptr(workspace),
-                                                   room, _stream(stream)), "stamp_fp8_linear_forward_q")
+                                                   room, _stream(stream, self.gpu)), "stamp_fp8_linear_forward_q")
 
     def grouped_forward(self, X, offsets, Y, workspace, stream=None):
         """Rows offsets[e] .. offsets[e + 1] - 1 of X times expert e's weights."""
         import torch
-        _current(self.device, stream)
         rows = X.shape[0]
-        ld_x, ld_y, room = self._x(X, rows), self._y(Y, rows), _room(workspace, self.device)
-        _flat(offsets, "offsets", self.desc.experts + 1, torch.int32, self.device)
+        ld_x, ld_y, room = self._x(X, rows), self._y(Y, rows), _room(workspace, self.gpu)
+        _flat(offsets, "offsets", self.desc.experts + 1, torch.int32, self.gpu)
         _check(self.lib.stamp_fp8_grouped_forward(self._h, rows, _ptr(offsets), _ptr(X), ld_x, _ptr(Y), ld_y, _ptr(workspace),
-                                                  room, _stream(stream)), "stamp_fp8_grouped_forward")
+                                                  room, _stream(stream, self.gpu)), "stamp_fp8_grouped_forward")
 
     def debug_weight_codes(self):
         """Codes (bytes) [experts][2 if gated][d_out][d_in] and scales [..][blocks of d_out][blocks of d_in], on the host."""
@@ -213,7 +201,7 @@ class Routing:
         self.weights = torch.empty((tokens, top_k), dtype=torch.float32, device=device)
         self.offsets, self.token_of_row = ints(experts + 1), ints(tokens * top_k)
         self.workspace = torch.empty(need, dtype=torch.uint8, device=device)
-        self.device = self.workspace.device
+        self.gpu = self.workspace.get_device()
         self._c = _Routing(self.tokens, self.experts, self.top_k, _ptr(self.ids), _ptr(self.weights), _ptr(self.offsets), _ptr(self.token_of_row),
                            _ptr(self.row_of_slot))
 
@@ -223,10 +211,9 @@ def route_topk(logits, routing: Routing, renormalize: bool = True, stream=None):
     import torch
     if logits.dtype not in (torch.float32, torch.bfloat16):
         raise ValueError("logits must be float32 or bfloat16")
-    _current(routing.device, stream)
-    ld = _matrix(logits, "logits", routing.tokens, routing.experts, logits.dtype, routing.device)
+    ld = _matrix(logits, "logits", routing.tokens, routing.experts, logits.dtype, routing.gpu)
     _check(routing.lib.stamp_route_topk(C.byref(routing._c), _ptr(logits), STAMP_BF16 if logits.dtype == torch.bfloat16 else STAMP_F32, ld,
-                                        int(bool(renormalize)), _ptr(routing.workspace), routing.workspace.numel(), _stream(stream)), "stamp_route_topk")
+                                        int(bool(renormalize)), _ptr(routing.workspace), routing.workspace.numel(), _stream(stream, routing.gpu)), "stamp_route_topk")
 
 
 def experts_workspace(up: Fp8Plan, down: Fp8Plan, tokens: int, top_k: int, device="cuda"):
@@ -237,9 +224,8 @@ def experts_workspace(up: Fp8Plan, down: Fp8Plan, tokens: int, top_k: int, devic
 
 def experts_forward(up: Fp8Plan, down: Fp8Plan, X, routing: Routing, Y, workspace, stream=None):
     """The gated MLP of the chosen experts of every token, summed with their weights."""
-    _current(up.device, stream)
-    if down.device != up.device or routing.device != up.device:
+    if down.gpu != up.gpu or routing.gpu != up.gpu:
         raise ValueError("both plans and the routing must lie on one GPU")
-    ld_x, ld_y, room = up._x(X, routing.tokens), down._y(Y, routing.tokens), _room(workspace, up.device)
+    ld_x, ld_y, room = up._x(X, routing.tokens), down._y(Y, routing.tokens), _room(workspace, up.gpu)
     _check(up.lib.stamp_experts_forward(up._h, down._h, C.byref(routing._c), _ptr(X), ld_x, _ptr(Y), ld_y, _ptr(workspace), room,
-                                        _stream(stream)), "stamp_experts_forward")
+                                        _stream(stream, up.gpu)), "stamp_experts_forward")

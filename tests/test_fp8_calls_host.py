@@ -31,7 +31,7 @@ class OnGpu:
     """A host tensor that says it lies on a GPU."""
 
     def __init__(self, tensor, index=0):
-        self.tensor, self.is_cuda, self.device = tensor, True, torch.device("cuda", index)
+        self.tensor, self.is_cuda, self.get_device = tensor, True, lambda: index
 
     def __getattr__(self, name):
         return getattr(self.tensor, name)
@@ -56,18 +56,18 @@ ROWS, D, N, EXPERTS = 6, 256, 128, 2
 
 @pytest.fixture
 def on_cpu(monkeypatch):
-    monkeypatch.setattr(fp8, "_stream", lambda stream: None)
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda gpu: 0)
     lib = Calls()
 
     def plan(**kw):
         p = object.__new__(fp8.Fp8Plan)
         p.lib, p.desc, p._h = lib, st.Fp8Desc(**{**dict(d_in=D, d_out=N), **kw}), None
         p._x_dtype = p._y_dtype = torch.bfloat16
-        p.device = torch.device("cuda", 0)
+        p.gpu = 0
         return p
     r = object.__new__(st.Routing)
-    r.lib, r.tokens, r.experts, r.top_k, r.device, r._c = lib, ROWS, EXPERTS, 1, torch.device("cuda", 0), fp8._Routing(ROWS, EXPERTS, 1)
+    r.lib, r.tokens, r.experts, r.top_k, r.gpu, r._c = lib, ROWS, EXPERTS, 1, 0, fp8._Routing(ROWS, EXPERTS, 1)
     r.workspace = OnGpu(torch.empty(512, dtype=torch.uint8))
     return lib, plan, r
 
@@ -120,7 +120,7 @@ def test_a_workspace_with_gaps_is_refused_and_any_type_counts_its_bytes(on_cpu, 
 
 def test_a_plan_of_another_gpu_than_the_current_is_refused(on_cpu, monkeypatch):
     lib, plan, r = on_cpu
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 1)
     for call, tensors in _calls(plan, r).values():
         with pytest.raises(ValueError):
             call(**{n: OnGpu(t) for n, t in tensors.items()})
