@@ -2,6 +2,7 @@
 import numpy as np
 import pytest
 
+import fp8_calls_reference as calls
 import fp8_reference as ref
 
 pytestmark = pytest.mark.gpu
@@ -139,5 +140,83 @@ def test_the_most_tokens_of_the_experts(st, d):
         r = fp8._Routing(tokens, 1, 1, 256, 256, 256, 256, 256)
         return up.lib.stamp_experts_forward(up._h, down._h, C.byref(r), 256, d, 256, d, None, 0, None)
     assert status(most) == 4 and status(most + 1) == 3
+    up.destroy()
+    down.destroy()
+
+
+# ---- fp32 results: sums of both products and the rows between them in fp32 ----
+
+def _plans(st, w_up, s_up, w_down, s_down, y, pow2, up_route, down_route):
+    E, _, ff, d = w_up.shape
+    up = st.Fp8Plan(st.Fp8Desc(d_in=d, d_out=ff, experts=E, gated=1, x_dtype=st.STAMP_F32, scale_format=pow2), _gpu(w_up), _gpu(s_up))
+    down = st.Fp8Plan(st.Fp8Desc(d_in=ff, d_out=d, experts=E, y_dtype=y, scale_format=pow2), _gpu(w_down), _gpu(s_down))
+    up.set_route(up_route)
+    down.set_route(down_route)
+    return up, down
+
+
+@pytest.mark.parametrize("route", ["", "rows", "tiles_64", "tiles_128"])
+@pytest.mark.parametrize("pow2", [0, 1])
+@pytest.mark.parametrize("tokens,experts,top_k,d,ff", [(1, 3, 2, 130, 200), (40, 3, 2, 150, 270), (150, 6, 3, 300, 257), (300, 2, 1, 257, 640)])
+def test_experts_in_fp32_against_the_definition(st, tokens, experts, top_k, d, ff, pow2, route):
+    import torch
+    rng = np.random.default_rng(tokens)
+    x = rng.standard_normal((tokens, d)).astype(np.float32)
+    w_up, w_down = (ref.encode(rng.standard_normal(s).astype(np.float32) * 40) for s in ((experts, 2, ff, d), (experts, d, ff)))
+    s_up = np.exp2(rng.integers(-10, -8, (experts, 2, -(-ff // 128), -(-d // 128)))).astype(np.float32)
+    s_down = np.exp2(rng.integers(-10, -8, (experts, -(-d // 128), -(-ff // 128)))).astype(np.float32)
+    l = rng.standard_normal((tokens, experts)).astype(np.float32)
+    up, down = _plans(st, w_up, s_up, w_down, s_down, st.STAMP_F32, pow2, route, route)
+    r, Y = st.Routing(tokens, experts, top_k), torch.empty((tokens, d), device="cuda")
+    st.route_topk(_gpu(l), r)
+    st.experts_forward(up, down, _gpu(x), r, Y, st.experts_workspace(up, down, tokens, top_k))
+    want, bound = calls.experts(x, l, w_up, s_up, w_down, s_down, top_k, 1, pow2, False)
+    far = np.abs(Y.cpu().numpy() - want) / bound
+    assert far.max() <= 1, f"{(far > 1).sum()} of {far.size} beyond the bound, worst {far.max():.3g} times it"
+    up.destroy()
+    down.destroy()
+
+
+@pytest.mark.parametrize("route", ["", "rows", "tiles_64", "tiles_128"])
+@pytest.mark.parametrize("rows", [3, 70, 300])
+@pytest.mark.parametrize("ff", [128, 256, 520])
+def test_fp32_results_hold_what_8_bit_sums_would_lose(st, rows, ff, route):
+    """Small products between large ones that cancel: of a layer, of one by expert, and of the experts' down product."""
+    import torch
+    rng = np.random.default_rng(ff)
+    n = 60
+    h, w = calls.cancelling(rng, ff, n)
+    blocks = -(-ff // 128)
+    ones = np.ones((1, blocks), np.float32)
+    x = ref.E4M3[h].astype(np.float32)[None].repeat(rows, 0)  # its codes are h: every block holds a 448
+    codes, scales = ref.quantize(x, 0)
+    assert (codes[:, :ff] == h).all() and (scales == 1).all()
+    y, S, G = ref.product(codes, scales, w, ones)
+    bound = ref.slack(S, G, ff, True)
+    plan = st.Fp8Plan(st.Fp8Desc(d_in=ff, d_out=n, x_dtype=st.STAMP_F32, y_dtype=st.STAMP_F32), _gpu(w), _gpu(ones))
+    two = st.Fp8Plan(st.Fp8Desc(d_in=ff, d_out=n, experts=2, x_dtype=st.STAMP_F32, y_dtype=st.STAMP_F32), _gpu(np.stack([w, w])), _gpu(np.stack([ones, ones])))
+    Y = torch.empty((rows, n), device="cuda")
+    for p, call in ((plan, lambda ws: plan.linear_forward(_gpu(x), Y, ws)), (two, lambda ws: two.grouped_forward(_gpu(x), _gpu(np.int32([0, 1, rows])), Y, ws))):
+        p.set_route(route)
+        Y.fill_(np.nan)
+        call(p.alloc_workspace(rows))
+        assert np.all(np.abs(Y.cpu().numpy() - y) <= bound + 2.0 ** -23 * np.abs(y))
+        p.destroy()
+    # experts of one channel: x = 1, gates of 16, up columns of h's values; h is 16 (1 - 1e-7) times those, its codes the same
+    gate = np.full(ff, 16.0)
+    w_up = ref.encode(np.stack([gate, ref.E4M3[h]])[None, :, :, None].repeat(2, 0).astype(np.float32))
+    w_down = np.zeros((2, 1, ff), np.uint8)
+    w_down[:] = w[:1]
+    up, down = _plans(st, w_up, np.ones((2, 2, blocks, 1), np.float32), w_down, np.ones((2, 1, blocks), np.float32), st.STAMP_F32, 0, route, route)
+    one = np.ones((rows, 1), np.float32)
+    l = rng.standard_normal((rows, 2)).astype(np.float32)
+    r, Y = st.Routing(rows, 2, 1), torch.empty((rows, 1), device="cuda")
+    st.route_topk(_gpu(l), r)
+    st.experts_forward(up, down, _gpu(one), r, Y, st.experts_workspace(up, down, rows, 1))
+    want, bound = calls.experts(one, l, w_up, np.ones((2, 2, blocks, 1), np.float32), w_down, np.ones((2, 1, blocks), np.float32), 1, 1, 0, False)
+    lost, _ = calls.experts(one, l, w_up, np.ones((2, 2, blocks, 1), np.float32), w_down, np.ones((2, 1, blocks), np.float32), 1, 1, 0, False,
+                            sums=calls.eight_bit_sums)
+    assert np.all(np.abs(lost - want) > bound), "the bound would let them pass"
+    assert np.all(np.abs(Y.cpu().numpy() - want) <= bound)
     up.destroy()
     down.destroy()
