@@ -220,3 +220,35 @@ def test_fp32_results_hold_what_8_bit_sums_would_lose(st, rows, ff, route):
     assert np.all(np.abs(Y.cpu().numpy() - want) <= bound)
     up.destroy()
     down.destroy()
+
+
+# ---- the router where a lane has two of the chosen, a wave more than one round of tokens, and at 1024 experts ----
+
+@pytest.mark.parametrize("kind", ["plain", "masked", "ties", "extreme"])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tokens,experts,top_k", [(130, 200, 32), (70, 40, 17), (65, 17, 32), (33, 1024, 32), (4096, 1024, 3), (4097, 1024, 3), (5000, 257, 20),
+                                                  (16384, 20, 2), (16385, 20, 2), (17000, 256, 18), (40000, 100, 4)])
+def test_router_over_many_tokens_and_choices(st, tokens, experts, top_k, dtype, kind):
+    import torch
+    rng = np.random.default_rng(tokens + experts)
+    l = rng.standard_normal((tokens, experts)).astype(np.float32)
+    if kind == "masked":
+        l[rng.random(l.shape) < 0.7] = -np.inf
+        l[rng.random(l.shape) < 0.1] = np.nan
+        l[tokens // 2] = -np.inf
+    if kind == "ties":
+        l = rng.integers(-1, 2, l.shape).astype(np.float32) * np.where(rng.random(l.shape) < 0.5, -1, 1).astype(np.float32)
+    if kind == "extreme":
+        l[rng.random(l.shape) < 0.3] = np.finfo(np.float32).min
+        l[tokens // 2, : experts // 2 + 1] = np.inf
+    t = torch.from_numpy(l).to(torch.float32 if dtype == "f32" else torch.bfloat16)
+    r = st.Routing(tokens, experts, top_k)
+    for renormalize in (0, 1):
+        for a in (r.ids, r.offsets, r.token_of_row, r.row_of_slot):
+            a.fill_(-77)
+        st.route_topk(t.cuda(), r, renormalize=renormalize)
+        ids, weights, offsets, token, row = calls.route(t.float().numpy(), top_k, renormalize)
+        for name, want in (("ids", ids), ("offsets", offsets), ("token_of_row", token), ("row_of_slot", row)):
+            assert np.array_equal(getattr(r, name).cpu().numpy(), want), name
+        w = r.weights.cpu().numpy().astype(np.float64)
+        assert np.all(np.abs(w - weights) <= calls.weight_bound(experts) * weights + 1e-37)
