@@ -252,3 +252,53 @@ def test_router_over_many_tokens_and_choices(st, tokens, experts, top_k, dtype, 
             assert np.array_equal(getattr(r, name).cpu().numpy(), want), name
         w = r.weights.cpu().numpy().astype(np.float64)
         assert np.all(np.abs(w - weights) <= calls.weight_bound(experts) * weights + 1e-37)
+
+
+# ---- loads far from even: one or two experts have nearly all rows, the rule knows only the average ----
+
+@pytest.mark.parametrize("x,y,pow2", [("f32", "f32", 0), ("bf16", "bf16", 1)])
+@pytest.mark.parametrize("experts,busy,d,n", [(64, {5: 200}, 256, 64), (64, {5: 700}, 256, 320), (128, {0: 740, 127: 760}, 300, 140), (40, {39: 352, 2: 1}, 520, 300),
+                                              (256, {200: 2990, 3: 17}, 128, 70), (20, {7: 600, 8: 1, 9: 33}, 1152, 200)])
+def test_grouped_with_uneven_loads(st, experts, busy, d, n, x, y, pow2):
+    import torch
+    rng = np.random.default_rng(experts + d)
+    counts = np.zeros(experts, int)
+    for e, c in busy.items():
+        counts[e] = c
+    rows = int(counts.sum())
+    offsets = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
+    types = {"f32": (torch.float32, st.STAMP_F32), "bf16": (torch.bfloat16, st.STAMP_BF16)}
+    X = torch.from_numpy(rng.standard_normal((rows, d)).astype(np.float32)).to(types[x][0])
+    w = ref.encode(rng.standard_normal((experts, n, d)).astype(np.float32) * 40)
+    ws = np.exp2(rng.integers(-10, -8, (experts, -(-n // 128), -(-d // 128)))).astype(np.float32)
+    plan = st.Fp8Plan(st.Fp8Desc(d_in=d, d_out=n, experts=experts, x_dtype=types[x][1], y_dtype=types[y][1], scale_format=pow2), _gpu(w), _gpu(ws))
+    Y = torch.full((rows, n), np.nan, dtype=types[y][0], device="cuda")
+    plan.grouped_forward(X.cuda(), _gpu(offsets), Y, plan.alloc_workspace(rows))
+    codes, scales = ref.quantize(X.float().numpy(), pow2)
+    got = Y.float().cpu().numpy()
+    for e in busy:
+        part = slice(offsets[e], offsets[e + 1])
+        want, S, G = ref.product(codes[part], scales[part], w[e], ws[e])
+        bound = ref.slack(S, G, d, y == "f32" or plan.route(rows) == "rows") + (2.0 ** -23 if y == "f32" else 2.0 ** -8) * np.abs(want)
+        assert np.all(np.abs(got[part] - want) <= bound), e
+    plan.destroy()
+
+
+@pytest.mark.parametrize("tokens,experts,top_k,d,ff", [(300, 64, 2, 256, 128), (700, 64, 2, 130, 200), (90, 128, 3, 256, 300)])
+def test_experts_with_one_that_every_token_chooses(st, tokens, experts, top_k, d, ff):
+    import torch
+    rng = np.random.default_rng(tokens)
+    x = rng.standard_normal((tokens, d)).astype(np.float32)
+    w_up, w_down = (ref.encode(rng.standard_normal(s).astype(np.float32) * 40) for s in ((experts, 2, ff, d), (experts, d, ff)))
+    s_up, s_down = (np.full((*s[:-2], -(-s[-2] // 128), -(-s[-1] // 128)), 2.0 ** -9, np.float32) for s in (w_up.shape, w_down.shape))
+    l = rng.standard_normal((tokens, experts)).astype(np.float32)
+    l[:, 9] += 20
+    up, down = _plans(st, w_up, s_up, w_down, s_down, st.STAMP_F32, 0, "", "")
+    r, Y = st.Routing(tokens, experts, top_k), torch.empty((tokens, d), device="cuda")
+    st.route_topk(_gpu(l), r, renormalize=False)
+    st.experts_forward(up, down, _gpu(x), r, Y, st.experts_workspace(up, down, tokens, top_k))
+    assert int(r.offsets.diff()[9]) == tokens
+    want, bound = calls.experts(x, l, w_up, s_up, w_down, s_down, top_k, 0, 0, False)
+    assert np.all(np.abs(Y.cpu().numpy() - want) <= bound)
+    up.destroy()
+    down.destroy()
