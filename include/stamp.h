@@ -452,6 +452,9 @@ typedef enum {
   STAMP_FP8_ROUTE_TILES_256 = 4
 } stamp_fp8_route_t;
 int32_t stamp_fp8_debug_route(const stamp_fp8_plan_t* plan, int32_t rows);
+/* And how its tiles are launched, three numbers to cut_host: output columns of the first of two launches (0: there is one), parts of the
+ * depth in the first or only launch, parts in the second.  All 0 where the kernel for few rows runs. */
+stamp_status_t stamp_fp8_debug_cut(const stamp_fp8_plan_t* plan, int32_t rows, int32_t* cut_host);
 /* For tests and measurements: that kernel for every call, 0 = by rule again.  Modifies the plan (not thread-safe, no call on the plan may
  * be in progress on another host thread).  STAMP_ERR_UNSUPPORTED for tiles of 256 rows where the products are summed in fp32. */
 stamp_status_t stamp_fp8_debug_set_route(stamp_fp8_plan_t* plan, int32_t route);

@@ -26,7 +26,7 @@ EXPORTS = ["stamp_plan_create", "stamp_plan_destroy", "stamp_plan_workspace_byte
            "stamp_debug_gemm_acc", "stamp_debug_weight_codes", "stamp_debug_run_stage", "stamp_plan_set_unfused", "stamp_plan_set_gemm_engine",
            "stamp_debug_set_choice", "stamp_debug_routes", "stamp_debug_layout", "stamp_debug_mfma_rate", "stamp_status_string",
            "stamp_fp8_plan_create", "stamp_fp8_plan_destroy", "stamp_fp8_workspace_bytes", "stamp_fp8_quantize_act", "stamp_fp8_linear_forward",
-           "stamp_fp8_linear_forward_q", "stamp_fp8_grouped_forward", "stamp_fp8_debug_weight_codes", "stamp_fp8_debug_route", "stamp_fp8_debug_set_route",
+           "stamp_fp8_linear_forward_q", "stamp_fp8_grouped_forward", "stamp_fp8_debug_weight_codes", "stamp_fp8_debug_route", "stamp_fp8_debug_cut", "stamp_fp8_debug_set_route",
            "stamp_route_workspace_bytes", "stamp_route_topk", "stamp_experts_workspace_bytes", "stamp_experts_forward"]
 
 # stamp_choice_t and stamp_route_t (include/stamp.h)
@@ -148,6 +148,8 @@ def load_library():
             ("stamp_fp8_grouped_forward", C.c_int, [vp, i32, vp, vp, i64, vp, i64, vp, sz, vp]),
             ("stamp_fp8_debug_weight_codes", C.c_int, [vp, vp, vp]),
             ("stamp_fp8_debug_route", i32, [vp, i32]),
+            ("stamp_fp8_debug_cut", C.c_int, [vp, i32, vp]),
+            ("stamp_fp8_debug_set_route", C.c_int, [vp, i32]),
             ("stamp_route_workspace_bytes", sz, [i32, i32, i32]),
             ("stamp_route_topk", C.c_int, [vp, vp, i32, i64, i32, vp, sz, vp]),
             ("stamp_experts_workspace_bytes", sz, [vp, vp, i32, i32]),

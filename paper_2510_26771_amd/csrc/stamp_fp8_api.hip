@@ -497,6 +497,19 @@ int32_t stamp_fp8_debug_route(const stamp_fp8_plan_t* p, int32_t rows) {
   return route_of(gemm_args(p), rows);
 }
 
+stamp_status_t stamp_fp8_debug_cut(const stamp_fp8_plan_t* p, int32_t rows, int32_t* cut_host) {
+  if (p == nullptr || cut_host == nullptr) return STAMP_ERR_NULL;
+  if (rows < 0 || rows > kMaxRows) return STAMP_ERR_SHAPE;
+  const StampF8Gemm a = gemm_args(p);
+  cut_host[0] = cut_host[1] = cut_host[2] = 0;
+  if (route_of(a, rows) == STAMP_FP8_ROUTE_ROWS) return STAMP_OK;
+  const F8Cut cut = stamp_f8_cut(a.sets, a.groups, a.Kb, rows, a.wide_sums, a.gated, a.forced);
+  cut_host[0] = cut.groups * kF8Group;
+  cut_host[1] = cut.parts;
+  cut_host[2] = cut.groups > 0 ? cut.rest_parts : 0;
+  return STAMP_OK;
+}
+
 stamp_status_t stamp_fp8_debug_set_route(stamp_fp8_plan_t* p, int32_t route) {
   if (p == nullptr) return STAMP_ERR_NULL;
   if (route < 0 || route > STAMP_FP8_ROUTE_TILES_256) return STAMP_ERR_SHAPE;

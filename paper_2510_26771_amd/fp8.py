@@ -117,6 +117,12 @@ class Fp8Plan:
         """Name (FP8_ROUTES) of the kernel that a call with so many rows runs."""
         return FP8_ROUTES[int(self.lib.stamp_fp8_debug_route(self._h, int(rows)))]
 
+    def cut(self, rows: int) -> tuple:
+        """(columns of the first of two launches or 0, parts of the depth in the first, in the second) of a call in tiles; zeros else."""
+        out = (C.c_int32 * 3)()
+        _check(self.lib.stamp_fp8_debug_cut(self._h, int(rows), out), "stamp_fp8_debug_cut")
+        return tuple(out)
+
     def set_route(self, route: str = ""):
         """For tests and measurements: that kernel for every call ("": by rule)."""
         code = {n: c for c, n in FP8_ROUTES.items()}[route] if route else 0

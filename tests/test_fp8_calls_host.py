@@ -25,6 +25,10 @@ def test_a_router_workspace_serves_every_smaller_call(lib, experts):
     assert not falls, f"{len(falls)} steps down, the first (tokens, bytes): {falls[0]}"
 
 
+def test_the_cut_of_no_plan(lib):
+    assert lib.stamp_fp8_debug_cut(None, 4, None) == 1
+
+
 # ---- what the Python calls refuse: the library gets addresses, and a host's or another GPU's would fault the kernels ----
 
 class OnGpu:

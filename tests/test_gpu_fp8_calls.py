@@ -302,3 +302,60 @@ def test_experts_with_one_that_every_token_chooses(st, tokens, experts, top_k, d
     assert np.all(np.abs(Y.cpu().numpy() - want) <= bound)
     up.destroy()
     down.destroy()
+
+
+# ---- tiles cut by depth and by columns: that the sizes which are meant to reach these launches do, by rule ----
+
+PARTS = [(200, 1290, 2), (130, 1500, 3), (130, 2000, 4), (100, 2500, 5), (100, 3000, 6), (100, 3500, 7), (100, 4096, 8)]
+
+
+@pytest.mark.parametrize("y", ["f32", "bf16"])
+@pytest.mark.parametrize("experts", [0, 2])
+@pytest.mark.parametrize("rows,d,parts", PARTS)
+def test_every_number_of_parts_of_the_depth(st, rows, d, parts, experts, y):
+    import torch
+    rng = np.random.default_rng(d)
+    n, wide = 130, y == "f32"
+    lead = (experts,) if experts else ()
+    x = torch.from_numpy(rng.standard_normal((rows, d)).astype(np.float32)).to(torch.bfloat16)
+    w = ref.encode(rng.standard_normal((*lead, n, d)).astype(np.float32) * 40)
+    ws = np.exp2(rng.uniform(-10, -8, (*lead, 2, -(-d // 128)))).astype(np.float32)
+    bias = rng.standard_normal((*lead, n)).astype(np.float32)
+    plan = st.Fp8Plan(st.Fp8Desc(d_in=d, d_out=n, experts=experts, y_dtype=st.STAMP_F32 if wide else st.STAMP_BF16), _gpu(w), _gpu(ws), _gpu(bias))
+    if experts:
+        plan.set_route("tiles_64")
+    assert plan.cut(rows) == (0, parts if wide or parts > 3 else 1, 0)  # 8-bit sums: short depths stay whole
+    buf = torch.full((rows + 1, n + 3), -7.0, dtype=torch.float32 if wide else torch.bfloat16, device="cuda")
+    Y = buf[:rows, 1:n + 1]
+    workspace = plan.alloc_workspace(rows)
+    workspace.fill_(255)
+    offsets = [0, rows // 3, rows] if experts else [0, rows]
+    if experts:
+        plan.grouped_forward(x.cuda(), _gpu(np.int32(offsets)), Y, workspace)
+    else:
+        plan.linear_forward(x.cuda(), Y, workspace)
+    codes, scales = ref.quantize(x.float().numpy(), 0)
+    got = Y.float().cpu().numpy()
+    for e in range(len(offsets) - 1):
+        part = slice(offsets[e], offsets[e + 1])
+        want, S, G = ref.product(codes[part], scales[part], *((w[e], ws[e]) if experts else (w, ws)))
+        b = bias[e] if experts else bias
+        bound = ref.slack(S + np.abs(b), G, d, wide) + (2.0 ** -23 if wide else 2.0 ** -8) * np.abs(want + b)
+        assert np.all(np.abs(got[part] - (want + b)) <= bound)
+    Y.fill_(-7.0)
+    assert (buf == -7.0).all()
+    plan.destroy()
+
+
+@pytest.mark.parametrize("rows,d,n,y,two", [
+    (200, 2000, 320, "bf16", 0), (200, 2000, 320, "f32", 0), (130, 4096, 300, "bf16", 0), (130, 4096, 300, "f32", 0), (90, 7000, 515, "bf16", 0),
+    (90, 7000, 515, "f32", 0), (3000, 520, 5700, "bf16", 1), (3000, 520, 5700, "f32", 1), (2900, 300, 5643, "bf16", 1), (2900, 300, 5643, "f32", 1),
+    (324, 4725, 10849, "bf16", 2), (323, 2998, 10965, "f32", 2)])
+def test_the_sizes_of_the_product_tests_reach_their_launches(st, rows, d, n, y, two):
+    """two: 0 the depth in parts, 1 columns in two launches, 2 the second of them in parts as well."""
+    plan = st.Fp8Plan(st.Fp8Desc(d_in=d, d_out=n, y_dtype=st.STAMP_F32 if y == "f32" else st.STAMP_BF16), _gpu(np.zeros((n, d), np.uint8)),
+                      _gpu(np.ones((-(-n // 128), -(-d // 128)), np.float32)))
+    columns, first, second = plan.cut(rows)
+    assert (columns > 0) == (two > 0) and (first if two == 0 else second) > (1 if two != 1 else 0)
+    assert plan.cut(1) == (0, 0, 0)
+    plan.destroy()
