@@ -108,7 +108,10 @@ ExpertsWs experts_ws(const stamp_fp8_plan* up, const stamp_fp8_plan* down, int32
   w.sh = w.h + align256((size_t)slots * down->Kp);
   w.rows = w.sh + align256((size_t)down->Kb * ld * sizeof(float));
   w.ld_rows = (down->desc.d_out + 7) / 8 * 8;
-  // the up product writes codes of one byte; a down product that wants them as bf16 has them widened here
+  // Rows in Y's type: a bf16 Y is a sum of terms rounded once each, 2.3e-3 off where rows in fp32 give 1.7e-3, which is Y's own rounding; but
+  // they are the most bytes of the call (8192 tokens, 8 of 64 experts, 4096 -> 1536: down product 529 -> 647 us, weighted sum 122 -> 242, the whole
+  // 2200 -> 2447).  An fp32 Y has them in fp32.
+  // The up product writes codes of one byte; a down product that wants them as bf16 has them widened here
   w.wide = w.rows + align256((size_t)slots * w.ld_rows * type_size(down->desc.y_dtype));
   w.partial = w.wide + (code_bytes(down) == 2 ? align256((size_t)slots * down->Kp * 2) : 0);
   w.total = w.partial + align256(stamp_f8_partial_bytes(down->groups, (int32_t)slots));
@@ -175,6 +178,8 @@ stamp_status_t forward(const stamp_fp8_plan* p, int32_t rows, const int32_t* off
 
 // Kernel for a product of `rows` rows over `sets` weights, by estimates in us.
 //
+// The host knows rows and sets, not how the rows lie on the sets: the estimates take them as even (the last paragraph: where they are not).
+//
 // Few rows: up to 12 a set always the rows kernel, which reads the weights at up to 6 TB/s; beyond that its pass over 16 rows is the bound, and
 // a set's last pass half empty.  Tiles of 64, 128, 256 rows: a workgroup a CU, so rounds of `cus` tiles, each of Kb steps and a start and end.
 // us per step and per round, measured on full rounds: 0.53 + 3.5, 0.9 + 4.5, 1.45 + 6; with sums in fp32 1.05 + 4, 1.75 + 6.  (2048 x 4096 -> 11008:
@@ -188,7 +193,17 @@ stamp_status_t forward(const stamp_fp8_plan* p, int32_t rows, const int32_t* off
 // bf16 Y 32: 17.9 / 17.4, 48: 24.1 / 18.2; of 1152 -> 4608 32: 8.8 / 9.4, 48: 11.7 / 9.8, fp32 Y 64: 13.5 / 15.1, 96: 19.1 / 15.2; of 8192 -> 1024 64: 22.4 / 18.4;
 // of 590 -> 7231 58: 11.2 / 13.2.  Over 88 layers of 13 to 16000 rows, 100 to 9000 channels and 100 to 15000 columns the choice takes 0.3 % more than the
 // best on average, 6 % at worst.
-// Over 120 products of 8 to 191 sets with 4 to 96 rows a set, gated ones among them, the choice takes 0.6 % more than the best on average, 17 % at worst.
+// Over 120 products of 8 to 191 sets with 4 to 96 rows a set, gated ones among them, every set with as many rows, the choice takes 0.6 % more
+// than the best on average, 17 % at worst.
+//
+// Rows that lie unevenly: the rows kernel walks a set's rows 16 by 16 in that set's workgroups alone, while tiles of 64 rows spread over the CUs.
+// us, rows kernel (the choice) / tiles of 64; "falling": shares 1, 1/2, 1/3, ...; two, one: sets that have all rows.
+//                                     even          half of the sets  falling      two          one
+//   96 over 32 sets, 4096 -> 1536    37 / 36        21 / 23           31 / 28      20 / 21      34 / 21
+//   760 over 64, 4096 -> 1536        80 / 85        72 / 37          117 / 85     142 / 24     236 / 24
+//   1500 over 128, 2048 -> 2048     100 / 112       84 / 55          143 / 120    205 / 21     284 / 22
+//   3000 over 256, 2048 -> 768       81 / 90        71 / 48          171 / 99     302 / 22     561 / 22
+// A rule on rows and sets alone has to lose on one side; this one is right for even loads and loses most where few of many sets are busy.
 namespace {
 constexpr float kStep[2][3] = {{0.53f, 0.9f, 1.45f}, {1.05f, 1.75f, 0.0f}}, kIdle[2][3] = {{0.43f, 0.7f, 1.1f}, {0.9f, 1.3f, 0.0f}},
                 kEnds[2][3] = {{3.5f, 4.5f, 6.0f}, {4.0f, 6.0f, 0.0f}}, kSetEnds[2][3] = {{7.5f, 7.5f, 9.0f}, {9.0f, 8.0f, 0.0f}};
@@ -240,8 +255,8 @@ int stamp_f8_route(int sets, int groups, int Kb, int rows, int wide_sums, int ga
 }
 
 // Tiles that leave most CUs idle in their last round: of one layer, the columns of the whole rounds first, the others in a launch of their own
-// in the tiles that suit them.  2048 x 4096 -> 11008: 344 tiles of 128 x 256 rows are 1.34 rounds, 100.7 us; 256 tiles of 256 rows and 88 of 256
-// in one launch each 95.7.  8192 x 1152 -> 4608 (powers of two): 60.0 -> 56.7.  Over 44 drawn sizes where the estimate fell by 5 % or more the
+// in the tiles that suit them.  2048 x 4096 -> 11008: 344 tiles of 256 rows x 256 columns are 1.34 rounds, 100.7 us; 256 such tiles, then the
+// other columns as 176 tiles of 128 rows 95.7.  8192 x 1152 -> 4608 (powers of two): 60.0 -> 56.7.  Over 44 drawn sizes where the estimate fell by 5 % or more the
 // two launches took 0.78 to 1.04 of the one's time; where it fell by 10 % or more 0.78 to 1.04 as well, by 5 to 10 % mostly nothing: the line.
 F8Cut stamp_f8_cut(int sets, int groups, int Kb, int rows, int wide_sums, int gated, int forced) {
   const TileChoice all = best_tiles(sets, groups, Kb, rows, wide_sums, gated, forced);

@@ -1,7 +1,7 @@
 // Product of the 8-bit floating point layers in tiles of BM rows x 256 places.
 //
 // Eight waves, 2 x 4, of BM / 2 x 64 each; the operands of a block of 128 channels are one stage in LDS, two stages of 256 rows or three of
-// fewer (a step of 128 rows takes 0.5 us, less than a load does).  The weights' stage is
+// fewer (a step of 64 or 128 rows takes 0.4 to 0.9 us, which a load asked for one step ahead does not always meet).  The weights' stage is
 // a copy of the operand image.  The rows' stage is [row][8 pieces of 16 bytes], piece p at p ^ (row / 2 % 8): the 16 lanes that are
 // read at a time then hit all 64 banks once (also where they are lanes 0-3, 12-15 and 20-27, which take pieces f and f + 1 of 8 rows each).
 //
@@ -13,8 +13,9 @@
 // the vector ALU its bound), 256 bytes a row, piece p of 16 at p ^ (row % 16); the weights are widened once per step and wave
 // (conversions among the matrix instructions, see wide_step: in a row of their own they leave the matrix pipe idle in both waves of a SIMD).
 //
-// Bound: the clock under the matrix load.  8192 x 8192 x 8192 425 us, 2.59 PFLOP/s (the instructions alone, operands constant: 4.25; with zeros as
-// operands this kernel 3.05); scales that are powers of two 2.85; sums in fp32 900 us, 1.22 PFLOP/s (instructions with their conversions and additions alone
+// Bound: the clock under the matrix load (1.8 to 1.9 of 2.4 GHz) and the matrix pipe's pauses (busy in 61 to 71 % of those cycles; counters at
+// 8192 x 8192 -> 8192).  There 425 to 448 us, 2.45 to 2.59 PFLOP/s (the instructions alone, operands constant: 4.25; with zeros as operands this
+// kernel 3.05); scales that are powers of two 2.76 to 2.85; sums in fp32 900 us, 1.22 PFLOP/s (instructions with their conversions and additions alone
 // 1.65).  Short depths add a tile's start and end, 3 to 9 us.
 //
 // Few tiles: the depth in parts, each tile by as many workgroups, whose fp32 rows k_f8_join adds up in order.

@@ -70,7 +70,8 @@ def _room(t, gpu):
 
 
 class Fp8Plan:
-    """Owns a stamp_fp8_plan_t: the weights of one layer, or of all experts of one layer."""
+    """Owns a stamp_fp8_plan_t: the weights of one layer, or of all experts of one layer.  W, w_scales and bias are read on the stream: with
+    a stream of one's own they have to live until it has drained."""
 
     def __init__(self, desc: Fp8Desc, W, w_scales=None, bias=None, stream=None):
         import torch
