@@ -193,8 +193,8 @@ stamp_status_t forward(const stamp_fp8_plan* p, int32_t rows, const int32_t* off
 // bf16 Y 32: 17.9 / 17.4, 48: 24.1 / 18.2; of 1152 -> 4608 32: 8.8 / 9.4, 48: 11.7 / 9.8, fp32 Y 64: 13.5 / 15.1, 96: 19.1 / 15.2; of 8192 -> 1024 64: 22.4 / 18.4;
 // of 590 -> 7231 58: 11.2 / 13.2.  Over 88 layers of 13 to 16000 rows, 100 to 9000 channels and 100 to 15000 columns the choice takes 0.3 % more than the
 // best on average, 6 % at worst.
-// Over 120 products of 8 to 191 sets with 4 to 96 rows a set, gated ones among them, every set with as many rows, the choice takes 0.6 % more
-// than the best on average, 17 % at worst.
+// Over 120 products of 8 to 191 sets with 4 to 96 rows a set, gated ones among them, rows dealt at random with all sets alike, the choice takes
+// 0.6 % more than the best on average, 17 % at worst.
 //
 // Rows that lie unevenly: the rows kernel walks a set's rows 16 by 16 in that set's workgroups alone, while tiles of 64 rows spread over the CUs.
 // us, rows kernel (the choice) / tiles of 64; "falling": shares 1, 1/2, 1/3, ...; two, one: sets that have all rows.
