@@ -440,6 +440,59 @@ stamp_status_t stamp_experts_forward(const stamp_fp8_plan_t* up, const stamp_fp8
                                      const void* X_dev, int64_t ld_x, void* Y_dev, int64_t ld_y, void* workspace_dev,
                                      size_t workspace_bytes, void* hip_stream);
 
+/* ---- with an epilogue: activation and residual ----
+ *
+ *     Y = act(X W + bias) + R      in fp32 behind the sums, rounded once
+ *
+ * act: x; max(x, 0); x / (1 + exp(-x)); x Phi(x), Phi the normal distribution; x / (1 + exp(-2 sqrt(2 / pi) (x + 0.044715 x^3))), which is
+ * x (1 + tanh(..)) / 2.  A NaN stays one.  R [rows, d_out] has Y's type, row m at R + m * ld_residual (as ld_y); it may be Y itself (same pointer and
+ * distance of rows) and must not overlap Y otherwise.  residual_dev NULL: none, ld_residual is then not looked at. */
+typedef enum { STAMP_ACT_NONE = 0, STAMP_ACT_RELU = 1, STAMP_ACT_SILU = 2, STAMP_ACT_GELU = 3, STAMP_ACT_GELU_TANH = 4 } stamp_activation_t;
+typedef struct {
+  int32_t activation; /* stamp_activation_t */
+  const void* residual_dev;
+  int64_t ld_residual;
+} stamp_epilogue_t;
+
+/* stamp_fp8_linear_forward, .._q and .._grouped_forward with an epilogue; the plan's workspace is the same. */
+stamp_status_t stamp_fp8_linear_forward_act(const stamp_fp8_plan_t* plan, int32_t rows, const void* X_dev, int64_t ld_x, const stamp_epilogue_t* epilogue,
+                                            void* Y_dev, int64_t ld_y, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+stamp_status_t stamp_fp8_linear_forward_q_act(const stamp_fp8_plan_t* plan, int32_t rows, const uint8_t* codes_dev, const float* scales_dev,
+                                              int64_t ld_scales, const stamp_epilogue_t* epilogue, void* Y_dev, int64_t ld_y, void* workspace_dev,
+                                              size_t workspace_bytes, void* hip_stream);
+stamp_status_t stamp_fp8_grouped_forward_act(const stamp_fp8_plan_t* plan, int32_t rows, const int32_t* offsets_dev, const void* X_dev, int64_t ld_x,
+                                             const stamp_epilogue_t* epilogue, void* Y_dev, int64_t ld_y, void* workspace_dev, size_t workspace_bytes,
+                                             void* hip_stream);
+
+/* The dense MLP:
+ *     h = act(Xq Wup + bias)  in fp32, or, where up is gated,  act(Xq Wgate) * (Xq Wup);     Y = Q8(h) Wdown + bias + R
+ * up: a plan [d_in -> ff] with experts = 0, or a gated one with experts = 1; down: a plan [ff -> d_out] with experts = 0 (or 1 beside a gated up) and
+ * the same scale_format.  X [rows, d_in] in up's x_dtype, Y and R [rows, d_out] in down's y_dtype; up's y_dtype and down's x_dtype are not looked at.
+ * rows <= 2^24, and of a gated up rows * d_in, d_in rounded up to 128, < 2^31.  The epilogue's activation is h's, its residual is added to Y. */
+size_t stamp_mlp_workspace_bytes(const stamp_fp8_plan_t* up, const stamp_fp8_plan_t* down, int32_t rows);
+stamp_status_t stamp_mlp_forward(const stamp_fp8_plan_t* up, const stamp_fp8_plan_t* down, int32_t rows, const void* X_dev, int64_t ld_x,
+                                 const stamp_epilogue_t* epilogue, void* Y_dev, int64_t ld_y, void* workspace_dev, size_t workspace_bytes,
+                                 void* hip_stream);
+
+/* The whole layer of experts, the router's product included:
+ *     logits = X Wrouter^T + bias,    the routing of them as in stamp_route_topk,    Y[t] = R[t] + sum over slots j of  weights[t, j] r[row(t, j)]
+ * with r as in stamp_experts_forward, the epilogue's activation in silu's place.  The router sees X as it is, not Q8 of it; a logit's sum is held in
+ * more than 32 bits (blocks of 32 channels in fp32, those in fp64) and rounded to fp32 once, so that what two near logits compare as hardly
+ * depends on the order of sums.  bias -infinity: an expert out of use.  A token that finds no expert gets R, or zeros.
+ * up, down, X, Y and their limits as in stamp_experts_forward.  routing: its arrays are written, as stamp_route_topk writes them; with 0 tokens its
+ * offsets alone.  The experts' rows are held in fp32 up to the sum, whatever Y's type. */
+typedef struct {
+  const void* W_dev;    /* [experts, d], rows one after the other, aligned as its elements are */
+  int32_t w_dtype;      /* STAMP_F32, STAMP_BF16 */
+  int32_t renormalize;  /* as in stamp_route_topk */
+  const float* bias_dev_or_null; /* [experts] */
+} stamp_router_t;
+/* Bytes of workspace (256-byte aligned pointer) for up to `tokens` tokens with that top_k; 0 for what stamp_moe_forward refuses. */
+size_t stamp_moe_workspace_bytes(const stamp_fp8_plan_t* up, const stamp_fp8_plan_t* down, int32_t tokens, int32_t top_k);
+stamp_status_t stamp_moe_forward(const stamp_router_t* router, const stamp_fp8_plan_t* up, const stamp_fp8_plan_t* down, const stamp_routing_t* routing,
+                                 const void* X_dev, int64_t ld_x, const stamp_epilogue_t* epilogue, void* Y_dev, int64_t ld_y, void* workspace_dev,
+                                 size_t workspace_bytes, void* hip_stream);
+
 /* For tests: a plan's codes [experts][2 if gated][d_out][d_in] and scales in the layout of w_scales_dev, copied to host.
  * Synchronizes the device. */
 stamp_status_t stamp_fp8_debug_weight_codes(const stamp_fp8_plan_t* plan, uint8_t* codes_host, float* scales_host);

@@ -26,6 +26,11 @@ from .fp8 import (  # noqa: F401
     route_topk,
     experts_forward,
     experts_workspace,
+    mlp_forward,
+    mlp_workspace,
+    moe_forward,
+    moe_workspace,
+    ACTIVATIONS,
     STAMP_E4M3,
     STAMP_SCALE_F32,
     STAMP_SCALE_POW2,

@@ -46,7 +46,7 @@ struct StampF8Gemm {
   const uint8_t* A;        // codes [a_rows][Kp], for tiles of wide_sums as bf16
   const float* SA;         // scales [Kb][ld_sa], by row of A
   int64_t ld_sa;
-  const int32_t* index;    // gated: row of A of every row of the product (else the same)
+  const int32_t* index;    // gated: row of A of every row of the product, nullptr: the same (and so it is where not gated)
   int32_t a_rows;
   const void* X;           // not nullptr: A's rows before Q8, quantized by the product itself (few rows)
   int64_t ld_x;
@@ -62,6 +62,9 @@ struct StampF8Gemm {
   int32_t wide_sums;       // products on the bf16 matrix instructions (f8_wide_sums)
   void* Y;                 // rows of N values; gated: codes [rows][ld_y] and scales [ld_y / 128][ld_sh]
   int64_t ld_y;
+  int32_t act;             // stamp_activation_t, of the gate where gated
+  const void* R;           // residual rows in Y's type, or nullptr
+  int64_t ld_r;
   float* SH;
   int64_t ld_sh;
   float* partial;          // [parts][rows][groups * 64] where the depth is split
@@ -108,8 +111,12 @@ hipError_t stamp_launch_f8_tiles(const StampF8Gemm& a, int bm, int parts, hipStr
 inline int f8_wide_sums(const StampF8Gemm& a) { return a.gated || !a.y_bf16; }
 hipError_t stamp_launch_route(const stamp_routing_t& r, const void* logits, int bf16, int64_t ld, int renorm, void* ws, hipStream_t st);
 size_t stamp_route_ws(int tokens, int experts, int top_k);
-hipError_t stamp_launch_combine(const stamp_routing_t& r, const void* rows, int y_bf16, int64_t ld_rows, int nrows, void* Y, int64_t ld_y, int d,
-                                hipStream_t st);
+hipError_t stamp_launch_combine(const stamp_routing_t& r, const void* rows, int rows_bf16, int y_bf16, int64_t ld_rows, int nrows, const void* R, int64_t ld_r,
+                                void* Y, int64_t ld_y, int d, hipStream_t st);
+
+// logits [tokens][experts] = X W^T + bias
+hipError_t stamp_launch_router(const stamp_router_t& router, const void* X, int x_bf16, int64_t ld_x, int tokens, int experts, int d, float* logits,
+                               hipStream_t st);
 
 // ---- device helpers ----
 #ifdef __HIPCC__
@@ -278,6 +285,31 @@ struct Raw16 {
   }
 };
 
+// Residual of 8 columns of a row, p + column: as they are stored, zeros from `left` columns on.
+template <bool BF16>
+struct Residual8 {
+  u4 w[BF16 ? 1 : 2];
+  __device__ __forceinline__ void load(const char* p, int left) {
+#pragma unroll
+    for (int q = 0; q < (BF16 ? 1 : 2); ++q) w[q] = u4{0, 0, 0, 0};
+    if (left >= 8) {
+#pragma unroll
+      for (int q = 0; q < (BF16 ? 1 : 2); ++q) w[q] = reinterpret_cast<const u4_any*>(p)[q];
+      return;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if (j >= left) continue;
+      if constexpr (BF16) w[0][j >> 1] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[j] << (16 * (j & 1));
+      else w[j >> 2][j & 3] = reinterpret_cast<const uint32_t*>(p)[j];
+    }
+  }
+  __device__ __forceinline__ float at(int j) const {
+    if constexpr (BF16) return (j & 1) ? bf16_hi(w[0][j >> 1]) : bf16_lo(w[0][j >> 1]);
+    else return __uint_as_float(w[j >> 2][j & 3]);
+  }
+};
+
 typedef __bf16 b2 __attribute__((ext_vector_type(2)));
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 // 8 codes as bf16: exact
@@ -288,6 +320,62 @@ __device__ __forceinline__ b8 widen8(int lo, int hi) {
 }
 
 __device__ __forceinline__ float silu(float g) { return g / (1.0f + __expf(-g)); }
+
+// x Phi(x).  Phi(-a) exp(a^2 / 2), which falls slowly from 1/2, as a polynomial in 1 / (1 + 0.23 a), fitted for a in 0 .. 14 by least squares with
+// weights raised where the error is largest: 5e-8 of its value.  With the roundings of exp's argument 2.4e-7 of |x| at most, measured over -12 .. 12.
+// 20 instructions, no branch.
+__device__ __forceinline__ float gelu(float x) {
+  const float a = __builtin_fabsf(x), t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.23f, a, 1.0f));
+  float p = -0.07846821454016081f;
+  p = __builtin_fmaf(p, t, 0.29041779012717694f);
+  p = __builtin_fmaf(p, t, -0.2781344748106574f);
+  p = __builtin_fmaf(p, t, 0.3014813343419948f);
+  p = __builtin_fmaf(p, t, -0.032926072837606936f);
+  p = __builtin_fmaf(p, t, 0.11951655952441825f);
+  p = __builtin_fmaf(p, t, 0.08576227432289371f);
+  p = __builtin_fmaf(p, t, 0.09237854797522843f);
+  p = __builtin_fmaf(p, t, -2.776791431630431e-05f);
+  p *= __builtin_amdgcn_exp2f(a * a * -0.72134752044448170f);
+  return x * (x < 0.0f ? p : 1.0f - p);
+}
+// x / (1 + exp(-y)) by the reciprocal instruction, one rounding more than a division
+__device__ __forceinline__ float logistic_times(float x, float y) {
+  return x * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(y * -1.44269504088896341f));
+}
+__device__ __forceinline__ float gelu_tanh(float x) {
+  const float c = 1.59576912160573071f;  // 2 sqrt(2 / pi)
+  return logistic_times(x, x * __builtin_fmaf(x * x, c * 0.044715f, c));
+}
+__device__ __forceinline__ float relu(float x) { return x < 0.0f ? 0.0f : x; }
+// one choice for N values: act is the same in all lanes
+template <int N>
+__device__ __forceinline__ void activate(float (&v)[N], int act) {
+  if (act == STAMP_ACT_RELU) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = relu(v[j]);
+  } else if (act == STAMP_ACT_SILU) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = logistic_times(v[j], v[j]);
+  } else if (act == STAMP_ACT_GELU) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = gelu(v[j]);
+  } else if (act == STAMP_ACT_GELU_TANH) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) v[j] = gelu_tanh(v[j]);
+  }
+}
+// act(g) u; silu as the gated products have had it, by a division
+template <int N>
+__device__ __forceinline__ void gate(float (&g)[N], const float (&u)[N], int act) {
+  if (act == STAMP_ACT_SILU) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) g[j] = silu(g[j]);
+  } else {
+    activate(g, act);
+  }
+#pragma unroll
+  for (int j = 0; j < N; ++j) g[j] *= u[j];
+}
 
 }  // namespace f8
 #endif

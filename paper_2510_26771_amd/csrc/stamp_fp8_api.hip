@@ -41,6 +41,7 @@ StampF8Gemm gemm_args(const stamp_fp8_plan* p) {
   a.pow2 = p->desc.scale_format == STAMP_SCALE_POW2;
   a.gated = p->desc.gated;
   a.y_bf16 = p->desc.y_dtype == STAMP_BF16;
+  a.act = p->desc.gated ? STAMP_ACT_SILU : STAMP_ACT_NONE;
   a.wide_sums = f8_wide_sums(a);
   a.forced = p->forced;
   return a;
@@ -76,6 +77,7 @@ hipError_t product(const StampF8Gemm& a, hipStream_t st) {
   rest.SW += (size_t)(cut.groups / 2) * a.Kb;
   if (a.bias != nullptr) rest.bias += columns;
   rest.Y = static_cast<char*>(a.Y) + (size_t)columns * (a.y_bf16 ? 2 : 4);
+  if (a.R != nullptr) rest.R = static_cast<const char*>(a.R) + (size_t)columns * (a.y_bf16 ? 2 : 4);
   const hipError_t e = stamp_launch_f8_tiles(first, 64 << cut.size, cut.parts, st);
   return e != hipSuccess ? e : stamp_launch_f8_tiles(rest, 64 << cut.rest_size, cut.rest_parts, st);
 }
@@ -99,7 +101,7 @@ struct ExpertsWs {
   size_t codes, scales, h, sh, rows, wide, partial, total;
   int64_t ld_rows;
 };
-ExpertsWs experts_ws(const stamp_fp8_plan* up, const stamp_fp8_plan* down, int32_t tokens, int32_t top_k) {
+ExpertsWs experts_ws(const stamp_fp8_plan* up, const stamp_fp8_plan* down, int32_t tokens, int32_t top_k, bool wide_rows = false) {
   ExpertsWs w;
   const int64_t slots = (int64_t)tokens * top_k, ld = scales_ld((int32_t)slots);
   w.codes = 0;
@@ -112,7 +114,7 @@ ExpertsWs experts_ws(const stamp_fp8_plan* up, const stamp_fp8_plan* down, int32
   // they are the most bytes of the call (8192 tokens, 8 of 64 experts, 4096 -> 1536: down product 529 -> 647 us, weighted sum 122 -> 242, the whole
   // 2200 -> 2447).  An fp32 Y has them in fp32.
   // The up product writes codes of one byte; a down product that wants them as bf16 has them widened here
-  w.wide = w.rows + align256((size_t)slots * w.ld_rows * type_size(down->desc.y_dtype));
+  w.wide = w.rows + align256((size_t)slots * w.ld_rows * (wide_rows ? 4 : type_size(down->desc.y_dtype)));
   w.partial = w.wide + (code_bytes(down) == 2 ? align256((size_t)slots * down->Kp * 2) : 0);
   w.total = w.partial + align256(stamp_f8_partial_bytes(down->groups, (int32_t)slots));
   return w;
@@ -141,9 +143,26 @@ stamp_status_t check_routing(const stamp_routing_t* r) {
 
 stamp_status_t done(hipError_t e) { return e == hipSuccess ? STAMP_OK : STAMP_ERR_DEVICE; }
 
+// nullptr: no epilogue.  in_place: X may be Y (it is not read any more where Y is written).
+stamp_status_t check_epilogue(const stamp_epilogue_t* e, int32_t rows, int32_t y_dtype, int32_t d_out, const void* Y, int64_t ld_y, const void* X, bool in_place) {
+  if (e == nullptr) return STAMP_OK;
+  if (e->activation < STAMP_ACT_NONE || e->activation > STAMP_ACT_GELU_TANH) return STAMP_ERR_SHAPE;
+  if (!in_place && X != nullptr && X == Y) return STAMP_ERR_SHAPE;
+  if (e->residual_dev == nullptr) return STAMP_OK;
+  const stamp_status_t s = check_matrix(e->residual_dev, y_dtype, e->ld_residual, d_out);
+  if (s != STAMP_OK) return s;
+  return e->residual_dev == Y && rows > 1 && e->ld_residual != ld_y ? STAMP_ERR_SHAPE : STAMP_OK;
+}
+void give_epilogue(StampF8Gemm* a, const stamp_epilogue_t* e) {
+  if (e == nullptr) return;
+  a->act = e->activation;
+  a->R = e->residual_dev;
+  a->ld_r = e->ld_residual;
+}
+
 // linear_forward, grouped_forward
-stamp_status_t forward(const stamp_fp8_plan* p, int32_t rows, const int32_t* offsets, bool grouped, const void* X, int64_t ld_x, void* Y, int64_t ld_y,
-                       void* ws, size_t ws_bytes, hipStream_t st) {
+stamp_status_t forward(const stamp_fp8_plan* p, int32_t rows, const int32_t* offsets, bool grouped, const void* X, int64_t ld_x, const stamp_epilogue_t* ep,
+                       void* Y, int64_t ld_y, void* ws, size_t ws_bytes, hipStream_t st) {
   if (p == nullptr) return STAMP_ERR_NULL;
   if (p->desc.gated || (p->desc.experts > 0) != grouped) return STAMP_ERR_UNSUPPORTED;
   if (rows < 0 || rows > kMaxRows) return STAMP_ERR_SHAPE;
@@ -151,12 +170,14 @@ stamp_status_t forward(const stamp_fp8_plan* p, int32_t rows, const int32_t* off
   if (rows == 0) return STAMP_OK;
   stamp_status_t s = check_matrix(X, p->desc.x_dtype, ld_x, p->desc.d_in);
   if (s == STAMP_OK) s = check_matrix(Y, p->desc.y_dtype, ld_y, p->desc.d_out);
+  if (s == STAMP_OK) s = check_epilogue(ep, rows, p->desc.y_dtype, p->desc.d_out, Y, ld_y, X, false);
   const LinearWs w = linear_ws(p, rows);
   if (s == STAMP_OK) s = check_ws(ws, ws_bytes, w.total);
   if (s != STAMP_OK) return s;
   uint8_t* codes = static_cast<uint8_t*>(ws) + w.codes;
   float* scales = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + w.scales);
   StampF8Gemm a = gemm_args(p);
+  give_epilogue(&a, ep);
   if (takes_x(a, rows)) {
     give_x(&a, p->desc, rows, X, ld_x);
   } else if (stamp_launch_f8_quant(X, p->desc.x_dtype == STAMP_BF16, ld_x, rows, p->desc.d_in, a.pow2, wide_codes(a, rows), codes, scales, scales_ld(rows),
@@ -172,6 +193,147 @@ stamp_status_t forward(const stamp_fp8_plan* p, int32_t rows, const int32_t* off
   a.Y = Y;
   a.ld_y = ld_y;
   return done(product(a, st));
+}
+
+stamp_status_t forward_q(const stamp_fp8_plan* p, int32_t rows, const uint8_t* codes, const float* scales, int64_t ld_scales, const stamp_epilogue_t* ep,
+                         void* Y, int64_t ld_y, void* ws, size_t ws_bytes, hipStream_t st) {
+  if (p == nullptr) return STAMP_ERR_NULL;
+  if (p->desc.experts > 0) return STAMP_ERR_UNSUPPORTED;
+  if (rows < 0 || rows > kMaxRows) return STAMP_ERR_SHAPE;
+  if (rows == 0) return STAMP_OK;
+  if (codes == nullptr || scales == nullptr) return STAMP_ERR_NULL;
+  if (ld_scales < rows || ld_scales % 4 != 0 || (reinterpret_cast<uintptr_t>(codes) | reinterpret_cast<uintptr_t>(scales)) % 16 != 0) return STAMP_ERR_SHAPE;
+  stamp_status_t s = check_matrix(Y, p->desc.y_dtype, ld_y, p->desc.d_out);
+  if (s == STAMP_OK) s = check_epilogue(ep, rows, p->desc.y_dtype, p->desc.d_out, Y, ld_y, nullptr, true);
+  const LinearWs w = linear_ws(p, rows);
+  if (s == STAMP_OK) s = check_ws(ws, ws_bytes, w.total);
+  if (s != STAMP_OK) return s;
+  StampF8Gemm a = gemm_args(p);
+  give_epilogue(&a, ep);
+  a.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + w.partial);
+  a.A = codes;
+  if (wide_codes(a, rows)) {
+    uint8_t* wide = static_cast<uint8_t*>(ws);
+    if (stamp_launch_f8_widen(codes, (int64_t)rows * p->Kp, wide, st) != hipSuccess) return STAMP_ERR_DEVICE;
+    a.A = wide;
+  }
+  a.SA = scales;
+  a.ld_sa = ld_scales;
+  a.a_rows = a.rows = rows;
+  a.Y = Y;
+  a.ld_y = ld_y;
+  return done(product(a, st));
+}
+
+// Places of the experts' MLP: the up product's rows of X, its results as codes, the rows behind the down product.
+struct ExpertsRun {
+  const stamp_fp8_plan *up, *down;
+  const stamp_routing_t* r;
+  const void* X;
+  int64_t ld_x;
+  stamp_epilogue_t ep;
+  void* Y;
+  int64_t ld_y;
+  bool wide_rows;  // the rows behind the down product in fp32 whatever Y's type
+};
+stamp_status_t check_experts(const ExpertsRun& e) {
+  const stamp_fp8_plan *up = e.up, *down = e.down;
+  if (!up->desc.gated || down->desc.gated || down->desc.experts == 0) return STAMP_ERR_UNSUPPORTED;
+  if (up->desc.experts != down->desc.experts || up->desc.d_out != down->desc.d_in || up->desc.d_in != down->desc.d_out ||
+      up->desc.scale_format != down->desc.scale_format || e.r->experts != up->desc.experts)
+    return STAMP_ERR_SHAPE;
+  const stamp_status_t s = check_routing(e.r);
+  if (s != STAMP_OK) return s;
+  if ((int64_t)e.r->tokens * e.r->top_k > kMaxRows || (int64_t)e.r->tokens * up->Kp * 2 >= (int64_t)0xfffffff0u) return STAMP_ERR_UNSUPPORTED;
+  return STAMP_OK;
+}
+stamp_status_t check_experts_rows(const ExpertsRun& e) {
+  const stamp_status_t s = check_matrix(e.X, e.up->desc.x_dtype, e.ld_x, e.up->desc.d_in);
+  return s == STAMP_OK ? check_matrix(e.Y, e.down->desc.y_dtype, e.ld_y, e.down->desc.d_out) : s;
+}
+// up product, down product, weighted sum, for a routing that is there
+stamp_status_t run_experts(const ExpertsRun& e, uint8_t* ws, hipStream_t st) {
+  const stamp_fp8_plan *up = e.up, *down = e.down;
+  const stamp_routing_t* r = e.r;
+  const ExpertsWs w = experts_ws(up, down, r->tokens, r->top_k, e.wide_rows);
+  const int32_t slots = r->tokens * r->top_k;
+  const int64_t ld = scales_ld(slots);
+
+  StampF8Gemm a = gemm_args(up);
+  a.act = e.ep.activation;
+  float* scales = reinterpret_cast<float*>(ws + w.scales);
+  if (takes_x(a, slots)) {
+    give_x(&a, up->desc, slots, e.X, e.ld_x);
+  } else if (stamp_launch_f8_quant(e.X, up->desc.x_dtype == STAMP_BF16, e.ld_x, r->tokens, up->desc.d_in, a.pow2, wide_codes(a, slots), ws + w.codes, scales,
+                                   scales_ld(r->tokens), st) != hipSuccess) {
+    return STAMP_ERR_DEVICE;
+  }
+  a.A = ws + w.codes;
+  a.SA = scales;
+  a.ld_sa = scales_ld(r->tokens);
+  a.index = r->token_of_row_dev;
+  a.a_rows = r->tokens;
+  a.rows = slots;
+  a.offsets = r->offsets_dev;
+  a.Y = ws + w.h;
+  a.ld_y = down->Kp;
+  a.SH = reinterpret_cast<float*>(ws + w.sh);
+  a.ld_sh = ld;
+  if (product(a, st) != hipSuccess) return STAMP_ERR_DEVICE;
+
+  StampF8Gemm b = gemm_args(down);
+  b.partial = reinterpret_cast<float*>(ws + w.partial);
+  b.A = ws + w.h;
+  if (wide_codes(b, slots)) {
+    if (stamp_launch_f8_widen(b.A, (int64_t)slots * down->Kp, ws + w.wide, st) != hipSuccess) return STAMP_ERR_DEVICE;
+    b.A = ws + w.wide;
+  }
+  b.SA = a.SH;
+  b.ld_sa = ld;
+  b.a_rows = b.rows = slots;
+  b.offsets = r->offsets_dev;
+  b.Y = ws + w.rows;
+  b.ld_y = w.ld_rows;
+  if (e.wide_rows) b.y_bf16 = 0;  // the instructions stay those of Y's type
+  if (product(b, st) != hipSuccess) return STAMP_ERR_DEVICE;
+  return done(stamp_launch_combine(*r, b.Y, b.y_bf16, down->desc.y_dtype == STAMP_BF16, w.ld_rows, slots, e.ep.residual_dev, e.ep.ld_residual, e.Y, e.ld_y, down->desc.d_out, st));
+}
+
+// The dense MLP's places: the rows of X as codes, h in fp32 or as codes, parts of the depth.
+struct MlpWs {
+  size_t codes, scales, h, hcodes, hscales, partial, total;
+};
+int64_t mlp_ld_h(const stamp_fp8_plan* up) { return up->desc.d_out; }
+MlpWs mlp_ws(const stamp_fp8_plan* up, const stamp_fp8_plan* down, int32_t rows) {
+  MlpWs w;
+  w.codes = 0;
+  w.scales = align256((size_t)rows * up->Kp * 2);  // bf16 codes: h is a sum in fp32
+  w.h = w.scales + align256((size_t)up->Kb * scales_ld(rows) * sizeof(float));
+  w.hcodes = w.h + (up->desc.gated ? 0 : align256((size_t)rows * mlp_ld_h(up) * sizeof(float)));
+  w.hscales = w.hcodes + align256((size_t)rows * down->Kp * (up->desc.gated && code_bytes(down) == 2 ? 3 : code_bytes(down)));
+  w.partial = w.hscales + align256((size_t)down->Kb * scales_ld(rows) * sizeof(float));
+  const size_t pu = up->desc.gated ? 0 : stamp_f8_partial_bytes(up->groups, rows), pd = stamp_f8_partial_bytes(down->groups, rows);
+  w.total = w.partial + align256(pu > pd ? pu : pd);
+  return w;
+}
+stamp_status_t check_mlp(const stamp_fp8_plan* up, const stamp_fp8_plan* down) {
+  if (up == nullptr || down == nullptr) return STAMP_ERR_NULL;
+  if (down->desc.gated || up->desc.experts != (up->desc.gated ? 1 : 0) || down->desc.experts > up->desc.experts) return STAMP_ERR_UNSUPPORTED;
+  if (up->desc.d_out != down->desc.d_in || up->desc.scale_format != down->desc.scale_format) return STAMP_ERR_SHAPE;
+  return STAMP_OK;
+}
+
+// The layer of experts' places: logits and the router's, then those of the experts.
+struct MoeWs {
+  size_t logits, route, experts, total;
+};
+MoeWs moe_ws(const stamp_fp8_plan* up, const stamp_fp8_plan* down, int32_t tokens, int32_t top_k) {
+  MoeWs w;
+  w.logits = 0;
+  w.route = align256((size_t)tokens * up->desc.experts * sizeof(float));
+  w.experts = w.route + align256(stamp_route_ws(tokens, up->desc.experts, top_k));
+  w.total = w.experts + experts_ws(up, down, tokens, top_k, true).total;
+  return w;
 }
 
 }  // namespace
@@ -362,40 +524,111 @@ stamp_status_t stamp_fp8_quantize_act(const stamp_fp8_plan_t* p, int32_t rows, c
 
 stamp_status_t stamp_fp8_linear_forward(const stamp_fp8_plan_t* p, int32_t rows, const void* X_dev, int64_t ld_x, void* Y_dev, int64_t ld_y,
                                         void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
-  return forward(p, rows, nullptr, false, X_dev, ld_x, Y_dev, ld_y, workspace_dev, workspace_bytes, reinterpret_cast<hipStream_t>(hip_stream));
+  return forward(p, rows, nullptr, false, X_dev, ld_x, nullptr, Y_dev, ld_y, workspace_dev, workspace_bytes, reinterpret_cast<hipStream_t>(hip_stream));
+}
+stamp_status_t stamp_fp8_linear_forward_act(const stamp_fp8_plan_t* p, int32_t rows, const void* X_dev, int64_t ld_x, const stamp_epilogue_t* epilogue,
+                                            void* Y_dev, int64_t ld_y, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
+  if (epilogue == nullptr) return STAMP_ERR_NULL;
+  return forward(p, rows, nullptr, false, X_dev, ld_x, epilogue, Y_dev, ld_y, workspace_dev, workspace_bytes, reinterpret_cast<hipStream_t>(hip_stream));
 }
 
 stamp_status_t stamp_fp8_linear_forward_q(const stamp_fp8_plan_t* p, int32_t rows, const uint8_t* codes_dev, const float* scales_dev, int64_t ld_scales,
                                           void* Y_dev, int64_t ld_y, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
-  if (p == nullptr) return STAMP_ERR_NULL;
-  if (p->desc.experts > 0) return STAMP_ERR_UNSUPPORTED;
-  if (rows < 0 || rows > kMaxRows) return STAMP_ERR_SHAPE;
-  if (rows == 0) return STAMP_OK;
-  if (codes_dev == nullptr || scales_dev == nullptr) return STAMP_ERR_NULL;
-  if (ld_scales < rows || ld_scales % 4 != 0 || (reinterpret_cast<uintptr_t>(codes_dev) | reinterpret_cast<uintptr_t>(scales_dev)) % 16 != 0) return STAMP_ERR_SHAPE;
-  stamp_status_t s = check_matrix(Y_dev, p->desc.y_dtype, ld_y, p->desc.d_out);
-  if (s == STAMP_OK) s = check_ws(workspace_dev, workspace_bytes, linear_ws(p, rows).total);
-  if (s != STAMP_OK) return s;
-  hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
-  StampF8Gemm a = gemm_args(p);
-  a.partial = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace_dev) + linear_ws(p, rows).partial);
-  a.A = codes_dev;
-  if (wide_codes(a, rows)) {
-    uint8_t* wide = static_cast<uint8_t*>(workspace_dev);
-    if (stamp_launch_f8_widen(codes_dev, (int64_t)rows * p->Kp, wide, st) != hipSuccess) return STAMP_ERR_DEVICE;
-    a.A = wide;
-  }
-  a.SA = scales_dev;
-  a.ld_sa = ld_scales;
-  a.a_rows = a.rows = rows;
-  a.Y = Y_dev;
-  a.ld_y = ld_y;
-  return done(product(a, st));
+  return forward_q(p, rows, codes_dev, scales_dev, ld_scales, nullptr, Y_dev, ld_y, workspace_dev, workspace_bytes, reinterpret_cast<hipStream_t>(hip_stream));
+}
+stamp_status_t stamp_fp8_linear_forward_q_act(const stamp_fp8_plan_t* p, int32_t rows, const uint8_t* codes_dev, const float* scales_dev, int64_t ld_scales,
+                                              const stamp_epilogue_t* epilogue, void* Y_dev, int64_t ld_y, void* workspace_dev, size_t workspace_bytes,
+                                              void* hip_stream) {
+  if (epilogue == nullptr) return STAMP_ERR_NULL;
+  return forward_q(p, rows, codes_dev, scales_dev, ld_scales, epilogue, Y_dev, ld_y, workspace_dev, workspace_bytes, reinterpret_cast<hipStream_t>(hip_stream));
 }
 
 stamp_status_t stamp_fp8_grouped_forward(const stamp_fp8_plan_t* p, int32_t rows, const int32_t* offsets_dev, const void* X_dev, int64_t ld_x, void* Y_dev,
                                          int64_t ld_y, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
-  return forward(p, rows, offsets_dev, true, X_dev, ld_x, Y_dev, ld_y, workspace_dev, workspace_bytes, reinterpret_cast<hipStream_t>(hip_stream));
+  return forward(p, rows, offsets_dev, true, X_dev, ld_x, nullptr, Y_dev, ld_y, workspace_dev, workspace_bytes, reinterpret_cast<hipStream_t>(hip_stream));
+}
+stamp_status_t stamp_fp8_grouped_forward_act(const stamp_fp8_plan_t* p, int32_t rows, const int32_t* offsets_dev, const void* X_dev, int64_t ld_x,
+                                             const stamp_epilogue_t* epilogue, void* Y_dev, int64_t ld_y, void* workspace_dev, size_t workspace_bytes,
+                                             void* hip_stream) {
+  if (epilogue == nullptr) return STAMP_ERR_NULL;
+  return forward(p, rows, offsets_dev, true, X_dev, ld_x, epilogue, Y_dev, ld_y, workspace_dev, workspace_bytes, reinterpret_cast<hipStream_t>(hip_stream));
+}
+
+size_t stamp_mlp_workspace_bytes(const stamp_fp8_plan_t* up, const stamp_fp8_plan_t* down, int32_t rows) {
+  if (check_mlp(up, down) != STAMP_OK || rows < 0 || rows > kMaxRows) return 0;
+  return mlp_ws(up, down, rows).total;
+}
+
+stamp_status_t stamp_mlp_forward(const stamp_fp8_plan_t* up, const stamp_fp8_plan_t* down, int32_t rows, const void* X_dev, int64_t ld_x,
+                                 const stamp_epilogue_t* epilogue, void* Y_dev, int64_t ld_y, void* workspace_dev, size_t workspace_bytes,
+                                 void* hip_stream) {
+  if (epilogue == nullptr) return STAMP_ERR_NULL;
+  stamp_status_t s = check_mlp(up, down);
+  if (s != STAMP_OK) return s;
+  if (rows < 0 || rows > kMaxRows) return STAMP_ERR_SHAPE;
+  if (up->desc.gated && (int64_t)rows * up->Kp * 2 >= (int64_t)0xfffffff0u) return STAMP_ERR_UNSUPPORTED;
+  if (rows == 0) return STAMP_OK;
+  s = check_matrix(X_dev, up->desc.x_dtype, ld_x, up->desc.d_in);
+  if (s == STAMP_OK) s = check_matrix(Y_dev, down->desc.y_dtype, ld_y, down->desc.d_out);
+  if (s == STAMP_OK) s = check_epilogue(epilogue, rows, down->desc.y_dtype, down->desc.d_out, Y_dev, ld_y, X_dev, true);
+  const MlpWs w = mlp_ws(up, down, rows);
+  if (s == STAMP_OK) s = check_ws(workspace_dev, workspace_bytes, w.total);
+  if (s != STAMP_OK) return s;
+  hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
+  uint8_t* ws = static_cast<uint8_t*>(workspace_dev);
+
+  StampF8Gemm a = gemm_args(up);
+  a.y_bf16 = 0;  // h in fp32
+  a.wide_sums = f8_wide_sums(a);
+  if (a.forced == STAMP_FP8_ROUTE_TILES_256) a.forced = 0;
+  a.act = epilogue->activation;
+  float* scales = reinterpret_cast<float*>(ws + w.scales);
+  if (takes_x(a, rows)) {
+    give_x(&a, up->desc, rows, X_dev, ld_x);
+  } else if (stamp_launch_f8_quant(X_dev, up->desc.x_dtype == STAMP_BF16, ld_x, rows, up->desc.d_in, a.pow2, wide_codes(a, rows), ws + w.codes, scales,
+                                   scales_ld(rows), st) != hipSuccess) {
+    return STAMP_ERR_DEVICE;
+  }
+  a.A = ws + w.codes;
+  a.SA = scales;
+  a.ld_sa = scales_ld(rows);
+  a.a_rows = a.rows = rows;
+  a.partial = reinterpret_cast<float*>(ws + w.partial);
+  StampF8Gemm b = gemm_args(down);
+  b.R = epilogue->residual_dev;
+  b.ld_r = epilogue->ld_residual;
+  b.partial = a.partial;
+  b.A = ws + w.hcodes;
+  b.SA = reinterpret_cast<float*>(ws + w.hscales);
+  b.ld_sa = scales_ld(rows);
+  b.a_rows = b.rows = rows;
+  b.Y = Y_dev;
+  b.ld_y = ld_y;
+  if (up->desc.gated) {
+    a.Y = ws + w.hcodes;
+    a.ld_y = down->Kp;
+    a.SH = reinterpret_cast<float*>(ws + w.hscales);
+    a.ld_sh = b.ld_sa;
+    if (product(a, st) != hipSuccess) return STAMP_ERR_DEVICE;
+    if (wide_codes(b, rows)) {
+      uint8_t* wide = ws + w.hcodes + (size_t)rows * down->Kp;
+      if (stamp_launch_f8_widen(b.A, (int64_t)rows * down->Kp, wide, st) != hipSuccess) return STAMP_ERR_DEVICE;
+      b.A = wide;
+    }
+  } else {
+    a.Y = ws + w.h;
+    a.ld_y = mlp_ld_h(up);
+    if (product(a, st) != hipSuccess) return STAMP_ERR_DEVICE;
+    stamp_fp8_desc_t h = down->desc;
+    h.x_dtype = STAMP_F32;
+    if (takes_x(b, rows)) {
+      give_x(&b, h, rows, a.Y, a.ld_y);
+    } else if (stamp_launch_f8_quant(a.Y, 0, a.ld_y, rows, h.d_in, b.pow2, wide_codes(b, rows), ws + w.hcodes, reinterpret_cast<float*>(ws + w.hscales), b.ld_sa,
+                                     st) != hipSuccess) {
+      return STAMP_ERR_DEVICE;
+    }
+  }
+  return done(product(b, st));
 }
 
 size_t stamp_route_workspace_bytes(int32_t tokens, int32_t experts, int32_t top_k) {
@@ -423,60 +656,48 @@ size_t stamp_experts_workspace_bytes(const stamp_fp8_plan_t* up, const stamp_fp8
 stamp_status_t stamp_experts_forward(const stamp_fp8_plan_t* up, const stamp_fp8_plan_t* down, const stamp_routing_t* r, const void* X_dev, int64_t ld_x,
                                      void* Y_dev, int64_t ld_y, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
   if (up == nullptr || down == nullptr || r == nullptr) return STAMP_ERR_NULL;
-  if (!up->desc.gated || down->desc.gated || down->desc.experts == 0) return STAMP_ERR_UNSUPPORTED;
-  if (up->desc.experts != down->desc.experts || up->desc.d_out != down->desc.d_in || up->desc.d_in != down->desc.d_out ||
-      up->desc.scale_format != down->desc.scale_format || r->experts != up->desc.experts)
-    return STAMP_ERR_SHAPE;
-  stamp_status_t s = check_routing(r);
+  const ExpertsRun e = {up, down, r, X_dev, ld_x, {STAMP_ACT_SILU, nullptr, 0}, Y_dev, ld_y, false};
+  stamp_status_t s = check_experts(e);
   if (s != STAMP_OK) return s;
-  if ((int64_t)r->tokens * r->top_k > kMaxRows || (int64_t)r->tokens * up->Kp * 2 >= (int64_t)0xfffffff0u) return STAMP_ERR_UNSUPPORTED;
   if (r->tokens == 0) return STAMP_OK;
-  s = check_matrix(X_dev, up->desc.x_dtype, ld_x, up->desc.d_in);
-  if (s == STAMP_OK) s = check_matrix(Y_dev, down->desc.y_dtype, ld_y, down->desc.d_out);
-  const ExpertsWs w = experts_ws(up, down, r->tokens, r->top_k);
+  s = check_experts_rows(e);
+  if (s == STAMP_OK) s = check_ws(workspace_dev, workspace_bytes, experts_ws(up, down, r->tokens, r->top_k).total);
+  if (s != STAMP_OK) return s;
+  return run_experts(e, static_cast<uint8_t*>(workspace_dev), reinterpret_cast<hipStream_t>(hip_stream));
+}
+
+size_t stamp_moe_workspace_bytes(const stamp_fp8_plan_t* up, const stamp_fp8_plan_t* down, int32_t tokens, int32_t top_k) {
+  if (up == nullptr || down == nullptr) return 0;
+  int32_t some = 0;  // an address, for the checks
+  const stamp_routing_t r = {tokens, up->desc.experts, top_k, &some, reinterpret_cast<float*>(&some), &some, &some, &some};
+  const ExpertsRun e = {up, down, &r, nullptr, 0, {STAMP_ACT_SILU, nullptr, 0}, nullptr, 0, true};
+  return check_experts(e) == STAMP_OK ? moe_ws(up, down, tokens, top_k).total : 0;
+}
+
+stamp_status_t stamp_moe_forward(const stamp_router_t* router, const stamp_fp8_plan_t* up, const stamp_fp8_plan_t* down, const stamp_routing_t* r,
+                                 const void* X_dev, int64_t ld_x, const stamp_epilogue_t* epilogue, void* Y_dev, int64_t ld_y, void* workspace_dev,
+                                 size_t workspace_bytes, void* hip_stream) {
+  if (router == nullptr || up == nullptr || down == nullptr || r == nullptr || epilogue == nullptr) return STAMP_ERR_NULL;
+  const ExpertsRun e = {up, down, r, X_dev, ld_x, *epilogue, Y_dev, ld_y, true};
+  stamp_status_t s = check_experts(e);
+  if (s != STAMP_OK) return s;
+  if (!is_float_type(router->w_dtype) || router->renormalize < 0 || router->renormalize > 1) return STAMP_ERR_SHAPE;
+  if (epilogue->activation < STAMP_ACT_NONE || epilogue->activation > STAMP_ACT_GELU_TANH) return STAMP_ERR_SHAPE;
+  if (r->tokens > 0) {
+    s = check_matrix(router->W_dev, router->w_dtype, up->desc.d_in, up->desc.d_in);
+    if (s == STAMP_OK) s = check_experts_rows(e);
+    if (s == STAMP_OK) s = check_epilogue(epilogue, r->tokens, down->desc.y_dtype, down->desc.d_out, Y_dev, ld_y, X_dev, true);
+  }
+  const MoeWs w = moe_ws(up, down, r->tokens, r->top_k);
   if (s == STAMP_OK) s = check_ws(workspace_dev, workspace_bytes, w.total);
   if (s != STAMP_OK) return s;
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
   uint8_t* ws = static_cast<uint8_t*>(workspace_dev);
-  const int32_t slots = r->tokens * r->top_k;
-  const int64_t ld = scales_ld(slots);
-
-  StampF8Gemm a = gemm_args(up);
-  float* scales = reinterpret_cast<float*>(ws + w.scales);
-  if (takes_x(a, slots)) {
-    give_x(&a, up->desc, slots, X_dev, ld_x);
-  } else if (stamp_launch_f8_quant(X_dev, up->desc.x_dtype == STAMP_BF16, ld_x, r->tokens, up->desc.d_in, a.pow2, wide_codes(a, slots), ws + w.codes, scales,
-                                   scales_ld(r->tokens), st) != hipSuccess) {
+  float* logits = reinterpret_cast<float*>(ws + w.logits);
+  if (r->tokens > 0 && stamp_launch_router(*router, X_dev, up->desc.x_dtype == STAMP_BF16, ld_x, r->tokens, r->experts, up->desc.d_in, logits, st) != hipSuccess)
     return STAMP_ERR_DEVICE;
-  }
-  a.A = ws + w.codes;
-  a.SA = scales;
-  a.ld_sa = scales_ld(r->tokens);
-  a.index = r->token_of_row_dev;
-  a.a_rows = r->tokens;
-  a.rows = slots;
-  a.offsets = r->offsets_dev;
-  a.Y = ws + w.h;
-  a.ld_y = down->Kp;
-  a.SH = reinterpret_cast<float*>(ws + w.sh);
-  a.ld_sh = ld;
-  if (product(a, st) != hipSuccess) return STAMP_ERR_DEVICE;
-
-  StampF8Gemm b = gemm_args(down);
-  b.partial = reinterpret_cast<float*>(ws + w.partial);
-  b.A = ws + w.h;
-  if (wide_codes(b, slots)) {
-    if (stamp_launch_f8_widen(b.A, (int64_t)slots * down->Kp, ws + w.wide, st) != hipSuccess) return STAMP_ERR_DEVICE;
-    b.A = ws + w.wide;
-  }
-  b.SA = a.SH;
-  b.ld_sa = ld;
-  b.a_rows = b.rows = slots;
-  b.offsets = r->offsets_dev;
-  b.Y = ws + w.rows;
-  b.ld_y = w.ld_rows;
-  if (product(b, st) != hipSuccess) return STAMP_ERR_DEVICE;
-  return done(stamp_launch_combine(*r, b.Y, b.y_bf16, w.ld_rows, slots, Y_dev, ld_y, down->desc.d_out, st));
+  if (stamp_launch_route(*r, logits, 0, r->experts, router->renormalize, ws + w.route, st) != hipSuccess) return STAMP_ERR_DEVICE;
+  return r->tokens > 0 ? run_experts(e, ws + w.experts, st) : STAMP_OK;
 }
 
 stamp_status_t stamp_fp8_debug_weight_codes(const stamp_fp8_plan_t* p, uint8_t* codes_host, float* scales_host) {

@@ -44,12 +44,15 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void* p) {
 // How the products are summed: FP8 instructions with the scales by multiplication or as their own, or bf16 instructions (f8_wide_sums).
 enum Sums { kScaled, kPow2, kWide };
 
+// What becomes of the sums: rows of Y, the same with activation and residual, codes of act(gate) * up.
+enum Out { kRows, kRowsAct, kGated };
+
 [[maybe_unused]] constexpr int kMaxBlocks = 65536 / kF8Block;
 
-template <int BM, Sums SUMS, bool GATED>
+template <int BM, Sums SUMS, Out OUT>
 __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  constexpr bool POW2 = SUMS == kPow2, WIDE = SUMS == kWide;
+  constexpr bool POW2 = SUMS == kPow2, WIDE = SUMS == kWide, GATED = OUT == kGated;
   constexpr int kRowBytes = WIDE ? 256 : 128;
   constexpr int kStageA = BM * kRowBytes, kStageB = 4 * kF8GroupBytes;
   constexpr int MI = BM / 32;         // row blocks of 16 per wave
@@ -281,7 +284,7 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
 #pragma unroll
   for (int i = 0; i <= LA; ++i) {
     from[i] = min(i < LA ? (WIDE ? (i * 512 + t) >> 4 : (i * 512 + t) >> 3) : t, nrows - 1);
-    if constexpr (GATED) from[i] = a.index[row0 + from[i]];
+    if constexpr (GATED) from[i] = a.index != nullptr ? a.index[row0 + from[i]] : row0 + from[i];
   }
   __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -376,6 +379,20 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
     // (8192 x 1152 -> 4607 79 us, rows 4608 apart 58): there a lane stores its words from the second element on, the last one with the next lane's
     // first element, and the ends of the wave's 64 columns one by one.
     const bool between = bf16 && ((reinterpret_cast<uintptr_t>(base) | ld) & 2) != 0 && 64 * g + 64 <= N;
+    // residual: of the row block being worked on and the next, which is on its way meanwhile
+    constexpr bool kBf16 = !WIDE;  // Y's type (f8_wide_sums)
+    [[maybe_unused]] Residual8<kBf16> res[2][2];
+    const bool add_r = OUT == kRowsAct && whole && a.R != nullptr;
+    [[maybe_unused]] auto ask = [&](int mi) __attribute__((always_inline)) {
+      const uint32_t ld_r = (uint32_t)a.ld_r * (kBf16 ? 2 : 4);
+      const int m = wm * (BM / 2) + 16 * mi + (lane & 15);
+      const char* const r = static_cast<const char*>(a.R) + (int64_t)row0 * a.ld_r * (kBf16 ? 2 : 4) + ((uint32_t)m * ld_r + (uint32_t)n0 * (kBf16 ? 2 : 4));
+#pragma unroll
+      for (int h = 0; h < 2; ++h) res[mi & 1][h].load(r + 32 * h * (kBf16 ? 2 : 4), m < nrows ? N - n0 - 32 * h : 0);
+    };
+    if constexpr (OUT == kRowsAct) {
+      if (add_r) ask(0);
+    }
 #pragma unroll
     for (int mi = 0; mi < MI; ++mi) {
       const int m = wm * (BM / 2) + 16 * mi + (lane & 15);
@@ -383,6 +400,14 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
       float v[16];
 #pragma unroll
       for (int j = 0; j < 16; ++j) v[j] = acc[mi][j >> 2][j & 3] + bias[j];
+      if constexpr (OUT == kRowsAct) {
+        if (add_r && mi + 1 < MI) ask(mi + 1);
+        if (whole) activate(v, a.act);
+        if (add_r) {
+#pragma unroll
+          for (int j = 0; j < 16; ++j) v[j] += res[mi & 1][j >> 3].at(j & 7);
+        }
+      }
       u4 w[2];
       if (bf16) {
 #pragma unroll
@@ -446,12 +471,15 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
 #pragma unroll
     for (int mi = 0; mi < MI; ++mi) {
       uint32_t amax = 0;
+      float h[8], up[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) h[j] = acc[mi][2 * (j >> 2)][j & 3], up[j] = acc[mi][2 * (j >> 2) + 1][j & 3];
+      gate(h, up, a.act);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const int b = 2 * (j >> 2), r = j & 3;
-        const float h = n0 + j < a.N ? silu(acc[mi][b][r]) * acc[mi][b + 1][r] : 0.0f;
-        acc[mi][b][r] = h;
-        amax = max(amax, abs_bits(h));
+        if (n0 + j >= a.N) h[j] = 0.0f;
+        acc[mi][2 * (j >> 2)][j & 3] = h[j];
+        amax = max(amax, abs_bits(h[j]));
       }
       amax = max(amax, (uint32_t)__shfl_xor((int)amax, 16));
       amax = max(amax, (uint32_t)__shfl_xor((int)amax, 32));
@@ -500,6 +528,15 @@ __global__ __launch_bounds__(256) void k_f8_join(StampF8Gemm a) {
   f4 s = v[0];
 #pragma unroll
   for (int i = 1; i < PARTS; ++i) s += v[i];
+  float(&e)[4] = reinterpret_cast<float(&)[4]>(s);
+  activate(e, a.act);
+  if (a.R != nullptr) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (c + j >= a.N) continue;
+      e[j] += a.y_bf16 ? bf16_lo(static_cast<const uint16_t*>(a.R)[m * a.ld_r + c + j]) : static_cast<const float*>(a.R)[m * a.ld_r + c + j];
+    }
+  }
   if (a.y_bf16) {
     uint16_t* y = static_cast<uint16_t*>(a.Y) + m * a.ld_y + c;
     if (c + 4 <= a.N) {
@@ -530,14 +567,15 @@ hipError_t go(const StampF8Gemm& a, int parts, hipStream_t st) {
     const dim3 grid(n, parts);
     StampF8Gemm part = a;
     part.first = (uint32_t)first;
+    const bool act = a.act != STAMP_ACT_NONE || a.R != nullptr;
     if constexpr (BM == 256) {
-      if (a.pow2) k_f8_tiles<BM, kPow2, false><<<grid, 512, 0, st>>>(part);
-      else k_f8_tiles<BM, kScaled, false><<<grid, 512, 0, st>>>(part);
+      if (a.pow2) (act ? k_f8_tiles<BM, kPow2, kRowsAct> : k_f8_tiles<BM, kPow2, kRows>)<<<grid, 512, 0, st>>>(part);
+      else (act ? k_f8_tiles<BM, kScaled, kRowsAct> : k_f8_tiles<BM, kScaled, kRows>)<<<grid, 512, 0, st>>>(part);
     } else {
-      if (a.gated) k_f8_tiles<BM, kWide, true><<<grid, 512, 0, st>>>(part);
-      else if (a.wide_sums) k_f8_tiles<BM, kWide, false><<<grid, 512, 0, st>>>(part);
-      else if (a.pow2) k_f8_tiles<BM, kPow2, false><<<grid, 512, 0, st>>>(part);
-      else k_f8_tiles<BM, kScaled, false><<<grid, 512, 0, st>>>(part);
+      if (a.gated) k_f8_tiles<BM, kWide, kGated><<<grid, 512, 0, st>>>(part);
+      else if (a.wide_sums) (act ? k_f8_tiles<BM, kWide, kRowsAct> : k_f8_tiles<BM, kWide, kRows>)<<<grid, 512, 0, st>>>(part);
+      else if (a.pow2) (act ? k_f8_tiles<BM, kPow2, kRowsAct> : k_f8_tiles<BM, kPow2, kRows>)<<<grid, 512, 0, st>>>(part);
+      else (act ? k_f8_tiles<BM, kScaled, kRowsAct> : k_f8_tiles<BM, kScaled, kRows>)<<<grid, 512, 0, st>>>(part);
     }
   });
   if (e != hipSuccess) return e;

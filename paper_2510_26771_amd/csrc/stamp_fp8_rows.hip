@@ -62,7 +62,9 @@ __global__ __launch_bounds__(kWaves * 64, IN == kCodes ? 2 : 4) void k_f8_rows(S
       const int m = min(16 * mi + (lane & 15), nr - 1);
       if constexpr (IN == kCodes) {
         int ar = r0 + m;
-        if constexpr (GATED) ar = min(max(a.index[ar], 0), a.a_rows - 1);
+        if constexpr (GATED) {
+          if (a.index != nullptr) ar = min(max(a.index[ar], 0), a.a_rows - 1);
+        }
         arow[mi] = a.A + (size_t)ar * Kp + 16 * f;
         srow[mi] = ar;
       } else {
@@ -126,7 +128,7 @@ __global__ __launch_bounds__(kWaves * 64, IN == kCodes ? 2 : 4) void k_f8_rows(S
         const int units = nr * a.Kb * 8, per = a.Kb * 8;
         auto row_of = [&](int u) __attribute__((always_inline)) {
           const int r = r0 + u / per;
-          const int ar = GATED ? min(max(a.index[r], 0), a.a_rows - 1) : r;
+          const int ar = GATED && a.index != nullptr ? min(max(a.index[r], 0), a.a_rows - 1) : r;
           return static_cast<const char*>(a.X) + (int64_t)ar * a.ld_x * (IN == kBf16 ? 2 : 4);
         };
         auto make = [&](int u, const Raw16<IN == kBf16>& x) __attribute__((always_inline)) {
@@ -188,6 +190,13 @@ __global__ __launch_bounds__(kWaves * 64, IN == kCodes ? 2 : 4) void k_f8_rows(S
 #pragma unroll
         for (int s = 1; s < S; ++s) v += red[s][m][pl];
         if (a.bias != nullptr) v += a.bias[(size_t)set * a.N + n];
+        float w[1] = {v};
+        activate(w, a.act);
+        v = w[0];
+        if (a.R != nullptr) {
+          const int64_t o = (int64_t)(r0 + m) * a.ld_r + n;
+          v += a.y_bf16 ? bf16_lo(static_cast<const uint16_t*>(a.R)[o]) : static_cast<const float*>(a.R)[o];
+        }
         const int64_t o = (int64_t)(r0 + m) * a.ld_y + n;
         if (a.y_bf16) static_cast<uint16_t*>(a.Y)[o] = to_bf16(v);
         else static_cast<float*>(a.Y)[o] = v;
@@ -197,16 +206,20 @@ __global__ __launch_bounds__(kWaves * 64, IN == kCodes ? 2 : 4) void k_f8_rows(S
       static_assert(kPlaces == 256, "a block of the next layer's input in one workgroup");
       for (int u = t; u < kRows * 8; u += kWaves * 64) {
         const int m = u >> 3, c0 = (u & 7) * 16;
-        float hv[16];
+        float hv[16], up[16];
         uint32_t amax = 0;
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-          const int c = c0 + j, ch = blockIdx.x * 128 + c;  // of group c / 32: lanes c / 8 % 4, pair c / 4 % 2
+          const int c = c0 + j;  // of group c / 32: lanes c / 8 % 4, pair c / 4 % 2
           const int pl = (c >> 5) * 64 + ((c >> 2) & 1) * 32 + ((c >> 3) & 3) * 4 + (c & 3);
-          float gt = red[0][m][pl], up = red[0][m][pl + 16];
+          hv[j] = red[0][m][pl], up[j] = red[0][m][pl + 16];
 #pragma unroll
-          for (int s = 1; s < S; ++s) gt += red[s][m][pl], up += red[s][m][pl + 16];
-          hv[j] = ch < a.N ? silu(gt) * up : 0.0f;
+          for (int s = 1; s < S; ++s) hv[j] += red[s][m][pl], up[j] += red[s][m][pl + 16];
+        }
+        gate(hv, up, a.act);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+          hv[j] = (int)blockIdx.x * 128 + c0 + j < a.N ? hv[j] : 0.0f;
           amax = max(amax, abs_bits(hv[j]));
         }
         amax = max8(amax);

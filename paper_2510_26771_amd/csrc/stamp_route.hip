@@ -312,8 +312,10 @@ int tokens_per_block(int tokens, int experts) {
 
 // Y[t] = sum of a token's rows times their weights, slots in order.  A thread has 8 columns and 8 rows in flight.  Bound by memory: 8192 tokens of
 // 4096 columns, 8 rows each, bf16: 122 us, 5 TB/s.
-template <bool BF16>
-__global__ __launch_bounds__(256) void k_combine(stamp_routing_t r, const void* rows, int64_t ld_rows, int nrows, void* Y, int64_t ld_y, int d) {
+// ROWS16, BF16: rows and Y in bf16.
+template <bool ROWS16, bool BF16>
+__global__ __launch_bounds__(256) void k_combine(stamp_routing_t r, const void* rows, int64_t ld_rows, int nrows, const void* R, int64_t ld_r, void* Y, int64_t ld_y,
+                                                 int d) {
   const int per = (d + 7) / 8;
   const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x;
   const int64_t t = u / per;
@@ -332,7 +334,7 @@ __global__ __launch_bounds__(256) void k_combine(stamp_routing_t r, const void* 
       w[j] = weight[jj];
       if (j0 + j >= r.top_k) row[j] = -1;
     }
-    if constexpr (BF16) {
+    if constexpr (ROWS16) {
       u4 v[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j)
@@ -359,6 +361,12 @@ __global__ __launch_bounds__(256) void k_combine(stamp_routing_t r, const void* 
         for (int i = 0; i < 8; ++i) y[i] = __builtin_fmaf(f, v[j][i >> 2][i & 3], y[i]);
       }
     }
+  }
+  if (R != nullptr) {
+    Residual8<BF16> res;
+    res.load(static_cast<const char*>(R) + (t * ld_r + c) * (BF16 ? 2 : 4), d - c);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] += res.at(i);
   }
   const int64_t o = t * ld_y + c;
   if constexpr (BF16) {
@@ -412,10 +420,10 @@ hipError_t stamp_launch_route(const stamp_routing_t& r, const void* logits, int 
   return hipGetLastError();
 }
 
-hipError_t stamp_launch_combine(const stamp_routing_t& r, const void* rows, int y_bf16, int64_t ld_rows, int nrows, void* Y, int64_t ld_y, int d,
-                                hipStream_t st) {
+hipError_t stamp_launch_combine(const stamp_routing_t& r, const void* rows, int rows_bf16, int y_bf16, int64_t ld_rows, int nrows, const void* R, int64_t ld_r,
+                                void* Y, int64_t ld_y, int d, hipStream_t st) {
   const int64_t blocks = ((int64_t)r.tokens * ((d + 7) / 8) + 255) / 256;
-  if (y_bf16) k_combine<true><<<(uint32_t)blocks, 256, 0, st>>>(r, rows, ld_rows, nrows, Y, ld_y, d);
-  else k_combine<false><<<(uint32_t)blocks, 256, 0, st>>>(r, rows, ld_rows, nrows, Y, ld_y, d);
+  auto* const k = !y_bf16 ? k_combine<false, false> : rows_bf16 ? k_combine<true, true> : k_combine<false, true>;
+  k<<<(uint32_t)blocks, 256, 0, st>>>(r, rows, ld_rows, nrows, R, ld_r, Y, ld_y, d);
   return hipGetLastError();
 }

@@ -12,6 +12,7 @@ from .binding import STAMP_BF16, STAMP_F32, _check, _ptr, _stream, load_library
 STAMP_E4M3 = 2
 STAMP_SCALE_F32, STAMP_SCALE_POW2 = 0, 1
 BLOCK = 128
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}  # stamp_activation_t
 FP8_ROUTES = {1: "rows", 2: "tiles_64", 3: "tiles_128", 4: "tiles_256"}  # stamp_fp8_route_t
 
 
@@ -22,6 +23,14 @@ class _Desc(C.Structure):
 class _Routing(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("tokens", "experts", "top_k")] + [
         (n, C.c_void_p) for n in ("ids", "weights", "offsets", "token_of_row", "row_of_slot")]
+
+
+class _Epilogue(C.Structure):
+    _fields_ = [("activation", C.c_int32), ("residual", C.c_void_p), ("ld_residual", C.c_int64)]
+
+
+class _Router(C.Structure):
+    _fields_ = [("W", C.c_void_p), ("w_dtype", C.c_int32), ("renormalize", C.c_int32), ("bias", C.c_void_p)]
 
 
 @dataclass
@@ -67,6 +76,13 @@ def _room(t, gpu):
     if t is None or t.get_device() != gpu or not t.is_contiguous():
         raise ValueError(f"workspace must be a contiguous tensor on GPU {gpu}")
     return t.nbytes
+
+
+def _activation(name):
+    code = ACTIVATIONS.get(name)
+    if code is None:
+        raise ValueError(f"activation must be one of {', '.join(ACTIVATIONS)}, not {name!r}")
+    return code
 
 
 class Fp8Plan:
@@ -151,30 +167,49 @@ class Fp8Plan:
     def _y(self, Y, rows):
         return _matrix(Y, "Y", rows, self.desc.d_out, self._y_dtype, self.gpu)
 
+    def _epilogue(self, activation, residual, rows):
+        if residual is None:
+            return C.byref(_Epilogue(_activation(activation), None, 0))
+        return C.byref(_Epilogue(_activation(activation), _ptr(residual), _matrix(residual, "residual", rows, self.desc.d_out, self._y_dtype, self.gpu)))
+
     def quantize_act(self, X, codes, scales, stream=None):
         ld = self._x(X, X.shape[0])
         lds = self._act_buffers(codes, scales, X.shape[0])
         _check(self.lib.stamp_fp8_quantize_act(self._h, X.shape[0], _ptr(X), ld, _ptr(codes), _ptr(scales), lds, _stream(stream, self.gpu)),
                "stamp_fp8_quantize_act")
 
-    def linear_forward(self, X, Y, workspace, stream=None):
+    def linear_forward(self, X, Y, workspace, stream=None, activation="none", residual=None):
+        """Y = activation(X W + bias) + residual; activation: one of ACTIVATIONS; residual: a tensor like Y (Y itself: added in place), or None.
+        With either, X must not be Y."""
         rows = X.shape[0]
         ld_x, ld_y, room = self._x(X, rows), self._y(Y, rows), _room(workspace, self.gpu)
+        if residual is not None or activation != "none":
+            _check(self.lib.stamp_fp8_linear_forward_act(self._h, rows, _ptr(X), ld_x, self._epilogue(activation, residual, rows), _ptr(Y), ld_y,
+                                                         _ptr(workspace), room, _stream(stream, self.gpu)), "stamp_fp8_linear_forward_act")
+            return
         _check(self.lib.stamp_fp8_linear_forward(self._h, rows, _ptr(X), ld_x, _ptr(Y), ld_y, _ptr(workspace), room, _stream(stream, self.gpu)),
                "stamp_fp8_linear_forward")
 
-    def linear_forward_q(self, codes, scales, Y, workspace, stream=None):
+    def linear_forward_q(self, codes, scales, Y, workspace, stream=None, activation="none", residual=None):
         rows = Y.shape[0]
         lds, ld_y, room = self._act_buffers(codes, scales, rows), self._y(Y, rows), _room(workspace, self.gpu)
+        if residual is not None or activation != "none":
+            _check(self.lib.stamp_fp8_linear_forward_q_act(self._h, rows, _ptr(codes), _ptr(scales), lds, self._epilogue(activation, residual, rows), _ptr(Y),
+                                                           ld_y, _ptr(workspace), room, _stream(stream, self.gpu)), "stamp_fp8_linear_forward_q_act")
+            return
         _check(self.lib.stamp_fp8_linear_forward_q(self._h, rows, _ptr(codes), _ptr(scales), lds, _ptr(Y), ld_y, _ptr(workspace),
                                                    room, _stream(stream, self.gpu)), "stamp_fp8_linear_forward_q")
 
-    def grouped_forward(self, X, offsets, Y, workspace, stream=None):
-        """Rows offsets[e] .. offsets[e + 1] - 1 of X times expert e's weights."""
+    def grouped_forward(self, X, offsets, Y, workspace, stream=None, activation="none", residual=None):
+        """Rows offsets[e] .. offsets[e + 1] - 1 of X times expert e's weights; activation and residual as in linear_forward."""
         import torch
         rows = X.shape[0]
         ld_x, ld_y, room = self._x(X, rows), self._y(Y, rows), _room(workspace, self.gpu)
         _flat(offsets, "offsets", self.desc.experts + 1, torch.int32, self.gpu)
+        if residual is not None or activation != "none":
+            _check(self.lib.stamp_fp8_grouped_forward_act(self._h, rows, _ptr(offsets), _ptr(X), ld_x, self._epilogue(activation, residual, rows), _ptr(Y),
+                                                          ld_y, _ptr(workspace), room, _stream(stream, self.gpu)), "stamp_fp8_grouped_forward_act")
+            return
         _check(self.lib.stamp_fp8_grouped_forward(self._h, rows, _ptr(offsets), _ptr(X), ld_x, _ptr(Y), ld_y, _ptr(workspace),
                                                   room, _stream(stream, self.gpu)), "stamp_fp8_grouped_forward")
 
@@ -236,3 +271,46 @@ def experts_forward(up: Fp8Plan, down: Fp8Plan, X, routing: Routing, Y, workspac
     ld_x, ld_y, room = up._x(X, routing.tokens), down._y(Y, routing.tokens), _room(workspace, up.gpu)
     _check(up.lib.stamp_experts_forward(up._h, down._h, C.byref(routing._c), _ptr(X), ld_x, _ptr(Y), ld_y, _ptr(workspace), room,
                                         _stream(stream, up.gpu)), "stamp_experts_forward")
+
+
+def mlp_workspace(up: Fp8Plan, down: Fp8Plan, rows: int, device="cuda"):
+    import torch
+    n = int(up.lib.stamp_mlp_workspace_bytes(up._h, down._h, int(rows)))
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+
+
+def mlp_forward(up: Fp8Plan, down: Fp8Plan, X, Y, workspace, activation, residual=None, stream=None):
+    """The dense MLP: Y = Q8(activation(X Wup + bias)) Wdown + bias + residual; with a gated up (a plan of one expert) activation(X Wgate) * (X Wup) in
+    the activation's place.  residual: a tensor like Y; X, Y and residual may be the same tensor."""
+    if down.gpu != up.gpu:
+        raise ValueError("both plans must lie on one GPU")
+    rows = X.shape[0]
+    ld_x, ld_y, room = up._x(X, rows), down._y(Y, rows), _room(workspace, up.gpu)
+    _check(up.lib.stamp_mlp_forward(up._h, down._h, rows, _ptr(X), ld_x, down._epilogue(activation, residual, rows), _ptr(Y), ld_y, _ptr(workspace), room,
+                                    _stream(stream, up.gpu)), "stamp_mlp_forward")
+
+
+def moe_workspace(up: Fp8Plan, down: Fp8Plan, tokens: int, top_k: int, device="cuda"):
+    import torch
+    n = int(up.lib.stamp_moe_workspace_bytes(up._h, down._h, int(tokens), int(top_k)))
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
+
+
+def moe_forward(router, up: Fp8Plan, down: Fp8Plan, X, routing: Routing, Y, workspace, router_bias=None, renormalize: bool = True, activation="silu",
+                residual=None, stream=None):
+    """A whole layer of experts: logits X router^T + router_bias (router: [experts, d] in float32 or bfloat16), their routing (-> routing), and the
+    weighted sum of the chosen experts' gated MLPs, plus residual.  X, Y and residual may be the same tensor."""
+    import torch
+    if down.gpu != up.gpu or routing.gpu != up.gpu:
+        raise ValueError("both plans and the routing must lie on one GPU")
+    if router.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("router must be float32 or bfloat16")
+    if router.shape != (routing.experts, up.desc.d_in):
+        raise ValueError(f"router must be a tensor of shape ({routing.experts}, {up.desc.d_in})")
+    _flat(router, "router", routing.experts * up.desc.d_in, router.dtype, up.gpu)
+    if router_bias is not None:
+        _flat(router_bias, "router_bias", routing.experts, torch.float32, up.gpu)
+    ld_x, ld_y, room = up._x(X, routing.tokens), down._y(Y, routing.tokens), _room(workspace, up.gpu)
+    r = _Router(_ptr(router), STAMP_BF16 if router.dtype == torch.bfloat16 else STAMP_F32, int(bool(renormalize)), _ptr(router_bias))
+    _check(up.lib.stamp_moe_forward(C.byref(r), up._h, down._h, C.byref(routing._c), _ptr(X), ld_x, down._epilogue(activation, residual, routing.tokens),
+                                    _ptr(Y), ld_y, _ptr(workspace), room, _stream(stream, up.gpu)), "stamp_moe_forward")
