@@ -60,8 +60,10 @@ struct StampF8Gemm {
   int32_t sets, groups, Kb, nblk, N, pow2, gated, y_bf16;
   int32_t forced;          // stamp_fp8_route_t, 0: by rule
   int32_t wide_sums;       // products on the bf16 matrix instructions (f8_wide_sums)
-  void* Y;                 // rows of N values; gated: codes [rows][ld_y] and scales [ld_y / 128][ld_sh]
+  void* Y;                 // rows of N values; gated, codes: codes [rows][ld_y] and scales [ld_y / 128][ld_sh]
   int64_t ld_y;
+  int32_t codes;           // not gated: Y as codes (in tiles alone)
+  int32_t h_wide;          // codes of Y as bf16
   int32_t act;             // stamp_activation_t, of the gate where gated
   const void* R;           // residual rows in Y's type, or nullptr
   int64_t ld_r;
@@ -91,6 +93,9 @@ struct F8Cut {
   int groups, size, parts, rest_size, rest_parts;
 };
 F8Cut stamp_f8_cut(int sets, int groups, int Kb, int rows, int wide_sums, int gated, int forced);
+// an up product's rows as codes, straight from tiles (quantized_below: the down product would quantize fp32 rows itself)
+int stamp_f8_codes_pay(int groups, int Kb, int rows, int quantized_below);
+int stamp_f8_codes_route(int groups, int Kb, int rows);
 constexpr int kF8MaxParts = 8;
 // bytes of the parts' rows, at most
 size_t stamp_f8_partial_bytes(int groups, int rows);
@@ -108,7 +113,7 @@ hipError_t stamp_launch_f8_tiles(const StampF8Gemm& a, int bm, int parts, hipStr
 // instructions, which the codes fit exactly, keep 4e-8 at half the rate.  A bf16 Y cannot tell (its own rounding is 2e-3), so its layers
 // take the FP8 instructions.  An fp32 Y and the codes of the next layer (an error of 6e-5 moves one in 1000 of them to its neighbour) take
 // the bf16 instructions.
-inline int f8_wide_sums(const StampF8Gemm& a) { return a.gated || !a.y_bf16; }
+inline int f8_wide_sums(const StampF8Gemm& a) { return a.gated || a.codes || !a.y_bf16; }
 hipError_t stamp_launch_route(const stamp_routing_t& r, const void* logits, int bf16, int64_t ld, int renorm, void* ws, hipStream_t st);
 size_t stamp_route_ws(int tokens, int experts, int top_k);
 hipError_t stamp_launch_combine(const stamp_routing_t& r, const void* rows, int rows_bf16, int y_bf16, int64_t ld_rows, int nrows, const void* R, int64_t ld_r,
@@ -317,6 +322,12 @@ __device__ __forceinline__ b8 widen8(int lo, int hi) {
   const b2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
   const b2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
   return b8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// 8 codes at element o of a row's codes, as bytes or as bf16
+__device__ __forceinline__ void put_codes(void* base, int64_t o, const u2& c, int wide) {
+  if (wide) reinterpret_cast<b8*>(base)[o >> 3] = widen8((int)c[0], (int)c[1]);
+  else reinterpret_cast<u2*>(base)[o >> 3] = c;
 }
 
 __device__ __forceinline__ float silu(float g) { return g / (1.0f + __expf(-g)); }

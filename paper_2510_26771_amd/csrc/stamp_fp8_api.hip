@@ -47,7 +47,9 @@ StampF8Gemm gemm_args(const stamp_fp8_plan* p) {
   return a;
 }
 
-int route_of(const StampF8Gemm& a, int rows) { return stamp_f8_route(a.sets, a.groups, a.Kb, rows, a.wide_sums, a.gated, a.forced); }
+// products whose results become codes have their depth in one piece
+bool in_one(const StampF8Gemm& a) { return a.gated || a.codes; }
+int route_of(const StampF8Gemm& a, int rows) { return stamp_f8_route(a.sets, a.groups, a.Kb, rows, a.wide_sums, in_one(a), a.forced); }
 // the codes are wanted as bf16
 bool wide_codes(const StampF8Gemm& a, int rows) { return a.wide_sums && route_of(a, rows) != STAMP_FP8_ROUTE_ROWS; }
 
@@ -63,7 +65,7 @@ void give_x(StampF8Gemm* a, const stamp_fp8_desc_t& d, int rows, const void* X, 
 
 hipError_t product(const StampF8Gemm& a, hipStream_t st) {
   if (route_of(a, a.rows) == STAMP_FP8_ROUTE_ROWS) return stamp_launch_f8_rows(a, st);
-  const F8Cut cut = stamp_f8_cut(a.sets, a.groups, a.Kb, a.rows, a.wide_sums, a.gated, a.forced);
+  const F8Cut cut = stamp_f8_cut(a.sets, a.groups, a.Kb, a.rows, a.wide_sums, in_one(a), a.forced);
   if (cut.groups == 0) return stamp_launch_f8_tiles(a, 64 << cut.size, cut.parts, st);
   StampF8Gemm first = a, rest = a;
   const int columns = cut.groups * kF8Group;
@@ -98,7 +100,7 @@ LinearWs linear_ws(const stamp_fp8_plan* p, int32_t rows) {
 }
 
 struct ExpertsWs {
-  size_t codes, scales, h, sh, rows, wide, partial, total;
+  size_t codes, scales, h, sh, rows, partial, total;
   int64_t ld_rows;
 };
 ExpertsWs experts_ws(const stamp_fp8_plan* up, const stamp_fp8_plan* down, int32_t tokens, int32_t top_k, bool wide_rows = false) {
@@ -107,15 +109,13 @@ ExpertsWs experts_ws(const stamp_fp8_plan* up, const stamp_fp8_plan* down, int32
   w.codes = 0;
   w.scales = align256((size_t)tokens * up->Kp * code_bytes(up));
   w.h = w.scales + align256((size_t)up->Kb * scales_ld(tokens) * sizeof(float));
-  w.sh = w.h + align256((size_t)slots * down->Kp);
+  w.sh = w.h + align256((size_t)slots * down->Kp * code_bytes(down));
   w.rows = w.sh + align256((size_t)down->Kb * ld * sizeof(float));
   w.ld_rows = (down->desc.d_out + 7) / 8 * 8;
   // Rows in Y's type: a bf16 Y is a sum of terms rounded once each, 2.3e-3 off where rows in fp32 give 1.7e-3, which is Y's own rounding; but
   // they are the most bytes of the call (8192 tokens, 8 of 64 experts, 4096 -> 1536: down product 529 -> 647 us, weighted sum 122 -> 242, the whole
   // 2200 -> 2447).  An fp32 Y has them in fp32.
-  // The up product writes codes of one byte; a down product that wants them as bf16 has them widened here
-  w.wide = w.rows + align256((size_t)slots * w.ld_rows * (wide_rows ? 4 : type_size(down->desc.y_dtype)));
-  w.partial = w.wide + (code_bytes(down) == 2 ? align256((size_t)slots * down->Kp * 2) : 0);
+  w.partial = w.rows + align256((size_t)slots * w.ld_rows * (wide_rows ? 4 : type_size(down->desc.y_dtype)));
   w.total = w.partial + align256(stamp_f8_partial_bytes(down->groups, (int32_t)slots));
   return w;
 }
@@ -279,15 +279,12 @@ stamp_status_t run_experts(const ExpertsRun& e, uint8_t* ws, hipStream_t st) {
   a.ld_y = down->Kp;
   a.SH = reinterpret_cast<float*>(ws + w.sh);
   a.ld_sh = ld;
+  StampF8Gemm b = gemm_args(down);
+  a.h_wide = wide_codes(b, slots);
   if (product(a, st) != hipSuccess) return STAMP_ERR_DEVICE;
 
-  StampF8Gemm b = gemm_args(down);
   b.partial = reinterpret_cast<float*>(ws + w.partial);
   b.A = ws + w.h;
-  if (wide_codes(b, slots)) {
-    if (stamp_launch_f8_widen(b.A, (int64_t)slots * down->Kp, ws + w.wide, st) != hipSuccess) return STAMP_ERR_DEVICE;
-    b.A = ws + w.wide;
-  }
   b.SA = a.SH;
   b.ld_sa = ld;
   b.a_rows = b.rows = slots;
@@ -303,14 +300,14 @@ stamp_status_t run_experts(const ExpertsRun& e, uint8_t* ws, hipStream_t st) {
 struct MlpWs {
   size_t codes, scales, h, hcodes, hscales, partial, total;
 };
-int64_t mlp_ld_h(const stamp_fp8_plan* up) { return up->desc.d_out; }
+constexpr int32_t kMlpRowsInFp32 = 1024;  // up to so many rows of h may lie in fp32
 MlpWs mlp_ws(const stamp_fp8_plan* up, const stamp_fp8_plan* down, int32_t rows) {
   MlpWs w;
   w.codes = 0;
   w.scales = align256((size_t)rows * up->Kp * 2);  // bf16 codes: h is a sum in fp32
   w.h = w.scales + align256((size_t)up->Kb * scales_ld(rows) * sizeof(float));
-  w.hcodes = w.h + (up->desc.gated ? 0 : align256((size_t)rows * mlp_ld_h(up) * sizeof(float)));
-  w.hscales = w.hcodes + align256((size_t)rows * down->Kp * (up->desc.gated && code_bytes(down) == 2 ? 3 : code_bytes(down)));
+  w.hcodes = w.h + (up->desc.gated ? 0 : align256((size_t)(rows < kMlpRowsInFp32 ? rows : kMlpRowsInFp32) * up->desc.d_out * sizeof(float)));
+  w.hscales = w.hcodes + align256((size_t)rows * down->Kp * code_bytes(down));
   w.partial = w.hscales + align256((size_t)down->Kb * scales_ld(rows) * sizeof(float));
   const size_t pu = up->desc.gated ? 0 : stamp_f8_partial_bytes(up->groups, rows), pd = stamp_f8_partial_bytes(down->groups, rows);
   w.total = w.partial + align256(pu > pd ? pu : pd);
@@ -321,6 +318,13 @@ stamp_status_t check_mlp(const stamp_fp8_plan* up, const stamp_fp8_plan* down) {
   if (down->desc.gated || up->desc.experts != (up->desc.gated ? 1 : 0) || down->desc.experts > up->desc.experts) return STAMP_ERR_UNSUPPORTED;
   if (up->desc.d_out != down->desc.d_in || up->desc.scale_format != down->desc.scale_format) return STAMP_ERR_SHAPE;
   return STAMP_OK;
+}
+
+// h straight to codes, in tiles, or in fp32 and by the quantizer: see stamp_f8_codes_pay
+bool mlp_codes_in_tiles(const StampF8Gemm& up, const StampF8Gemm& down, int rows) {
+  if (rows > kMlpRowsInFp32) return true;
+  if (up.forced != 0) return up.forced != STAMP_FP8_ROUTE_ROWS;
+  return stamp_f8_codes_pay(up.groups, up.Kb, rows, takes_x(down, rows));
 }
 
 // The layer of experts' places: logits and the router's, then those of the experts.
@@ -435,6 +439,15 @@ F8Cut stamp_f8_cut(int sets, int groups, int Kb, int rows, int wide_sums, int ga
     if (us < best) best = us, cut = F8Cut{cols * 4, i, 1, rest.size, rest.parts};
   }
   return cut;
+}
+
+// An up product of tiles whose results become codes has its depth in one piece; with rows in fp32 it may have parts or be the rows kernel's, but they
+// are written and, unless the down product does it (few rows), quantized by a launch of 3.5 us: 4 + 4 + 1 bytes for 1.
+int stamp_f8_codes_route(int groups, int Kb, int rows) { return STAMP_FP8_ROUTE_TILES_64 + best_tiles(1, groups, Kb, rows, 1, 1, 0).size; }
+int stamp_f8_codes_pay(int groups, int Kb, int rows, int quantized_below) {
+  const float codes = best_tiles(1, groups, Kb, rows, 1, 1, 0).us;
+  const float tiles = best_tiles(1, groups, Kb, rows, 1, 0, 0).us, few = rows_us(1, groups, Kb, rows), elements = (float)rows * groups * 64;
+  return codes < (tiles < few ? tiles : few) + (quantized_below ? 0.0f : 3.5f + elements * 8.0f / kBytesPerUs);
 }
 
 // parts * tiles <= CUs, and the rows are at most the tiles' (a set's half tile is counted, and one more)
@@ -577,10 +590,14 @@ stamp_status_t stamp_mlp_forward(const stamp_fp8_plan_t* up, const stamp_fp8_pla
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
   uint8_t* ws = static_cast<uint8_t*>(workspace_dev);
 
-  StampF8Gemm a = gemm_args(up);
-  a.y_bf16 = 0;  // h in fp32
+  StampF8Gemm a = gemm_args(up), b = gemm_args(down);
+  b.R = epilogue->residual_dev;
+  b.ld_r = epilogue->ld_residual;
+  a.y_bf16 = 0;
   a.wide_sums = f8_wide_sums(a);
   if (a.forced == STAMP_FP8_ROUTE_TILES_256) a.forced = 0;
+  a.codes = !up->desc.gated && mlp_codes_in_tiles(a, b, rows);
+  if (a.codes && a.forced <= STAMP_FP8_ROUTE_ROWS) a.forced = stamp_f8_codes_route(a.groups, a.Kb, rows);
   a.act = epilogue->activation;
   float* scales = reinterpret_cast<float*>(ws + w.scales);
   if (takes_x(a, rows)) {
@@ -593,41 +610,32 @@ stamp_status_t stamp_mlp_forward(const stamp_fp8_plan_t* up, const stamp_fp8_pla
   a.SA = scales;
   a.ld_sa = scales_ld(rows);
   a.a_rows = a.rows = rows;
-  a.partial = reinterpret_cast<float*>(ws + w.partial);
-  StampF8Gemm b = gemm_args(down);
-  b.R = epilogue->residual_dev;
-  b.ld_r = epilogue->ld_residual;
-  b.partial = a.partial;
+  a.partial = b.partial = reinterpret_cast<float*>(ws + w.partial);
+  float* const hscales = reinterpret_cast<float*>(ws + w.hscales);
+  if (a.gated || a.codes) {
+    a.Y = ws + w.hcodes;
+    a.ld_y = down->Kp;
+    a.SH = hscales;
+    a.ld_sh = scales_ld(rows);
+    a.h_wide = wide_codes(b, rows);
+  } else {
+    a.Y = ws + w.h;
+    a.ld_y = up->desc.d_out;
+  }
+  if (product(a, st) != hipSuccess) return STAMP_ERR_DEVICE;
+  if (!a.gated && !a.codes) {
+    stamp_fp8_desc_t h = down->desc;
+    h.x_dtype = STAMP_F32;
+    if (takes_x(b, rows)) give_x(&b, h, rows, a.Y, a.ld_y);
+    else if (stamp_launch_f8_quant(a.Y, 0, a.ld_y, rows, h.d_in, b.pow2, wide_codes(b, rows), ws + w.hcodes, hscales, scales_ld(rows), st) != hipSuccess)
+      return STAMP_ERR_DEVICE;
+  }
   b.A = ws + w.hcodes;
-  b.SA = reinterpret_cast<float*>(ws + w.hscales);
+  b.SA = hscales;
   b.ld_sa = scales_ld(rows);
   b.a_rows = b.rows = rows;
   b.Y = Y_dev;
   b.ld_y = ld_y;
-  if (up->desc.gated) {
-    a.Y = ws + w.hcodes;
-    a.ld_y = down->Kp;
-    a.SH = reinterpret_cast<float*>(ws + w.hscales);
-    a.ld_sh = b.ld_sa;
-    if (product(a, st) != hipSuccess) return STAMP_ERR_DEVICE;
-    if (wide_codes(b, rows)) {
-      uint8_t* wide = ws + w.hcodes + (size_t)rows * down->Kp;
-      if (stamp_launch_f8_widen(b.A, (int64_t)rows * down->Kp, wide, st) != hipSuccess) return STAMP_ERR_DEVICE;
-      b.A = wide;
-    }
-  } else {
-    a.Y = ws + w.h;
-    a.ld_y = mlp_ld_h(up);
-    if (product(a, st) != hipSuccess) return STAMP_ERR_DEVICE;
-    stamp_fp8_desc_t h = down->desc;
-    h.x_dtype = STAMP_F32;
-    if (takes_x(b, rows)) {
-      give_x(&b, h, rows, a.Y, a.ld_y);
-    } else if (stamp_launch_f8_quant(a.Y, 0, a.ld_y, rows, h.d_in, b.pow2, wide_codes(b, rows), ws + w.hcodes, reinterpret_cast<float*>(ws + w.hscales), b.ld_sa,
-                                     st) != hipSuccess) {
-      return STAMP_ERR_DEVICE;
-    }
-  }
   return done(product(b, st));
 }
 

@@ -44,8 +44,8 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void* p) {
 // How the products are summed: FP8 instructions with the scales by multiplication or as their own, or bf16 instructions (f8_wide_sums).
 enum Sums { kScaled, kPow2, kWide };
 
-// What becomes of the sums: rows of Y, the same with activation and residual, codes of act(gate) * up.
-enum Out { kRows, kRowsAct, kGated };
+// What becomes of the sums: rows of Y, the same with activation and residual, codes of act(gate) * up, codes of the activated rows.
+enum Out { kRows, kRowsAct, kGated, kCodes };
 
 [[maybe_unused]] constexpr int kMaxBlocks = 65536 / kF8Block;
 
@@ -362,7 +362,49 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
   __builtin_amdgcn_s_waitcnt(0x0070);  // no load into LDS may outlive the workgroup
 
   const int g = g0 + wn;
-  if constexpr (!GATED) {
+  if constexpr (OUT == kCodes) {
+    // the tile's 256 columns are two blocks of the next layer's input, a block two waves side by side
+    float* part = reinterpret_cast<float*>(stage0);  // [4][BM] largest magnitudes of the waves' 64 columns, as bits
+    const int n0 = 64 * g + 8 * f;                   // and 32 further on
+    float bias[16];
+#pragma unroll
+    for (int j = 0; j < 16; ++j) bias[j] = bias_of[64 * wn + 32 * (j >> 3) + 8 * f + (j & 7)];
+    turn(none);
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) {
+      uint32_t amax = 0;
+      float h[16];
+#pragma unroll
+      for (int j = 0; j < 16; ++j) h[j] = acc[mi][j >> 2][j & 3] + bias[j];
+      activate(h, a.act);
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        if (n0 + 32 * (j >> 3) + (j & 7) >= a.N) h[j] = 0.0f;
+        acc[mi][j >> 2][j & 3] = h[j];
+        amax = max(amax, abs_bits(h[j]));
+      }
+      amax = max(amax, (uint32_t)__shfl_xor((int)amax, 16));
+      amax = max(amax, (uint32_t)__shfl_xor((int)amax, 32));
+      if (f == 0) part[wn * BM + wm * (BM / 2) + 16 * mi + lane] = __uint_as_float(amax);
+    }
+    turn(none);
+    if (64 * g >= a.ld_y) return;  // columns behind the last block
+#pragma unroll
+    for (int mi = 0; mi < MI; ++mi) {
+      const int m = wm * (BM / 2) + 16 * mi + (lane & 15);
+      const uint32_t amax = max(__float_as_uint(part[(wn & 2) * BM + m]), __float_as_uint(part[((wn & 2) + 1) * BM + m]));
+      float scale, inv;
+      scale_of(amax, a.pow2, &scale, &inv);
+      if (m >= nrows) continue;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const f4 v0 = acc[mi][2 * h], v1 = acc[mi][2 * h + 1];
+        const u2 o = {pack4(v0[0] * inv, v0[1] * inv, v0[2] * inv, v0[3] * inv), pack4(v1[0] * inv, v1[1] * inv, v1[2] * inv, v1[3] * inv)};
+        put_codes(a.Y, (int64_t)(row0 + m) * a.ld_y + n0 + 32 * h, o, a.h_wide);
+      }
+      if ((wn & 1) == 0 && f == 0) a.SH[(int64_t)(2 * col + (wn >> 1)) * a.ld_sh + row0 + m] = scale;
+    }
+  } else if constexpr (!GATED) {
     const int n0 = 64 * g + 8 * f;  // and 32 further on
     float bias[16];
 #pragma unroll
@@ -498,7 +540,7 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
       u2 o;
       o[0] = pack4(acc[mi][0][0] * inv, acc[mi][0][1] * inv, acc[mi][0][2] * inv, acc[mi][0][3] * inv);
       o[1] = pack4(acc[mi][2][0] * inv, acc[mi][2][1] * inv, acc[mi][2][2] * inv, acc[mi][2][3] * inv);
-      *reinterpret_cast<u2*>(static_cast<uint8_t*>(a.Y) + (int64_t)(row0 + m) * a.ld_y + 32 * g + 8 * f) = o;
+      put_codes(a.Y, (int64_t)(row0 + m) * a.ld_y + 32 * g + 8 * f, o, a.h_wide);
       if (wn == 0 && f == 0) a.SH[(int64_t)col * a.ld_sh + row0 + m] = scale;
     }
   }
@@ -573,6 +615,7 @@ hipError_t go(const StampF8Gemm& a, int parts, hipStream_t st) {
       else (act ? k_f8_tiles<BM, kScaled, kRowsAct> : k_f8_tiles<BM, kScaled, kRows>)<<<grid, 512, 0, st>>>(part);
     } else {
       if (a.gated) k_f8_tiles<BM, kWide, kGated><<<grid, 512, 0, st>>>(part);
+      else if (a.codes) k_f8_tiles<BM, kWide, kCodes><<<grid, 512, 0, st>>>(part);
       else if (a.wide_sums) (act ? k_f8_tiles<BM, kWide, kRowsAct> : k_f8_tiles<BM, kWide, kRows>)<<<grid, 512, 0, st>>>(part);
       else if (a.pow2) (act ? k_f8_tiles<BM, kPow2, kRowsAct> : k_f8_tiles<BM, kPow2, kRows>)<<<grid, 512, 0, st>>>(part);
       else (act ? k_f8_tiles<BM, kScaled, kRowsAct> : k_f8_tiles<BM, kScaled, kRows>)<<<grid, 512, 0, st>>>(part);

@@ -229,7 +229,13 @@ __global__ __launch_bounds__(kWaves * 64, IN == kCodes ? 2 : 4) void k_f8_rows(S
 #pragma unroll
         for (int j = 0; j < 4; ++j) o[j] = pack4(hv[4 * j] * inv, hv[4 * j + 1] * inv, hv[4 * j + 2] * inv, hv[4 * j + 3] * inv);
         if (m < nr) {
-          *reinterpret_cast<u4*>(static_cast<uint8_t*>(a.Y) + (int64_t)(r0 + m) * a.ld_y + blockIdx.x * 128 + c0) = o;
+          const int64_t at = (int64_t)(r0 + m) * a.ld_y + blockIdx.x * 128 + c0;
+          if (a.h_wide) {
+            put_codes(a.Y, at, u2{o[0], o[1]}, 1);
+            put_codes(a.Y, at + 8, u2{o[2], o[3]}, 1);
+          } else {
+            *reinterpret_cast<u4*>(static_cast<uint8_t*>(a.Y) + at) = o;
+          }
           if ((u & 7) == 0) a.SH[(int64_t)blockIdx.x * a.ld_sh + r0 + m] = scale;
         }
       }
