@@ -493,6 +493,9 @@ stamp_status_t stamp_moe_forward(const stamp_router_t* router, const stamp_fp8_p
                                  const void* X_dev, int64_t ld_x, const stamp_epilogue_t* epilogue, void* Y_dev, int64_t ld_y, void* workspace_dev,
                                  size_t workspace_bytes, void* hip_stream);
 
+/* How a call with so many tokens runs: 1 = in two kernels of its own (few tokens), 0 = by the kernels of the other calls; 0 too for what is refused. */
+int32_t stamp_moe_debug_route(const stamp_fp8_plan_t* up, const stamp_fp8_plan_t* down, int32_t tokens, int32_t top_k);
+
 /* For tests: a plan's codes [experts][2 if gated][d_out][d_in] and scales in the layout of w_scales_dev, copied to host.
  * Synchronizes the device. */
 stamp_status_t stamp_fp8_debug_weight_codes(const stamp_fp8_plan_t* plan, uint8_t* codes_host, float* scales_host);

@@ -30,6 +30,7 @@ from .fp8 import (  # noqa: F401
     mlp_workspace,
     moe_forward,
     moe_workspace,
+    moe_route,
     ACTIVATIONS,
     STAMP_E4M3,
     STAMP_SCALE_F32,

@@ -123,6 +123,32 @@ hipError_t stamp_launch_combine(const stamp_routing_t& r, const void* rows, int 
 hipError_t stamp_launch_router(const stamp_router_t& router, const void* X, int x_bf16, int64_t ld_x, int tokens, int experts, int d, float* logits,
                                hipStream_t st);
 
+// The whole layer in two kernels for few tokens and few rows, as long as a token's h for every token fits the LDS beside each other; else the kernels of the
+// other calls one after the other.  us, two kernels / the others (weights not in the cache):
+//                               1 token     2           4            8            16
+//   6 of 64,  2048 -> 1408        29 / 37     39 / 49     50 / 59      73 / 79      99 / 106
+//   8 of 256, 4096 -> 1536        49 / 59     69 / 107    119 / 152    202 / 227    336 / 358
+//   2 of 16,  1024 -> 512         14 / 25     16 / 26     17 / 26      22 / 28      25 / 29
+//   2 of 8,   4096 -> 2048        30 / 50     35 / 54     52 / 61      57 / 66      64 / 70
+//   16 of 64, 2048 -> 1408        48 / 62     66 / 74     82 / 91      113 / 119    142 / 126
+//   32 of 128, 1024 -> 512        40 / 48     48 / 64     56 / 60      67 / 67      80 / 71
+// Beyond 128 rows Q8 of h, which every workgroup does again for its part of the rows, is what loses.
+constexpr int kMoeTokens = 16, kMoeSlots = 128;
+constexpr int kMoeChunkBytes = 96 << 10;
+// workgroups that share 64 columns of Y, at most: as many as fit the CUs
+inline int stamp_moe_parts(int groups) {
+  const int fit = stamp_device_cus() / groups;
+  return fit < 1 ? 1 : fit > 16 ? 16 : fit;
+}
+inline size_t stamp_moe_sync_bytes(int groups) { return (size_t)(1 + kMoeSlots + groups) * 4; }
+inline bool stamp_moe_fits(int tokens, int top_k, int Kb_down) {
+  return tokens <= kMoeTokens && tokens * top_k <= kMoeSlots && (int64_t)tokens * (Kb_down * 132 + 16) <= kMoeChunkBytes;
+}
+// up: act, Y for h in fp32 (ld_y whole blocks); down: R, Y.  sync: stamp_moe_sync_bytes of any content; sums: parts * tokens * groups * 64.
+hipError_t stamp_launch_moe(const stamp_router_t& router, const stamp_routing_t& r, const void* X, int x_bf16, int64_t ld_x, const StampF8Gemm& up,
+                            const StampF8Gemm& down, uint8_t* codes, float* scales, float* logits, uint32_t* sync, float* sums,
+                            hipStream_t st);
+
 // ---- device helpers ----
 #ifdef __HIPCC__
 namespace f8 {

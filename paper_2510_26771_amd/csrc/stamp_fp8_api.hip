@@ -329,12 +329,20 @@ bool mlp_codes_in_tiles(const StampF8Gemm& up, const StampF8Gemm& down, int rows
 
 // The layer of experts' places: logits and the router's, then those of the experts.
 struct MoeWs {
-  size_t logits, route, experts, total;
+  size_t logits, sync, h, sums, route, experts, total;
 };
+bool moe_few(const stamp_fp8_plan* up, const stamp_fp8_plan* down, int32_t tokens, int32_t top_k) {
+  return stamp_moe_fits(tokens, top_k, down->Kb) && up->forced == 0 && down->forced == 0;  // a plan's forced kernel is one of the others
+}
 MoeWs moe_ws(const stamp_fp8_plan* up, const stamp_fp8_plan* down, int32_t tokens, int32_t top_k) {
   MoeWs w;
   w.logits = 0;
-  w.route = align256((size_t)tokens * up->desc.experts * sizeof(float));
+  w.sync = align256((size_t)tokens * up->desc.experts * sizeof(float));
+  // for the two kernels of few tokens: h in fp32, parts of Y
+  w.h = w.sync + align256(stamp_moe_sync_bytes(down->groups));
+  const int few = tokens < kMoeTokens ? tokens : kMoeTokens, slots = few * top_k;
+  w.sums = w.h + align256((size_t)(slots < kMoeSlots ? slots : kMoeSlots) * down->Kp * sizeof(float));
+  w.route = w.sums + align256((size_t)stamp_moe_parts(down->groups) * few * down->groups * 64 * sizeof(float));
   w.experts = w.route + align256(stamp_route_ws(tokens, up->desc.experts, top_k));
   w.total = w.experts + experts_ws(up, down, tokens, top_k, true).total;
   return w;
@@ -682,6 +690,10 @@ size_t stamp_moe_workspace_bytes(const stamp_fp8_plan_t* up, const stamp_fp8_pla
   return check_experts(e) == STAMP_OK ? moe_ws(up, down, tokens, top_k).total : 0;
 }
 
+int32_t stamp_moe_debug_route(const stamp_fp8_plan_t* up, const stamp_fp8_plan_t* down, int32_t tokens, int32_t top_k) {
+  return stamp_moe_workspace_bytes(up, down, tokens, top_k) > 0 && tokens > 0 && moe_few(up, down, tokens, top_k);
+}
+
 stamp_status_t stamp_moe_forward(const stamp_router_t* router, const stamp_fp8_plan_t* up, const stamp_fp8_plan_t* down, const stamp_routing_t* r,
                                  const void* X_dev, int64_t ld_x, const stamp_epilogue_t* epilogue, void* Y_dev, int64_t ld_y, void* workspace_dev,
                                  size_t workspace_bytes, void* hip_stream) {
@@ -702,6 +714,23 @@ stamp_status_t stamp_moe_forward(const stamp_router_t* router, const stamp_fp8_p
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
   uint8_t* ws = static_cast<uint8_t*>(workspace_dev);
   float* logits = reinterpret_cast<float*>(ws + w.logits);
+  if (r->tokens > 0 && moe_few(up, down, r->tokens, r->top_k)) {
+    // the places of the experts' rows serve here, too
+    const ExpertsWs v = experts_ws(up, down, r->tokens, r->top_k, true);
+    uint8_t* const rows = ws + w.experts;
+    StampF8Gemm a = gemm_args(up), b = gemm_args(down);
+    a.d = up->desc.d_in;
+    a.act = epilogue->activation;
+    a.ld_sa = scales_ld(r->tokens);
+    a.Y = ws + w.h;
+    a.ld_y = down->Kp;
+    b.R = epilogue->residual_dev;
+    b.ld_r = epilogue->ld_residual;
+    b.Y = Y_dev;
+    b.ld_y = ld_y;
+    return done(stamp_launch_moe(*router, *r, X_dev, up->desc.x_dtype == STAMP_BF16, ld_x, a, b, rows + v.codes, reinterpret_cast<float*>(rows + v.scales), logits,
+                                 reinterpret_cast<uint32_t*>(ws + w.sync), reinterpret_cast<float*>(ws + w.sums), st));
+  }
   if (r->tokens > 0 && stamp_launch_router(*router, X_dev, up->desc.x_dtype == STAMP_BF16, ld_x, r->tokens, r->experts, up->desc.d_in, logits, st) != hipSuccess)
     return STAMP_ERR_DEVICE;
   if (stamp_launch_route(*r, logits, 0, r->experts, router->renormalize, ws + w.route, st) != hipSuccess) return STAMP_ERR_DEVICE;

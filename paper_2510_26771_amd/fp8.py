@@ -296,6 +296,11 @@ def moe_workspace(up: Fp8Plan, down: Fp8Plan, tokens: int, top_k: int, device="c
     return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
 
 
+def moe_route(up: Fp8Plan, down: Fp8Plan, tokens: int, top_k: int) -> str:
+    """How moe_forward runs so many tokens: "few" (two kernels of its own) or "many" (the other calls' kernels)."""
+    return "few" if up.lib.stamp_moe_debug_route(up._h, down._h, int(tokens), int(top_k)) else "many"
+
+
 def moe_forward(router, up: Fp8Plan, down: Fp8Plan, X, routing: Routing, Y, workspace, router_bias=None, renormalize: bool = True, activation="silu",
                 residual=None, stream=None):
     """A whole layer of experts: logits X router^T + router_bias (router: [experts, d] in float32 or bfloat16), their routing (-> routing), and the

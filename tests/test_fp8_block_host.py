@@ -24,6 +24,7 @@ def test_null(lib):  # noqa: F811
         assert lib.stamp_moe_forward(router, None, None, C.byref(r), None, 0, e, None, 0, None, 0, None) == 1
     assert lib.stamp_mlp_workspace_bytes(None, None, 4) == 0
     assert lib.stamp_moe_workspace_bytes(None, None, 4, 2) == 0
+    assert lib.stamp_moe_debug_route(None, None, 4, 2) == 0
 
 
 def _calls(plan, r):

@@ -305,6 +305,32 @@ def test_layer_of_experts_against_the_definition(st, tokens, E, top_k, d, ff, x,
     down.destroy()
 
 
+# few tokens go through two kernels of their own; the same by the other calls' kernels, one after the other; and where the rows become too many or too long
+@pytest.mark.parametrize("tokens,E,top_k,d,ff,two", [(1, 20, 4, 384, 300, 1), (16, 40, 8, 256, 140, 1), (16, 40, 9, 256, 140, 0), (4, 200, 32, 256, 64, 1), (16, 3, 2, 128, 6100, 0),
+                                                     (3, 3, 2, 130, 5000, 1), (1, 2, 2, 128, 20000, 1), (17, 9, 2, 256, 256, 0), (16, 12, 1, 1600, 200, 1)])
+def test_layer_of_experts_in_two_kernels_and_in_others(st, tokens, E, top_k, d, ff, two):
+    import torch
+    rng = np.random.default_rng(tokens * 100 + E)
+    xv, xg, w_up, s_up, w_down, s_down, b, rt, rtg, up, down = _moe_case(st, rng, tokens, E, d, ff, "bf16", "f32", "f32", 0, 1)
+    res, R, _ = _values(rng, tokens, d, "f32", 1)
+    want, tol, ids, weights, offsets, token, row, dw = block.moe(xv, rt, None, w_up, s_up, w_down, s_down, b, top_k, 1, "silu", res, "f32", 0)
+    r, room = st.Routing(tokens, E, top_k), st.moe_workspace(up, down, tokens, top_k)
+    got = []
+    for route in ("", "rows", "tiles_64"):
+        up.set_route(route)
+        down.set_route(route)
+        assert st.moe_route(up, down, tokens, top_k) == ("few" if two and not route else "many")
+        Y = torch.full((tokens, d), -7.0, device="cuda")
+        room.fill_(255)
+        st.moe_forward(rtg, up, down, xg, r, Y, room, residual=R)
+        _held(Y, want, tol, route)
+        assert np.array_equal(r.ids.cpu().numpy(), ids) and np.array_equal(r.offsets.cpu().numpy(), offsets)
+        assert np.array_equal(r.token_of_row.cpu().numpy(), token) and np.array_equal(r.row_of_slot.cpu().numpy(), row)
+        got.append(Y)
+    up.destroy()
+    down.destroy()
+
+
 @pytest.mark.parametrize("tokens", [1, 4, 16, 33])
 def test_tokens_without_an_expert_and_in_place(st, tokens):
     """All experts out of use: Y is the residual, or zeros.  X, the residual and Y as one tensor."""
