@@ -64,6 +64,7 @@ struct StampF8Gemm {
   int64_t ld_y;
   int32_t codes;           // not gated: Y as codes (in tiles alone)
   int32_t h_wide;          // codes of Y as bf16
+  int32_t h_rows;          // gated, few rows: Y as rows of N values in fp32 instead of codes
   int32_t act;             // stamp_activation_t, of the gate where gated
   const void* R;           // residual rows in Y's type, or nullptr
   int64_t ld_r;

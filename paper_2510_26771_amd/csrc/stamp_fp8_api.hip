@@ -300,13 +300,15 @@ stamp_status_t run_experts(const ExpertsRun& e, uint8_t* ws, hipStream_t st) {
 struct MlpWs {
   size_t codes, scales, h, hcodes, hscales, partial, total;
 };
-constexpr int32_t kMlpRowsInFp32 = 1024;  // up to so many rows of h may lie in fp32
+// up to so many rows of h may lie in fp32, of a gated layer
+constexpr int32_t kMlpRowsInFp32 = 1024, kMlpGatedRows = 16;
 MlpWs mlp_ws(const stamp_fp8_plan* up, const stamp_fp8_plan* down, int32_t rows) {
   MlpWs w;
   w.codes = 0;
   w.scales = align256((size_t)rows * up->Kp * 2);  // bf16 codes: h is a sum in fp32
   w.h = w.scales + align256((size_t)up->Kb * scales_ld(rows) * sizeof(float));
-  w.hcodes = w.h + (up->desc.gated ? 0 : align256((size_t)(rows < kMlpRowsInFp32 ? rows : kMlpRowsInFp32) * up->desc.d_out * sizeof(float)));
+  const int32_t most = up->desc.gated ? kMlpGatedRows : kMlpRowsInFp32;
+  w.hcodes = w.h + align256((size_t)(rows < most ? rows : most) * up->desc.d_out * sizeof(float));
   w.hscales = w.hcodes + align256((size_t)rows * down->Kp * code_bytes(down));
   w.partial = w.hscales + align256((size_t)down->Kb * scales_ld(rows) * sizeof(float));
   const size_t pu = up->desc.gated ? 0 : stamp_f8_partial_bytes(up->groups, rows), pd = stamp_f8_partial_bytes(down->groups, rows);
@@ -607,6 +609,8 @@ stamp_status_t stamp_mlp_forward(const stamp_fp8_plan_t* up, const stamp_fp8_pla
   a.codes = !up->desc.gated && mlp_codes_in_tiles(a, b, rows);
   if (a.codes && a.forced <= STAMP_FP8_ROUTE_ROWS) a.forced = stamp_f8_codes_route(a.groups, a.Kb, rows);
   a.act = epilogue->activation;
+  a.h_rows = a.gated && rows <= kMlpGatedRows && route_of(a, rows) == STAMP_FP8_ROUTE_ROWS;
+  const bool coded = (a.gated || a.codes) && !a.h_rows;
   float* scales = reinterpret_cast<float*>(ws + w.scales);
   if (takes_x(a, rows)) {
     give_x(&a, up->desc, rows, X_dev, ld_x);
@@ -620,7 +624,7 @@ stamp_status_t stamp_mlp_forward(const stamp_fp8_plan_t* up, const stamp_fp8_pla
   a.a_rows = a.rows = rows;
   a.partial = b.partial = reinterpret_cast<float*>(ws + w.partial);
   float* const hscales = reinterpret_cast<float*>(ws + w.hscales);
-  if (a.gated || a.codes) {
+  if (coded) {
     a.Y = ws + w.hcodes;
     a.ld_y = down->Kp;
     a.SH = hscales;
@@ -631,7 +635,7 @@ stamp_status_t stamp_mlp_forward(const stamp_fp8_plan_t* up, const stamp_fp8_pla
     a.ld_y = up->desc.d_out;
   }
   if (product(a, st) != hipSuccess) return STAMP_ERR_DEVICE;
-  if (!a.gated && !a.codes) {
+  if (!coded) {
     stamp_fp8_desc_t h = down->desc;
     h.x_dtype = STAMP_F32;
     if (takes_x(b, rows)) give_x(&b, h, rows, a.Y, a.ld_y);

@@ -18,7 +18,8 @@ using namespace f8;
 enum Rows { kCodes, kBf16, kF32 };
 
 // MT: tiles of 16 rows held at once.  NB: blocks of 16 places per wave.  S: parts of the depth; kWaves / S waves lie side by side.
-template <int MT, int NB, int S, int kWaves, bool GATED, Rows IN>
+// GATED: codes of act(gate) * up, in workgroups of 256 places, or (H_ROWS) those values in fp32, in workgroups of any even number of blocks.
+template <int MT, int NB, int S, int kWaves, bool GATED, Rows IN, bool H_ROWS = false>
 __global__ __launch_bounds__(kWaves * 64, IN == kCodes ? 2 : 4) void k_f8_rows(StampF8Gemm a) {
   constexpr int kSide = kWaves / S;             // waves side by side
   constexpr int kPlaces = kSide * NB * 16;      // places of the workgroup
@@ -180,7 +181,20 @@ __global__ __launch_bounds__(kWaves * 64, IN == kCodes ? 2 : 4) void k_f8_rows(S
 #pragma unroll
       for (int b = 0; b < NB; ++b) *reinterpret_cast<f4*>(&red[part][16 * mi + (lane & 15)][(side * NB + b) * 16 + 4 * f]) = acc[mi][b];
     __syncthreads();
-    if constexpr (!GATED) {
+    if constexpr (H_ROWS) {
+      static_assert(GATED && NB % 2 == 0, "gate and up side by side");
+      for (int u = t; u < nr * (kPlaces / 2); u += kWaves * 64) {
+        const int m = u / (kPlaces / 2), q = u % (kPlaces / 2), pl = (q >> 4) * 32 + (q & 15);
+        const int blk = blockIdx.x * (kSide * NB) + (pl >> 4);
+        const int n = f8_column(1, blk >> 2, blk & 3, pl & 15);
+        if (n >= a.N) continue;
+        float h[1] = {red[0][m][pl]}, up[1] = {red[0][m][pl + 16]};
+#pragma unroll
+        for (int s = 1; s < S; ++s) h[0] += red[s][m][pl], up[0] += red[s][m][pl + 16];
+        gate(h, up, a.act);
+        static_cast<float*>(a.Y)[(int64_t)(r0 + m) * a.ld_y + n] = h[0];
+      }
+    } else if constexpr (!GATED) {
       for (int u = t; u < nr * kPlaces; u += kWaves * 64) {
         const int m = u / kPlaces, pl = u % kPlaces;
         const int blk = blockIdx.x * (kSide * NB) + (pl >> 4);
@@ -246,18 +260,19 @@ __global__ __launch_bounds__(kWaves * 64, IN == kCodes ? 2 : 4) void k_f8_rows(S
 int row_bytes(int Kb) { return Kb * 128 + 16 + Kb * 4; }  // of a row quantized here
 constexpr int kCodesLds = 68 << 10;                       // 16 rows of 4096 channels, two workgroups a CU
 
-template <int MT, int NB, int S, int WV, bool GATED, Rows IN>
+template <int MT, int NB, int S, int WV, bool GATED, Rows IN, bool H_ROWS = false>
 hipError_t go(const StampF8Gemm& a, hipStream_t st) {
   const int places = WV / S * NB * 16, sums = S * 16 * MT * (places + 4) * 4, codes = IN == kCodes ? 0 : a.chunk * row_bytes(a.Kb);
   const int lds = codes > sums ? codes : sums;
   static size_t done[kStampMaxDevices];
-  const hipError_t e = stamp_allow_lds(reinterpret_cast<const void*>(&k_f8_rows<MT, NB, S, WV, GATED, IN>), (size_t)lds, done);
+  const hipError_t e = stamp_allow_lds(reinterpret_cast<const void*>(&k_f8_rows<MT, NB, S, WV, GATED, IN, H_ROWS>), (size_t)lds, done);
   if (e != hipSuccess) return e;
-  k_f8_rows<MT, NB, S, WV, GATED, IN><<<dim3((a.groups * 64 + places - 1) / places, a.sets), WV * 64, lds, st>>>(a);
+  k_f8_rows<MT, NB, S, WV, GATED, IN, H_ROWS><<<dim3((a.groups * 64 + places - 1) / places, a.sets), WV * 64, lds, st>>>(a);
   return hipGetLastError();
 }
 template <Rows IN>
 hipError_t quantizing(const StampF8Gemm& a, int nb, hipStream_t st) {
+  if (a.h_rows) return go<1, 2, 8, 8, true, IN, true>(a, st);
   if (a.gated) return go<1, 2, 2, 16, true, IN>(a, st);
   return nb >= 2 ? go<1, 2, 8, 8, false, IN>(a, st) : go<1, 1, 8, 8, false, IN>(a, st);
 }
@@ -282,6 +297,7 @@ hipError_t stamp_launch_f8_rows(const StampF8Gemm& a, hipStream_t st) {
   const int cus = stamp_device_cus();
   const int nb = groups >= cus ? 4 : 2 * groups >= cus ? 2 : 1;
   if (a.X != nullptr) return a.x_bf16 ? quantizing<kBf16>(a, nb, st) : quantizing<kF32>(a, nb, st);
+  if (a.h_rows) return go<1, 2, 8, 8, true, kCodes, true>(a, st);
   if (a.gated) return avg <= 16 ? go<1, 4, 2, 8, true, kCodes>(a, st) : go<2, 4, 2, 8, true, kCodes>(a, st);
   if (avg <= 16)
     return nb == 4 ? go<1, 4, 8, 8, false, kCodes>(a, st) : nb == 2 ? go<1, 2, 8, 8, false, kCodes>(a, st) : go<1, 1, 8, 8, false, kCodes>(a, st);
