@@ -421,19 +421,23 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
     // (8192 x 1152 -> 4607 79 us, rows 4608 apart 58): there a lane stores its words from the second element on, the last one with the next lane's
     // first element, and the ends of the wave's 64 columns one by one.
     const bool between = bf16 && ((reinterpret_cast<uintptr_t>(base) | ld) & 2) != 0 && 64 * g + 64 <= N;
-    // residual: of the row block being worked on and the next, which is on its way meanwhile
+    // residual: of the row block being worked on and the next ones, which are on their way meanwhile (the operands' registers are free by now)
+    constexpr int kAhead = MI < 4 ? MI : 4;
     constexpr bool kBf16 = !WIDE;  // Y's type (f8_wide_sums)
-    [[maybe_unused]] Residual8<kBf16> res[2][2];
+    [[maybe_unused]] Residual8<kBf16> res[kAhead][2];
     const bool add_r = OUT == kRowsAct && whole && a.R != nullptr;
     [[maybe_unused]] auto ask = [&](int mi) __attribute__((always_inline)) {
       const uint32_t ld_r = (uint32_t)a.ld_r * (kBf16 ? 2 : 4);
       const int m = wm * (BM / 2) + 16 * mi + (lane & 15);
       const char* const r = static_cast<const char*>(a.R) + (int64_t)row0 * a.ld_r * (kBf16 ? 2 : 4) + ((uint32_t)m * ld_r + (uint32_t)n0 * (kBf16 ? 2 : 4));
 #pragma unroll
-      for (int h = 0; h < 2; ++h) res[mi & 1][h].load(r + 32 * h * (kBf16 ? 2 : 4), m < nrows ? N - n0 - 32 * h : 0);
+      for (int h = 0; h < 2; ++h) res[mi % kAhead][h].load(r + 32 * h * (kBf16 ? 2 : 4), m < nrows ? N - n0 - 32 * h : 0);
     };
     if constexpr (OUT == kRowsAct) {
-      if (add_r) ask(0);
+      if (add_r) {
+#pragma unroll
+        for (int mi = 0; mi < kAhead; ++mi) ask(mi);
+      }
     }
 #pragma unroll
     for (int mi = 0; mi < MI; ++mi) {
@@ -443,11 +447,11 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
 #pragma unroll
       for (int j = 0; j < 16; ++j) v[j] = acc[mi][j >> 2][j & 3] + bias[j];
       if constexpr (OUT == kRowsAct) {
-        if (add_r && mi + 1 < MI) ask(mi + 1);
         if (whole) activate(v, a.act);
         if (add_r) {
 #pragma unroll
-          for (int j = 0; j < 16; ++j) v[j] += res[mi & 1][j >> 3].at(j & 7);
+          for (int j = 0; j < 16; ++j) v[j] += res[mi % kAhead][j >> 3].at(j & 7);
+          if (mi + kAhead < MI) ask(mi + kAhead);
         }
       }
       u4 w[2];

@@ -32,8 +32,8 @@ def activation(z, name):
 def activated(z, dz, name):
     """(act(z), bound) of an argument that is dz off.  No activation is steeper than 1.13.  Of its own an fp32 evaluation is off by
     |z| times at most 4 U: the logistic's slope times its argument is at most 0.23 (of gelu's Phi: its density times a, 0.25), so an argument's relative
-    error of 3 U counts less than U; the exponential, 1 + it, the reciprocal (or Phi's polynomial, 5e-8 and its roundings) and the product U each at
-    most, halved where they are single roundings."""
+    error of 3 U counts less than U (Phi's argument is a polynomial's value, which is as much off); the exponential, 1 + it, the reciprocal and the product U
+    each at most, halved where they are single roundings."""
     return activation(z, name), 1.13 * dz + (0.0 if name in ("none", "relu") else 4 * U * np.abs(z))
 
 
