@@ -74,6 +74,8 @@ struct StampF8Gemm {
   uint32_t first;          // workgroups of the launches before this one (tiles)
 };
 
+inline bool f8_has_epilogue(const StampF8Gemm& a) { return !a.gated && (a.act != STAMP_ACT_NONE || a.R != nullptr); }
+
 // A launch of 2^32 threads or more is refused: units beyond that many workgroups are taken by further launches.
 constexpr int64_t kF8MaxThreads = (int64_t)1 << 31;
 template <typename F>

@@ -560,7 +560,7 @@ __global__ __launch_bounds__(256) void k_f8_widen(const uint8_t* codes, int64_t 
 }
 
 // Y = sum of the parts, in order.  A thread has 4 columns of a row and all parts in flight.  Bound by its launch: 4 parts of 1310 x 384 4.3 us.
-template <int PARTS>
+template <int PARTS, bool ACT>
 __global__ __launch_bounds__(256) void k_f8_join(StampF8Gemm a) {
   const int N = a.groups * 64, per = (a.N + 3) / 4;
   const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x, m = u / per;
@@ -574,13 +574,15 @@ __global__ __launch_bounds__(256) void k_f8_join(StampF8Gemm a) {
   f4 s = v[0];
 #pragma unroll
   for (int i = 1; i < PARTS; ++i) s += v[i];
-  float(&e)[4] = reinterpret_cast<float(&)[4]>(s);
-  activate(e, a.act);
-  if (a.R != nullptr) {
+  if constexpr (ACT) {
+    float(&e)[4] = reinterpret_cast<float(&)[4]>(s);
+    activate(e, a.act);
+    if (a.R != nullptr) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      if (c + j >= a.N) continue;
-      e[j] += a.y_bf16 ? bf16_lo(static_cast<const uint16_t*>(a.R)[m * a.ld_r + c + j]) : static_cast<const float*>(a.R)[m * a.ld_r + c + j];
+      for (int j = 0; j < 4; ++j) {
+        if (c + j >= a.N) continue;
+        e[j] += a.y_bf16 ? bf16_lo(static_cast<const uint16_t*>(a.R)[m * a.ld_r + c + j]) : static_cast<const float*>(a.R)[m * a.ld_r + c + j];
+      }
     }
   }
   if (a.y_bf16) {
@@ -604,6 +606,21 @@ __global__ __launch_bounds__(256) void k_f8_join(StampF8Gemm a) {
   }
 }
 
+template <bool ACT>
+hipError_t join(const StampF8Gemm& a, int parts, hipStream_t st) {
+  const int64_t n = (int64_t)a.rows * ((a.N + 3) / 4);
+  static_assert(kF8MaxParts == 8, "a kernel for every number of parts");
+  auto* const k = parts == 2   ? k_f8_join<2, ACT>
+                  : parts == 3 ? k_f8_join<3, ACT>
+                  : parts == 4 ? k_f8_join<4, ACT>
+                  : parts == 5 ? k_f8_join<5, ACT>
+                  : parts == 6 ? k_f8_join<6, ACT>
+                  : parts == 7 ? k_f8_join<7, ACT>
+                               : k_f8_join<8, ACT>;
+  k<<<(uint32_t)((n + 255) / 256), 256, 0, st>>>(a);
+  return hipGetLastError();
+}
+
 template <int BM>
 hipError_t go(const StampF8Gemm& a, int parts, hipStream_t st) {
   const int64_t tiles = a.offsets == nullptr ? ((int64_t)a.rows + BM - 1) / BM : (int64_t)a.rows / BM + (a.sets < a.rows ? a.sets : a.rows);
@@ -613,7 +630,7 @@ hipError_t go(const StampF8Gemm& a, int parts, hipStream_t st) {
     const dim3 grid(n, parts);
     StampF8Gemm part = a;
     part.first = (uint32_t)first;
-    const bool act = a.act != STAMP_ACT_NONE || a.R != nullptr;
+    const bool act = f8_has_epilogue(a);
     if constexpr (BM == 256) {
       if (a.pow2) (act ? k_f8_tiles<BM, kPow2, kRowsAct> : k_f8_tiles<BM, kPow2, kRows>)<<<grid, 512, 0, st>>>(part);
       else (act ? k_f8_tiles<BM, kScaled, kRowsAct> : k_f8_tiles<BM, kScaled, kRows>)<<<grid, 512, 0, st>>>(part);
@@ -626,18 +643,7 @@ hipError_t go(const StampF8Gemm& a, int parts, hipStream_t st) {
     }
   });
   if (e != hipSuccess) return e;
-  if (parts > 1) {
-    const int64_t n = (int64_t)a.rows * ((a.N + 3) / 4);
-    static_assert(kF8MaxParts == 8, "a kernel for every number of parts");
-    auto* const join = parts == 2   ? k_f8_join<2>
-                       : parts == 3 ? k_f8_join<3>
-                       : parts == 4 ? k_f8_join<4>
-                       : parts == 5 ? k_f8_join<5>
-                       : parts == 6 ? k_f8_join<6>
-                       : parts == 7 ? k_f8_join<7>
-                                    : k_f8_join<8>;
-    join<<<(uint32_t)((n + 255) / 256), 256, 0, st>>>(a);
-  }
+  if (parts > 1) return f8_has_epilogue(a) ? join<true>(a, parts, st) : join<false>(a, parts, st);
   return hipGetLastError();
 }
 }  // namespace

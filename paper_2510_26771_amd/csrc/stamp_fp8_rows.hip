@@ -18,9 +18,13 @@ using namespace f8;
 enum Rows { kCodes, kBf16, kF32 };
 
 // MT: tiles of 16 rows held at once.  NB: blocks of 16 places per wave.  S: parts of the depth; kWaves / S waves lie side by side.
-// GATED: codes of act(gate) * up, in workgroups of 256 places, or (H_ROWS) those values in fp32, in workgroups of any even number of blocks.
-template <int MT, int NB, int S, int kWaves, bool GATED, Rows IN, bool H_ROWS = false>
+// What becomes of the sums: rows of Y, the same with activation and residual (a kernel of its own: the choice costs a small layer 0.2 of 10 us), codes of
+// act(gate) * up in workgroups of 256 places, those values in fp32 in workgroups of any even number of blocks.
+enum Out { kRows, kRowsAct, kGated, kGatedRows };
+
+template <int MT, int NB, int S, int kWaves, Out OUT, Rows IN>
 __global__ __launch_bounds__(kWaves * 64, IN == kCodes ? 2 : 4) void k_f8_rows(StampF8Gemm a) {
+  constexpr bool GATED = OUT == kGated || OUT == kGatedRows;
   constexpr int kSide = kWaves / S;             // waves side by side
   constexpr int kPlaces = kSide * NB * 16;      // places of the workgroup
   constexpr int kLd = kPlaces + 4;              // floats of a row of partial sums
@@ -181,8 +185,8 @@ __global__ __launch_bounds__(kWaves * 64, IN == kCodes ? 2 : 4) void k_f8_rows(S
 #pragma unroll
       for (int b = 0; b < NB; ++b) *reinterpret_cast<f4*>(&red[part][16 * mi + (lane & 15)][(side * NB + b) * 16 + 4 * f]) = acc[mi][b];
     __syncthreads();
-    if constexpr (H_ROWS) {
-      static_assert(GATED && NB % 2 == 0, "gate and up side by side");
+    if constexpr (OUT == kGatedRows) {
+      static_assert(NB % 2 == 0, "gate and up side by side");
       for (int u = t; u < nr * (kPlaces / 2); u += kWaves * 64) {
         const int m = u / (kPlaces / 2), q = u % (kPlaces / 2), pl = (q >> 4) * 32 + (q & 15);
         const int blk = blockIdx.x * (kSide * NB) + (pl >> 4);
@@ -204,12 +208,14 @@ __global__ __launch_bounds__(kWaves * 64, IN == kCodes ? 2 : 4) void k_f8_rows(S
 #pragma unroll
         for (int s = 1; s < S; ++s) v += red[s][m][pl];
         if (a.bias != nullptr) v += a.bias[(size_t)set * a.N + n];
-        float w[1] = {v};
-        activate(w, a.act);
-        v = w[0];
-        if (a.R != nullptr) {
-          const int64_t o = (int64_t)(r0 + m) * a.ld_r + n;
-          v += a.y_bf16 ? bf16_lo(static_cast<const uint16_t*>(a.R)[o]) : static_cast<const float*>(a.R)[o];
+        if constexpr (OUT == kRowsAct) {
+          float w[1] = {v};
+          activate(w, a.act);
+          v = w[0];
+          if (a.R != nullptr) {
+            const int64_t o = (int64_t)(r0 + m) * a.ld_r + n;
+            v += a.y_bf16 ? bf16_lo(static_cast<const uint16_t*>(a.R)[o]) : static_cast<const float*>(a.R)[o];
+          }
         }
         const int64_t o = (int64_t)(r0 + m) * a.ld_y + n;
         if (a.y_bf16) static_cast<uint16_t*>(a.Y)[o] = to_bf16(v);
@@ -260,21 +266,33 @@ __global__ __launch_bounds__(kWaves * 64, IN == kCodes ? 2 : 4) void k_f8_rows(S
 int row_bytes(int Kb) { return Kb * 128 + 16 + Kb * 4; }  // of a row quantized here
 constexpr int kCodesLds = 68 << 10;                       // 16 rows of 4096 channels, two workgroups a CU
 
-template <int MT, int NB, int S, int WV, bool GATED, Rows IN, bool H_ROWS = false>
+template <int MT, int NB, int S, int WV, Out OUT, Rows IN>
 hipError_t go(const StampF8Gemm& a, hipStream_t st) {
   const int places = WV / S * NB * 16, sums = S * 16 * MT * (places + 4) * 4, codes = IN == kCodes ? 0 : a.chunk * row_bytes(a.Kb);
   const int lds = codes > sums ? codes : sums;
   static size_t done[kStampMaxDevices];
-  const hipError_t e = stamp_allow_lds(reinterpret_cast<const void*>(&k_f8_rows<MT, NB, S, WV, GATED, IN, H_ROWS>), (size_t)lds, done);
+  const hipError_t e = stamp_allow_lds(reinterpret_cast<const void*>(&k_f8_rows<MT, NB, S, WV, OUT, IN>), (size_t)lds, done);
   if (e != hipSuccess) return e;
-  k_f8_rows<MT, NB, S, WV, GATED, IN, H_ROWS><<<dim3((a.groups * 64 + places - 1) / places, a.sets), WV * 64, lds, st>>>(a);
+  k_f8_rows<MT, NB, S, WV, OUT, IN><<<dim3((a.groups * 64 + places - 1) / places, a.sets), WV * 64, lds, st>>>(a);
   return hipGetLastError();
+}
+template <Rows IN, Out OUT>
+hipError_t quantizing_rows(const StampF8Gemm& a, int nb, hipStream_t st) {
+  return nb >= 2 ? go<1, 2, 8, 8, OUT, IN>(a, st) : go<1, 1, 8, 8, OUT, IN>(a, st);
 }
 template <Rows IN>
 hipError_t quantizing(const StampF8Gemm& a, int nb, hipStream_t st) {
-  if (a.h_rows) return go<1, 2, 8, 8, true, IN, true>(a, st);
-  if (a.gated) return go<1, 2, 2, 16, true, IN>(a, st);
-  return nb >= 2 ? go<1, 2, 8, 8, false, IN>(a, st) : go<1, 1, 8, 8, false, IN>(a, st);
+  if (a.h_rows) return go<1, 2, 8, 8, kGatedRows, IN>(a, st);
+  if (a.gated) return go<1, 2, 2, 16, kGated, IN>(a, st);
+  return f8_has_epilogue(a) ? quantizing_rows<IN, kRowsAct>(a, nb, st) : quantizing_rows<IN, kRows>(a, nb, st);
+}
+template <Out OUT>
+hipError_t rows_of_codes(const StampF8Gemm& a, int avg, int nb, hipStream_t st) {
+  if (avg <= 16)
+    return nb == 4 ? go<1, 4, 8, 8, OUT, kCodes>(a, st) : nb == 2 ? go<1, 2, 8, 8, OUT, kCodes>(a, st) : go<1, 1, 8, 8, OUT, kCodes>(a, st);
+  if (avg <= 32)
+    return nb == 4 ? go<2, 4, 8, 8, OUT, kCodes>(a, st) : nb == 2 ? go<2, 2, 8, 8, OUT, kCodes>(a, st) : go<2, 1, 8, 8, OUT, kCodes>(a, st);
+  return nb >= 2 ? go<4, 2, 8, 8, OUT, kCodes>(a, st) : go<4, 1, 8, 8, OUT, kCodes>(a, st);
 }
 int average(const StampF8Gemm& a, int rows) { return (int)(((int64_t)rows + a.sets - 1) / a.sets); }
 }  // namespace
@@ -297,11 +315,8 @@ hipError_t stamp_launch_f8_rows(const StampF8Gemm& a, hipStream_t st) {
   const int cus = stamp_device_cus();
   const int nb = groups >= cus ? 4 : 2 * groups >= cus ? 2 : 1;
   if (a.X != nullptr) return a.x_bf16 ? quantizing<kBf16>(a, nb, st) : quantizing<kF32>(a, nb, st);
-  if (a.h_rows) return go<1, 2, 8, 8, true, kCodes, true>(a, st);
-  if (a.gated) return avg <= 16 ? go<1, 4, 2, 8, true, kCodes>(a, st) : go<2, 4, 2, 8, true, kCodes>(a, st);
-  if (avg <= 16)
-    return nb == 4 ? go<1, 4, 8, 8, false, kCodes>(a, st) : nb == 2 ? go<1, 2, 8, 8, false, kCodes>(a, st) : go<1, 1, 8, 8, false, kCodes>(a, st);
-  if (avg <= 32)
-    return nb == 4 ? go<2, 4, 8, 8, false, kCodes>(a, st) : nb == 2 ? go<2, 2, 8, 8, false, kCodes>(a, st) : go<2, 1, 8, 8, false, kCodes>(a, st);
-  return nb >= 2 ? go<4, 2, 8, 8, false, kCodes>(a, st) : go<4, 1, 8, 8, false, kCodes>(a, st);
+  // one row of 4096 -> 11008 -> 4096, gated: 34 us by rows of h and workgroups of 32 places, 46 by codes and workgroups of 256, which are 86
+  if (a.h_rows) return go<1, 2, 8, 8, kGatedRows, kCodes>(a, st);
+  if (a.gated) return avg <= 16 ? go<1, 4, 2, 8, kGated, kCodes>(a, st) : go<2, 4, 2, 8, kGated, kCodes>(a, st);
+  return f8_has_epilogue(a) ? rows_of_codes<kRowsAct>(a, avg, nb, st) : rows_of_codes<kRows>(a, avg, nb, st);
 }
