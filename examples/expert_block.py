@@ -1,5 +1,5 @@
-"""The MLP of a language model with experts, in 8-bit floating point: a dense layer, the router, the chosen experts and their sum, for a
-prompt and then token by token.
+"""The MLP of a language model with experts, in 8-bit floating point: the layer of experts with its router and residual, a dense MLP beside it and a
+dense layer, for a prompt and then token by token.
 
     python examples/expert_block.py [--tokens 512] [--steps 8] [--d 1024] [--ff 512] [--experts 16] [--top-k 2]
 
@@ -13,7 +13,7 @@ sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 
 
 class ExpertBlock:
-    """x -> x + experts(x), then a dense layer: what a decoder layer does between two attentions."""
+    """x -> y = x + experts(x), y -> y + mlp(y) (an MLP that all tokens share), then a dense layer: what decoder layers do between two attentions."""
 
     def __init__(self, d, ff, experts, top_k, seed=0):
         import torch
@@ -26,10 +26,13 @@ class ExpertBlock:
         self.st, self.d, self.experts, self.top_k = st, d, experts, top_k
         self.w_router = matrix(experts, d).float()
         self.w_up, self.w_down, self.w_dense = matrix(experts, 2, ff, d), matrix(experts, d, ff), matrix(d, d)
+        self.w_shared_up, self.w_shared_down = matrix(ff, d), matrix(d, ff) * 0.5
         bf16 = st.STAMP_BF16
         self.up = st.Fp8Plan(st.Fp8Desc(d_in=d, d_out=ff, experts=experts, gated=1, w_dtype=bf16), self.w_up)
         self.down = st.Fp8Plan(st.Fp8Desc(d_in=ff, d_out=d, experts=experts, w_dtype=bf16), self.w_down)
         self.dense = st.Fp8Plan(st.Fp8Desc(d_in=d, d_out=d, w_dtype=bf16), self.w_dense)
+        self.shared_up = st.Fp8Plan(st.Fp8Desc(d_in=d, d_out=ff, w_dtype=bf16), self.w_shared_up)
+        self.shared_down = st.Fp8Plan(st.Fp8Desc(d_in=ff, d_out=d, w_dtype=bf16), self.w_shared_down)
         self.room = {}
 
     def buffers(self, tokens):
@@ -37,16 +40,16 @@ class ExpertBlock:
         import torch
         if tokens not in self.room:
             st = self.st
-            self.room[tokens] = (st.Routing(tokens, self.experts, self.top_k), st.experts_workspace(self.up, self.down, tokens, self.top_k),
-                                 self.dense.alloc_workspace(tokens), *(torch.empty((tokens, self.d), dtype=torch.bfloat16, device="cuda") for _ in range(2)))
+            self.room[tokens] = (st.Routing(tokens, self.experts, self.top_k), st.moe_workspace(self.up, self.down, tokens, self.top_k),
+                                 st.mlp_workspace(self.shared_up, self.shared_down, tokens), self.dense.alloc_workspace(tokens), *(torch.empty((tokens, self.d), dtype=torch.bfloat16, device="cuda") for _ in range(2)))
         return self.room[tokens]
 
     def __call__(self, x):
         st = self.st
-        routing, ws, ws_dense, y, out = self.buffers(x.shape[0])
-        st.route_topk(x.float() @ self.w_router.t(), routing)
-        st.experts_forward(self.up, self.down, x, routing, y, ws)
-        self.dense.linear_forward(x + y, out, ws_dense)
+        routing, ws, ws_mlp, ws_dense, y, out = self.buffers(x.shape[0])
+        st.moe_forward(self.w_router, self.up, self.down, x, routing, y, ws, residual=x)
+        st.mlp_forward(self.shared_up, self.shared_down, y, y, ws_mlp, "gelu", residual=y)
+        self.dense.linear_forward(y, out, ws_dense)
         return out
 
     def reference(self, x):
@@ -60,7 +63,9 @@ class ExpertBlock:
             if t.numel():
                 gate, up = (x[t] @ self.w_up[e, i].float().t() for i in (0, 1))
                 y.index_add_(0, t, weights[t, j, None] * ((torch.nn.functional.silu(gate) * up) @ self.w_down[e].float().t()))
-        return (x + y) @ self.w_dense.float().t()
+        y = x + y
+        y = y + torch.nn.functional.gelu(y @ self.w_shared_up.float().t()) @ self.w_shared_down.float().t()
+        return y @ self.w_dense.float().t()
 
 
 def main(argv=None):
