@@ -528,3 +528,57 @@ def test_refusals(st):
     assert (r0.offsets == 0).all()
     for p in (lin, sq, down, gated1, gated2, down2):
         p.destroy()
+
+
+# ---- large calls: places beyond 2^32 bytes ----
+
+def test_rows_beyond_4_gib(st):
+    """Y, the residual and the codes of h pass 2^32 bytes; rows from all over are held against the definition."""
+    import torch
+    rng = np.random.default_rng(11)
+    rows, d, n = (1 << 20) + 77, 128, 4100
+    w, ws = _weights(rng, (), n, d, 0)
+    ws = _smaller(ws)
+    X = torch.empty((rows, d), dtype=torch.bfloat16, device="cuda").normal_()
+    R = torch.empty((rows, n), dtype=torch.bfloat16, device="cuda").normal_()
+    plan = st.Fp8Plan(st.Fp8Desc(d_in=d, d_out=n), _gpu(w), _gpu(ws))
+    Y, room = torch.empty_like(R), plan.alloc_workspace(rows)
+    some = np.concatenate([rng.integers(0, rows, 60), [0, 1, rows - 2, rows - 1]])
+    at = _gpu(some)
+    plan.linear_forward(X, Y, room, activation="gelu", residual=R)
+    x, res = X[at].float().cpu().numpy(), R[at].float().cpu().numpy().astype(np.float64)
+    _held(Y[at], *block.layer(x, w, ws, None, "gelu", res, "bf16", 0, False), "layer")
+    plan.destroy()
+    del R, Y, room
+    ff, m = 4224, 64
+    w1, s1 = _weights(rng, (), ff, d, 0)
+    w2, s2 = _weights(rng, (), m, ff, 0)
+    s1 = _smaller(s1)
+    up, down = st.Fp8Plan(st.Fp8Desc(d_in=d, d_out=ff), _gpu(w1), _gpu(s1)), st.Fp8Plan(st.Fp8Desc(d_in=ff, d_out=m, y_dtype=st.STAMP_F32), _gpu(w2), _gpu(s2))
+    room = st.mlp_workspace(up, down, rows)
+    assert room.numel() > 1 << 32
+    Y = torch.empty((rows, m), device="cuda")
+    st.mlp_forward(up, down, X, Y, room, "silu")
+    _held(Y[at], *block.mlp(x, w1, s1, None, w2, s2, None, "silu", None, "f32", 0), "mlp")
+    up.destroy()
+    down.destroy()
+
+
+def test_many_tokens_through_the_layer_of_experts(st):
+    import torch
+    rng = np.random.default_rng(12)
+    tokens, E, top_k, d, ff = 70000, 9, 3, 256, 200
+    _, _, w_up, s_up, w_down, s_down, b, rt, rtg, up, down = _moe_case(st, rng, 1, E, d, ff, "bf16", "bf16", "bf16", 0, 1)
+    X = torch.empty((tokens, d), dtype=torch.bfloat16, device="cuda").normal_()
+    r, room, Y = st.Routing(tokens, E, top_k), st.moe_workspace(up, down, tokens, top_k), torch.empty_like(X)
+    st.moe_forward(rtg, up, down, X, r, Y, room, residual=X)
+    x = X.float().cpu().numpy().astype(np.float64)
+    l, err = block.logits(x, rt, None)
+    apart = [i for i in rng.integers(0, tokens, 400) if block.clear(l[i:i + 1], err[i:i + 1], top_k)][:150]
+    assert len(apart) == 150
+    want, tol, ids, weights, *_, dw = block.moe(x[apart], rt, None, w_up, s_up, w_down, s_down, b, top_k, 1, "silu", x[apart], "bf16", 0)
+    at = _gpu(np.array(apart))
+    assert np.array_equal(r.ids[at].cpu().numpy(), ids) and int(r.offsets[-1]) == tokens * top_k
+    _held(Y[at], want, tol, "sampled tokens")
+    up.destroy()
+    down.destroy()
