@@ -20,6 +20,7 @@ constexpr int kF8Block = 128;
 constexpr int kF8Group = 64;                        // places of a group
 constexpr int kF8GroupBytes = kF8Group * kF8Block;  // of a group and block of channels
 constexpr int kF8MaxExperts = 1024;
+constexpr int kF8DividedSilu = 16;  // beside stamp_activation_t, for gated products
 
 struct stamp_fp8_plan {
   stamp_fp8_desc_t desc;
@@ -65,7 +66,7 @@ struct StampF8Gemm {
   int32_t codes;           // not gated: Y as codes (in tiles alone)
   int32_t h_wide;          // codes of Y as bf16
   int32_t h_rows;          // gated, few rows: Y as rows of N values in fp32 instead of codes
-  int32_t act;             // stamp_activation_t, of the gate where gated
+  int32_t act;             // stamp_activation_t, of the gate where gated (or kF8DividedSilu)
   const void* R;           // residual rows in Y's type, or nullptr
   int64_t ld_r;
   float* SH;
@@ -122,9 +123,17 @@ size_t stamp_route_ws(int tokens, int experts, int top_k);
 hipError_t stamp_launch_combine(const stamp_routing_t& r, const void* rows, int rows_bf16, int y_bf16, int64_t ld_rows, int nrows, const void* R, int64_t ld_r,
                                 void* Y, int64_t ld_y, int d, hipStream_t st);
 
-// logits [tokens][experts] = X W^T + bias
-hipError_t stamp_launch_router(const stamp_router_t& router, const void* X, int x_bf16, int64_t ld_x, int tokens, int experts, int d, float* logits,
-                               hipStream_t st);
+// logits [tokens][experts] = X W^T + bias; in the same launch Q8 of X (codes nullptr: not wanted; wide: as bf16) and zeros to `zeros` words
+struct RouterQ8 {
+  uint8_t* codes;
+  float* scales;
+  int64_t ld_s;
+  int32_t pow2, wide;
+  uint32_t* zero;
+  int32_t zeros;
+};
+hipError_t stamp_launch_router(const stamp_router_t& router, const void* X, int x_bf16, int64_t ld_x, int tokens, int experts, int d, const RouterQ8& q,
+                               float* logits, hipStream_t st);
 
 // The whole layer in two kernels for few tokens and few rows, as long as a token's h for every token fits the LDS beside each other; else the kernels of the
 // other calls one after the other.  us, two kernels / the others (weights not in the cache):
@@ -403,10 +412,10 @@ __device__ __forceinline__ void activate(float (&v)[N], int act) {
     for (int j = 0; j < N; ++j) v[j] = gelu_tanh(v[j]);
   }
 }
-// act(g) u; silu as the gated products have had it, by a division
+// act(g) u; kF8DividedSilu: silu by a division, as stamp_experts_forward has had it (8192 x 4096 -> 11008, gated: 1290 us of tiles by the reciprocal, 1310 so)
 template <int N>
 __device__ __forceinline__ void gate(float (&g)[N], const float (&u)[N], int act) {
-  if (act == STAMP_ACT_SILU) {
+  if (act == kF8DividedSilu) {
 #pragma unroll
     for (int j = 0; j < N; ++j) g[j] = silu(g[j]);
   } else {

@@ -41,7 +41,7 @@ StampF8Gemm gemm_args(const stamp_fp8_plan* p) {
   a.pow2 = p->desc.scale_format == STAMP_SCALE_POW2;
   a.gated = p->desc.gated;
   a.y_bf16 = p->desc.y_dtype == STAMP_BF16;
-  a.act = p->desc.gated ? STAMP_ACT_SILU : STAMP_ACT_NONE;
+  a.act = p->desc.gated ? kF8DividedSilu : STAMP_ACT_NONE;
   a.wide_sums = f8_wide_sums(a);
   a.forced = p->forced;
   return a;
@@ -235,6 +235,7 @@ struct ExpertsRun {
   void* Y;
   int64_t ld_y;
   bool wide_rows;  // the rows behind the down product in fp32 whatever Y's type
+  bool coded;      // Q8 of X is there, where run_experts would put it
 };
 stamp_status_t check_experts(const ExpertsRun& e) {
   const stamp_fp8_plan *up = e.up, *down = e.down;
@@ -264,7 +265,7 @@ stamp_status_t run_experts(const ExpertsRun& e, uint8_t* ws, hipStream_t st) {
   float* scales = reinterpret_cast<float*>(ws + w.scales);
   if (takes_x(a, slots)) {
     give_x(&a, up->desc, slots, e.X, e.ld_x);
-  } else if (stamp_launch_f8_quant(e.X, up->desc.x_dtype == STAMP_BF16, e.ld_x, r->tokens, up->desc.d_in, a.pow2, wide_codes(a, slots), ws + w.codes, scales,
+  } else if (!e.coded && stamp_launch_f8_quant(e.X, up->desc.x_dtype == STAMP_BF16, e.ld_x, r->tokens, up->desc.d_in, a.pow2, wide_codes(a, slots), ws + w.codes, scales,
                                    scales_ld(r->tokens), st) != hipSuccess) {
     return STAMP_ERR_DEVICE;
   }
@@ -676,7 +677,7 @@ size_t stamp_experts_workspace_bytes(const stamp_fp8_plan_t* up, const stamp_fp8
 stamp_status_t stamp_experts_forward(const stamp_fp8_plan_t* up, const stamp_fp8_plan_t* down, const stamp_routing_t* r, const void* X_dev, int64_t ld_x,
                                      void* Y_dev, int64_t ld_y, void* workspace_dev, size_t workspace_bytes, void* hip_stream) {
   if (up == nullptr || down == nullptr || r == nullptr) return STAMP_ERR_NULL;
-  const ExpertsRun e = {up, down, r, X_dev, ld_x, {STAMP_ACT_SILU, nullptr, 0}, Y_dev, ld_y, false};
+  const ExpertsRun e = {up, down, r, X_dev, ld_x, {kF8DividedSilu, nullptr, 0}, Y_dev, ld_y, false, false};
   stamp_status_t s = check_experts(e);
   if (s != STAMP_OK) return s;
   if (r->tokens == 0) return STAMP_OK;
@@ -690,7 +691,7 @@ size_t stamp_moe_workspace_bytes(const stamp_fp8_plan_t* up, const stamp_fp8_pla
   if (up == nullptr || down == nullptr) return 0;
   int32_t some = 0;  // an address, for the checks
   const stamp_routing_t r = {tokens, up->desc.experts, top_k, &some, reinterpret_cast<float*>(&some), &some, &some, &some};
-  const ExpertsRun e = {up, down, &r, nullptr, 0, {STAMP_ACT_SILU, nullptr, 0}, nullptr, 0, true};
+  const ExpertsRun e = {up, down, &r, nullptr, 0, {STAMP_ACT_SILU, nullptr, 0}, nullptr, 0, true, true};
   return check_experts(e) == STAMP_OK ? moe_ws(up, down, tokens, top_k).total : 0;
 }
 
@@ -702,7 +703,7 @@ stamp_status_t stamp_moe_forward(const stamp_router_t* router, const stamp_fp8_p
                                  const void* X_dev, int64_t ld_x, const stamp_epilogue_t* epilogue, void* Y_dev, int64_t ld_y, void* workspace_dev,
                                  size_t workspace_bytes, void* hip_stream) {
   if (router == nullptr || up == nullptr || down == nullptr || r == nullptr || epilogue == nullptr) return STAMP_ERR_NULL;
-  const ExpertsRun e = {up, down, r, X_dev, ld_x, *epilogue, Y_dev, ld_y, true};
+  const ExpertsRun e = {up, down, r, X_dev, ld_x, *epilogue, Y_dev, ld_y, true, true};
   stamp_status_t s = check_experts(e);
   if (s != STAMP_OK) return s;
   if (!is_float_type(router->w_dtype) || router->renormalize < 0 || router->renormalize > 1) return STAMP_ERR_SHAPE;
@@ -735,8 +736,15 @@ stamp_status_t stamp_moe_forward(const stamp_router_t* router, const stamp_fp8_p
     return done(stamp_launch_moe(*router, *r, X_dev, up->desc.x_dtype == STAMP_BF16, ld_x, a, b, rows + v.codes, reinterpret_cast<float*>(rows + v.scales), logits,
                                  reinterpret_cast<uint32_t*>(ws + w.sync), reinterpret_cast<float*>(ws + w.sums), st));
   }
-  if (r->tokens > 0 && stamp_launch_router(*router, X_dev, up->desc.x_dtype == STAMP_BF16, ld_x, r->tokens, r->experts, up->desc.d_in, logits, st) != hipSuccess)
-    return STAMP_ERR_DEVICE;
+  if (r->tokens > 0) {
+    const ExpertsWs v = experts_ws(up, down, r->tokens, r->top_k, true);
+    StampF8Gemm a = gemm_args(up);
+    const int slots = r->tokens * r->top_k;
+    RouterQ8 q = {ws + w.experts + v.codes, reinterpret_cast<float*>(ws + w.experts + v.scales), scales_ld(r->tokens), a.pow2, wide_codes(a, slots), nullptr, 0};
+    if (takes_x(a, slots)) q.codes = nullptr;
+    if (stamp_launch_router(*router, X_dev, up->desc.x_dtype == STAMP_BF16, ld_x, r->tokens, r->experts, up->desc.d_in, q, logits, st) != hipSuccess)
+      return STAMP_ERR_DEVICE;
+  }
   if (stamp_launch_route(*r, logits, 0, r->experts, router->renormalize, ws + w.route, st) != hipSuccess) return STAMP_ERR_DEVICE;
   return r->tokens > 0 ? run_experts(e, ws + w.experts, st) : STAMP_OK;
 }

@@ -12,7 +12,6 @@
 // expert), and its factor carries the router's weight.  So there are no rows to be written; the parts of a column are added up by the last of its workgroups, in
 // the parts' order, and nothing depends on the order of workgroups.
 #include "stamp_route.h"
-#include "stamp_router.h"
 
 namespace {
 using namespace f8;
@@ -24,7 +23,7 @@ constexpr int kUpLd = kF8Group + 4;    // floats of a row of an up product's par
 constexpr int kRoom = kWaves * 16 * kUpLd * 4 > kMoeChunkBytes ? kWaves * 16 * kUpLd * 4 : kMoeChunkBytes;
 
 struct MoeArgs {
-  RouterArgs router;
+  const float* logits;
   stamp_routing_t r;
   int32_t renorm;
   StampF8Gemm up, down;  // X as rows of up.X, codes and scales in up.A and up.SA; h in up.Y, fp32
@@ -35,29 +34,6 @@ struct MoeArgs {
   // [0] up products taken; [1 + i] of the i-th expert with rows: rows of h finished, 32 columns each; [1 + kMaxSlots + g] parts of 64 columns of Y finished
   uint32_t* sync;
 };
-
-constexpr int kFirstThreads = kRouterWaves * 64;
-template <bool XBF16, bool WBF16>
-__global__ __launch_bounds__(kFirstThreads) void k_moe_logits(MoeArgs a) {
-  __shared__ double red[kRouterWaves][256];
-  const int tiles = (a.router.experts + 15) / 16;
-  if ((int)blockIdx.x < tiles) {
-    router_tile<XBF16, WBF16>(a.router, blockIdx.x * 16, 0, red);
-    return;
-  }
-  const int t = threadIdx.x, block = blockIdx.x - tiles;
-  if (block == 0)
-    for (int i = t; i <= kMaxSlots + a.down.groups; i += kFirstThreads) a.sync[i] = 0;
-  const int per = a.up.Kb * 8, u = block * kFirstThreads + t;  // 16 channels of a row, 8 lanes a block of 128
-  const int m = u / per, c = (u - m * per) * 16;
-  if (m >= a.router.tokens) return;  // whole groups of 8 lanes
-  Raw16<XBF16> x;
-  x.load(static_cast<const char*>(a.router.X) + m * a.router.ld_x * (XBF16 ? 2 : 4), c, a.router.d);
-  float scale, inv;
-  scale_of(max8(x.amax()), a.up.pow2, &scale, &inv);
-  *reinterpret_cast<u4*>(a.codes + (int64_t)m * a.up.Kb * 128 + c) = x.codes(inv);
-  if ((t & 7) == 0) a.scales[(c >> 7) * a.up.ld_sa + m] = scale;
-}
 
 struct Chosen {
   uint32_t mask[kF8MaxExperts];      // tokens of an expert
@@ -81,7 +57,7 @@ __device__ void choose(const MoeArgs& a, Chosen& s) {
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, E = a.r.experts, K = a.r.top_k, T = a.r.tokens;
   for (int e = t; e < kF8MaxExperts; e += kThreads) s.mask[e] = 0;
   __syncthreads();
-  const TopArgs top = {a.router.logits, E, E, K, a.renorm};
+  const TopArgs top = {a.logits, E, E, K, a.renorm};
   auto put = [&](int tok, int k, int id, float weight) __attribute__((always_inline)) {
     s.id[tok * K + k] = id;
     s.slot_weight[tok * K + k] = weight;
@@ -465,7 +441,7 @@ hipError_t stamp_launch_moe(const stamp_router_t& router, const stamp_routing_t&
                             const StampF8Gemm& down, uint8_t* codes, float* scales, float* logits, uint32_t* sync, float* sums,
                             hipStream_t st) {
   MoeArgs a;
-  a.router = RouterArgs{router.W_dev, router.bias_dev_or_null, X, ld_x, r.tokens, r.experts, up.d, logits};
+  a.logits = logits;
   a.r = r;
   a.renorm = router.renormalize;
   a.up = up;
@@ -479,10 +455,8 @@ hipError_t stamp_launch_moe(const stamp_router_t& router, const stamp_routing_t&
   const int64_t slots = (int64_t)r.tokens * r.top_k, units = (slots < r.experts ? slots : r.experts) * down.Kb;
   const int most_parts = stamp_moe_parts(down.groups), busy = (int)(units / kWaves);
   a.parts = busy < 1 ? 1 : busy < most_parts ? busy : most_parts;
-  const bool wb = router.w_dtype == STAMP_BF16;
-  auto* const first = x_bf16 ? (wb ? k_moe_logits<true, true> : k_moe_logits<true, false>) : (wb ? k_moe_logits<false, true> : k_moe_logits<false, false>);
-  first<<<(r.experts + 15) / 16 + (r.tokens * up.Kb * 8 + kFirstThreads - 1) / kFirstThreads, kFirstThreads, 0, st>>>(a);
-  const hipError_t e = hipGetLastError();
+  const RouterQ8 q = {codes, scales, up.ld_sa, up.pow2, 0, sync, (int32_t)(stamp_moe_sync_bytes(down.groups) / 4)};
+  const hipError_t e = stamp_launch_router(router, X, x_bf16, ld_x, r.tokens, r.experts, up.d, q, logits, st);
   if (e != hipSuccess) return e;
   const int64_t products = (slots < r.experts ? slots : r.experts) * up.groups, columns = (int64_t)down.groups * a.parts;
   const int64_t most = products > columns ? products : columns, cus = stamp_device_cus();
