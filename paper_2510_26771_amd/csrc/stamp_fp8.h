@@ -412,7 +412,7 @@ __device__ __forceinline__ void activate(float (&v)[N], int act) {
     for (int j = 0; j < N; ++j) v[j] = gelu_tanh(v[j]);
   }
 }
-// act(g) u; kF8DividedSilu: silu by a division, as stamp_experts_forward has had it (8192 x 4096 -> 11008, gated: 1290 us of tiles by the reciprocal, 1310 so)
+// act(g) u; kF8DividedSilu: silu by a division, as stamp_experts_forward has had it (8192 x 4096 -> 11008, gated: 1260 us of tiles by the reciprocal, 1294 so)
 template <int N>
 __device__ __forceinline__ void gate(float (&g)[N], const float (&u)[N], int act) {
   if (act == kF8DividedSilu) {

@@ -301,7 +301,13 @@ stamp_status_t run_experts(const ExpertsRun& e, uint8_t* ws, hipStream_t st) {
 struct MlpWs {
   size_t codes, scales, h, hcodes, hscales, partial, total;
 };
-// up to so many rows of h may lie in fp32, of a gated layer
+// Up to so many rows h may lie in fp32: beyond, codes straight from the tiles are as fast or faster (stamp_f8_codes_pay).  Of a gated layer up to 16 rows; us, rows in fp32 by
+// workgroups of 32 places / codes by workgroups of 256:
+//                               1 row         2            4            6            8            12           16
+//   4096 -> 11008 -> 4096         34 / 47       36 / 48      39 / 49      37 / 44      38 / 45      40 / 47      42 / 50
+//   2048 -> 5632 -> 2048          17 / 26       18 / 27      20 / 27      22 / 25      23 / 25      24 / 27      26 / 28
+//   1024 -> 2816 -> 1024          10 / 16       11 / 17      11 / 18      17 / 16      17 / 16      17 / 18      17 / 18
+//   8192 -> 28672 -> 8192         133 / 148     135 / 149    131 / 150    130 / 127    130 / 127    133 / 127    149 / 149
 constexpr int32_t kMlpRowsInFp32 = 1024, kMlpGatedRows = 16;
 MlpWs mlp_ws(const stamp_fp8_plan* up, const stamp_fp8_plan* down, int32_t rows) {
   MlpWs w;
@@ -454,6 +460,12 @@ F8Cut stamp_f8_cut(int sets, int groups, int Kb, int rows, int wide_sums, int ga
 
 // An up product of tiles whose results become codes has its depth in one piece; with rows in fp32 it may have parts or be the rows kernel's, but they
 // are written and, unless the down product does it (few rows), quantized by a launch of 3.5 us: 4 + 4 + 1 bytes for 1.
+// us, rows in fp32 / codes, bf16 Y, the first the choice up to the bar, the second behind it:
+//   rows                         1           16          32          64          100           200           400           1024
+//   1152 -> 4608 -> 1152         13 / 21     25 / 24     21 / 25     29 / 30  |  34 / 32       37 / 34       41 / 37       63 / 55
+//   4096 -> 11008 -> 4096        28 / 52     35 / 57     47 / 63     54 / 67     60 / 66  |    73 / 69       104 / 99      175 / 175
+//   590 -> 1185 -> 590           11 / 18     18 / 21     16 / 20  |  20 / 23     28 / 26       28 / 26       29 / 26       33 / 27
+// Over 88 sizes the choice takes 1 % more than the better one on average, 16 % at worst (64 rows).
 int stamp_f8_codes_route(int groups, int Kb, int rows) { return STAMP_FP8_ROUTE_TILES_64 + best_tiles(1, groups, Kb, rows, 1, 1, 0).size; }
 int stamp_f8_codes_pay(int groups, int Kb, int rows, int quantized_below) {
   const float codes = best_tiles(1, groups, Kb, rows, 1, 1, 0).us;

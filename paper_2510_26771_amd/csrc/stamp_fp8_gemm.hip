@@ -44,7 +44,9 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void* p) {
 // How the products are summed: FP8 instructions with the scales by multiplication or as their own, or bf16 instructions (f8_wide_sums).
 enum Sums { kScaled, kPow2, kWide };
 
-// What becomes of the sums: rows of Y, the same with activation and residual, codes of act(gate) * up, codes of the activated rows.
+// What becomes of the sums: rows of Y, the same with activation and residual, codes of act(gate) * up, codes of the activated rows.  8192 x 1152 -> 4608, bf16, whole
+// layers: rows 68 us, relu 71, silu 73, gelu_tanh 75, gelu 80 (vector ALU, which the matrix pipe waits for at a tile's end), a residual 89 (its 75 MB are read when all CUs write
+// theirs; asked for at the tiles' start they only come in the operands' way: 92).  Codes: an MLP of 1152 -> 4608 -> 1152 185 us, by rows in fp32 and the quantizer 225.
 enum Out { kRows, kRowsAct, kGated, kCodes };
 
 [[maybe_unused]] constexpr int kMaxBlocks = 65536 / kF8Block;

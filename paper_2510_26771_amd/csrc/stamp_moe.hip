@@ -1,16 +1,22 @@
 // The layer of experts for few tokens in two kernels: what is left of the time beside the chosen experts' weights is launches and waits.
 //
-// First kernel: logits, codes of X, and zeros in the two counters of the second.  Second kernel: every workgroup chooses the experts from the logits by itself
-// (16 tokens at most: 2 to 3 us, a launch of its own would take as long and its results as long again to arrive), then takes up products of 32 columns of
-// an expert from a counter until none is left, then has 64 columns of Y for a part of the experts.
+// First kernel (k_router): logits, codes of X, and zeros in the counters of the second.  Second kernel: every workgroup chooses the experts from the logits by
+// itself (2 to 4 us; a launch of its own would take as long, and its results as long again to arrive), then takes products of 32 columns of h of an expert from a
+// counter until none is left, then has 64 columns of Y for a part of the experts.
 //
-// The down product reads all of h, so it waits for all up products: for a counter of finished rows, and not before its first weights are on their way.
-// The wait ends: up products are taken in order by workgroups that run already, so whoever waits waits for products that are being worked on, and those wait
-// for nobody.  That holds for any number of workgroups on the chip, other kernels' among them.
+// The down product reads all columns of h, so it waits for its experts' rows, each counted by those who finish a piece of it, and not before its first weights
+// are on their way.  The wait ends: up products are taken in order by workgroups that run already, so whoever waits, waits for products that are being worked on, and
+// those wait for nobody.  That holds for any number of workgroups on the chip, other kernels' among them.
 //
-// Y's sum over a token's experts stays in the accumulators: a column of the down product's matrix instruction is a token (zeros where it has not chosen the
-// expert), and its factor carries the router's weight.  So there are no rows to be written; the parts of a column are added up by the last of its workgroups, in
-// the parts' order, and nothing depends on the order of workgroups.
+// h passes between workgroups in fp32: whoever reads it makes Q8 of it (few rows; a block of 128 columns would be four workgroups' otherwise).  Y's sum over a token's
+// experts stays in the accumulators: a column of the down product's matrix instruction is a token (one that has not chosen the expert takes nothing from it), and its
+// factor carries the router's weight.  So there are no rows to be written; the parts of a column are added up by the last of its workgroups, in the parts' order, and
+// nothing depends on the order of workgroups.
+//
+// Bound by the weights' bytes where they are many: 16 tokens, 8 of 256 experts, 4096 -> 1536: 312 us, 6.1 TB/s (up products 5.8).  Else by the chain of steps: 1 token, 6 of
+// 64, 2048 -> 1408 (52 MB) 24 us: chosen after 4.5, up products 7 more and, as 264 of them are one round of the CUs and 8 more, 6 for those; down product and sum of the
+// parts 7.  What a CU gets from memory is what counts (20 to 30 KB a us): runs of 8 KB of a weight matrix, one after the other, with the next ones on their way; in pieces of
+// 2 or 4 KB of every 8 the same bytes take 1.3 times as long.
 #include "stamp_route.h"
 
 namespace {
@@ -26,8 +32,8 @@ struct MoeArgs {
   const float* logits;
   stamp_routing_t r;
   int32_t renorm;
-  StampF8Gemm up, down;  // X as rows of up.X, codes and scales in up.A and up.SA; h in up.Y, fp32
-  uint8_t* codes;
+  StampF8Gemm up, down;  // h in up.Y
+  uint8_t* codes;        // Q8 of X
   float* scales;
   int32_t parts;         // workgroups that share 64 columns of Y
   float* sums;           // [parts][tokens][down.groups * 64]

@@ -6,8 +6,7 @@ using namespace f8;
 
 constexpr int kThreads = kRouterWaves * 64;
 
-// Workgroups 0 .. tiles - 1: 16 experts x 16 tokens of the logits; the others: Q8 of X as in k_f8_quant, 16 channels of a row a thread, 8 lanes a block.  1 token, 64 experts,
-// 2048 channels: 5.8 us, most of it the way of the first loads.
+// Workgroups 0 .. tiles - 1: 16 experts x 16 tokens of the logits; the others: Q8 of X as in k_f8_quant, 16 channels of a row a thread, 8 lanes a block.
 template <bool XBF16, bool WBF16>
 __global__ __launch_bounds__(kThreads) void k_router(RouterArgs a, RouterQ8 q, int64_t tiles, int64_t first) {
   __shared__ double red[kRouterWaves][256];
