@@ -353,6 +353,31 @@ def test_tokens_without_an_expert_and_in_place(st, tokens):
     down.destroy()
 
 
+@pytest.mark.parametrize("tokens", [1, 7, 16, 50])
+def test_experts_masked_by_the_lowest_number(st, tokens):
+    """A bias of the type's lowest value instead of minus infinity: such experts are chosen behind all others, with weight 0, and change nothing."""
+    import torch
+    rng = np.random.default_rng(tokens)
+    E, k, d, ff = 10, 6, 384, 256
+    *_, rtg, up, down = _moe_case(st, rng, tokens, E, d, ff, "bf16", "f32", "f32", 0, 1)
+    X = torch.randn((tokens, d), device="cuda").to(torch.bfloat16)
+    low = [1, 2, 5, 6, 8, 9]  # four are left
+    outs = []
+    for value in (-np.inf, float(np.finfo(np.float32).min)):
+        b = torch.zeros(E, device="cuda")
+        b[low] = value
+        r, Y = st.Routing(tokens, E, k), torch.empty((tokens, d), device="cuda")
+        st.moe_forward(rtg, up, down, X, r, Y, st.moe_workspace(up, down, tokens, k), router_bias=b)
+        assert (r.weights[:, 4:] == 0).all() and not torch.isin(r.ids[:, :4], torch.tensor(low, dtype=torch.int32, device="cuda")).any()
+        assert (r.ids[:, 4:] == (-1 if value == -np.inf else torch.tensor([1, 2], device="cuda"))).all()
+        outs.append((Y, r.ids[:, :4].clone(), r.weights.clone()))
+    assert torch.equal(outs[0][1], outs[1][1]) and torch.equal(outs[0][2], outs[1][2])
+    a, b = outs[0][0], outs[1][0]
+    assert float((a - b).abs().max()) <= 2.0 ** -18 * float(a.abs().max())  # the same terms, summed in another order
+    up.destroy()
+    down.destroy()
+
+
 @pytest.mark.parametrize("tokens", [3, 16, 40])
 def test_tokens_that_are_no_numbers(st, tokens):
     """A token with a NaN or an infinity: its logits are NaN or infinite, no other token's row changes."""
