@@ -6,7 +6,8 @@
 //
 // The down product reads all columns of h, so it waits for its experts' rows, each counted by those who finish a piece of it, and not before its first weights
 // are on their way.  The wait ends: up products are taken in order by workgroups that run already, so whoever waits, waits for products that are being worked on, and
-// those wait for nobody.  That holds for any number of workgroups on the chip, other kernels' among them.
+// those wait for nobody.  That holds for any number of workgroups on the chip, other kernels' among them.  (Two calls that use one workspace at once, against the rules, may
+// take a counter back under a waiter: so it gives up after some seconds, and their results are unspecified as with any other call's workspace.)
 //
 // h passes between workgroups in fp32: whoever reads it makes Q8 of it (few rows; a block of 128 columns would be four workgroups' otherwise).  Y's sum over a token's
 // experts stays in the accumulators: a column of the down product's matrix instruction is a token (one that has not chosen the expert takes nothing from it), and its
@@ -25,6 +26,7 @@ using namespace f8;
 constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * 64;
 constexpr int kMaxSlots = kMoeSlots;
+constexpr int kMaxLooks = 1 << 22;     // at a counter, some 0.7 us each: more than all weights that the memory holds take
 constexpr int kUpLd = kF8Group + 4;    // floats of a row of an up product's partial sums
 constexpr int kRoom = kWaves * 16 * kUpLd * 4 > kMoeChunkBytes ? kWaves * 16 * kUpLd * 4 : kMoeChunkBytes;
 
@@ -318,7 +320,8 @@ __global__ __launch_bounds__(kThreads) void k_moe_few(MoeArgs a) {
       if (wave == 0) {  // the experts' rows of h; one wave looks, and drops what its CU and L2 hold of before, for all
         for (int i = i0 + lane; i < i1; i += 64) {
           const uint32_t all = (uint32_t)((s.first[i + 1] - s.first[i]) * groups);
-          while (__hip_atomic_load(&a.sync[1 + i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) < all) __builtin_amdgcn_s_sleep(1);
+          for (int look = 0; look < kMaxLooks && __hip_atomic_load(&a.sync[1 + i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) < all; ++look)
+            __builtin_amdgcn_s_sleep(1);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
       }
