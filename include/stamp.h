@@ -497,6 +497,11 @@ stamp_status_t stamp_moe_forward(const stamp_router_t* router, const stamp_fp8_p
 /* How a call with so many tokens runs: 1 = in two kernels of its own (few tokens), 0 = by the kernels of the other calls; 0 too for what is refused. */
 int32_t stamp_moe_debug_route(const stamp_fp8_plan_t* up, const stamp_fp8_plan_t* down, int32_t tokens, int32_t top_k);
 
+/* In those two kernels workgroups wait for rows of others.  A wait that has looked some seconds long in vain, which takes a second call that uses the same
+ * workspace at the same time, gives up, and what depends on those rows is NaN in Y.  For tests: after how many looks behind the first; -1: as always.
+ * Modifies the plan, as stamp_fp8_debug_set_route does. */
+stamp_status_t stamp_moe_debug_set_looks(stamp_fp8_plan_t* up, int32_t looks);
+
 /* For tests: a plan's codes [experts][2 if gated][d_out][d_in] and scales in the layout of w_scales_dev, copied to host.
  * Synchronizes the device. */
 stamp_status_t stamp_fp8_debug_weight_codes(const stamp_fp8_plan_t* plan, uint8_t* codes_host, float* scales_host);

@@ -29,6 +29,7 @@ struct stamp_fp8_plan {
   int32_t groups;      // of a set
   int32_t nblk;        // blocks of 128 output columns of one matrix
   int32_t forced;      // stamp_fp8_debug_set_route
+  int32_t looks;       // stamp_moe_debug_set_looks
   uint8_t* w_dev;      // operand image
   float* sw_dev;       // [sets][2 if gated][nblk][Kb]
   float* bias_dev;     // [sets][d_out] or nullptr
@@ -156,10 +157,10 @@ inline size_t stamp_moe_sync_bytes(int groups) { return (size_t)(1 + kMoeSlots +
 inline bool stamp_moe_fits(int tokens, int top_k, int Kb_down) {
   return tokens <= kMoeTokens && tokens * top_k <= kMoeSlots && (int64_t)tokens * (Kb_down * 132 + 16) <= kMoeChunkBytes;
 }
-// up: act, Y for h in fp32 (ld_y whole blocks); down: R, Y.  sync: stamp_moe_sync_bytes of any content; sums: parts * tokens * groups * 64.
+// up: act, Y for h in fp32 (ld_y whole blocks); down: R, Y.  sync: stamp_moe_sync_bytes of any content; sums: parts * tokens * groups * 64.  looks: of a wait, -1: as many as ever needed.
 hipError_t stamp_launch_moe(const stamp_router_t& router, const stamp_routing_t& r, const void* X, int x_bf16, int64_t ld_x, const StampF8Gemm& up,
                             const StampF8Gemm& down, uint8_t* codes, float* scales, float* logits, uint32_t* sync, float* sums,
-                            hipStream_t st);
+                            int32_t looks, hipStream_t st);
 
 // ---- device helpers ----
 #ifdef __HIPCC__

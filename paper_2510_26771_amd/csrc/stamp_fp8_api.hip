@@ -499,6 +499,7 @@ stamp_status_t stamp_fp8_plan_create(const stamp_fp8_desc_t* desc, const void* W
   p->groups = (desc->d_out + per_group - 1) / per_group;
   p->nblk = (desc->d_out + kF8Block - 1) / kF8Block;
   p->forced = 0;
+  p->looks = -1;
   p->w_dev = nullptr;
   p->sw_dev = p->bias_dev = nullptr;
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
@@ -711,6 +712,13 @@ int32_t stamp_moe_debug_route(const stamp_fp8_plan_t* up, const stamp_fp8_plan_t
   return stamp_moe_workspace_bytes(up, down, tokens, top_k) > 0 && tokens > 0 && moe_few(up, down, tokens, top_k);
 }
 
+stamp_status_t stamp_moe_debug_set_looks(stamp_fp8_plan_t* up, int32_t looks) {
+  if (up == nullptr) return STAMP_ERR_NULL;
+  if (looks < -1) return STAMP_ERR_SHAPE;
+  up->looks = looks;
+  return STAMP_OK;
+}
+
 stamp_status_t stamp_moe_forward(const stamp_router_t* router, const stamp_fp8_plan_t* up, const stamp_fp8_plan_t* down, const stamp_routing_t* r,
                                  const void* X_dev, int64_t ld_x, const stamp_epilogue_t* epilogue, void* Y_dev, int64_t ld_y, void* workspace_dev,
                                  size_t workspace_bytes, void* hip_stream) {
@@ -746,7 +754,7 @@ stamp_status_t stamp_moe_forward(const stamp_router_t* router, const stamp_fp8_p
     b.Y = Y_dev;
     b.ld_y = ld_y;
     return done(stamp_launch_moe(*router, *r, X_dev, up->desc.x_dtype == STAMP_BF16, ld_x, a, b, rows + v.codes, reinterpret_cast<float*>(rows + v.scales), logits,
-                                 reinterpret_cast<uint32_t*>(ws + w.sync), reinterpret_cast<float*>(ws + w.sums), st));
+                                 reinterpret_cast<uint32_t*>(ws + w.sync), reinterpret_cast<float*>(ws + w.sums), up->looks, st));
   }
   if (r->tokens > 0) {
     const ExpertsWs v = experts_ws(up, down, r->tokens, r->top_k, true);

@@ -7,7 +7,7 @@
 // The down product reads all columns of h, so it waits for its experts' rows, each counted by those who finish a piece of it, and not before its first weights
 // are on their way.  The wait ends: up products are taken in order by workgroups that run already, so whoever waits, waits for products that are being worked on, and
 // those wait for nobody.  That holds for any number of workgroups on the chip, other kernels' among them.  (Two calls that use one workspace at once, against the rules, may
-// take a counter back under a waiter: so it gives up after some seconds, and their results are unspecified as with any other call's workspace.)
+// take a counter back under a waiter: so it gives up after some seconds, and what it would have added to Y becomes NaN.)
 //
 // h passes between workgroups in fp32: whoever reads it makes Q8 of it (few rows; a block of 128 columns would be four workgroups' otherwise).  Y's sum over a token's
 // experts stays in the accumulators: a column of the down product's matrix instruction is a token (one that has not chosen the expert takes nothing from it), and its
@@ -26,7 +26,7 @@ using namespace f8;
 constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * 64;
 constexpr int kMaxSlots = kMoeSlots;
-constexpr int kMaxLooks = 1 << 22;     // at a counter, some 0.7 us each: more than all weights that the memory holds take
+constexpr int kMaxLooks = 1 << 22;     // at a counter behind the first, some 0.7 us each: more than all weights that the memory holds take
 constexpr int kUpLd = kF8Group + 4;    // floats of a row of an up product's partial sums
 constexpr int kRoom = kWaves * 16 * kUpLd * 4 > kMoeChunkBytes ? kWaves * 16 * kUpLd * 4 : kMoeChunkBytes;
 
@@ -38,6 +38,7 @@ struct MoeArgs {
   uint8_t* codes;        // Q8 of X
   float* scales;
   int32_t parts;         // workgroups that share 64 columns of Y
+  int32_t looks;         // kMaxLooks, or a test's
   float* sums;           // [parts][tokens][down.groups * 64]
   // [0] up products taken; [1 + i] of the i-th expert with rows: rows of h finished, 32 columns each; [1 + kMaxSlots + g] parts of 64 columns of Y finished
   uint32_t* sync;
@@ -55,6 +56,7 @@ struct Chosen {
   uint32_t wave_sum[kWaves];
   int32_t experts;
   uint32_t ticket;
+  int32_t late;                      // a wait of this workgroup gave up: what follows is NaN
 };
 
 __device__ __forceinline__ v8i load_w(const uint8_t* w) {
@@ -64,6 +66,7 @@ __device__ __forceinline__ v8i load_w(const uint8_t* w) {
 __device__ void choose(const MoeArgs& a, Chosen& s) {
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, E = a.r.experts, K = a.r.top_k, T = a.r.tokens;
   for (int e = t; e < kF8MaxExperts; e += kThreads) s.mask[e] = 0;
+  if (t == 0) s.late = 0;
   __syncthreads();
   const TopArgs top = {a.logits, E, E, K, a.renorm};
   auto put = [&](int tok, int k, int id, float weight) __attribute__((always_inline)) {
@@ -320,8 +323,13 @@ __global__ __launch_bounds__(kThreads) void k_moe_few(MoeArgs a) {
       if (wave == 0) {  // the experts' rows of h; one wave looks, and drops what its CU and L2 hold of before, for all
         for (int i = i0 + lane; i < i1; i += 64) {
           const uint32_t all = (uint32_t)((s.first[i + 1] - s.first[i]) * groups);
-          for (int look = 0; look < kMaxLooks && __hip_atomic_load(&a.sync[1 + i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) < all; ++look)
+          auto finished = [&]() __attribute__((always_inline)) { return __hip_atomic_load(&a.sync[1 + i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) >= all; };
+          bool there = finished();
+          for (int look = 0; !there && look < a.looks; ++look) {
             __builtin_amdgcn_s_sleep(1);
+            there = finished();
+          }
+          if (!there) s.late = 1;
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
       }
@@ -343,7 +351,7 @@ __global__ __launch_bounds__(kThreads) void k_moe_few(MoeArgs a) {
             float scale, inv;
             scale_of(max8(x[q].amax()), p.pow2, &scale, &inv);
             *reinterpret_cast<u4*>(h + m * ld_row + c) = x[q].codes(inv);
-            if ((t & 7) == 0) sh[m * Kb + (c >> 7)] = scale * s.weight[r0 + m];
+            if ((t & 7) == 0) sh[m * Kb + (c >> 7)] = s.late ? __builtin_nanf("") : scale * s.weight[r0 + m];
           }
         }
       }
@@ -448,8 +456,9 @@ __global__ __launch_bounds__(kThreads) void k_moe_few(MoeArgs a) {
 
 hipError_t stamp_launch_moe(const stamp_router_t& router, const stamp_routing_t& r, const void* X, int x_bf16, int64_t ld_x, const StampF8Gemm& up,
                             const StampF8Gemm& down, uint8_t* codes, float* scales, float* logits, uint32_t* sync, float* sums,
-                            hipStream_t st) {
+                            int32_t looks, hipStream_t st) {
   MoeArgs a;
+  a.looks = looks < 0 ? kMaxLooks : looks;
   a.logits = logits;
   a.r = r;
   a.renorm = router.renormalize;

@@ -145,6 +145,10 @@ class Fp8Plan:
         code = {n: c for c, n in FP8_ROUTES.items()}[route] if route else 0
         _check(self.lib.stamp_fp8_debug_set_route(self._h, code), "stamp_fp8_debug_set_route")
 
+    def set_looks(self, looks: int = -1):
+        """For tests, of moe_forward's up plan: after so many looks behind the first a wait gives up, which Y shows as NaN (-1: as always)."""
+        _check(self.lib.stamp_moe_debug_set_looks(self._h, int(looks)), "stamp_moe_debug_set_looks")
+
     # -- compute (asynchronous on the stream) --
     def alloc_act_buffers(self, rows: int, device="cuda"):
         """Codes [rows, d_in rounded up to 128] and scales [blocks, rows rounded up to 4] for quantize_act."""
