@@ -123,3 +123,7 @@ def test_the_bounds_tell_one_activation_from_another_and_see_lost_terms():
     rounded = torch.from_numpy(h.astype(np.float32)).to(torch.bfloat16).float().numpy()  # h held in bf16 ahead of its codes
     lost = ref.values(*ref.quantize(rounded, 0), ff) @ ref.weight_values(w2, ws2).T
     assert np.mean(np.abs(lost - want) > tol) > 0.3
+
+
+def test_looks_of_no_plan(lib):  # noqa: F811
+    assert lib.stamp_moe_debug_set_looks(None, 0) == 1

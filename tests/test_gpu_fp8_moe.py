@@ -1,9 +1,10 @@
-"""The two kernels of the layer of experts for few tokens where they can go wrong: waits that give up."""
+"""The two kernels of the layer of experts for few tokens where they can go wrong: waits that give up, widths and rows that take every loop round again; against the definition in 64 bits (fp8_block_reference.py)."""
 import numpy as np
 import pytest
 
-from test_gpu_fp8 import _dt
-from test_gpu_fp8_block import _moe_case, st  # noqa: F401  (fixture)
+import fp8_block_reference as block
+from test_gpu_fp8 import _activations, _code, _dt, _gpu, _weights
+from test_gpu_fp8_block import _held, _moe_case, _values, st  # noqa: F401  (fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -43,3 +44,86 @@ def test_a_wait_that_gives_up_leaves_no_number(st, tokens, E, top_k, d, ff, y): 
     up.destroy()
     down.destroy()
 
+
+# ---- loops that go round again ----
+
+def _rounds(tokens, offsets, top_k, d, ff):
+    """What a call takes beyond the first round: blocks of channels that a wave of an up product asks for behind its first 4; sets of experts whose rows of h a part of the
+    columns holds one after the other; units (128 rows of an expert's down matrix) of a wave beyond 60; columns beyond a workgroup's first 64."""
+    import torch
+    cus, E, groups, kb, kb_up = torch.cuda.get_device_properties(0).multi_processor_count, len(offsets) - 1, -(-d // 64), -(-ff // 128), -(-d // 128)
+    parts = max(1, min(min(tokens * top_k, E) * kb // 8, max(1, min(16, cus // groups))))
+    first = [0] + [int(b) for a, b in zip(offsets[:-1], offsets[1:]) if b > a]
+    units, most, held, longest = (len(first) - 1) * kb, (96 << 10) // (132 * kb + 16), 0, 0
+    for p in range(parts):
+        a, b = units * p // parts, units * (p + 1) // parts
+        i, end, sets = a // kb, (b - 1) // kb + 1, 0
+        while a < b and i < end:
+            j = i + 1
+            while j < end and first[j + 1] - first[i] <= most:
+                j += 1
+            longest = max(longest, -(-(min(b, j * kb) - max(a, i * kb)) // 8))
+            i, sets = j, sets + 1
+        held = max(held, sets)
+    return dict(channels=-(-kb_up // 8) > 4, rows=held > 1, units=longest > 64, columns=groups * parts > cus)
+
+
+@pytest.mark.parametrize("tokens,E,top_k,d,ff,again", [
+    (5, 6, 2, 5000, 200, "channels"), (16, 9, 3, 9001, 130, "channels"), (1, 2, 2, 4097, 77, "channels"), (16, 3, 3, 300, 5504, "rows"), (16, 5, 4, 4500, 2700, "channels rows"),
+    (15, 7, 5, 200, 6000, "rows"), (2, 2, 1, 16700, 128, "channels columns"), (16, 4, 2, 16390, 300, "channels columns")])
+@pytest.mark.parametrize("x,y,pow2", [("bf16", "f32", 0), ("f32", "bf16", 1)])
+def test_few_tokens_where_loops_go_round_again(st, tokens, E, top_k, d, ff, again, x, y, pow2):  # noqa: F811
+    import torch
+    rng = np.random.default_rng(tokens * 1000 + d)
+    xv, X, w_up, s_up, w_down, s_down, b, rt, rtg, up, down = _moe_case(st, rng, tokens, E, d, ff, x, y, "f32", pow2, 1)
+    res, R, _ = _values(rng, tokens, d, y, 1)
+    want, tol, ids, weights, offsets, token, row, dw = block.moe(xv, rt, None, w_up, s_up, w_down, s_down, b, top_k, 1, "silu", res, y, pow2)
+    assert st.moe_route(up, down, tokens, top_k) == "few"
+    assert [n for n, v in _rounds(tokens, offsets, top_k, d, ff).items() if v] == again.split()
+    r, room = st.Routing(tokens, E, top_k), st.moe_workspace(up, down, tokens, top_k)
+    Y = torch.full((tokens, d), -7.0, dtype=_dt(y), device="cuda")
+    for value in (255, 0):
+        room.fill_(value)
+        first = Y.clone()
+        st.moe_forward(rtg, up, down, X, r, Y, room, residual=R)
+        _held(Y, want, tol, f"workspace of {value}")
+        assert np.array_equal(r.ids.cpu().numpy(), ids) and np.array_equal(r.row_of_slot.cpu().numpy(), row)
+    assert torch.equal(first, Y)
+    up.destroy()
+    down.destroy()
+
+
+def test_few_tokens_where_a_wave_has_many_units(st):  # noqa: F811
+    """More than 64 blocks of h a wave takes weights of 2 GB: the up matrices are zero behind their first 256 channels, Y is looked at in some blocks of columns."""
+    import torch
+    rng = np.random.default_rng(5)
+    E, top_k, d, ff, used = 3, 3, 8256, 240 * 128 - 50, 256
+    gen = torch.Generator(device="cuda").manual_seed(5)
+
+    def codes(*shape):
+        c = torch.randint(0, 256, shape, dtype=torch.uint8, device="cuda", generator=gen)
+        return c.masked_fill_((c & 0x7f) == 0x7f, 0x3a)
+
+    def scales(low, *shape):
+        return (2.0 ** rng.uniform(low - 8, low, shape)).astype(np.float32)
+    nb, nf = -(-d // 128), -(-ff // 128)
+    w_up = torch.zeros((E, 2, ff, d), dtype=torch.uint8, device="cuda")
+    w_up[..., :used] = codes(E, 2, ff, used)
+    w_down, s_up, s_down = codes(E, d, ff), scales(-10, E, 2, nf, nb), scales(-4, E, nb, nf)
+    up = st.Fp8Plan(st.Fp8Desc(d_in=d, d_out=ff, experts=E, gated=1), w_up, _gpu(s_up))
+    down = st.Fp8Plan(st.Fp8Desc(d_in=ff, d_out=d, experts=E, y_dtype=st.STAMP_F32), w_down, _gpu(s_down))
+    xv, X = _activations(rng, 1, d, "bf16")
+    rt = (rng.standard_normal((E, d)) / np.sqrt(30.0 * d)).astype(np.float32)
+    assert st.moe_route(up, down, 1, top_k) == "few" and _rounds(1, [0, 1, 2, 3], top_k, d, ff)["units"]
+    r, room, Y = st.Routing(1, E, top_k), st.moe_workspace(up, down, 1, top_k), torch.empty((1, d), device="cuda")
+    room.fill_(255)
+    st.moe_forward(_gpu(rt), up, down, X, r, Y, room)
+    w_up = w_up[..., :used].cpu().numpy()
+    for at in (0, 31, 63):  # blocks of 128 columns
+        cols = slice(128 * at, 128 * at + 128)
+        want, tol, ids, *_ = block.moe(xv.astype(np.float64), rt.astype(np.float64), None, w_up, s_up[..., :used // 128], w_down[:, cols].cpu().numpy(), s_down[:, at:at + 1], None, top_k, 1,
+                                       "silu", None, "f32", 0)
+        assert np.array_equal(r.ids.cpu().numpy(), ids)
+        _held(Y[:, cols], want, tol, f"columns {cols}")
+    up.destroy()
+    down.destroy()
