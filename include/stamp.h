@@ -481,7 +481,9 @@ stamp_status_t stamp_mlp_forward(const stamp_fp8_plan_t* up, const stamp_fp8_pla
  * more than 32 bits (blocks of 32 channels in fp32, those in fp64) and rounded to fp32 once, so that what two near logits compare as hardly
  * depends on the order of sums.  bias -infinity: an expert out of use.  A token that finds no expert gets R, or zeros.
  * up, down, X, Y and their limits as in stamp_experts_forward.  routing: its arrays are written, as stamp_route_topk writes them; with 0 tokens its
- * offsets alone.  The experts' rows are held in fp32 up to the sum, whatever Y's type. */
+ * offsets alone.  The experts' rows are held in fp32 up to the sum, whatever Y's type.
+ * The same call gives the same bits again.  With few tokens (stamp_moe_debug_route) the order in which a token's terms are summed follows from all experts
+ * that the call's tokens have chosen: other tokens beside it may move a row by the roundings of its fp32 sums, and by nothing else. */
 typedef struct {
   const void* W_dev;    /* [experts, d], rows one after the other, aligned as its elements are */
   int32_t w_dtype;      /* STAMP_F32, STAMP_BF16 */

@@ -1,8 +1,10 @@
-"""The two kernels of the layer of experts for few tokens where they can go wrong: waits that give up, widths and rows that take every loop round again; against the definition in 64 bits (fp8_block_reference.py)."""
+"""The two kernels of the layer of experts for few tokens where they can go wrong: waits that give up, widths and rows that take every loop round again, and what a
+token's result depends on; against the definition in 64 bits (fp8_block_reference.py)."""
 import numpy as np
 import pytest
 
 import fp8_block_reference as block
+import fp8_reference as ref
 from test_gpu_fp8 import _activations, _code, _dt, _gpu, _weights
 from test_gpu_fp8_block import _held, _moe_case, _values, st  # noqa: F401  (fixture)
 
@@ -125,5 +127,40 @@ def test_few_tokens_where_a_wave_has_many_units(st):  # noqa: F811
                                        "silu", None, "f32", 0)
         assert np.array_equal(r.ids.cpu().numpy(), ids)
         _held(Y[:, cols], want, tol, f"columns {cols}")
+    up.destroy()
+    down.destroy()
+
+
+# ---- a token and the others of its call ----
+
+@pytest.mark.parametrize("tokens,top_k", [(3, 2), (9, 5), (16, 8)])
+def test_other_tokens_move_a_row_by_the_order_of_its_sums_alone(st, tokens, top_k):  # noqa: F811
+    """Two tokens of a call stay, the others become NaN, infinite or other ones: the rows that stay have the same terms, one for each expert and 128 channels of h,
+    and at most that many sums of theirs plus those of 8 waves, 16 parts, the bias of every slot; either call rounds each by at most 2^-24 of the magnitudes."""
+    import torch
+    rng = np.random.default_rng(tokens)
+    E, d, ff = 20, 384, 700
+    xv, X, w_up, s_up, w_down, s_down, b, rt, rtg, up, down = _moe_case(st, rng, tokens, E, d, ff, "bf16", "f32", "f32", 0, 1)
+    keep = [0, tokens - 1]
+    r, room, Y, Z = st.Routing(tokens, E, top_k), st.moe_workspace(up, down, tokens, top_k), *(torch.empty((tokens, d), device="cuda") for _ in range(2))
+    st.moe_forward(rtg, up, down, X, r, Y, room)
+    ids, weights = r.ids.cpu().numpy(), r.weights.cpu().numpy().astype(np.float64)
+    size = np.zeros((len(keep), d))  # the terms' magnitudes
+    codes, scales = ref.quantize(xv, 0)
+    for i, t in enumerate(keep):
+        for e, w in zip(ids[t], weights[t]):
+            h, _ = block.hidden(codes[t:t + 1], scales[t:t + 1], w_up[e], s_up[e], None, "silu")
+            size[i] += w * (ref.product(*ref.quantize(h.astype(np.float32), 0), w_down[e], s_down[e])[1][0] + np.abs(b[e]))
+    sums = top_k * -(-ff // 128) + 8 + 16 + top_k
+    others = X.clone()
+    others[1, 5] = float("nan")
+    if tokens > 3:
+        others[2, 300] = float("inf")
+        others[3:-1] = torch.randn_like(others[3:-1])
+    room.fill_(255)
+    st.moe_forward(rtg, up, down, others, r, Z, room)
+    assert np.array_equal(r.ids.cpu().numpy()[keep], ids[keep]) and (r.ids[1] == -1).all() and (Z[1] == 0).all() and (tokens == 3 or torch.isnan(Z[2]).all())
+    off = (Y[keep].double() - Z[keep].double()).abs().cpu().numpy()
+    assert (off <= 2 * sums * 2.0 ** -24 * size * 1.01).all(), np.max(off / size) * 2.0 ** 24
     up.destroy()
     down.destroy()
