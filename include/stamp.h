@@ -504,6 +504,12 @@ int32_t stamp_moe_debug_route(const stamp_fp8_plan_t* up, const stamp_fp8_plan_t
  * Modifies the plan, as stamp_fp8_debug_set_route does. */
 stamp_status_t stamp_moe_debug_set_looks(stamp_fp8_plan_t* up, int32_t looks);
 
+/* How stamp_mlp_forward runs so many rows (>= 1), three numbers to route_host: the up product's and the down product's kernel (stamp_fp8_route_t), and whether h
+ * leaves the up product as codes (1) or as rows in fp32 (0).  Kernels forced by stamp_fp8_debug_set_route are taken where the up product has them: its
+ * sums are in fp32, so tiles of 256 rows count as no choice, and beyond 1024 rows of an ungated layer h is codes, which the kernel for few rows does not make: there
+ * its tiles are by rule. */
+stamp_status_t stamp_mlp_debug_route(const stamp_fp8_plan_t* up, const stamp_fp8_plan_t* down, int32_t rows, int32_t* route_host);
+
 /* For tests: a plan's codes [experts][2 if gated][d_out][d_in] and scales in the layout of w_scales_dev, copied to host.
  * Synchronizes the device. */
 stamp_status_t stamp_fp8_debug_weight_codes(const stamp_fp8_plan_t* plan, uint8_t* codes_host, float* scales_host);
@@ -520,7 +526,8 @@ int32_t stamp_fp8_debug_route(const stamp_fp8_plan_t* plan, int32_t rows);
  * depth in the first or only launch, parts in the second.  All 0 where the kernel for few rows runs. */
 stamp_status_t stamp_fp8_debug_cut(const stamp_fp8_plan_t* plan, int32_t rows, int32_t* cut_host);
 /* For tests and measurements: that kernel for every call, 0 = by rule again.  Modifies the plan (not thread-safe, no call on the plan may
- * be in progress on another host thread).  STAMP_ERR_UNSUPPORTED for tiles of 256 rows where the products are summed in fp32. */
+ * be in progress on another host thread).  STAMP_ERR_UNSUPPORTED for tiles of 256 rows where the products are summed in fp32.  In stamp_mlp_forward the up
+ * product does not have every kernel: stamp_mlp_debug_route tells. */
 stamp_status_t stamp_fp8_debug_set_route(stamp_fp8_plan_t* plan, int32_t route);
 
 const char* stamp_status_string(stamp_status_t status);

@@ -28,6 +28,7 @@ from .fp8 import (  # noqa: F401
     experts_workspace,
     mlp_forward,
     mlp_workspace,
+    mlp_route,
     moe_forward,
     moe_workspace,
     moe_route,

@@ -29,7 +29,7 @@ EXPORTS = ["stamp_plan_create", "stamp_plan_destroy", "stamp_plan_workspace_byte
            "stamp_fp8_linear_forward_q", "stamp_fp8_grouped_forward", "stamp_fp8_debug_weight_codes", "stamp_fp8_debug_route", "stamp_fp8_debug_cut", "stamp_fp8_debug_set_route",
            "stamp_route_workspace_bytes", "stamp_route_topk", "stamp_experts_workspace_bytes", "stamp_experts_forward",
            "stamp_fp8_linear_forward_act", "stamp_fp8_linear_forward_q_act", "stamp_fp8_grouped_forward_act", "stamp_mlp_workspace_bytes", "stamp_mlp_forward",
-           "stamp_moe_workspace_bytes", "stamp_moe_forward", "stamp_moe_debug_route", "stamp_moe_debug_set_looks"]
+           "stamp_moe_workspace_bytes", "stamp_moe_forward", "stamp_moe_debug_route", "stamp_moe_debug_set_looks", "stamp_mlp_debug_route"]
 
 # stamp_choice_t and stamp_route_t (include/stamp.h)
 CHOICES = {"hi_rows": 0, "operands": 1}
@@ -161,6 +161,7 @@ def load_library():
             ("stamp_fp8_grouped_forward_act", C.c_int, [vp, i32, vp, vp, i64, vp, vp, i64, vp, sz, vp]),
             ("stamp_mlp_workspace_bytes", sz, [vp, vp, i32]),
             ("stamp_mlp_forward", C.c_int, [vp, vp, i32, vp, i64, vp, vp, i64, vp, sz, vp]),
+            ("stamp_mlp_debug_route", C.c_int, [vp, vp, i32, vp]),
             ("stamp_moe_workspace_bytes", sz, [vp, vp, i32, i32]),
             ("stamp_moe_debug_route", i32, [vp, vp, i32, i32]),
             ("stamp_moe_debug_set_looks", C.c_int, [vp, i32]),

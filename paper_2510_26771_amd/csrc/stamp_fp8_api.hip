@@ -336,6 +336,23 @@ bool mlp_codes_in_tiles(const StampF8Gemm& up, const StampF8Gemm& down, int rows
   return stamp_f8_codes_pay(up.groups, up.Kb, rows, takes_x(down, rows));
 }
 
+struct MlpProducts {
+  StampF8Gemm up, down;
+  bool coded;  // the up product's results are codes, else rows in fp32
+};
+MlpProducts mlp_products(const stamp_fp8_plan* up, const stamp_fp8_plan* down, int32_t rows) {
+  MlpProducts p = {gemm_args(up), gemm_args(down), false};
+  StampF8Gemm& a = p.up;
+  a.y_bf16 = 0;
+  a.wide_sums = f8_wide_sums(a);
+  if (a.forced == STAMP_FP8_ROUTE_TILES_256) a.forced = 0;
+  a.codes = !a.gated && mlp_codes_in_tiles(a, p.down, rows);
+  if (a.codes && a.forced <= STAMP_FP8_ROUTE_ROWS) a.forced = stamp_f8_codes_route(a.groups, a.Kb, rows);
+  a.h_rows = a.gated && rows <= kMlpGatedRows && route_of(a, rows) == STAMP_FP8_ROUTE_ROWS;
+  p.coded = (a.gated || a.codes) && !a.h_rows;
+  return p;
+}
+
 // The layer of experts' places: logits and the router's, then those of the experts.
 struct MoeWs {
   size_t logits, sync, h, sums, route, experts, total;
@@ -614,17 +631,12 @@ stamp_status_t stamp_mlp_forward(const stamp_fp8_plan_t* up, const stamp_fp8_pla
   hipStream_t st = reinterpret_cast<hipStream_t>(hip_stream);
   uint8_t* ws = static_cast<uint8_t*>(workspace_dev);
 
-  StampF8Gemm a = gemm_args(up), b = gemm_args(down);
+  const MlpProducts products = mlp_products(up, down, rows);
+  StampF8Gemm a = products.up, b = products.down;
+  const bool coded = products.coded;
+  a.act = epilogue->activation;
   b.R = epilogue->residual_dev;
   b.ld_r = epilogue->ld_residual;
-  a.y_bf16 = 0;
-  a.wide_sums = f8_wide_sums(a);
-  if (a.forced == STAMP_FP8_ROUTE_TILES_256) a.forced = 0;
-  a.codes = !up->desc.gated && mlp_codes_in_tiles(a, b, rows);
-  if (a.codes && a.forced <= STAMP_FP8_ROUTE_ROWS) a.forced = stamp_f8_codes_route(a.groups, a.Kb, rows);
-  a.act = epilogue->activation;
-  a.h_rows = a.gated && rows <= kMlpGatedRows && route_of(a, rows) == STAMP_FP8_ROUTE_ROWS;
-  const bool coded = (a.gated || a.codes) && !a.h_rows;
   float* scales = reinterpret_cast<float*>(ws + w.scales);
   if (takes_x(a, rows)) {
     give_x(&a, up->desc, rows, X_dev, ld_x);
@@ -663,6 +675,18 @@ stamp_status_t stamp_mlp_forward(const stamp_fp8_plan_t* up, const stamp_fp8_pla
   b.Y = Y_dev;
   b.ld_y = ld_y;
   return done(product(b, st));
+}
+
+stamp_status_t stamp_mlp_debug_route(const stamp_fp8_plan_t* up, const stamp_fp8_plan_t* down, int32_t rows, int32_t* route_host) {
+  if (route_host == nullptr) return STAMP_ERR_NULL;
+  const stamp_status_t s = check_mlp(up, down);
+  if (s != STAMP_OK) return s;
+  if (rows < 1 || rows > kMaxRows) return STAMP_ERR_SHAPE;
+  const MlpProducts p = mlp_products(up, down, rows);
+  route_host[0] = route_of(p.up, rows);
+  route_host[1] = route_of(p.down, rows);
+  route_host[2] = p.coded;
+  return STAMP_OK;
 }
 
 size_t stamp_route_workspace_bytes(int32_t tokens, int32_t experts, int32_t top_k) {

@@ -283,6 +283,13 @@ def mlp_workspace(up: Fp8Plan, down: Fp8Plan, rows: int, device="cuda"):
     return torch.empty(max(n, 256), dtype=torch.uint8, device=device)
 
 
+def mlp_route(up: Fp8Plan, down: Fp8Plan, rows: int) -> tuple:
+    """How mlp_forward runs so many rows: the up and the down product's kernel (names of FP8_ROUTES), and what h leaves the first as, "codes" or "rows" (fp32)."""
+    out = (C.c_int32 * 3)()
+    _check(up.lib.stamp_mlp_debug_route(up._h, down._h, int(rows), out), "stamp_mlp_debug_route")
+    return FP8_ROUTES[out[0]], FP8_ROUTES[out[1]], "codes" if out[2] else "rows"
+
+
 def mlp_forward(up: Fp8Plan, down: Fp8Plan, X, Y, workspace, activation, residual=None, stream=None):
     """The dense MLP: Y = Q8(activation(X Wup + bias)) Wdown + bias + residual; with a gated up (a plan of one expert) activation(X Wgate) * (X Wup) in
     the activation's place.  residual: a tensor like Y; X, Y and residual may be the same tensor."""

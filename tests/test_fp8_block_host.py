@@ -127,3 +127,9 @@ def test_the_bounds_tell_one_activation_from_another_and_see_lost_terms():
 
 def test_looks_of_no_plan(lib):  # noqa: F811
     assert lib.stamp_moe_debug_set_looks(None, 0) == 1
+
+
+def test_the_route_of_no_mlp(lib):  # noqa: F811
+    out = (C.c_int32 * 3)(7, 7, 7)
+    assert lib.stamp_mlp_debug_route(None, None, 4, out) == 1 and lib.stamp_mlp_debug_route(None, None, 4, None) == 1
+    assert list(out) == [7, 7, 7]
