@@ -1,5 +1,5 @@
 """The dense MLP: every kernel of the up product with every one of the down product, whichever way h goes between them, against the definition in 64 bits
-(fp8_block_reference.py)."""
+(fp8_block_reference.py), and rows that are no numbers."""
 import numpy as np
 import pytest
 
@@ -111,4 +111,54 @@ def test_what_runs_by_rule(st, rows, d, ff, gated, f32, bf16, y):  # noqa: F811
     some = np.random.default_rng(2).permutation(rows)[:60]
     _held(Y[_gpu(some)], *want("silu", some), "")
     up.destroy()
+    down.destroy()
+
+
+@pytest.mark.parametrize("y", ["f32", "bf16"])
+@pytest.mark.parametrize("gated", [0, 1])
+@pytest.mark.parametrize("rows", [4, 16, 60, 300])
+def test_rows_that_are_no_numbers(st, rows, gated, y):  # noqa: F811
+    """A NaN or an infinity in a row of X makes that row of Y NaN and no other, whichever way h goes; the other rows keep their bits."""
+    import torch
+    X, up, down, R, _ = _case(st, rows, 300, 450, 200, gated, "bf16", y, 0)
+    bad = X.clone()
+    bad[1, 5], bad[2, 299], bad[rows - 1, 128] = float("nan"), float("inf"), -float("inf")
+    lost = sorted({1, 2, rows - 1})
+    keep = [i for i in range(rows) if i not in lost]
+    room, Y, Z = st.mlp_workspace(up, down, rows), torch.empty_like(R), torch.empty_like(R)
+    for first in ("", "rows", "tiles_64", "tiles_128"):
+        up.set_route(first)
+        for second in ("", "rows", "tiles_64", "tiles_128"):
+            down.set_route(second)
+            for act in ("relu", "gelu"):
+                st.mlp_forward(up, down, X, Y, room, act, residual=R)
+                st.mlp_forward(up, down, bad, Z, room, act, residual=R)
+                assert torch.isfinite(Y).all() and torch.isnan(Z[lost]).all() and torch.equal(Y[keep], Z[keep]), (first, second, act)
+    up.destroy()
+    down.destroy()
+
+
+@pytest.mark.parametrize("rows", [3, 60])
+def test_infinite_values_of_h(st, rows):  # noqa: F811
+    """An infinity or NaN in h makes its row NaN (Q8); minus infinity through relu is a zero like any other."""
+    import torch
+    rng = np.random.default_rng(3)
+    d, ff, n = 256, 300, 130
+    w1, s1 = _weights(rng, (), ff, d, 0)
+    w2, s2 = _weights(rng, (), n, ff, 0)
+    xv, X = _activations(rng, rows, d, "bf16")
+    down = st.Fp8Plan(st.Fp8Desc(d_in=ff, d_out=n, y_dtype=st.STAMP_F32), _gpu(w2), _gpu(s2))
+    for value, act, number in ((np.inf, "relu", 0), (np.inf, "gelu", 0), (-np.inf, "relu", 1), (-np.inf, "silu", 0), (np.nan, "relu", 0)):
+        b = rng.standard_normal(ff).astype(np.float32)
+        b[290] = value
+        up = st.Fp8Plan(st.Fp8Desc(d_in=d, d_out=ff), _gpu(w1), _gpu(_smaller(s1)), _gpu(b))
+        Y, room = torch.empty((rows, n), device="cuda"), st.mlp_workspace(up, down, rows)
+        for route in ("rows", "tiles_64", "tiles_128"):
+            up.set_route(route)
+            st.mlp_forward(up, down, X, Y, room, act)
+            if number:
+                _held(Y, *block.mlp(xv, w1, _smaller(s1), np.where(np.isinf(b), -1e30, b).astype(np.float32), w2, s2, None, act, None, "f32", 0), f"{value} {act} {route}")
+            else:
+                assert torch.isnan(Y).all(), (value, act, route)
+        up.destroy()
     down.destroy()
