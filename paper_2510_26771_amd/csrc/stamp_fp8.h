@@ -376,8 +376,9 @@ __device__ __forceinline__ float logistic_times(float x, float y) {
   return x * __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(y * -1.44269504088896341f));
 }
 // x Phi(x) as x / (1 + 2^y), y = x p(x^2): log2 of (1 - Phi) / Phi is odd in x, and its quotient by x a polynomial of degree 7 in x^2, fitted for |x| up to
-// sqrt(30) by least squares with weights raised where Phi's error is largest, and held beyond.  With all roundings 1.9e-7 of |x| at most, measured over -12 .. 12
-// (5e-8 in the middle; the form by erf loses as much where 1 + erf cancels); of itself 3e-4 at most down to x = -5.  13 instructions, two of them of a quarter rate:
+// sqrt(30) by least squares with weights raised where Phi's error is largest, and held beyond.  With all roundings 2.0e-7 of |x| at most, measured over -100 .. 100
+// (the form by erf loses as much where 1 + erf cancels).  That is no bound of gelu's own last places: of itself 4e-7 down to x = -1, 5e-5 to -3, 3.3e-4 to -5, 6 % at -5.5, and four
+// times the value at -6, where that is 6e-9; beyond it falls to zero.  14 instructions, two of them of a quarter rate:
 // 8192 x 1152 -> 4608, bf16: 68 us without, 75 with gelu_tanh, 85 with the form by exp(-x^2 / 2) and a polynomial in 1 / (1 + 0.23 |x|).
 __device__ __forceinline__ float gelu(float x) {
   const float s = __builtin_fminf(x * x, 30.0f);
