@@ -300,11 +300,22 @@ int average(const StampF8Gemm& a, int rows) { return (int)(((int64_t)rows + a.se
 // Where all workgroups run at once and the rows are few: 1 x 4096 -> 11008 9.9 us, with a launch for the codes 12.1; with more workgroups
 // than that the registers of the quantizer cost more than the launch (1 x 8192 -> 28672: 49 us and 38.5; 96 rows over 24 of 32 experts,
 // 4096 -> 1536: 29.9 and 29.8; 24 rows over 24 experts, gated 2048 -> 1408: 33 and 29).
+// A gated layer's rows in fp32 come from twice as many workgroups as there are groups, of 32 places.  There it pays with several of them a CU as well, or loses 1.6 % at most (3 and 4
+// rows of the widest); beyond 8 a CU was not measured.  us of a gated MLP, quantized here / by a launch:
+//                               1 row           2               3               4             workgroups
+//   1024 -> 2816 -> 1024          9.6 / 11.6      10.1 / 12.0     10.3 / 12.2     10.5 / 12.5     176
+//   2048 -> 8192 -> 2048          19.2 / 21.9     20.2 / 23.0     21.3 / 24.0     22.0 / 24.7     512
+//   4096 -> 11008 -> 4096         33.8 / 35.3     35.2 / 36.3     37.1 / 37.6     38.2 / 38.3     688
+//   4096 -> 14336 -> 4096         40.7 / 42.3     42.6 / 43.5     44.8 / 44.9     46.4 / 46.3     896
+//   16384 -> 16384 -> 16384       146.9 / 149.8   149.0 / 151.0   152.5 / 152.5   157.2 / 154.7   1024
+//   8192 -> 28672 -> 8192         132.0 / 132.4   134.3 / 135.1   128.9 / 128.7   129.7 / 128.6   1792
+//   1024 -> 28672 -> 1024         34.3 / 37.6     37.1 / 40.5     38.6 / 41.9     39.4 / 42.7     1792
 int stamp_f8_rows_quantize(const StampF8Gemm& a, int rows) {
   const int fit = kCodesLds / row_bytes(a.Kb), busy = a.sets < rows ? a.sets : rows;
   const int chunk = fit > 16 ? 16 : fit;  // 65536 channels: one row
-  const int64_t workgroups = (int64_t)busy * (a.gated ? (a.groups + 3) / 4 : a.groups);  // gated: one a CU; else two, of half a group at least
-  return workgroups <= stamp_device_cus() && average(a, rows) <= (chunk < 4 ? chunk : 4) ? chunk : 0;
+  // gated, to codes: one workgroup of 256 places a CU; rows in fp32: up to 8 of 32; else two, of half a group at least
+  const int64_t workgroups = (int64_t)busy * (a.h_rows ? 2 * a.groups : a.gated ? (a.groups + 3) / 4 : a.groups);
+  return workgroups <= (a.h_rows ? 8 : 1) * stamp_device_cus() && average(a, rows) <= (chunk < 4 ? chunk : 4) ? chunk : 0;
 }
 
 hipError_t stamp_launch_f8_rows(const StampF8Gemm& a, hipStream_t st) {
