@@ -145,6 +145,11 @@ hipError_t stamp_launch_router(const stamp_router_t& router, const void* X, int 
 //   2 of 8,   4096 -> 2048        30 / 50     35 / 54     52 / 61      57 / 66      64 / 70
 //   16 of 64, 2048 -> 1408        48 / 62     66 / 74     82 / 91      113 / 119    142 / 126
 //   32 of 128, 1024 -> 512        40 / 48     48 / 64     56 / 60      67 / 67      80 / 71
+//   6 of 64,  6144 -> 1536        55 / 76     77 / 95     120 / 137    194 / 214    260 / 274
+//   4 of 128, 7168 -> 2048        53 / 87     84 / 112    140 / 181    231 / 250    404 / 413
+//   8 of 256, 7168 -> 2048        82 / 114    140 / 197   249 / 275    453 / 463    765 / 769
+//   2 of 8,   6144 -> 4096        44 / 69     71 / 84     95 / 107     117 / 138    132 / 153
+//   2 of 16,  8192 -> 2048        45 / 74     54 / 87     85 / 105     123 / 145    150 / 171
 // Beyond 128 rows Q8 of h, which every workgroup does again for its part of the rows, is what loses.
 constexpr int kMoeTokens = 16, kMoeSlots = 128;
 constexpr int kMoeChunkBytes = 96 << 10;

@@ -5,7 +5,7 @@
 // Two logits decide by their order, so their sums are held in more than 32 bits: a block of 32 channels in fp32 (one matrix instruction of bf16
 // operands, or eight of fp32 ones, a bf16 operand widened), the blocks in fp64, one rounding at the end.
 // 1 token, 64 experts, 2048 channels (with Q8 of X beside it) 4.5 us; 16 tokens, 256 experts, 4096 channels 10.5; 512 tokens, 64 experts, 2048 channels, fp32 9.  Narrower
-// tiles on more workgroups: 6, 10 and 11.
+// tiles on more workgroups: 6, 10 and 11.  Made for few tokens: 8192 tokens, 256 experts, 4096 channels take 306, as each of 16 tiles side by side reads X again.
 #include "stamp_fp8.h"
 
 namespace {

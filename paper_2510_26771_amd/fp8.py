@@ -38,7 +38,7 @@ class Fp8Desc:
     d_in: int
     d_out: int
     experts: int = 0          # 0: one layer
-    gated: int = 0            # 1: gate and up matrices, for experts_forward
+    gated: int = 0            # 1: gate and up matrices, for experts_forward, moe_forward and (one expert) mlp_forward
     x_dtype: int = STAMP_BF16
     y_dtype: int = STAMP_BF16
     w_dtype: int = STAMP_E4M3
