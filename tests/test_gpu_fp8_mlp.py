@@ -162,3 +162,27 @@ def test_infinite_values_of_h(st, rows):  # noqa: F811
                 assert torch.isnan(Y).all(), (value, act, route)
         up.destroy()
     down.destroy()
+
+
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+@pytest.mark.parametrize("gated", [0, 1])
+@pytest.mark.parametrize("rows", [1, 13, 40, 300, 1100])
+def test_rows_at_any_place_and_a_workspace_of_a_larger_call(st, rows, gated, x):  # noqa: F811
+    """X in rows that lie apart and begin anywhere, a stream of its own, the workspace of 1500 rows before and after: the bits of the plain call."""
+    import torch
+    X, up, down, R, _ = _case(st, rows, 333, 450, 200, gated, x, "bf16", 0)
+    Y, room = torch.empty_like(R), st.mlp_workspace(up, down, 1500)
+    st.mlp_forward(up, down, X, Y, st.mlp_workspace(up, down, rows), "silu", residual=R)
+    apart, _ = _strided(rows, 333, x, 4, 1)
+    apart.copy_(X)
+    more, Y1500 = torch.randn((1500, 333), device="cuda").to(X.dtype), torch.empty((1500, 200), dtype=torch.bfloat16, device="cuda")
+    stream = torch.cuda.Stream()
+    for _ in range(2):
+        Z = torch.full_like(Y, -7.0)
+        torch.cuda.synchronize()
+        st.mlp_forward(up, down, more, Y1500, room, "silu", stream=stream)
+        st.mlp_forward(up, down, apart, Z, room, "silu", residual=R, stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(Y, Z)
+    up.destroy()
+    down.destroy()

@@ -5,7 +5,7 @@ import pytest
 
 import fp8_block_reference as block
 import fp8_reference as ref
-from test_gpu_fp8 import _activations, _code, _dt, _gpu, _weights
+from test_gpu_fp8 import _activations, _dt, _gpu, _strided
 from test_gpu_fp8_block import _held, _moe_case, _values, st  # noqa: F401  (fixture)
 
 pytestmark = pytest.mark.gpu
@@ -162,5 +162,37 @@ def test_other_tokens_move_a_row_by_the_order_of_its_sums_alone(st, tokens, top_
     assert np.array_equal(r.ids.cpu().numpy()[keep], ids[keep]) and (r.ids[1] == -1).all() and (Z[1] == 0).all() and (tokens == 3 or torch.isnan(Z[2]).all())
     off = (Y[keep].double() - Z[keep].double()).abs().cpu().numpy()
     assert (off <= 2 * sums * 2.0 ** -24 * size * 1.01).all(), np.max(off / size) * 2.0 ** 24
+    up.destroy()
+    down.destroy()
+
+
+# ---- where tensors lie ----
+
+@pytest.mark.parametrize("tokens", [1, 5, 16, 30])
+@pytest.mark.parametrize("x,router", [("bf16", "bf16"), ("f32", "bf16"), ("bf16", "f32")])
+def test_rows_at_any_place_and_a_workspace_of_a_larger_call(st, tokens, x, router):  # noqa: F811
+    """X in rows that lie apart and begin anywhere, the router's matrix too, a stream of its own, the workspace of 64 tokens before and after: the bits of
+    the plain call."""
+    import torch
+    rng = np.random.default_rng(tokens)
+    E, top_k, d, ff = 9, 3, 333, 200
+    xv, X, *_, rtg, up, down = _moe_case(st, rng, tokens, E, d, ff, x, "bf16", router, 0, 1)
+    r, Y = st.Routing(tokens, E, top_k), torch.empty((tokens, d), dtype=torch.bfloat16, device="cuda")
+    st.moe_forward(rtg, up, down, X, r, Y, st.moe_workspace(up, down, tokens, top_k))
+    apart, _ = _strided(tokens, d, x, 4, 1)
+    apart.copy_(X)
+    moved = torch.empty(E * d + 1, dtype=rtg.dtype, device="cuda")[1:].view(E, d)
+    moved.copy_(rtg)
+    room, more = st.moe_workspace(up, down, 64, top_k), torch.randn((64, d), device="cuda").to(X.dtype)
+    r64, Y64 = st.Routing(64, E, top_k), torch.empty((64, d), dtype=torch.bfloat16, device="cuda")
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(2):
+        Z = torch.full_like(Y, -7.0)
+        torch.cuda.synchronize()
+        st.moe_forward(rtg, up, down, more, r64, Y64, room, stream=stream)
+        st.moe_forward(moved, up, down, apart, r, Z, room, stream=stream)
+        torch.cuda.synchronize()
+        assert torch.equal(Y, Z)
     up.destroy()
     down.destroy()
