@@ -1,10 +1,10 @@
-"""Activations at minus infinity and in every kernel, and how near they are to their definitions (fp8_block_reference.py)."""
+"""Activations at minus infinity and in every kernel, how near they are to their definitions (fp8_block_reference.py), and that calls repeat."""
 import numpy as np
 import pytest
 
 import fp8_block_reference as block
-from test_gpu_fp8 import _code, _dt, _gpu
-from test_gpu_fp8_block import st  # noqa: F401  (fixture)
+from test_gpu_fp8 import _activations, _code, _dt, _gpu, _weights
+from test_gpu_fp8_block import _smaller, st  # noqa: F401  (fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -53,3 +53,45 @@ def test_activations_beside_their_argument(st):  # noqa: F811
         off = np.abs(Y[0].cpu().numpy() - block.activation(z.astype(np.float64), act))
         assert (off <= bound * np.abs(z) + 1e-37).all(), (act, np.max(off / np.abs(z)))
     plan.destroy()
+
+
+@pytest.mark.parametrize("rows,d,n", [(2048, 1152, 1500), (700, 4096, 300), (8192, 256, 1152)])
+def test_the_same_call_gives_the_same_bits(st, rows, d, n):  # noqa: F811
+    """A layer's epilogue in tiles, dense and by expert, an MLP and a layer of experts, with other calls between and anything in the workspace; a bf16 Y is as far from the
+    definition as the nearest bf16 numbers are, in norm, but for 1e-4: the FP8 instructions lose 6e-5 of a sum at most for exponents all over the range."""
+    import torch
+    rng = np.random.default_rng(rows)
+    x, X = _activations(rng, rows, d, "bf16")
+    X2 = torch.randn_like(X)
+
+    def plan(d_in, d_out, experts=0, gated=0):
+        lead = ((experts,) if experts else ()) + ((2,) if gated else ())
+        w, ws = _weights(rng, lead, d_out, d_in, 0)
+        return st.Fp8Plan(st.Fp8Desc(d_in=d_in, d_out=d_out, experts=experts, gated=gated), _gpu(w), _gpu(_smaller(ws))), w, _smaller(ws)
+    (lin, w, ws), (grp, *_), (up, *_), (down, *_), (gup, *_), (gdown, *_) = plan(d, n), plan(d, n, 4), plan(d, 520), plan(520, d), plan(d, 520, 4, 1), plan(520, d, 4)
+    offsets = _gpu(np.int32([0, rows // 3, rows // 3, rows - 5, rows - 5]))
+    rt, r = torch.randn((4, d), device="cuda"), st.Routing(rows, 4, 2)
+    R, Rd = (torch.randn((rows, c), device="cuda").to(torch.bfloat16) for c in (n, d))
+    calls = [(n, lin.alloc_workspace(rows), lambda x, y, room: lin.linear_forward(x, y, room, activation="gelu", residual=R)),
+             (n, grp.alloc_workspace(rows), lambda x, y, room: grp.grouped_forward(x, offsets, y, room, activation="silu", residual=R)),
+             (d, st.mlp_workspace(up, down, rows), lambda x, y, room: st.mlp_forward(up, down, x, y, room, "gelu_tanh", residual=Rd)),
+             (d, st.moe_workspace(gup, gdown, rows, 2), lambda x, y, room: st.moe_forward(rt, gup, gdown, x, r, y, room, residual=Rd))]
+    for i, (cols, room, call) in enumerate(calls):
+        first, Y = (torch.full((rows, cols), -7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        call(X, first, room)
+        for value in (255, 0, 60):
+            call(X2, Y, room)
+            assert not torch.equal(Y, first)
+            room.fill_(value)
+            Y.fill_(-7.0)
+            call(X, Y, room)
+            assert torch.equal(Y, first), i
+        if i == 0:
+            some = rng.permutation(rows)[:200]
+            want, _ = block.layer(x[some], w, ws, None, "gelu", R[_gpu(some)].double().cpu().numpy(), "bf16", 0, False)
+            got = first[_gpu(some)].double().cpu().numpy()
+            nearest = torch.from_numpy(want).to(torch.bfloat16).double().numpy()
+            off, own = (np.linalg.norm(a - want) / np.linalg.norm(want) for a in (got, nearest))
+            assert off <= own + 1e-4, (off, own)
+    for p in (lin, grp, up, down, gup, gdown):
+        p.destroy()
