@@ -50,13 +50,12 @@ struct Chosen {
   uint16_t expert[kMaxSlots + 1];    // experts with rows, in order; their first rows, and behind the last the number of rows
   uint16_t first[kMaxSlots + 1];
   uint8_t token[kMaxSlots];          // of a row
-  float weight[kMaxSlots];           // of a row
+  float weight[kMaxSlots];           // of a row; NaN where a wait for it gave up
   int32_t id[kMaxSlots];             // of a slot
   float slot_weight[kMaxSlots];
   uint32_t wave_sum[kWaves];
   int32_t experts;
   uint32_t ticket;
-  int32_t late;                      // a wait of this workgroup gave up: what follows is NaN
 };
 
 __device__ __forceinline__ v8i load_w(const uint8_t* w) {
@@ -66,7 +65,6 @@ __device__ __forceinline__ v8i load_w(const uint8_t* w) {
 __device__ void choose(const MoeArgs& a, Chosen& s) {
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, E = a.r.experts, K = a.r.top_k, T = a.r.tokens;
   for (int e = t; e < kF8MaxExperts; e += kThreads) s.mask[e] = 0;
-  if (t == 0) s.late = 0;
   __syncthreads();
   const TopArgs top = {a.logits, E, E, K, a.renorm};
   auto put = [&](int tok, int k, int id, float weight) __attribute__((always_inline)) {
@@ -323,13 +321,13 @@ __global__ __launch_bounds__(kThreads) void k_moe_few(MoeArgs a) {
       if (wave == 0) {  // the experts' rows of h; one wave looks, and drops what its CU and L2 hold of before, for all
         for (int i = i0 + lane; i < i1; i += 64) {
           const uint32_t all = (uint32_t)((s.first[i + 1] - s.first[i]) * groups);
-          auto finished = [&]() __attribute__((always_inline)) { return __hip_atomic_load(&a.sync[1 + i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) >= all; };
-          bool there = finished();
-          for (int look = 0; !there && look < a.looks; ++look) {
+          for (int look = 0; __hip_atomic_load(&a.sync[1 + i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) < all; ++look) {
+            if (look >= a.looks) {  // in vain: its rows count as NaN from here on
+              for (int r = s.first[i]; r < s.first[i + 1]; ++r) s.weight[r] = __builtin_nanf("");
+              break;
+            }
             __builtin_amdgcn_s_sleep(1);
-            there = finished();
           }
-          if (!there) s.late = 1;
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
       }
@@ -351,7 +349,7 @@ __global__ __launch_bounds__(kThreads) void k_moe_few(MoeArgs a) {
             float scale, inv;
             scale_of(max8(x[q].amax()), p.pow2, &scale, &inv);
             *reinterpret_cast<u4*>(h + m * ld_row + c) = x[q].codes(inv);
-            if ((t & 7) == 0) sh[m * Kb + (c >> 7)] = s.late ? __builtin_nanf("") : scale * s.weight[r0 + m];
+            if ((t & 7) == 0) sh[m * Kb + (c >> 7)] = scale * s.weight[r0 + m];
           }
         }
       }
