@@ -445,9 +445,9 @@ stamp_status_t stamp_experts_forward(const stamp_fp8_plan_t* up, const stamp_fp8
  *     Y = act(X W + bias) + R      in fp32 behind the sums, rounded once
  *
  * act: x; max(x, 0); x / (1 + exp(-x)); x Phi(x), Phi the normal distribution; x / (1 + exp(-2 sqrt(2 / pi) (x + 0.044715 x^3))), which is
- * x (1 + tanh(..)) / 2.  A NaN stays one; of minus infinity silu, gelu and gelu_tanh make NaN (-infinity times 0), relu 0.  Evaluated in fp32: silu and gelu_tanh within 1.5e-7 |x| of
- * these, gelu within 2.1e-7 |x|.  Those are bounds beside x: relative to its own value, which falls faster than any power of x, gelu is 3.3e-4 off at x = -5 and of the
- * right size no more below -5.5.  R [rows, d_out] has Y's type, row m at R + m * ld_residual (as ld_y); it may be Y itself (same pointer and
+ * x (1 + tanh(..)) / 2.  A NaN stays one; of minus infinity silu, gelu and gelu_tanh make NaN (-infinity times 0), relu 0.  Evaluated in fp32, of these: silu and
+ * gelu_tanh within 1.5e-7 |x|, gelu within 2.7e-7 |x|; and for x >= -6 of their own value within 1e-5 (silu 1e-6).  Where many rows become a bf16 Y, gelu keeps 3.3e-4 of its value down to
+ * x = -5 alone: below -5.5, where it is under 1e-7, it may be any number of that size, zero among them.  R [rows, d_out] has Y's type, row m at R + m * ld_residual (as ld_y); it may be Y itself (same pointer and
  * distance of rows) and must not overlap Y otherwise.  residual_dev NULL: none, ld_residual is then not looked at.  X must not overlap Y in the calls of one layer
  * (STAMP_ERR_SHAPE where they begin at one address); in stamp_mlp_forward and stamp_moe_forward it may, also be Y. */
 typedef enum { STAMP_ACT_NONE = 0, STAMP_ACT_RELU = 1, STAMP_ACT_SILU = 2, STAMP_ACT_GELU = 3, STAMP_ACT_GELU_TANH = 4 } stamp_activation_t;

@@ -449,7 +449,7 @@ __global__ __launch_bounds__(512) void k_f8_tiles(StampF8Gemm a) {
 #pragma unroll
       for (int j = 0; j < 16; ++j) v[j] = acc[mi][j >> 2][j & 3] + bias[j];
       if constexpr (OUT == kRowsAct) {
-        if (whole) activate(v, a.act);
+        if (whole) activate<16, kBf16>(v, a.act);
         if (add_r) {
 #pragma unroll
           for (int j = 0; j < 16; ++j) v[j] += res[mi % kAhead][j >> 3].at(j & 7);

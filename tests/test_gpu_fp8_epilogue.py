@@ -43,15 +43,38 @@ def test_activations_at_the_ends_of_their_range(st, rows, d, parts, y):  # noqa:
     plan.destroy()
 
 
+def _arguments():
+    rng = np.random.default_rng(0)
+    return np.concatenate([rng.uniform(-12, 12, 1 << 19), rng.uniform(-100, 100, 1 << 18), rng.uniform(-1, 1, 1 << 18)]).astype(np.float32)
+
+
 def test_activations_beside_their_argument(st):  # noqa: F811
     """The bounds that stamp.h states, over a million arguments."""
-    rng = np.random.default_rng(0)
-    z = np.concatenate([rng.uniform(-12, 12, 1 << 19), rng.uniform(-100, 100, 1 << 18), rng.uniform(-1, 1, 1 << 18)]).astype(np.float32)
+    z = _arguments()
     plan, X, Y, ws = _of_bias(st, z, "f32", 1)
-    for act, bound in (("silu", 1.5e-7), ("gelu", 2.1e-7), ("gelu_tanh", 1.5e-7)):
+    for act, bound, own in (("silu", 1.5e-7, 1e-6), ("gelu", 2.7e-7, 1e-5), ("gelu_tanh", 1.5e-7, 1e-5)):
         plan.linear_forward(X, Y, ws, activation=act)
-        off = np.abs(Y[0].cpu().numpy() - block.activation(z.astype(np.float64), act))
+        want = block.activation(z.astype(np.float64), act)
+        off = np.abs(Y[0].cpu().numpy() - want)
         assert (off <= bound * np.abs(z) + 1e-37).all(), (act, np.max(off / np.abs(z)))
+        assert (off <= own * np.abs(want) + 1e-37)[z >= -6].all(), (act, np.max((off / np.abs(want))[z >= -6]))
+    plan.destroy()
+
+
+@pytest.mark.parametrize("rows,d", [(1, 128), (80, 128), (200, 128), (130, 4096)])
+def test_gelu_keeps_its_digits_in_fp32(st, rows, d):  # noqa: F811
+    """exp(-t^2 / 2): two products and a constant's half rounding, each 2^-24 of an exponent that counts t^2 / 2 times; 14 such roundings for the fit (2.7), the
+    polynomial (3), the reciprocal (2), the power of two (2), the products and the sum."""
+    n = 1 << 10 if rows > 1 else 1 << 20
+    z = _arguments()[:: (1 << 20) // n]
+    z = z[z >= -8]
+    want = block.activation(z.astype(np.float64), "gelu")
+    plan, X, Y, ws = _of_bias(st, z, "f32", rows, d)
+    for route in ("", "rows", "tiles_64", "tiles_128"):
+        plan.set_route(route)
+        plan.linear_forward(X, Y, ws, activation="gelu")
+        off = np.abs(Y.cpu().numpy() - want)
+        assert (off <= (1.25 * z.astype(np.float64) ** 2 + 14) * 2.0 ** -24 * np.abs(want) + 1e-37).all(), (route, np.max(off / np.abs(want)))
     plan.destroy()
 
 
