@@ -383,7 +383,7 @@ __device__ __forceinline__ float logistic_times(float x, float y) {
 // x Phi(x) as max(x, 0) - |x| Q(|x|), Q(t) = 1 - Phi(t) = exp(-t^2 / 2) r(t): r falls slowly (as 1 / t) and is a polynomial of degree 7 in 1 / (1 + t / 4), fitted for t up to 10 by
 // least squares of its relative error with weights raised where that is largest (1.6e-7; beyond 10 gelu is below 1e-22).  So the tail keeps its own digits: 6e-7 of the value down to x = -3, 2e-6
 // to -6 (0.5 x (1 + erf) has none left below -5.5), and 2.7e-7 of |x| at most.  An fp32 Y shows them, and so do codes of h: with x normal, deviation 3, 13 of 5.2 million values came to a code
-// beside their own, 464 by the shorter form below, 318 by erf in fp32.  It takes 20 instructions: an MLP of 8192 x 1152 -> 4608 -> 1152 167 us, with the shorter form 163.5.
+// beside their own, 464 by the shorter form below, 318 by erf in fp32.  It takes 18 instructions: an MLP of 8192 x 1152 -> 4608 -> 1152 167 us, with the shorter form 163.5.
 __device__ __forceinline__ float gelu(float x) {
   const float t = __builtin_fabsf(__builtin_fminf(x, 20.0f));  // infinity times Q's zero would be NaN; minus infinity's is meant to be
   const float u = __builtin_amdgcn_rcpf(__builtin_fmaf(0.25f, t, 1.0f));
